@@ -396,6 +396,121 @@ sp_status sp_attn_grpo_loss(const float* logp, const float* logp_old, const floa
                             const int32_t* Gs, const int32_t* resp_lens_flat,
                             void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Rollout: the step that produces the responses (Section 4.3 for tokens as they come) ------------
+ * A rollout step of a layer appends the new token's key and value to a paged cache and attends from its query; the G
+ * sequences that answer one prompt share the prompt's pages, as they share its tokens in a pack.
+ *
+ * Cache: k and v [n_pages, n_kv_heads, page_size, head_dim] each.  A sequence's token j lies in page table[j / page_size], row
+ * j % page_size.  Tables, lengths and position bases are DEVICE int32 arrays, read when the kernels run, so that a captured
+ * graph of a step is replayed with other lengths.  They are checked there: a page index outside [0, n_pages) is never
+ * followed (a token that it would receive is not stored, keys on it are not attended to), lengths are cut to what the table holds, and a
+ * negative length marks a sequence that takes no part. */
+typedef struct {
+    void* k;                  /* DEVICE, 16-byte aligned */
+    void* v;
+    int64_t n_pages;          /* >= 1 */
+    int32_t page_size;        /* 16, 32, 64, 128 or 256 */
+    int32_t n_kv_heads;
+    int32_t head_dim;         /* 64 or 128, either type */
+    sp_dtype dtype;           /* of the caches and of every tensor of the call */
+} sp_kv_cache;
+
+/* Append new tokens, with the rotary embedding of sp_attn_rope on the way.  Sequence s brings new_lens[s] tokens; the tokens of all
+ * sequences lie one sequence behind the other in k, v and q.  Its token i becomes token j = lens[s] + i of the sequence
+ * and stands at position pos_base[s] + j: its rotated key and its value go to the cache.
+ *   q, q_out      NULL both, or q [T, n_q_heads, head_dim] and its rotation q_out (contiguous; may be q itself if that is contiguous)
+ *   k, v          [T, n_kv_heads, head_dim], T = sum of new_lens
+ *   q_stride, k_stride, v_stride   elements from token to token (heads of a token are contiguous), so that they may be parts of one
+ *                 projection's output; multiples of 16 bytes, at least heads * head_dim
+ *   k_out         NULL, or the rotated keys [T, n_kv_heads, head_dim] contiguous as well (for the attention over a prompt; may be k itself
+ *                 if that is contiguous)
+ *   new_lens      HOST array of n_seqs entries >= 0, or NULL: one token each
+ *   tables        [n_seqs, table_width];  lens [n_seqs] tokens in the cache before the call
+ *   pos_base      [n_seqs] or NULL (0): a response's is its prompt's length, a prompt's 0
+ *   lens_out      [n_seqs] or NULL: lens + new_lens, at most table_width * page_size (tokens beyond are not stored).  Not lens
+ *                 itself, which the call reads meanwhile.
+ * Of a sequence with a negative length nothing is read or written (lens_out: its length).  Two tokens of one call must not
+ * fall on one row of a page: such a row's contents would be either's, or parts of both.  Needs no workspace.  Asynchronous on `stream`; errors as
+ * sp_attn_fwd (SP_ERR_INVALID_ARG also for rope_base <= 1 or a stride that is too small). */
+sp_status sp_attn_cache_append(const sp_kv_cache* cache, const void* q, int64_t q_stride, void* q_out, int32_t n_q_heads,
+                               const void* k, int64_t k_stride, void* k_out, const void* v, int64_t v_stride,
+                               int32_t n_seqs, const int32_t* new_lens, const int32_t* tables, int32_t table_width,
+                               const int32_t* lens, const int32_t* pos_base, int32_t* lens_out, double rope_base, void* stream);
+
+/* Attention of one new token per sequence over the cache.  Row s of q [n_seqs, n_q_heads, head_dim] attends to its group's prompt (the first
+ * prompt_lens[g] tokens of prompt table g) and to its own first resp_lens[s] tokens (those of resp table s, its new token's key
+ * among them), which is the row that the new token would have in sp_attn_fwd on the pack.  Writes o like q and
+ * lse [n_q_heads, n_seqs] float32; without a key o = 0 and lse = -inf (a negative resp_lens[s]: the prompt's are not attended to either).
+ * The prompt's keys and values are read once for all rows of the group.
+ *   Gs            HOST: sequences of each group, in order, n_seqs in all; NULL: one each (n_groups = n_seqs)
+ *   prompt_tables [n_groups, prompt_width], prompt_lens [n_groups]; both NULL and prompt_width 0: no shared prompts
+ *   resp_tables   [n_seqs, resp_width] (NULL if resp_width is 0), resp_lens [n_seqs]
+ *   workspace     DEVICE, at least sp_attn_decode_workspace_bytes(...) bytes, which grow with n_groups and n_seqs; it carries nothing from
+ *                 call to call.
+ * Deterministic: no atomics are used.  Asynchronous on `stream`; errors as sp_attn_fwd. */
+size_t    sp_attn_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads,
+                                         int32_t head_dim, sp_dtype dtype);
+sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float* lse, int32_t n_q_heads,
+                         int32_t n_groups, int32_t n_seqs, const int32_t* Gs,
+                         const int32_t* prompt_tables, int32_t prompt_width, const int32_t* prompt_lens,
+                         const int32_t* resp_tables, int32_t resp_width, const int32_t* resp_lens,
+                         float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rules by which logits are adjusted before a token is drawn, in this order: bias, repetition, frequency and presence,
+ * temperature, mask.  With h_v: id v occurs in the row's history (its prompt and its response so far), and c_v: how often it occurs
+ * in the response so far (counted up to 32767),
+ *     a = z_v + bias_v;   b = h_v ? (a > 0 ? a / repetition : a * repetition) : a;
+ *     d = b - frequency * c_v - (c_v > 0 ? presence : 0);   z'_v = bit v of the row's mask set ? d / temperature : -inf.
+ * A mask row has its bits in uint32 words, id v in bit v % 32 of word v / 32; where masks are NULL everything is allowed.  Products and sums
+ * are float32, z' is rounded once to the output's type.  What a masked place holds does not matter, NaN included. */
+typedef struct {
+    float repetition;         /* finite, > 0; 1: none */
+    float presence;           /* finite; 0: none */
+    float frequency;          /* finite; 0: none */
+    float temperature;        /* finite, > 0 */
+    const float* bias;        /* DEVICE [vocab], or NULL */
+} sp_logit_rules;
+
+/* Adjusted logits of one row per sequence: out = z' of logits [n_seqs, vocab].
+ *   logits_stride, out_stride   elements from row to row, >= vocab;  out may be logits itself (same stride), else they must not overlap
+ *   mask          DEVICE uint32 [n_seqs, mask_stride], mask_stride >= ceil(vocab / 32) words, or NULL
+ *   Gs            HOST as in sp_attn_decode (NULL: one sequence per group)
+ *   prompt_tokens DEVICE int32 [n_groups, prompt_stride], prompt_lens DEVICE [n_groups]: how many of them count;  both NULL: no prompts
+ *   resp_tokens   DEVICE int32 [n_seqs, resp_stride], resp_lens DEVICE [n_seqs];  both NULL: nothing generated yet
+ * Lengths are cut to [0, stride]; ids outside [0, vocab) are passed over.  vocab <= 2^30.  Needs no workspace.  Asynchronous on
+ * `stream`; errors as sp_attn_fwd. */
+sp_status sp_attn_adjust_logits(const void* logits, int64_t logits_stride, void* out, int64_t out_stride, int64_t vocab,
+                                const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride,
+                                int32_t n_groups, int32_t n_seqs, const int32_t* Gs,
+                                const int32_t* prompt_tokens, int32_t prompt_stride, const int32_t* prompt_lens,
+                                const int32_t* resp_tokens, int32_t resp_stride, const int32_t* resp_lens,
+                                sp_dtype dtype, void* stream);
+
+/* Log-probabilities under the adjusted distribution, and their gradient: sp_attn_logprob_fwd / _bwd with z' in place of z, which is
+ * never stored.  Arguments as there, and
+ *   tokens        DEVICE int32 [T_total]: the pack's token ids.  The history of response row t is its group's prompt and the tokens of
+ *                 its response ahead of row t (what a sampler had seen when labels[t] = tokens[t] was drawn); with SP_FLAG_OWN_TOKEN
+ *                 tokens[t] as well (for rows that predict the token behind them).
+ *   mask          DEVICE uint32 [T_total, mask_stride] or NULL, prompt rows not read
+ *   workspace     DEVICE, at least sp_attn_adjusted_logprob_workspace_bytes(T_total, n_groups, total_responses, vocab) bytes
+ * Forward: logp[t] = z'[t, labels[t]] - lse[t], lse[t] = ln sum_v exp(z'[t, v]); a label outside [0, vocab) or masked, and any label of a row that
+ * allows nothing, gives -inf.  Backward: dlogits[t, v] = g[t] (1[v == labels[t]] - exp(z'[t, v] - lse[t])) dz'[t, v] / dz[t, v], which is
+ * 0 in masked places and throughout a row that allows nothing; bias and penalties are constants.  dlogits may be logits itself.
+ * flags: SP_FLAG_OWN_TOKEN (the same in both calls), backward also SP_FLAG_ZERO_PROMPT_ROWS.  Bitwise repeatable. */
+#define SP_FLAG_OWN_TOKEN 8u               /* sp_attn_adjusted_logprob_fwd / _bwd only */
+size_t    sp_attn_adjusted_logprob_workspace_bytes(int64_t total_tokens, int32_t n_groups, int64_t total_responses, int64_t vocab);
+sp_status sp_attn_adjusted_logprob_fwd(const void* logits, const int32_t* labels, const int32_t* tokens, float* logp, float* lse,
+                                       int64_t vocab, const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride,
+                                       int32_t n_groups, const int32_t* prompt_lens, const int32_t* Gs,
+                                       const int32_t* resp_lens_flat, sp_dtype dtype, uint32_t flags,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+sp_status sp_attn_adjusted_logprob_bwd(const void* logits, const int32_t* labels, const int32_t* tokens, const float* lse,
+                                       const float* g, void* dlogits, int64_t vocab, const sp_logit_rules* rules,
+                                       const uint32_t* mask, int64_t mask_stride,
+                                       int32_t n_groups, const int32_t* prompt_lens, const int32_t* Gs,
+                                       const int32_t* resp_lens_flat, sp_dtype dtype, uint32_t flags,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* The segment table that every call builds from its host arrays and hands to its kernels (Section
  * 4.3, packing and mask: the table is the only form in which they reach the device).  Written to
  * HOST memory `words` (capacity in int32 words); *n_words receives the count needed, also when

@@ -19,14 +19,26 @@ SP_BF16, SP_F32 = 0, 1
 SP_SCHED_SHARED, SP_SCHED_NAIVE_CAUSAL = 0, 1
 
 SP_BWD_STAGE_ROWSUM, SP_BWD_STAGE_DKDV, SP_BWD_STAGE_DQ, SP_BWD_STAGE_ALL = 1, 2, 4, 7
-SP_FLAG_RESPONSE_ROWS, SP_FLAG_ACCUMULATE_DKDV, SP_FLAG_ZERO_PROMPT_ROWS = 1, 2, 4
+SP_FLAG_RESPONSE_ROWS, SP_FLAG_ACCUMULATE_DKDV, SP_FLAG_ZERO_PROMPT_ROWS, SP_FLAG_OWN_TOKEN = 1, 2, 4, 8
 
 EXPORTS = ("sp_attn_workspace_bytes", "sp_attn_reserve_bytes", "sp_attn_row_parts_bytes", "sp_attn_full_workspace_bytes", "sp_attn_kept_workspace_bytes", "sp_attn_sums_bytes", "sp_attn_fwd", "sp_attn_bwd", "sp_attn_fwd_batched",
            "sp_attn_bwd_batched", "sp_attn_bwd_batched_static", "sp_attn_bwd_batched_stages", "sp_attn_fwd_multi", "sp_attn_rope", "sp_attn_rope_qk", "sp_attn_fwd_batched_ex", "sp_attn_bwd_batched_ex", "sp_attn_fwd_batched_sums", "sp_attn_bwd_batched_sums",
            "sp_attn_loss_workspace_bytes", "sp_attn_logprob_fwd", "sp_attn_logprob_bwd", "sp_attn_logprob_bwd_ex", "sp_attn_grpo_loss",
+           "sp_attn_cache_append", "sp_attn_decode_workspace_bytes", "sp_attn_decode", "sp_attn_adjust_logits",
+           "sp_attn_adjusted_logprob_workspace_bytes", "sp_attn_adjusted_logprob_fwd", "sp_attn_adjusted_logprob_bwd",
            "sp_attn_segment_table", "sp_attn_row_tile", "sp_attn_dkdv_waves", "sp_attn_pieces", "sp_attn_f32_rows", "sp_attn_mfma_ceiling", "sp_attn_probe_atomic_add", "sp_attn_set_small_shape_steps", "sp_attn_last_error", "sp_attn_version")
 
 _lib = None
+
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class _LogitRulesStruct(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float),
+                ("temperature", ctypes.c_float), ("bias", ctypes.c_void_p)]
 
 
 class SpAttnError(RuntimeError):
@@ -104,6 +116,21 @@ def load_library() -> ctypes.CDLL:
     lib.sp_attn_rope.argtypes = [vp, vp, i32, i32, i32, ip, ip, ip, i32, ctypes.c_double, ctypes.c_int, vp, sz, vp]
     lib.sp_attn_rope_qk.restype = ctypes.c_int
     lib.sp_attn_rope_qk.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, ip, ip, ip, i32, ctypes.c_double, ctypes.c_int, vp, sz, vp]
+    cache_p, rules_p = ctypes.POINTER(_KvCacheStruct), ctypes.POINTER(_LogitRulesStruct)
+    lib.sp_attn_cache_append.restype = ctypes.c_int
+    lib.sp_attn_cache_append.argtypes = [cache_p, vp, i64, vp, i32, vp, i64, vp, vp, i64, i32, ip, vp, i32, vp, vp, vp, ctypes.c_double, vp]
+    lib.sp_attn_decode_workspace_bytes.restype = sz
+    lib.sp_attn_decode_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int]
+    lib.sp_attn_decode.restype = ctypes.c_int
+    lib.sp_attn_decode.argtypes = [cache_p, vp, vp, vp, i32, i32, i32, ip, vp, i32, vp, vp, i32, vp, f32, vp, sz, vp]
+    lib.sp_attn_adjust_logits.restype = ctypes.c_int
+    lib.sp_attn_adjust_logits.argtypes = [vp, i64, vp, i64, i64, rules_p, vp, i64, i32, i32, ip, vp, i32, vp, vp, i32, vp, ctypes.c_int, vp]
+    lib.sp_attn_adjusted_logprob_workspace_bytes.restype = sz
+    lib.sp_attn_adjusted_logprob_workspace_bytes.argtypes = [i64, i32, i64, i64]
+    lib.sp_attn_adjusted_logprob_fwd.restype = ctypes.c_int
+    lib.sp_attn_adjusted_logprob_fwd.argtypes = [vp, vp, vp, vp, vp, i64, rules_p, vp, i64, i32, ip, ip, ip, ctypes.c_int, ctypes.c_uint32, vp, sz, vp]
+    lib.sp_attn_adjusted_logprob_bwd.restype = ctypes.c_int
+    lib.sp_attn_adjusted_logprob_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, rules_p, vp, i64, i32, ip, ip, ip, ctypes.c_int, ctypes.c_uint32, vp, sz, vp]
     lib.sp_attn_segment_table.restype = ctypes.c_int
     lib.sp_attn_segment_table.argtypes = [i32, ip, ip, ip, ip, sz, ctypes.POINTER(sz)]
     lib.sp_attn_dkdv_waves.restype = ctypes.c_int
@@ -543,3 +570,280 @@ def sp_attn_bwd_batched_stages(q, k, v, o, lse, d_o, prompt_lens: Sequence[int],
     room = (workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     _check(lib.sp_attn_bwd_batched_stages(*args, *room) if sums is None else
            lib.sp_attn_bwd_batched_sums(*args, 0, None, sums.data_ptr(), sums.numel(), *room))
+
+
+# ---- rollout: paged cache, attention of one new token per sequence, adjusted logits ----------------------------------
+
+def _refuse(message: str):
+    raise SpAttnError(SP_ERR_INVALID_ARG, message)
+
+
+def _tensor(name, t, dtype, shape, device, contiguous=True):
+    """Checks what the library cannot see behind a pointer.  A None in `shape` stands for any size."""
+    if t.dtype != dtype or t.device != device or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        _refuse(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {shape} on {device}")
+    if contiguous and not t.is_contiguous():
+        _refuse(f"{name} is not contiguous")
+
+
+class _on:
+    """The device and stream on which a call allocates and enqueues: those of its tensors, or the caller's stream."""
+
+    def __init__(self, device, stream):
+        self.switch = None
+        if device.type != "cuda":
+            _refuse(f"the tensors are on {device}, not on a GPU")
+        if stream is not None:
+            if stream.device != device:
+                _refuse(f"the stream is on {stream.device}, the tensors are on {device}")
+            self.switch = torch.cuda.stream(stream)
+        elif device.index != torch.cuda.current_device():
+            self.switch = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.switch is not None:
+            self.switch.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *error):
+        if self.switch is not None:
+            self.switch.__exit__(*error)
+
+
+class KvCache:
+    """A paged cache: k and v [n_pages, n_kv_heads, page_size, head_dim], contiguous, bf16 or float32."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 4:
+            _refuse(f"k: {tuple(k.shape)}, expected [n_pages, n_kv_heads, page_size, head_dim]")
+        _tensor("k", k, k.dtype, k.shape, k.device)
+        _tensor("v", v, k.dtype, k.shape, k.device)
+        self.k, self.v = k, v
+        self.dtype, self.device = k.dtype, k.device
+        n_pages, self.n_kv_heads, page_size, self.head_dim = k.shape
+        self.code = _dtype_code(k)
+        self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), n_pages, page_size, self.n_kv_heads, self.head_dim, self.code)
+        self._ref = ctypes.pointer(self._struct)
+
+
+class LogitRules:
+    """How logits are adjusted ahead of a draw: bias (float32 [vocab] or None), then penalties, then the temperature."""
+
+    def __init__(self, repetition: float = 1.0, presence: float = 0.0, frequency: float = 0.0, temperature: float = 1.0, bias=None):
+        if bias is not None:
+            _tensor("bias", bias, torch.float32, (None,), bias.device)
+        self.bias = bias
+        self._struct = _LogitRulesStruct(repetition, presence, frequency, temperature, None if bias is None else bias.data_ptr())
+        self._ref = ctypes.pointer(self._struct)
+
+    def _fits(self, vocab, device):
+        if self.bias is not None:
+            _tensor("bias", self.bias, torch.float32, (vocab,), device)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _token_rows(name, t, cache, heads):
+    """Tokens of `heads` heads with any stride from token to token; returns that stride."""
+    d = cache.head_dim
+    _tensor(name, t, cache.dtype, (None, heads, d), cache.device, contiguous=False)
+    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+        _refuse(f"{name}: the heads of a token are not contiguous (strides {t.stride()})")
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def sp_attn_cache_append(cache: KvCache, k, v, tables, lens, rope_base: float, q=None, new_lens: Optional[Sequence[int]] = None,
+                         pos_base=None, q_out=None, k_out=None, lens_out=None, stream=None):
+    """Append the rotated keys k and the values v of new tokens [T, n_kv_heads, d] to the cache.  Sequence s brings new_lens[s] tokens
+    (host integers; None: one each), which become its tokens lens[s], lens[s] + 1, ... in the pages tables[s].  q [T, n_q_heads, d] is rotated
+    along (into q_out), and the rotated keys also go to k_out where that is given.  k, v and q may be parts of one
+    projection's output.  Returns (q_out, lens_out); q_out is None without q."""
+    lib = load_library()
+    dev, hkv = cache.device, cache.n_kv_heads
+    ks, vs = _token_rows("k", k, cache, hkv), _token_rows("v", v, cache, hkv)
+    T, n_seqs = k.shape[0], lens.shape[0]
+    counts = None if new_lens is None else _i32(new_lens)
+    if v.shape[0] != T or T != (n_seqs if new_lens is None else sum(new_lens)) or (new_lens is not None and len(new_lens) != n_seqs):
+        _refuse(f"{T} keys, {v.shape[0]} values and {n_seqs} sequences do not fit the new tokens")
+    _tensor("lens", lens, torch.int32, (n_seqs,), dev)
+    _tensor("tables", tables, torch.int32, (n_seqs, None), dev)
+    if pos_base is not None:
+        _tensor("pos_base", pos_base, torch.int32, (n_seqs,), dev)
+    hq, qs = 0, 0
+    if q is not None:
+        hq = q.shape[1]
+        qs = _token_rows("q", q, cache, hq)
+        if q.shape[0] != T:
+            _refuse(f"q has {q.shape[0]} tokens, k has {T}")
+        if q_out is not None:
+            _tensor("q_out", q_out, cache.dtype, (T, hq, cache.head_dim), dev)
+    elif q_out is not None:
+        _refuse("q_out without q")
+    if k_out is not None:
+        _tensor("k_out", k_out, cache.dtype, (T, hkv, cache.head_dim), dev)
+    if lens_out is not None:
+        _tensor("lens_out", lens_out, torch.int32, (n_seqs,), dev)
+    with _on(dev, stream) as s:
+        if q is not None and q_out is None:
+            q_out = torch.empty((T, hq, cache.head_dim), dtype=cache.dtype, device=dev)
+        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
+        if T == 0:                     # nothing to store; the pointers of empty tensors are null
+            lens_out.copy_(lens)
+            return q_out, lens_out
+        _check(lib.sp_attn_cache_append(cache._ref, _ptr(q), qs, _ptr(q_out), hq, k.data_ptr(), ks, _ptr(k_out), v.data_ptr(), vs, n_seqs, counts,
+                                        tables.data_ptr(), tables.shape[1], lens.data_ptr(), _ptr(pos_base), lens_out.data_ptr(),
+                                        float(rope_base), s))
+    return q_out, lens_out
+
+
+def decode_workspace_bytes(n_groups: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype_code: int) -> int:
+    return load_library().sp_attn_decode_workspace_bytes(n_groups, n_seqs, n_q_heads, n_kv_heads, head_dim, dtype_code)
+
+
+def _pages_of(name, tables, lens, rows, device):
+    """(pointer, width, pointer of the lengths) of a table, which may be None or have no columns."""
+    if lens is not None:
+        _tensor(name + "_lens", lens, torch.int32, (rows,), device)
+    if tables is None:
+        return None, 0, _ptr(lens)
+    _tensor(name + "_tables", tables, torch.int32, (rows, None), device)
+    return (tables.data_ptr() if tables.shape[1] else None), tables.shape[1], _ptr(lens)
+
+
+def sp_attn_decode(cache: KvCache, q, Gs: Optional[Sequence[int]], prompt_tables, prompt_lens, resp_tables, resp_lens, softmax_scale: float,
+                   o=None, lse=None, workspace=None, stream=None):
+    """Attention of one new token per sequence.  Row s of q [n_seqs, n_q_heads, d] attends to its group's prompt and to the first
+    resp_lens[s] tokens of its own.  Gs: sequences of each group (host integers), None: one each.  prompt_tables [n_groups, width] and
+    prompt_lens may be None (no shared prompts).  Returns (o, lse [n_q_heads, n_seqs])."""
+    lib = load_library()
+    dev = cache.device
+    _tensor("q", q, cache.dtype, (None, None, cache.head_dim), dev)
+    n_seqs, hq, d = q.shape
+    n_groups = n_seqs if Gs is None else len(Gs)
+    pt, pw, pl = _pages_of("prompt", prompt_tables, prompt_lens, n_groups, dev)
+    rt, rw, rl = _pages_of("resp", resp_tables, resp_lens, n_seqs, dev)
+    if o is not None:
+        _tensor("o", o, cache.dtype, (n_seqs, hq, d), dev)
+    if lse is not None:
+        _tensor("lse", lse, torch.float32, (hq, n_seqs), dev)
+    with _on(dev, stream) as s:
+        o = torch.empty_like(q) if o is None else o
+        lse = torch.empty((hq, n_seqs), dtype=torch.float32, device=dev) if lse is None else lse
+        if workspace is None:
+            need = lib.sp_attn_decode_workspace_bytes(n_groups, n_seqs, hq, cache.n_kv_heads, d, cache.code)
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _check(lib.sp_attn_decode(cache._ref, q.data_ptr(), o.data_ptr(), lse.data_ptr(), hq, n_groups, n_seqs, None if Gs is None else _i32(Gs),
+                                  pt, pw, pl if pw else None, rt, rw, rl, softmax_scale, workspace.data_ptr(), workspace.numel(), s))
+    return o, lse
+
+
+def _logit_rows(name, t, shape, dtype, device):
+    """Rows of logits with any stride from row to row; returns that stride."""
+    _tensor(name, t, dtype, shape, device, contiguous=False)
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        _refuse(f"{name}: the elements of a row are not contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _mask_rows(mask, rows, device):
+    if mask is None:
+        return None, 0
+    if mask.dtype not in (torch.int32, torch.uint32):
+        _refuse(f"mask: {mask.dtype}, expected int32 or uint32 words")
+    _tensor("mask", mask, mask.dtype, (rows, None), device)
+    return mask.data_ptr(), mask.shape[1]
+
+
+def sp_attn_adjust_logits(logits, rules: LogitRules, Gs: Optional[Sequence[int]], prompt_tokens, prompt_lens, resp_tokens, resp_lens,
+                          mask=None, out=None, stream=None):
+    """Adjusted logits [n_seqs, vocab] of one row per sequence.  Its history is the first prompt_lens[g] ids of its group's row of
+    prompt_tokens [n_groups, .] and the first resp_lens[s] ids of its row of resp_tokens [n_seqs, .] (either pair may be None).  mask [n_seqs, words]:
+    bit v % 32 of word v / 32 allows id v.  ``out`` may be logits itself."""
+    lib = load_library()
+    dev = logits.device
+    n_seqs, vocab = logits.shape
+    n_groups = n_seqs if Gs is None else len(Gs)
+    stride = _logit_rows("logits", logits, (n_seqs, vocab), logits.dtype, dev)
+    rules._fits(vocab, dev)
+    mp, ms = _mask_rows(mask, n_seqs, dev)
+
+    def tokens_of(name, tokens, lens, rows):
+        if tokens is None and lens is None:
+            return None, 0, None
+        if tokens is None or lens is None:
+            _refuse(f"{name}_tokens and {name}_lens go together")
+        _tensor(name + "_tokens", tokens, torch.int32, (rows, None), dev)
+        _tensor(name + "_lens", lens, torch.int32, (rows,), dev)
+        return (tokens.data_ptr(), tokens.shape[1], lens.data_ptr()) if tokens.shape[1] else (None, 0, None)
+
+    history = (*tokens_of("prompt", prompt_tokens, prompt_lens, n_groups), *tokens_of("resp", resp_tokens, resp_lens, n_seqs))
+    with _on(dev, stream) as s:
+        out = torch.empty((n_seqs, vocab), dtype=logits.dtype, device=dev) if out is None else out
+        out_stride = _logit_rows("out", out, (n_seqs, vocab), logits.dtype, dev)
+        _check(lib.sp_attn_adjust_logits(logits.data_ptr(), stride, out.data_ptr(), out_stride, vocab, rules._ref, mp, ms, n_groups, n_seqs,
+                                         None if Gs is None else _i32(Gs), *history, _dtype_code(logits), s))
+    return out
+
+
+def _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace):
+    """What the forward and the backward check alike; returns the mask's pointer and stride and the workspace's size where it is to be made."""
+    dev = logits.device
+    T, V = logits.shape
+    _tensor("logits", logits, logits.dtype, (T, V), dev)
+    if T != sum(prompt_lens) + sum(resp_lens_flat):
+        _refuse(f"logits have {T} rows, the pack has {sum(prompt_lens) + sum(resp_lens_flat)}")
+    _tensor("labels", labels, torch.int32, (T,), dev)
+    _tensor("tokens", tokens, torch.int32, (T,), dev)
+    rules._fits(V, dev)
+    mp, ms = _mask_rows(mask, T, dev)
+    need = 0
+    if workspace is None:
+        need = max(256, load_library().sp_attn_adjusted_logprob_workspace_bytes(T, len(prompt_lens), len(resp_lens_flat), V))
+    return mp, ms, need
+
+
+def sp_attn_adjusted_logprob_fwd(logits, labels, tokens, rules: LogitRules, prompt_lens: Sequence[int], Gs: Sequence[int],
+                                 resp_lens_flat: Sequence[int], mask=None, flags: int = 0, logp=None, lse=None, workspace=None, stream=None):
+    """Log-probability of labels[t] under the adjusted distribution at every response row t of logits [T, V]; tokens [T] are the pack's ids.
+    mask [T, words] as in sp_attn_adjust_logits.  Returns (logp, lse); prompt rows keep whatever the output tensors held (zeros when
+    allocated here)."""
+    lib = load_library()
+    dev = logits.device
+    mp, ms, need = _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace)
+    T, V = logits.shape
+    for name, t in (("logp", logp), ("lse", lse)):
+        if t is not None:
+            _tensor(name, t, torch.float32, (T,), dev)
+    with _on(dev, stream) as s:
+        logp = torch.zeros(T, dtype=torch.float32, device=dev) if logp is None else logp
+        lse = torch.zeros(T, dtype=torch.float32, device=dev) if lse is None else lse
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
+        _check(lib.sp_attn_adjusted_logprob_fwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), V,
+                                                rules._ref, mp, ms, len(prompt_lens), _i32(prompt_lens), _i32(Gs), _i32(resp_lens_flat),
+                                                _dtype_code(logits), flags, workspace.data_ptr(), workspace.numel(), s))
+    return logp, lse
+
+
+def sp_attn_adjusted_logprob_bwd(logits, labels, tokens, lse, g, rules: LogitRules, prompt_lens: Sequence[int], Gs: Sequence[int],
+                                 resp_lens_flat: Sequence[int], mask=None, flags: int = 0, dlogits=None, workspace=None, stream=None):
+    """Gradient with respect to the raw logits of sum_t g[t] logp[t], logp of sp_attn_adjusted_logprob_fwd.  Prompt rows of dlogits are zero
+    when it is allocated here, otherwise they keep what they held (SP_FLAG_ZERO_PROMPT_ROWS: zero).  ``dlogits`` may be logits itself."""
+    lib = load_library()
+    dev = logits.device
+    mp, ms, need = _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace)
+    T, V = logits.shape
+    _tensor("lse", lse, torch.float32, (T,), dev)
+    _tensor("g", g, torch.float32, (T,), dev)
+    if dlogits is None:
+        flags |= SP_FLAG_ZERO_PROMPT_ROWS
+    else:
+        _tensor("dlogits", dlogits, logits.dtype, (T, V), dev)
+    with _on(dev, stream) as s:
+        dlogits = torch.empty_like(logits) if dlogits is None else dlogits
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
+        _check(lib.sp_attn_adjusted_logprob_bwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), lse.data_ptr(), g.data_ptr(),
+                                                dlogits.data_ptr(), V, rules._ref, mp, ms, len(prompt_lens), _i32(prompt_lens), _i32(Gs),
+                                                _i32(resp_lens_flat), _dtype_code(logits), flags, workspace.data_ptr(), workspace.numel(), s))
+    return dlogits

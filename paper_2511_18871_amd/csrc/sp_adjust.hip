@@ -1,0 +1,454 @@
+// Adjusted logits: what a sampler does to a row of logits before it draws, and log-probabilities under the distribution
+// that it really drew from.  With h_v = id v occurs in the row's history (the prompt of its group and the tokens of
+// its response ahead of it) and c_v = how often among the latter, an element goes through
+//   a = z_v + bias_v,   b = h_v ? (a > 0 ? a / rho : a rho) : a,   d = b - frequency c_v - presence [c_v > 0],
+//   z'_v = mask bit v ? d / T : -inf.
+//  adjust        z' of one row per sequence
+//  logprob fwd   logp = z'_y - L, L = ln sum_v e^(z'_v), at every response row of a pack; z' is never stored
+//  logprob bwd   dz_v = g (1[v = y] - e^(z'_v - L)) dz'_v / dz_v, the slope being (h_v ? (a > 0 ? 1 / rho : rho) : 1) / T, 0 where masked
+//
+// The history reaches a row as counters in LDS, 16 bits per id: bit 15 "in the prompt", below it the occurrences in the
+// response (they stop at 32767).  A workgroup takes a slice of the vocabulary, so that its counters fit, and a run of rows; the
+// counters are filled once, and from row to row only the tokens between them are added.  Integer atomics: the order does not matter.
+#include "sp_common.hpp"
+#include "sp_launch.hpp"
+#include <type_traits>
+
+namespace sp {
+namespace {
+
+constexpr int AT = 512;                    // threads of a workgroup
+constexpr int AWAVES = AT / 64;
+constexpr int SLICE_MAX = 32768;           // ids of a slice at most: 64 KB of counters, two workgroups to a CU
+constexpr float A_LOWEST = -3.402823466e38f;
+
+// eight consecutive elements, at any alignment of their own type
+template <typename T> struct Pack8;
+template <> struct Pack8<__bf16> {
+    typedef __bf16 vec __attribute__((ext_vector_type(8), aligned(2)));
+    vec x;
+    __device__ __forceinline__ void load(const __bf16* p) { x = *reinterpret_cast<const vec*>(p); }
+    __device__ __forceinline__ void store(__bf16* p) const { *reinterpret_cast<vec*>(p) = x; }
+};
+template <> struct Pack8<float> {
+    typedef float half __attribute__((ext_vector_type(4), aligned(4)));
+    typedef float vec __attribute__((ext_vector_type(8)));
+    vec x;
+    __device__ __forceinline__ void load(const float* p) {
+        const half a = *reinterpret_cast<const half*>(p), b = *reinterpret_cast<const half*>(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[e + 4] = b[e]; }
+    }
+    __device__ __forceinline__ void store(float* p) const {
+        half a, b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { a[e] = x[e]; b[e] = x[e + 4]; }
+        *reinterpret_cast<half*>(p) = a;
+        *reinterpret_cast<half*>(p + 4) = b;
+    }
+};
+
+// A slice [v0, v0 + n) of the vocabulary and the counters of its ids (two to a word)
+struct Slice { int v0, n; unsigned* counts; };
+
+__device__ __forceinline__ Slice slice_of(int index, int len, int vocab, unsigned* lds) {
+    const int v0 = index * len;
+    return Slice{v0, min(len, vocab - v0), lds};
+}
+
+__device__ __forceinline__ void clear_counts(const Slice& s) {
+    for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) reinterpret_cast<i32x4*>(s.counts)[i] = i32x4{0, 0, 0, 0};
+}
+
+// adds `count` tokens of the prompt, or of the response; those outside the slice (or the vocabulary) are passed over
+__device__ __forceinline__ void add_prompt(const Slice& s, const int* tokens, int count) {
+    for (int i = threadIdx.x; i < count; i += AT) {
+        const unsigned k = (unsigned)tokens[i] - (unsigned)s.v0;
+        if (k < (unsigned)s.n) atomicOr(&s.counts[k >> 1], 0x8000u << (16 * (k & 1)));
+    }
+}
+__device__ __forceinline__ void add_generated(const Slice& s, const int* tokens, int count, bool may_saturate) {
+    for (int i = threadIdx.x; i < count; i += AT) {
+        const unsigned k = (unsigned)tokens[i] - (unsigned)s.v0;
+        if (k >= (unsigned)s.n) continue;
+        const int sh = 16 * (k & 1);
+        unsigned* const w = &s.counts[k >> 1];
+        if (!may_saturate) { atomicAdd(w, 1u << sh); continue; }
+        unsigned have = *w;
+        while (((have >> sh) & 0x7fffu) != 0x7fffu) {
+            const unsigned seen = atomicCAS(w, have, have + (1u << sh));
+            if (seen == have) break;
+            have = seen;
+        }
+    }
+}
+
+// Eight elements of a row after bias, penalties and mask, ahead of the division by the temperature; slope (SLOPE): their
+// derivative with respect to the raw elements, but for the temperature.
+template <bool SLOPE, bool HIST>
+__device__ __forceinline__ void adjust8(float (&a)[8], float (&slope)[8], const AdjustRules& r, i32x4 counts, unsigned bits) {
+    if constexpr (SLOPE)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) slope[e] = 1.f;
+    if constexpr (HIST) {
+        if ((counts[0] | counts[1]) | (counts[2] | counts[3])) {       // some of the eight are in the history
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned c = ((unsigned)counts[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+                const float f = c ? (a[e] > 0.f ? r.inv_repetition : r.repetition) : 1.f;
+                const float n = (float)(c & 0x7fffu);
+                a[e] = a[e] * f - (n * r.frequency + (n > 0.f ? r.presence : 0.f));
+                if constexpr (SLOPE) slope[e] = f;
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bool off = !(bits >> e & 1);
+        a[e] = off ? -INFINITY : a[e];
+        if constexpr (SLOPE) slope[e] = off ? 0.f : slope[e];
+    }
+}
+
+// Visits the slice of one row in vectors of eight, UNROLL of them in flight per thread: f(values, counts, mask bits, index
+// of the first element within the slice, how many of them there are).
+template <typename T, bool HIST, int UNROLL, typename F>
+__device__ __forceinline__ void for_vectors(const T* row, const uint8_t* mask, const AdjustRules& r, const Slice& s, F f) {
+    const int vecs = s.n / 8;
+    const T* const z = row + s.v0;
+    const float* const bias = r.bias ? r.bias + s.v0 : nullptr;
+    const uint8_t* const bits = mask ? mask + s.v0 / 8 : nullptr;
+    auto one = [&](const Pack8<T>& x, const Pack8<float>& b, unsigned m, int i) {
+        float a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = (float)x.x[e] + b.x[e];
+        i32x4 c{0, 0, 0, 0};
+        if constexpr (HIST) c = reinterpret_cast<const i32x4*>(s.counts)[i];
+        f(a, c, m, 8 * i, 8);
+    };
+    int i = threadIdx.x;
+    for (; i + (UNROLL - 1) * AT < vecs; i += UNROLL * AT) {
+        Pack8<T> x[UNROLL];
+        Pack8<float> b[UNROLL];
+        unsigned m[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            x[u].load(z + 8 * (i + u * AT));
+            if (bias) b[u].load(bias + 8 * (i + u * AT)); else b[u].x = (typename Pack8<float>::vec)(0.f);
+            m[u] = bits ? bits[i + u * AT] : 0xffu;
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) one(x[u], b[u], m[u], i + u * AT);
+    }
+    for (; i < vecs; i += AT) {
+        Pack8<T> x;
+        Pack8<float> b;
+        x.load(z + 8 * i);
+        if (bias) b.load(bias + 8 * i); else b.x = (typename Pack8<float>::vec)(0.f);
+        one(x, b, bits ? bits[i] : 0xffu, i);
+    }
+    if (i == vecs && (s.n & 7)) {                       // the vocabulary's last, incomplete vector
+        float a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = 8 * vecs + e < s.n ? (float)z[8 * vecs + e] + (bias ? bias[8 * vecs + e] : 0.f) : -INFINITY;
+        i32x4 c{0, 0, 0, 0};
+        if constexpr (HIST) c = reinterpret_cast<const i32x4*>(s.counts)[vecs];
+        f(a, c, bits ? bits[vecs] : 0xffu, 8 * vecs, s.n & 7);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8], int n) {
+    if (n == 8) {
+        Pack8<T> y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y.x[e] = (T)x[e];
+        y.store(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (e < n) p[e] = (T)x[e];
+    }
+}
+
+struct AdjustArgs {
+    const void* logits; void* out; int64_t stride, out_stride;
+    const uint8_t* mask; int64_t mask_stride;            // bytes
+    const int* prompt_tokens; const int* prompt_lens; int64_t prompt_stride;
+    const int* resp_tokens; const int* resp_lens; int64_t resp_stride;
+    AdjustRules rules;
+    int first, n_groups, vocab, slice_len;               // first: sequence of the launch's first row
+};
+
+// One workgroup per (sequence, slice).  words[g] = first sequence of the launch's group g, ahead of one word past the last.
+template <typename T, bool HIST>
+__global__ __launch_bounds__(AT) void adjust_kernel(TabArg starts, AdjustArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned lds[];
+    const int seq = a.first + blockIdx.y;
+    const Slice s = slice_of(blockIdx.x, a.slice_len, a.vocab, lds);
+    if constexpr (HIST) {
+        clear_counts(s);
+        __syncthreads();
+        if (a.prompt_tokens) {
+            const int* const w = table_of(starts);
+            int lo = 0, hi = a.n_groups;
+            while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (w[mid] <= seq) lo = mid; else hi = mid; }
+            const int g = w[a.n_groups + 1] + lo;
+            const int n = max(0, (int)min((int64_t)a.prompt_lens[g], a.prompt_stride));
+            add_prompt(s, a.prompt_tokens + g * a.prompt_stride, n);
+        }
+        if (a.resp_tokens) {
+            const int n = max(0, (int)min((int64_t)a.resp_lens[seq], a.resp_stride));
+            add_generated(s, a.resp_tokens + seq * a.resp_stride, n, n > 0x7fff);
+        }
+        __syncthreads();
+    }
+    T* const out = (T*)a.out + seq * a.out_stride + s.v0;
+    for_vectors<T, HIST, 2>((const T*)a.logits + seq * a.stride, a.mask ? a.mask + seq * a.mask_stride : nullptr, a.rules, s,
+        [&](float (&x)[8], i32x4 c, unsigned bits, int at, int n) {
+            float none[8];
+            adjust8<false, HIST>(x, none, a.rules, c, bits);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= a.rules.inv_temperature;
+            store8(out + at, x, n);
+        });
+}
+
+struct LogprobArgs {
+    const void* logits; const int* labels; const int* tokens;
+    const uint8_t* mask; int64_t mask_stride;            // bytes
+    float* logp; float* lse;                             // forward out; backward: lse in
+    const float* g; void* dlogits;
+    uint32_t* tag;                                       // forward: the workspace's tag block, cleared as by every call that writes there
+    float* parts;                                        // forward: (max, sum) per row, slice and wave, then a label's z' per row
+    AdjustRules rules;
+    int vocab, slice_len, n_slices, run, own, zero_prompt;
+};
+
+// (m, s) stands for s e^(m / T): differences are taken ahead of their scaling, so that they are exact at any magnitude, and start
+// from the lowest finite value, so that elements of -inf contribute 0.
+__device__ __forceinline__ void scaled_merge(float& m, float& s, float m2, float s2, float c) {
+    const float mn = fmaxf(m, m2);
+    s = s * __builtin_amdgcn_exp2f((m - mn) * c) + s2 * __builtin_amdgcn_exp2f((m2 - mn) * c);
+    m = mn;
+}
+__device__ __forceinline__ float log_of(float m, float s, float inv_t) { return m * inv_t + __logf(s); }
+// no id allowed: L = -inf, and the log-probability of any label is -inf
+__device__ __forceinline__ float label_logp(float z, float L) { return L == -INFINITY ? -INFINITY : z - L; }
+
+// One workgroup per (slice, run of rows of the pack).
+template <typename T, bool HIST, bool BWD>
+__global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, LogprobArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned lds[];
+    const int* const tab = table_of(table);
+    const Slice s = slice_of(blockIdx.x, a.slice_len, a.vocab, lds);
+    const int T_total = tab[1], t0 = blockIdx.y * a.run, t1 = min(t0 + a.run, T_total);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const float c = a.rules.inv_temperature * LOG2E;
+    if (!BWD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) a.tag[threadIdx.x] = 0u;
+    int seg_end = t0, counted = 0;
+    bool prompt = false, may_saturate = false;
+    for (int t = t0; t < t1; ++t) {
+        if (t == seg_end) {                              // another segment: its prompt, its history up to this row
+            const GroupDesc gd = load_group(tab, find_group_of_token(tab, t));
+            const int local = t - gd.tok_base;
+            prompt = local < gd.Lp;
+            if (prompt) {
+                seg_end = gd.tok_base + gd.Lp;
+            } else {
+                seg_end = gd.tok_base + sp::seg_end(gd, local);
+                counted = gd.tok_base + seg_start(gd, local);
+                may_saturate = seg_end - counted > 0x7fff;
+                if constexpr (HIST) {
+                    __syncthreads();
+                    clear_counts(s);
+                    __syncthreads();
+                    add_prompt(s, a.tokens + gd.tok_base, gd.Lp);
+                }
+            }
+        }
+        if (prompt) {
+            if (BWD && a.zero_prompt) {
+                T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
+                const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) store8(out + 8 * i, zero, min(8, s.n - 8 * i));
+            }
+            continue;
+        }
+        if constexpr (HIST) {
+            __syncthreads();                             // every wave is through with the row before
+            add_generated(s, a.tokens + counted, t + a.own - counted, may_saturate);
+            counted = t + a.own;
+            __syncthreads();
+        }
+        const T* const row = (const T*)a.logits + (int64_t)t * a.vocab;
+        const uint8_t* const mask = a.mask ? a.mask + t * a.mask_stride : nullptr;
+        const int label = a.labels[t];
+        if constexpr (BWD) {
+            T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
+            const float L = a.lse[t], g = L == -INFINITY ? 0.f : a.g[t], Lf = L == -INFINITY ? 0.f : L;
+            const float gt = g * a.rules.inv_temperature;
+            for_vectors<T, HIST, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) {
+                float slope[8];
+                adjust8<true, HIST>(x, slope, a.rules, cnt, bits);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float p = __builtin_amdgcn_exp2f((x[e] * a.rules.inv_temperature - Lf) * LOG2E);
+                    x[e] = gt * slope[e] * ((s.v0 + at + e == label ? 1.f : 0.f) - p);
+                }
+                store8(out + at, x, n);
+            });
+        } else {
+            float m = A_LOWEST, sum = 0.f, z_label = -INFINITY;
+            bool has = false;
+            for_vectors<T, HIST, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) {
+                float none[8];
+                adjust8<false, HIST>(x, none, a.rules, cnt, bits);
+                float mx = x[0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+                const float mn = fmaxf(m, mx);
+                float part = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part += __builtin_amdgcn_exp2f((x[e] - mn) * c);
+                sum = sum * __builtin_amdgcn_exp2f((m - mn) * c) + part;
+                m = mn;
+                const int k = label - s.v0 - at;
+                if (k >= 0 && k < n) {
+                    has = true;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) if (e == k) z_label = x[e] * a.rules.inv_temperature;
+                }
+            });
+            for (int o = 32; o >= 1; o >>= 1) {
+                const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(sum, o, 64);
+                scaled_merge(m, sum, m2, s2, c);
+            }
+            float* const labels_z = a.parts + (int64_t)T_total * a.n_slices * AWAVES * 2;
+            if (has) labels_z[t] = z_label;
+            if (lane == 0) {
+                float* const p = a.parts + (((int64_t)t * a.n_slices + blockIdx.x) * AWAVES + wave) * 2;
+                p[0] = m;
+                p[1] = sum;
+            }
+        }
+    }
+}
+
+// One wave per row joins the row's slices.
+__global__ __launch_bounds__(256) void logprob_join_kernel(TabArg table, const int* __restrict__ labels, const float* __restrict__ parts,
+                                                           float* __restrict__ logp, float* __restrict__ lse, int per_row, int vocab, float inv_t) {
+    const int* const tab = table_of(table);
+    const int T_total = tab[1], t = blockIdx.x * 4 + (threadIdx.x >> 6), l = threadIdx.x & 63;
+    if (t >= T_total) return;
+    const GroupDesc gd = load_group(tab, find_group_of_token(tab, t));
+    if (t - gd.tok_base < gd.Lp) return;
+    const float c = inv_t * LOG2E;
+    float m = A_LOWEST, s = 0.f;
+    for (int i = l; i < per_row; i += 64) {
+        const float* const p = parts + ((int64_t)t * per_row + i) * 2;
+        scaled_merge(m, s, p[0], p[1], c);
+    }
+    for (int o = 32; o >= 1; o >>= 1) {
+        const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
+        scaled_merge(m, s, m2, s2, c);
+    }
+    if (l == 0) {
+        const float L = log_of(m, s, inv_t);
+        const int y = labels[t];
+        lse[t] = L;
+        logp[t] = y >= 0 && y < vocab ? label_logp(parts[(int64_t)T_total * per_row * 2 + t], L) : -INFINITY;
+    }
+}
+
+template <typename F> void with_kernel(bool f32, bool hist, F f) {
+    auto typed = [&](auto elem) { if (hist) f(elem, std::true_type{}); else f(elem, std::false_type{}); };
+    if (f32) typed(float{}); else typed(__bf16{});
+}
+
+bool uses_history(const AdjustRules& r) { return r.repetition != 1.f || r.presence != 0.f || r.frequency != 0.f; }
+
+}  // namespace
+
+int adjust_slices(int64_t vocab) { return (int)((vocab + SLICE_MAX - 1) / SLICE_MAX); }
+static int slice_length(int64_t vocab, int slices) { return (int)(((vocab + slices - 1) / slices + 7) / 8 * 8); }
+
+size_t adjust_parts_bytes(int64_t total_tokens, int64_t vocab) {
+    return (size_t)total_tokens * ((size_t)adjust_slices(vocab) * AWAVES * 8 + 4);
+}
+
+hipError_t launch_adjust_logits(const void* logits, int64_t stride, void* out, int64_t out_stride, int64_t vocab, const AdjustRules& rules,
+                                const uint32_t* mask, int64_t mask_stride, int n_groups, const int32_t* Gs,
+                                const int* prompt_tokens, int prompt_stride, const int* prompt_lens,
+                                const int* resp_tokens, int resp_stride, const int* resp_lens, bool f32, hipStream_t s) {
+    AdjustArgs a{};
+    a.logits = logits; a.out = out; a.stride = stride; a.out_stride = out_stride;
+    a.mask = (const uint8_t*)mask; a.mask_stride = mask_stride * 4;
+    a.prompt_tokens = prompt_stride > 0 ? prompt_tokens : nullptr; a.prompt_lens = prompt_lens; a.prompt_stride = prompt_stride;
+    a.resp_tokens = resp_stride > 0 ? resp_tokens : nullptr; a.resp_lens = resp_lens; a.resp_stride = resp_stride;
+    a.rules = rules;
+    a.vocab = (int)vocab;
+    const int slices = adjust_slices(vocab);
+    a.slice_len = slice_length(vocab, slices);
+    const bool hist = uses_history(rules) && (a.prompt_tokens || a.resp_tokens);
+    const size_t lds = hist ? (size_t)a.slice_len * 2 : 0;
+    // the groups of a launch are a kernel argument, and its rows a grid's second dimension: larger calls are several launches
+    constexpr int MAX_GROUPS = ARG_WORDS - 2, MAX_ROWS = 32768;
+    int seq = 0, g = 0, left = 0;                        // left: sequences of group g that the launches so far have not served
+    while (true) {
+        while (g < n_groups && left == 0) { left = Gs ? Gs[g] : 1; if (left == 0) ++g; }
+        if (g >= n_groups) break;
+        TabArg starts{};
+        const int g0 = g;
+        int n = 0, rows = 0;
+        while (g < n_groups && n < MAX_GROUPS && rows < MAX_ROWS) {
+            starts.words[n++] = seq + rows;
+            const int take = left < MAX_ROWS - rows ? left : MAX_ROWS - rows;
+            rows += take;
+            left -= take;
+            if (left > 0) break;
+            ++g;
+            if (g < n_groups) left = Gs ? Gs[g] : 1;
+        }
+        starts.words[n] = seq + rows;
+        starts.words[n + 1] = g0;
+        a.first = seq; a.n_groups = n;
+        with_kernel(f32, hist, [&](auto elem, auto with) {
+            hipLaunchKernelGGL((adjust_kernel<decltype(elem), decltype(with)::value>), dim3((unsigned)slices, (unsigned)rows), dim3(AT), lds, s, starts, a);
+        });
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        seq += rows;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labels, const int* tokens, const uint32_t* mask, int64_t mask_stride,
+                                   float* logp, float* lse, const float* g, void* dlogits, const AdjustRules& rules, const TabArg& tab,
+                                   int64_t total_tokens, int64_t vocab, bool own_token, bool zero_prompt, float* parts, uint32_t* tag, bool f32,
+                                   hipStream_t s) {
+    LogprobArgs a{};
+    a.logits = logits; a.labels = labels; a.tokens = tokens; a.mask = (const uint8_t*)mask; a.mask_stride = mask_stride * 4;
+    a.logp = logp; a.lse = lse; a.g = g; a.dlogits = dlogits; a.parts = parts; a.tag = tag; a.rules = rules;
+    a.vocab = (int)vocab;
+    a.n_slices = adjust_slices(vocab);
+    a.slice_len = slice_length(vocab, a.n_slices);
+    a.own = own_token; a.zero_prompt = zero_prompt;
+    const int64_t run = total_tokens * a.n_slices / 1024;
+    a.run = (int)(run < 1 ? 1 : run > 16 ? 16 : run);
+    while ((total_tokens + a.run - 1) / a.run > 65535) a.run *= 2;
+    const bool hist = uses_history(rules);
+    const size_t lds = hist ? (size_t)a.slice_len * 2 : 0;
+    const dim3 grid((unsigned)a.n_slices, (unsigned)((total_tokens + a.run - 1) / a.run));
+    with_kernel(f32, hist, [&](auto elem, auto with) {
+        typedef decltype(elem) T;
+        constexpr bool H = decltype(with)::value;
+        if (bwd) hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, true>), grid, dim3(AT), lds, s, tab, a);
+        else hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, false>), grid, dim3(AT), lds, s, tab, a);
+    });
+    if (!bwd)
+        hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)((total_tokens + 3) / 4)), dim3(256), 0, s, tab, labels, parts, logp, lse,
+                           a.n_slices * AWAVES, (int)vocab, rules.inv_temperature);
+    return hipGetLastError();
+}
+
+}  // namespace sp

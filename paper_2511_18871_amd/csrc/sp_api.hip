@@ -9,6 +9,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <exception>
 #include <vector>
 
 // Device memory of the entry point that takes no workspace (sp_attn_bwd_batched_static): segment
@@ -640,6 +641,225 @@ sp_status sp_attn_grpo_loss(const float* logp, const float* logp_old, const floa
                                    (int)L.total_responses, nonempty, eps_low, eps_high, beta, (hipStream_t)stream);
     if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
     return SP_OK;
+}
+
+namespace {
+// What the rollout calls have in common: a cache's geometry, and how its sequences form groups
+sp_status check_cache(const sp_kv_cache* c, sp::KvCache& out) {
+    if (!c) return fail(SP_ERR_INVALID_ARG, "cache is NULL");
+    if (!c->k || !c->v) return fail(SP_ERR_INVALID_ARG, "a cache pointer is NULL");
+    if (misaligned(c->k) || misaligned(c->v)) return fail(SP_ERR_INVALID_ARG, "cache pointer is not 16-byte aligned");
+    if (c->n_pages < 1 || c->n_pages > 0x7fffffffLL) return fail(SP_ERR_INVALID_ARG, "n_pages=%lld", (long long)c->n_pages);
+    if (c->n_kv_heads < 1) return fail(SP_ERR_INVALID_ARG, "n_kv_heads=%d", c->n_kv_heads);
+    if (c->dtype != SP_BF16 && c->dtype != SP_F32) return fail(SP_ERR_UNSUPPORTED, "unknown dtype %d", (int)c->dtype);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(SP_ERR_UNSUPPORTED, "head_dim=%d (64 or 128)", c->head_dim);
+    int log_page = 4;
+    while (log_page <= 8 && (1 << log_page) != c->page_size) ++log_page;
+    if (log_page > 8) return fail(SP_ERR_UNSUPPORTED, "page_size=%d (16, 32, 64, 128 or 256)", c->page_size);
+    out = sp::KvCache{c->k, c->v, c->n_pages, log_page, c->n_kv_heads, c->head_dim, c->dtype == SP_F32};
+    return SP_OK;
+}
+sp_status check_members(int32_t n_groups, int32_t n_seqs, const int32_t* Gs) {
+    if (n_groups < 1 || n_seqs < 1) return fail(SP_ERR_INVALID_ARG, "n_groups=%d, n_seqs=%d", n_groups, n_seqs);
+    if (!Gs) return n_groups == n_seqs ? SP_OK : fail(SP_ERR_INVALID_ARG, "Gs is NULL but n_groups=%d is not n_seqs=%d", n_groups, n_seqs);
+    int64_t sum = 0;
+    for (int g = 0; g < n_groups; ++g) {
+        if (Gs[g] < 0) return fail(SP_ERR_INVALID_ARG, "group %d: G=%d is negative", g, Gs[g]);
+        sum += Gs[g];
+    }
+    if (sum != n_seqs) return fail(SP_ERR_INVALID_ARG, "the groups hold %lld sequences, n_seqs=%d", (long long)sum, n_seqs);
+    return SP_OK;
+}
+sp_status check_rules(const sp_logit_rules* r, sp::AdjustRules& out) {
+    if (!r) return fail(SP_ERR_INVALID_ARG, "rules is NULL");
+    if (!(r->repetition > 0.f) || !std::isfinite(r->repetition) || !std::isfinite(r->presence) || !std::isfinite(r->frequency) ||
+        !(r->temperature > 0.f) || !std::isfinite(r->temperature))
+        return fail(SP_ERR_INVALID_ARG, "repetition and temperature must be finite and > 0, presence and frequency finite");
+    const float inv_rep = 1.f / r->repetition, inv_t = 1.f / r->temperature;
+    if (!std::isfinite(inv_rep) || !std::isfinite(inv_t))
+        return fail(SP_ERR_INVALID_ARG, "repetition or temperature is too small: its reciprocal is not finite");
+    if ((uintptr_t)r->bias & 3) return fail(SP_ERR_INVALID_ARG, "bias pointer is not 4-byte aligned");
+    out = sp::AdjustRules{r->repetition, inv_rep, r->presence, r->frequency, inv_t, r->bias};
+    return SP_OK;
+}
+sp_status check_vocab(int64_t vocab, const uint32_t* mask, int64_t mask_stride, sp_dtype dtype) {
+    if (vocab < 1 || vocab > (int64_t)1 << 30) return fail(SP_ERR_INVALID_ARG, "vocab=%lld", (long long)vocab);
+    if (mask && ((uintptr_t)mask & 3)) return fail(SP_ERR_INVALID_ARG, "mask pointer is not 4-byte aligned");
+    if (mask && mask_stride < (vocab + 31) / 32)
+        return fail(SP_ERR_INVALID_ARG, "mask_stride=%lld words do not hold %lld bits", (long long)mask_stride, (long long)vocab);
+    if (dtype != SP_BF16 && dtype != SP_F32) return fail(SP_ERR_UNSUPPORTED, "unknown dtype %d", (int)dtype);
+    return SP_OK;
+}
+inline bool off4(const void* p) { return ((uintptr_t)p & 3) != 0; }
+size_t decode_table_bytes(int32_t n_groups) { return align256(((size_t)n_groups + 1) * 4); }
+}  // namespace
+
+sp_status sp_attn_cache_append(const sp_kv_cache* cache, const void* q, int64_t q_stride, void* q_out, int32_t n_q_heads,
+                               const void* k, int64_t k_stride, void* k_out, const void* v, int64_t v_stride,
+                               int32_t n_seqs, const int32_t* new_lens, const int32_t* tables, int32_t table_width,
+                               const int32_t* lens, const int32_t* pos_base, int32_t* lens_out, double rope_base, void* stream) {
+    g_err[0] = 0;
+    sp::KvCache c;
+    sp_status st = check_cache(cache, c);
+    if (st != SP_OK) return st;
+    if (!k || !v || (!q != !q_out)) return fail(SP_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    for (const void* p : {q, (const void*)q_out, k, (const void*)k_out, v})
+        if (misaligned(p)) return fail(SP_ERR_INVALID_ARG, "tensor pointer %p is not 16-byte aligned", p);
+    if (q ? n_q_heads < 1 : n_q_heads != 0) return fail(SP_ERR_INVALID_ARG, "n_q_heads=%d", n_q_heads);
+    const int64_t unit = 16 / (c.f32 ? 4 : 2), kv = (int64_t)c.n_kv_heads * c.head_dim;
+    if (k_stride < kv || v_stride < kv || (q && q_stride < (int64_t)n_q_heads * c.head_dim) || k_stride % unit || v_stride % unit || (q && q_stride % unit))
+        return fail(SP_ERR_INVALID_ARG, "token strides %lld, %lld, %lld: multiples of 16 bytes that hold the heads of a token",
+                    (long long)(q ? q_stride : 0), (long long)k_stride, (long long)v_stride);
+    if ((q_out == q && q && q_stride != (int64_t)n_q_heads * c.head_dim) || (k_out == k && k_stride != kv))
+        return fail(SP_ERR_INVALID_ARG, "an output that is its input must be contiguous");
+    if (n_seqs < 1 || table_width < 1) return fail(SP_ERR_INVALID_ARG, "n_seqs=%d, table_width=%d", n_seqs, table_width);
+    if (!tables || !lens) return fail(SP_ERR_INVALID_ARG, "tables / lens is NULL");
+    if (off4(tables) || off4(lens) || off4(pos_base) || off4(lens_out)) return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
+    if (lens_out == lens) return fail(SP_ERR_INVALID_ARG, "lens_out must not be lens");
+    if (!(rope_base > 1.0) || !std::isfinite(rope_base)) return fail(SP_ERR_INVALID_ARG, "rope_base must be finite and > 1");
+    int64_t total = 0;
+    for (int s = 0; new_lens && s < n_seqs; ++s) {
+        if (new_lens[s] < 0) return fail(SP_ERR_INVALID_ARG, "sequence %d: new_lens=%d is negative", s, new_lens[s]);
+        total += new_lens[s];
+        if (total > 0x7fff0000LL) return fail(SP_ERR_INVALID_ARG, "total token count exceeds the int32 range");
+    }
+    const hipError_t e = sp::launch_append(c, q, q_stride, q_out, q ? n_q_heads : 0, k, k_stride, k_out, v, v_stride, n_seqs, new_lens, tables,
+                                           table_width, lens, pos_base, lens_out, rope_base, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+    return SP_OK;
+}
+
+size_t sp_attn_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, sp_dtype dtype) {
+    if (n_groups < 1 || n_seqs < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) ||
+        (dtype != SP_BF16 && dtype != SP_F32)) return 0;
+    return TAG_BYTES + decode_table_bytes(n_groups) + sp::decode_partial_bytes(n_groups, n_seqs, n_q_heads, n_kv_heads, head_dim);
+}
+
+sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float* lse, int32_t n_q_heads, int32_t n_groups, int32_t n_seqs,
+                         const int32_t* Gs, const int32_t* prompt_tables, int32_t prompt_width, const int32_t* prompt_lens,
+                         const int32_t* resp_tables, int32_t resp_width, const int32_t* resp_lens, float softmax_scale,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    sp::KvCache c;
+    sp_status st = check_cache(cache, c);
+    if (st != SP_OK) return st;
+    if (!q || !o || !lse) return fail(SP_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (misaligned(q) || misaligned(o)) return fail(SP_ERR_INVALID_ARG, "tensor pointer is not 16-byte aligned");
+    if (n_q_heads < 1 || n_q_heads % c.n_kv_heads != 0)
+        return fail(SP_ERR_INVALID_ARG, "n_q_heads=%d must be a positive multiple of n_kv_heads=%d", n_q_heads, c.n_kv_heads);
+    if (!std::isfinite(softmax_scale) || softmax_scale <= 0.f) return fail(SP_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    st = check_members(n_groups, n_seqs, Gs);
+    if (st != SP_OK) return st;
+    if (prompt_width < 0 || resp_width < 0 || (prompt_width > 0) != (prompt_tables != nullptr) || (prompt_width > 0) != (prompt_lens != nullptr) ||
+        (resp_width > 0) != (resp_tables != nullptr) || !resp_lens)
+        return fail(SP_ERR_INVALID_ARG, "prompt_tables, prompt_lens and prompt_width, and resp_tables and resp_width, go together; resp_lens is needed");
+    if (off4(prompt_tables) || off4(prompt_lens) || off4(resp_tables) || off4(resp_lens) || off4(lse))
+        return fail(SP_ERR_INVALID_ARG, "a 32-bit array is not 4-byte aligned");
+    const size_t need = sp_attn_decode_workspace_bytes(n_groups, n_seqs, n_q_heads, c.n_kv_heads, c.head_dim, cache->dtype);
+    if (!workspace || misaligned(workspace) || workspace_bytes < need)
+        return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
+    hipStream_t s = (hipStream_t)stream;
+    hipError_t e = hipSuccess;
+    sp::TabArg starts;
+    try {       // first sequence of each group: a kernel argument, or in the workspace
+        std::vector<int32_t> words((size_t)n_groups + 1, 0);
+        for (int g = 0; g < n_groups; ++g) words[g + 1] = words[g] + (Gs ? Gs[g] : 1);
+        starts = sp::make_tab_arg(words.data(), words.size(), table_of(workspace));
+        if (starts.dev)
+            e = sp::launch_prepare(words.data(), (int)words.size(), table_of(workspace), (uint32_t*)workspace, sp::ReserveTag{}, sp::TAG_CLEAR, false,
+                                   n_groups, n_seqs, 0, 0, sp::Schedule{}, sp::KEYS_AS_PACKED, s);
+    } catch (const std::exception&) {
+        return fail(SP_ERR_INVALID_ARG, "no host memory for %d groups", n_groups);
+    }
+    if (e == hipSuccess)
+        e = sp::launch_decode(c, q, o, lse, n_q_heads, n_groups, n_seqs, starts, prompt_tables, prompt_width, prompt_lens, resp_tables, resp_width,
+                              resp_lens, softmax_scale, (uint32_t*)workspace, (float*)((char*)workspace + TAG_BYTES + decode_table_bytes(n_groups)), s);
+    if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+    return SP_OK;
+}
+
+sp_status sp_attn_adjust_logits(const void* logits, int64_t logits_stride, void* out, int64_t out_stride, int64_t vocab,
+                                const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride, int32_t n_groups, int32_t n_seqs,
+                                const int32_t* Gs, const int32_t* prompt_tokens, int32_t prompt_stride, const int32_t* prompt_lens,
+                                const int32_t* resp_tokens, int32_t resp_stride, const int32_t* resp_lens, sp_dtype dtype, void* stream) {
+    g_err[0] = 0;
+    if (!logits || !out) return fail(SP_ERR_INVALID_ARG, "a pointer is NULL");
+    if (misaligned(logits) || misaligned(out)) return fail(SP_ERR_INVALID_ARG, "tensor pointer is not 16-byte aligned");
+    sp::AdjustRules r;
+    sp_status st = check_rules(rules, r);
+    if (st == SP_OK) st = check_vocab(vocab, mask, mask_stride, dtype);
+    if (st == SP_OK) st = check_members(n_groups, n_seqs, Gs);
+    if (st != SP_OK) return st;
+    if (logits_stride < vocab || out_stride < vocab) return fail(SP_ERR_INVALID_ARG, "row strides %lld, %lld are below vocab", (long long)logits_stride, (long long)out_stride);
+    if (out == logits && out_stride != logits_stride) return fail(SP_ERR_INVALID_ARG, "out that is logits needs its stride");
+    if (!prompt_tokens != !prompt_lens || !resp_tokens != !resp_lens || (prompt_tokens && prompt_stride < 0) || (resp_tokens && resp_stride < 0))
+        return fail(SP_ERR_INVALID_ARG, "tokens and lengths of prompts, and of responses, go together, with a stride >= 0");
+    if (off4(prompt_tokens) || off4(prompt_lens) || off4(resp_tokens) || off4(resp_lens))
+        return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
+    const hipError_t e = sp::launch_adjust_logits(logits, logits_stride, out, out_stride, vocab, r, mask, mask_stride, n_groups, Gs, prompt_tokens,
+                                                  prompt_stride, prompt_lens, resp_tokens, resp_stride, resp_lens, dtype == SP_F32, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+    return SP_OK;
+}
+
+size_t sp_attn_adjusted_logprob_workspace_bytes(int64_t total_tokens, int32_t n_groups, int64_t total_responses, int64_t vocab) {
+    const size_t base = sp_attn_loss_workspace_bytes(total_tokens, n_groups, total_responses);
+    if (base == 0 || vocab < 1 || vocab > (int64_t)1 << 30) return 0;
+    return base + align256(sp::adjust_parts_bytes(total_tokens, vocab));
+}
+
+namespace {
+sp_status adjusted_logprob(bool bwd, const void* logits, const int32_t* labels, const int32_t* tokens, float* logp, float* lse, const float* g,
+                           void* dlogits, int64_t vocab, const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride,
+                           int32_t n_groups, const int32_t* prompt_lens, const int32_t* Gs, const int32_t* resp_lens_flat, sp_dtype dtype,
+                           uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    if (flags & ~(SP_FLAG_OWN_TOKEN | (bwd ? SP_FLAG_ZERO_PROMPT_ROWS : 0u))) return fail(SP_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+    if (!logits || !labels || !tokens || !lse || (bwd ? !g || !dlogits : !logp)) return fail(SP_ERR_INVALID_ARG, "a pointer is NULL");
+    if (misaligned(logits) || misaligned(dlogits)) return fail(SP_ERR_INVALID_ARG, "tensor pointer is not 16-byte aligned");
+    if (off4(labels) || off4(tokens) || off4(lse) || off4(g) || off4(logp)) return fail(SP_ERR_INVALID_ARG, "a 32-bit array is not 4-byte aligned");
+    sp::AdjustRules r;
+    sp_status st = check_rules(rules, r);
+    if (st == SP_OK) st = check_vocab(vocab, mask, mask_stride, dtype);
+    if (st != SP_OK) return st;
+    try {
+        Layout L;
+        float* scratch = nullptr;
+        sp::TabArg tab;
+        st = build_table(n_groups, prompt_lens, Gs, resp_lens_flat, L);
+        if (st != SP_OK) return st;
+        const size_t need = sp_attn_adjusted_logprob_workspace_bytes(L.total_tokens, n_groups, L.total_responses, vocab);
+        if (!workspace || misaligned(workspace) || workspace_bytes < need)
+            return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
+        hipStream_t s = (hipStream_t)stream;
+        scratch = (float*)((char*)workspace + sp_attn_loss_workspace_bytes(L.total_tokens, n_groups, L.total_responses));
+        hipError_t e = table_for(L, workspace, s, tab);
+        if (e == hipSuccess)
+            e = sp::launch_adjusted_logprob(bwd, logits, labels, tokens, mask, mask_stride, logp, lse, g, dlogits, r, tab, L.total_tokens, vocab,
+                                            (flags & SP_FLAG_OWN_TOKEN) != 0, (flags & SP_FLAG_ZERO_PROMPT_ROWS) != 0, scratch, (uint32_t*)workspace,
+                                            dtype == SP_F32, s);
+        if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+        return SP_OK;
+    } catch (const std::exception&) {
+        return fail(SP_ERR_INVALID_ARG, "no host memory for %d groups", n_groups);
+    }
+}
+}  // namespace
+
+sp_status sp_attn_adjusted_logprob_fwd(const void* logits, const int32_t* labels, const int32_t* tokens, float* logp, float* lse, int64_t vocab,
+                                       const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride, int32_t n_groups,
+                                       const int32_t* prompt_lens, const int32_t* Gs, const int32_t* resp_lens_flat, sp_dtype dtype,
+                                       uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+    return adjusted_logprob(false, logits, labels, tokens, logp, lse, nullptr, nullptr, vocab, rules, mask, mask_stride, n_groups, prompt_lens, Gs,
+                            resp_lens_flat, dtype, flags, workspace, workspace_bytes, stream);
+}
+
+sp_status sp_attn_adjusted_logprob_bwd(const void* logits, const int32_t* labels, const int32_t* tokens, const float* lse, const float* g,
+                                       void* dlogits, int64_t vocab, const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride,
+                                       int32_t n_groups, const int32_t* prompt_lens, const int32_t* Gs, const int32_t* resp_lens_flat,
+                                       sp_dtype dtype, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+    return adjusted_logprob(true, logits, labels, tokens, nullptr, const_cast<float*>(lse), g, dlogits, vocab, rules, mask, mask_stride, n_groups,
+                            prompt_lens, Gs, resp_lens_flat, dtype, flags, workspace, workspace_bytes, stream);
 }
 
 sp_status sp_attn_segment_table(int32_t n_groups, const int32_t* prompt_lens, const int32_t* Gs,

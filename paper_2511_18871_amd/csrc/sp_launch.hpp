@@ -355,4 +355,28 @@ int f32_rows(const Problem& p, int kernel);
 // Waves per workgroup (8 or 4) of a dkdv pass that is not split over the q heads (rule and reasons: sp_bwd.hip).
 int dkdv_waves(const Problem& p);
 
+// Paged cache of the rollout calls (sp_kv_cache, its page size as a power of two)
+struct KvCache { void* k; void* v; int64_t n_pages; int log_page, n_kv_heads, head_dim; bool f32; };
+hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, void* q_out, int Hq, const void* k, int64_t k_stride,
+                         void* k_out, const void* v, int64_t v_stride, int n_seqs, const int32_t* new_lens, const int* tables, int width,
+                         const int* lens, const int* pos_base, int* lens_out, double base, hipStream_t s);
+
+// starts: first sequence of each group, one past the last behind them.  partials: decode_partial_bytes() bytes.
+size_t decode_partial_bytes(int n_groups, int n_seqs, int Hq, int Hkv, int d);
+hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const TabArg& starts,
+                         const int* prompt_tables, int prompt_width, const int* prompt_lens, const int* resp_tables, int resp_width,
+                         const int* resp_lens, float scale, uint32_t* tag, float* partials, hipStream_t s);
+
+// Rules of adjusted logits (sp_logit_rules)
+struct AdjustRules { float repetition, inv_repetition, presence, frequency, inv_temperature; const float* bias; };
+hipError_t launch_adjust_logits(const void* logits, int64_t stride, void* out, int64_t out_stride, int64_t vocab, const AdjustRules& rules,
+                                const uint32_t* mask, int64_t mask_stride, int n_groups, const int32_t* Gs,
+                                const int* prompt_tokens, int prompt_stride, const int* prompt_lens,
+                                const int* resp_tokens, int resp_stride, const int* resp_lens, bool f32, hipStream_t s);
+size_t adjust_parts_bytes(int64_t total_tokens, int64_t vocab);
+hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labels, const int* tokens, const uint32_t* mask, int64_t mask_stride,
+                                   float* logp, float* lse, const float* g, void* dlogits, const AdjustRules& rules, const TabArg& tab,
+                                   int64_t total_tokens, int64_t vocab, bool own_token, bool zero_prompt, float* parts, uint32_t* tag, bool f32,
+                                   hipStream_t s);
+
 }  // namespace sp
