@@ -772,8 +772,8 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
         return fail(SP_ERR_INVALID_ARG, "no host memory for %d groups", n_groups);
     }
     if (e == hipSuccess)
-        e = sp::launch_decode(c, q, o, lse, n_q_heads, n_groups, n_seqs, starts, prompt_tables, prompt_width, prompt_lens, resp_tables, resp_width,
-                              resp_lens, softmax_scale, (uint32_t*)workspace, (float*)((char*)workspace + TAG_BYTES + decode_table_bytes(n_groups)), s);
+        e = sp::launch_decode(c, q, o, lse, n_q_heads, n_groups, n_seqs, Gs, starts, prompt_tables, prompt_width, prompt_lens, resp_tables, resp_width,
+                              resp_lens, softmax_scale, (uint32_t*)workspace, (char*)workspace + TAG_BYTES + decode_table_bytes(n_groups), s);
     if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
     return SP_OK;
 }
