@@ -36,7 +36,7 @@ struct DecodeArgs {
     int nc;                                // row tiles per wave of a shared piece
     float c, m_none;                       // softmax_scale * log2(e); reference point of a row that has not seen a key
     uint32_t* tag;
-    int2* desc;                            // per list: first row of its sums, chunks
+    int2* desc;                            // per list: first row of its sums, chunks (-1: a sequence that takes no part)
     float* stats;                          // per row of sums: m, l, l of the rounded weights, 0
     float* sums;                           // per row: sum p v
 };
@@ -59,7 +59,7 @@ __device__ __forceinline__ double sum64(double x) {
 }
 
 struct ListShape { int rows, tiles, blocks; bool shared; };      // tiles of 32 keys; blocks of rows that a piece holds
-struct Piece { int list, chunk, kvh, block, chunks, base, chunk_tiles; };
+struct Piece { int list, chunk, kvh, block, base, chunk_tiles; };
 
 struct Lists {
     const int* starts; const int* lens;      // first sequence of each group; lengths in LDS, or nullptr
@@ -100,7 +100,6 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
     t_shared = sum64(t_shared) * a.Hkv;
     t_solo = sum64(t_solo) * a.Hkv;
     const double total = t_shared + t_solo;
-    if (total == 0) return false;
     int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * (t_shared / total))) : 0;
     if (t_solo > 0) shared_wgs = min(shared_wgs, PLAN_WGS - 1);
     const int chunk_shared = shared_wgs ? max(2, 2 * (int)ceil(t_shared / (2.0 * shared_wgs))) : 2;          // whole stages of 64 keys
@@ -111,6 +110,16 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
         const int chunks = (s.tiles + (s.shared ? chunk_shared : chunk_solo) - 1) / (s.shared ? chunk_shared : chunk_solo);
         (s.shared ? n_shared : n_solo) += chunks * s.blocks * a.Hkv;
         rows += chunks * a.Hkv * s.rows;
+    }
+    if (blockIdx.x == 0 && wave == 0) {         // what the join needs to know of each list
+        int base = scan64(rows) - rows;
+        for (int i = i0; i < i1; ++i) {
+            const ListShape s = ls.shape<F32>(i);
+            const int chunks = (s.tiles + (s.shared ? chunk_shared : chunk_solo) - 1) / (s.shared ? chunk_shared : chunk_solo);
+            const bool out = i >= a.n_groups && a.resp_lens[i - a.n_groups] < 0;
+            a.desc[i] = int2{base, out ? -1 : chunks};
+            base += chunks * a.Hkv * s.rows;
+        }
     }
     const int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
     const int all_shared = __builtin_amdgcn_readlane(to_shared, 63), all_solo = __builtin_amdgcn_readlane(to_solo, 63);
@@ -126,7 +135,7 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
         const ListShape s = ls.shape<F32>(i);
         const int ct = s.shared ? chunk_shared : chunk_solo, chunks = (s.tiles + ct - 1) / ct, count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
         if (left < count) {
-            p.list = i; p.chunks = chunks; p.base = base; p.chunk_tiles = ct;
+            p.list = i; p.base = base; p.chunk_tiles = ct;
             p.kvh = left % a.Hkv; left /= a.Hkv;
             p.block = left % s.blocks; p.chunk = left / s.blocks;
             shape = s;
@@ -137,7 +146,7 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
     }
     // the same in every lane, which the compiler does not see
     auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
-    scalar(p.list); scalar(p.chunk); scalar(p.kvh); scalar(p.block); scalar(p.chunks); scalar(p.base); scalar(p.chunk_tiles);
+    scalar(p.list); scalar(p.chunk); scalar(p.kvh); scalar(p.block); scalar(p.base); scalar(p.chunk_tiles);
     scalar(shape.rows); scalar(shape.tiles); scalar(shape.blocks);
     shape.shared = shared;
     return true;
@@ -191,13 +200,15 @@ template <int N> __device__ __forceinline__ void wait_copies() {
 }
 
 // Scores of 32 keys at LDS address `k`, keys not in `bits` masked: s[c][kt][i] is key 16 kt + 4 (l / 16) + i of row l % 16 of tile c
+// (an operand's granule is its first one's with a constant xored in, which leaves the address of the first in a register only)
 template <int D, int NC>
 __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigned bits, int tiles, int l, f32x4 (&s)[NC][2]) {
+    const unsigned at = k + kv_off<D>(l & 15, l >> 4);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
         bf16x8 a[D / 32];
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) a[ks] = lds_at_row8(k + kv_off<D>(16 * kt + (l & 15), 4 * ks + (l >> 4)));
+        for (int ks = 0; ks < D / 32; ++ks) a[ks] = lds_at_row8((at ^ (ks << 6)) + kt * (32 * D));
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             if (c > 0 && c >= tiles) continue;
@@ -253,13 +264,13 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
 // O^T += V^T P^T over 32 keys at LDS address `v`
 template <int D, int NC>
 __device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf16x8 (&p)[NC], int tiles, int l) {
-    const int row = 4 * (l >> 4) + ((l & 15) >> 2), col = 4 * (l & 3);
+    const unsigned at = v + kv_off<D>(4 * (l >> 4) + ((l & 15) >> 2), (l & 3) >> 1) + ((l & 1) << 3);
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
         s16x4 half[2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
-            half[kt] = lds_at_tr4(v + kv_off<D>(16 * kt + row, 2 * dt + (col >> 3)) + ((col & 4) << 1));
+            half[kt] = lds_at_tr4((at ^ (dt << 5)) + kt * (32 * D));
         const bf16x8 a = cat4(half[0], half[1]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -380,7 +391,6 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     if (!has) return;
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
-    if (l == 0 && p.chunk == 0 && p.kvh == 0 && p.block == 0 && (!shape.shared || w == 0)) a.desc[p.list] = int2{p.base, p.chunks};
     const int len = __builtin_amdgcn_readfirstlane(ls.length(p.list)), key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
     PieceRows pr{prompt ? ls.starts[p.list] : own, a.rep, shape.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * shape.rows};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
@@ -463,7 +473,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
             half ^= 1;
             if (key + 64 < key1) issue(key + 64, buf + half * 8 * KEYS16);
             if (tiles > 0) {
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     f32x4 s[NC][2];
                     bf16x8 pw[NC];
@@ -494,7 +504,6 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, Decod
     if (!find_piece<true>(ls, w, l, p, shape)) return;
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
-    if (l == 0 && p.chunk == 0 && p.kvh == 0 && p.block == 0) a.desc[p.list] = int2{p.base, p.chunks};
     const int len = __builtin_amdgcn_readfirstlane(ls.length(p.list)), key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
     PieceRows pr{prompt ? ls.starts[p.list] : own, a.rep, shape.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * shape.rows};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
@@ -578,27 +587,41 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, Decod
 
 // ---- the join ------------------------------------------------------------------------------------------------
 
-// One wave per sequence and q head: o = sum_c e^(m_c - M) O_c / sum_c e^(m_c - M) l_c over the chunks of the prompt and of the response
+// One wave per sequence and q head: o = sum_c e^(m_c - M) O_c / sum_c e^(m_c - M) l_c over the chunks of the prompt and of the response.
+// Bound: the latency of three loads that wait for each other (where the sums are, the statistics, the sums); the first sums are
+// therefore asked for with the statistics.  D / 4 lanes hold a row, so that a wave has 4 x 256 / D rows in flight.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeArgs a) {
+    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, DEPTH = 4;
     const int* const w = table_of(starts);
-    const int l = threadIdx.x & 63;
+    const int l = threadIdx.x & 63, mine = l / LANES, e0 = 4 * (l % LANES);
     const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (item >= (int64_t)a.n_seqs * a.Hq) return;
     const int seq = (int)(item / a.Hq), h = (int)(item - (int64_t)seq * a.Hq), kvh = h / a.rep, hr = h - kvh * a.rep;
     int g = 0, hi = a.n_groups;
     while (hi - g > 1) { const int mid = (g + hi) >> 1; if (w[mid] <= seq) g = mid; else hi = mid; }
-    const Lists ls{w, nullptr, a};
-    const bool active = a.resp_lens[seq] >= 0, has_prompt = active && ls.length(g) > 0, has_resp = active && ls.length(a.n_groups + seq) > 0;
-    const int2 dp = has_prompt ? a.desc[g] : int2{0, 0}, dr = has_resp ? a.desc[a.n_groups + seq] : int2{0, 0};
+    int2 dp = a.desc[g];
+    const int2 dr = a.desc[a.n_groups + seq];
+    if (dr.y < 0) dp.y = 0;
     const int prompt_rows = (w[g + 1] - w[g]) * a.rep;
     const int64_t base_p = dp.x + (int64_t)kvh * prompt_rows + (seq - w[g]) * a.rep + hr, base_r = dr.x + (int64_t)kvh * a.rep + hr;
-    const int n = dp.y + dr.y;
-    auto row_of = [&](int i) { return i < dp.y ? base_p + (int64_t)i * a.Hkv * prompt_rows : base_r + (int64_t)(i - dp.y) * a.Hkv * a.rep; };
-    float M = a.m_none, L = 0.f, LR = 0.f, acc[D / 64] = {};
+    const int n = dp.y + max(dr.y, 0);
+    auto row_of = [&](int i) { return i < dp.y ? base_p + (int64_t)i * (a.Hkv * prompt_rows) : base_r + (int64_t)(i - dp.y) * (a.Hkv * a.rep); };
+    float M = a.m_none, L = 0.f, LR = 0.f;
+    f32x4 acc = {0, 0, 0, 0};
     for (int i0 = 0; i0 < n; i0 += 64) {
-        f32x4 st = {a.m_none, 0.f, 0.f, 0.f};
-        if (i0 + l < n) st = *reinterpret_cast<const f32x4*>(a.stats + row_of(i0 + l) * 4);
+        const int count = min(64, n - i0);
+        f32x4 st = {a.m_none, 0.f, 0.f, 0.f}, x[DEPTH];
+        if (l < count) st = *reinterpret_cast<const f32x4*>(a.stats + row_of(i0 + l) * 4);
+        auto fetch = [&](int i) {
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u) {
+                const int k = i + u * AT_ONCE + mine;
+                x[u] = f32x4{0, 0, 0, 0};
+                if (k < count) x[u] = *reinterpret_cast<const f32x4*>(a.sums + row_of(i0 + k) * D + e0);
+            }
+        };
+        fetch(0);
         float mx = st[0];
         for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
         const float mn = fmaxf(M, mx), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
@@ -606,21 +629,30 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
         L = L * alpha + wt * st[1];            // lanes hold their chunks' shares of the sums
         LR = LR * alpha + wt * st[2];
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) acc[e] *= alpha;
-        const int count = min(64, n - i0);
-#pragma unroll 4
-        for (int i = 0; i < count; ++i) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wt), i));
-            const float* const src = a.sums + row_of(i0 + i) * D + (D / 64) * l;
+        for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+        for (int i = 0; i < count; i += DEPTH * AT_ONCE) {
+            if (i > 0) fetch(i);
 #pragma unroll
-            for (int e = 0; e < D / 64; ++e) acc[e] += f * src[e];
+            for (int u = 0; u < DEPTH; ++u) {
+                const float f = __shfl(wt, (i + u * AT_ONCE + mine) & 63, 64);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += f * x[u][e];
+            }
         }
     }
     for (int o = 32; o >= 1; o >>= 1) { L += __shfl_xor(L, o, 64); LR += __shfl_xor(LR, o, 64); }
-    const float inv = LR > 0.f ? 1.f / LR : 0.f;
-    T* const out = (T*)a.o + item * D + (D / 64) * l;
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) out[e] = (T)(L > 0.f ? acc[e] * inv : 0.f);
+    for (int o = 32; o >= LANES; o >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+    const float inv = L > 0.f ? 1.f / LR : 0.f;
+    if (mine == 0) {
+        typedef T out4 __attribute__((ext_vector_type(4)));
+        out4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (T)(L > 0.f ? acc[e] * inv : 0.f);
+        *reinterpret_cast<out4*>((T*)a.o + item * D + e0) = y;
+    }
     if (l == 0) a.lse[(int64_t)h * a.n_seqs + seq] = L > 0.f ? M * (a.c * LN2) + __logf(L) : -INFINITY;
 }
 
