@@ -33,7 +33,8 @@ struct DecodeArgs {
     const int* prompt_tables; const int* prompt_lens; const int* resp_tables; const int* resp_lens;
     int64_t prompt_width, resp_width;
     int n_pages, n_groups, n_seqs, Hq, Hkv, rep, log_page;
-    int nc;                                // row tiles per wave of a shared piece
+    int nc, tile_shift;                    // row tiles per wave of a shared piece; see find_piece()
+    Div kv_heads;
     float c, m_none;                       // softmax_scale * log2(e); reference point of a row that has not seen a key
     uint32_t* tag;
     int2* desc;                            // per list: first row of its sums, chunks (-1: a sequence that takes no part)
@@ -45,7 +46,7 @@ __device__ const i32x4 zero_granule = {0, 0, 0, 0};      // what keys that are n
 
 // ---- the plan --------------------------------------------------------------------------------------------
 
-// inclusive sum over the lanes of a wave
+// over the lanes of a wave: inclusive sums, and the maximum or the sum in every lane
 template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int x) {
     return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
 }
@@ -53,12 +54,30 @@ __device__ __forceinline__ int scan64(int x) {
     x = dpp_add<0x111, 0xf>(x); x = dpp_add<0x112, 0xf>(x); x = dpp_add<0x114, 0xf>(x); x = dpp_add<0x118, 0xf>(x);      // within 16 lanes
     x = dpp_add<0x142, 0xa>(x); return dpp_add<0x143, 0xc>(x);                                                      // across them
 }
-__device__ __forceinline__ double sum64(double x) {
-    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
-    return x;
+template <int CTRL> __device__ __forceinline__ float rotated16(float x) {
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
+}
+// the four lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float quad_max(float x) {
+    x = pair_max(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    x = pair_sum(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, rotated16<0x128>(x)); x = fmaxf(x, rotated16<0x124>(x)); x = fmaxf(x, rotated16<0x122>(x)); x = fmaxf(x, rotated16<0x121>(x));
+    return quad_max(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += rotated16<0x128>(x); x += rotated16<0x124>(x); x += rotated16<0x122>(x); x += rotated16<0x121>(x);
+    return quad_sum(x);
 }
 
-struct ListShape { int rows, tiles, blocks; bool shared; };      // tiles of 32 keys; blocks of rows that a piece holds
+struct ListShape { int rows, len, tiles, blocks; bool shared; };      // tiles of 32 keys; blocks of rows that a piece holds
 struct Piece { int list, chunk, kvh, block, base, chunk_tiles; };
 
 struct Lists {
@@ -72,56 +91,65 @@ struct Lists {
     }
     template <bool F32> __device__ __forceinline__ ListShape shape(int i) const {
         ListShape s;
-        const int len = lens ? lens[i] : length(i);
+        s.len = lens ? lens[i] : length(i);
         s.rows = a.rep * (i < a.n_groups ? starts[i + 1] - starts[i] : 1);
-        s.tiles = s.rows > 0 ? (int)(((unsigned)len + 31u) >> 5) : 0;
+        s.tiles = s.rows > 0 ? (int)(((unsigned)s.len + 31u) >> 5) : 0;
         s.shared = !F32 && s.rows > SOLO_ROWS;
+        s.blocks = 1;                        // (an unsigned division is some twenty instructions: only where there is more than one block)
         const int per = s.shared ? 64 * a.nc : SOLO_ROWS;
-        s.blocks = (s.rows + per - 1) / per;
+        if (s.rows > per) s.blocks = (int)((unsigned)(s.rows + per - 1) / (unsigned)per);
         return s;
     }
 };
 
+// the least chunk, a multiple of `unit`, with chunk * places >= total
+__device__ __forceinline__ int chunk_for(int64_t total, int places, int unit) {
+    const int64_t step = (int64_t)places * unit;
+    int64_t c = (int64_t)((float)total / (float)step);
+    while (c * step < total) ++c;
+    while (c > 1 && (c - 1) * step >= total) --c;
+    return (int)min(max(c, (int64_t)1) * unit, (int64_t)1 << 28);
+}
+__device__ __forceinline__ int chunks_of(int tiles, int chunk) { return tiles <= chunk ? tiles > 0 : (int)((unsigned)(tiles + chunk - 1) / (unsigned)chunk); }
+
 // Every wave makes the plan by itself: a lane adds up its share of the lists, then the lanes their sums.  Pieces of shared lists come
-// first, one per workgroup, then those of single waves, four per workgroup.  The chunk of either kind follows from the tiles (rows
+// first, one per workgroup, then those of single waves, four per workgroup.  The chunk of either kind follows from the tiles (row
 // blocks counted) per place, the places being dealt by tiles, so there are no more pieces than PLAN_WGS (PLAN_SOLO) and one per
-// list, block and kv head.
+// list, block and kv head.  (tile_shift: tiles are added up in units that keep their sum within 31 bits, rounded up.)
 template <bool F32>
 __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, Piece& p, ListShape& shape) {
-    p = Piece{};
-    shape = ListShape{};
     const DecodeArgs& a = ls.a;
     const int n = a.n_groups + a.n_seqs, per = (n + 63) >> 6, i0 = min(n, lane * per), i1 = min(n, i0 + per);
-    double t_shared = 0, t_solo = 0;
+    int shared_tiles = 0, solo_tiles = 0;
     for (int i = i0; i < i1; ++i) {
         const ListShape s = ls.shape<F32>(i);
-        (s.shared ? t_shared : t_solo) += (double)s.tiles * s.blocks;
+        const int t = (int)(((int64_t)s.tiles * s.blocks + (1 << a.tile_shift) - 1) >> a.tile_shift);
+        (s.shared ? shared_tiles : solo_tiles) += t;
     }
-    t_shared = sum64(t_shared) * a.Hkv;
-    t_solo = sum64(t_solo) * a.Hkv;
-    const double total = t_shared + t_solo;
-    int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * (t_shared / total))) : 0;
+    auto all = [](int x) { return __builtin_amdgcn_readlane(scan64(x), 63); };
+    const int64_t t_shared = ((int64_t)all(shared_tiles) << a.tile_shift) * a.Hkv, t_solo = ((int64_t)all(solo_tiles) << a.tile_shift) * a.Hkv;
+    int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * ((float)t_shared / (float)(t_shared + t_solo)))) : 0;
     if (t_solo > 0) shared_wgs = min(shared_wgs, PLAN_WGS - 1);
-    const int chunk_shared = shared_wgs ? max(2, 2 * (int)ceil(t_shared / (2.0 * shared_wgs))) : 2;          // whole stages of 64 keys
-    const int chunk_solo = max(1, (int)ceil(t_solo / (4.0 * (PLAN_WGS - shared_wgs))));
+    const int chunk_shared = shared_wgs ? chunk_for(t_shared, shared_wgs, 2) : 2;          // whole stages of 64 keys
+    const int chunk_solo = t_solo > 0 ? chunk_for(t_solo, 4 * (PLAN_WGS - shared_wgs), 1) : 1;
     int n_shared = 0, n_solo = 0, rows = 0;
     for (int i = i0; i < i1; ++i) {
         const ListShape s = ls.shape<F32>(i);
-        const int chunks = (s.tiles + (s.shared ? chunk_shared : chunk_solo) - 1) / (s.shared ? chunk_shared : chunk_solo);
+        const int chunks = chunks_of(s.tiles, s.shared ? chunk_shared : chunk_solo);
         (s.shared ? n_shared : n_solo) += chunks * s.blocks * a.Hkv;
         rows += chunks * a.Hkv * s.rows;
     }
+    const int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
     if (blockIdx.x == 0 && wave == 0) {         // what the join needs to know of each list
-        int base = scan64(rows) - rows;
+        int base = to_rows - rows;
         for (int i = i0; i < i1; ++i) {
             const ListShape s = ls.shape<F32>(i);
-            const int chunks = (s.tiles + (s.shared ? chunk_shared : chunk_solo) - 1) / (s.shared ? chunk_shared : chunk_solo);
+            const int chunks = chunks_of(s.tiles, s.shared ? chunk_shared : chunk_solo);
             const bool out = i >= a.n_groups && a.resp_lens[i - a.n_groups] < 0;
             a.desc[i] = int2{base, out ? -1 : chunks};
             base += chunks * a.Hkv * s.rows;
         }
     }
-    const int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
     const int all_shared = __builtin_amdgcn_readlane(to_shared, 63), all_solo = __builtin_amdgcn_readlane(to_solo, 63);
     const bool shared = (int)blockIdx.x < all_shared;
     const int index = shared ? (int)blockIdx.x : ((int)blockIdx.x - all_shared) * 4 + wave;
@@ -131,13 +159,13 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
     const int src = __ffsll((unsigned long long)here) - 1;                  // the lane whose lists hold the piece
     int left = index - __builtin_amdgcn_readlane(to - own, src), base = __builtin_amdgcn_readlane(to_rows - rows, src);
     const int j1 = min(n, (src + 1) * per);
+    p = Piece{};
+    shape = ListShape{};
     for (int i = src * per; i < j1; ++i) {
         const ListShape s = ls.shape<F32>(i);
-        const int ct = s.shared ? chunk_shared : chunk_solo, chunks = (s.tiles + ct - 1) / ct, count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
+        const int ct = s.shared ? chunk_shared : chunk_solo, chunks = chunks_of(s.tiles, ct), count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
         if (left < count) {
             p.list = i; p.base = base; p.chunk_tiles = ct;
-            p.kvh = left % a.Hkv; left /= a.Hkv;
-            p.block = left % s.blocks; p.chunk = left / s.blocks;
             shape = s;
             break;
         }
@@ -146,25 +174,18 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
     }
     // the same in every lane, which the compiler does not see
     auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
-    scalar(p.list); scalar(p.chunk); scalar(p.kvh); scalar(p.block); scalar(p.base); scalar(p.chunk_tiles);
-    scalar(shape.rows); scalar(shape.tiles); scalar(shape.blocks);
+    scalar(p.list); scalar(p.base); scalar(p.chunk_tiles); scalar(left);
+    scalar(shape.rows); scalar(shape.len); scalar(shape.tiles); scalar(shape.blocks);
     shape.shared = shared;
+    unsigned rest;
+    left = (int)divmod((unsigned)left, a.kv_heads, rest);
+    p.kvh = (int)rest;
+    if (shape.blocks > 1) { p.block = left % shape.blocks; left /= shape.blocks; }
+    p.chunk = left;
     return true;
 }
 
 // ---- rows of a wave ---------------------------------------------------------------------------------------
-
-// max and sum over the four lanes that hold a row (l, l ^ 16, l ^ 32, l ^ 48)
-__device__ __forceinline__ float quad_max(float x) {
-    x = pair_max(x);
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-    x = pair_sum(x);
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 // LDS tiles: a row per key, its granules of 16 bytes permuted so that neither 16 rows of one granule (K) nor four rows of a block
 // of 16 columns (V, read transposed) meet in a bank
@@ -391,7 +412,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     if (!has) return;
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
-    const int len = __builtin_amdgcn_readfirstlane(ls.length(p.list)), key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
+    const int len = shape.len, key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
     PieceRows pr{prompt ? ls.starts[p.list] : own, a.rep, shape.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * shape.rows};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
     pages.load(key0 >> a.log_page);
@@ -504,7 +525,7 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, Decod
     if (!find_piece<true>(ls, w, l, p, shape)) return;
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
-    const int len = __builtin_amdgcn_readfirstlane(ls.length(p.list)), key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
+    const int len = shape.len, key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
     PieceRows pr{prompt ? ls.starts[p.list] : own, a.rep, shape.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * shape.rows};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
     pages.load(key0 >> a.log_page);
@@ -622,9 +643,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
             }
         };
         fetch(0);
-        float mx = st[0];
-        for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-        const float mn = fmaxf(M, mx), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
+        const float mn = fmaxf(M, wave_max(st[0])), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
         M = mn;
         L = L * alpha + wt * st[1];            // lanes hold their chunks' shares of the sums
         LR = LR * alpha + wt * st[2];
@@ -640,7 +659,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
             }
         }
     }
-    for (int o = 32; o >= 1; o >>= 1) { L += __shfl_xor(L, o, 64); LR += __shfl_xor(LR, o, 64); }
+    L = wave_sum(L);
+    LR = wave_sum(LR);
 #pragma unroll
     for (int o = 32; o >= LANES; o >>= 1)
 #pragma unroll
@@ -697,6 +717,12 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
         if (prompts && rows_of(g) > SOLO_ROWS && !cache.f32) widest = std::max(widest, per_wave(rows_of(g)));
     if (a.rep > SOLO_ROWS && !cache.f32) widest = std::max(widest, per_wave(a.rep));
     a.nc = std::max(1, widest);
+    a.kv_heads = make_div(a.Hkv);
+    {   // tiles at most
+        const double most = ((double)n_groups * prompt_width + (double)n_seqs * resp_width) * (1 << a.log_page) / 32 *
+                            ((double)n_seqs * a.rep / SOLO_ROWS + 1) + n_groups + n_seqs;
+        while (most / (double)((int64_t)1 << a.tile_shift) + n_groups + n_seqs > 2e9) ++a.tile_shift;
+    }
     auto count = [&](int64_t rows, int64_t lists) {
         if (rows > SOLO_ROWS && !cache.f32) shared += lists * ((rows + 64 * a.nc - 1) / (64 * a.nc));
         else solo += lists * ((rows + SOLO_ROWS - 1) / SOLO_ROWS);
