@@ -25,7 +25,6 @@ constexpr int SOLO_ROWS = 32;              // rows of a list that a wave takes b
 constexpr int MAX_NC = 3;                  // row tiles of 16 of a wave that shares its keys: 192 rows to a workgroup
 constexpr int PLAN_WGS = 512;              // workgroups that the pieces are made for: two to a CU
 constexpr int PLAN_SOLO = 4 * PLAN_WGS;    // pieces of single waves, at most, that the chunk is made for
-constexpr int LENS_IN_LDS = 8192;
 
 struct DecodeArgs {
     const void* q; void* o; float* lse;
@@ -78,24 +77,27 @@ __device__ __forceinline__ float wave_sum(float x) {
 }
 
 struct ListShape { int rows, len, tiles, blocks; bool shared; };      // tiles of 32 keys; blocks of rows that a piece holds
-struct Piece { int list, chunk, kvh, block, base, chunk_tiles; };
+struct Piece { int list, chunk, kvh, block, base, chunk_tiles, rows, len, blocks; bool shared; };
+struct PlanShare { int sums[4][3]; int left[4], list[4], base[4]; };     // of the waves of a workgroup; their pieces
 
 struct Lists {
-    const int* starts; const int* lens;      // first sequence of each group; lengths in LDS, or nullptr
+    const int* starts;                       // first sequence of each group
+    const i32x2* held;                       // rows and length of each list in LDS, or nullptr
     const DecodeArgs& a;
-    __device__ __forceinline__ int length(int i) const {      // raw, from memory
+    __device__ __forceinline__ i32x2 read(int i) const {
         const bool prompt = i < a.n_groups;
         const int64_t cap = (prompt ? a.prompt_width : a.resp_width) << a.log_page;
         const int n = prompt ? (a.prompt_lens ? a.prompt_lens[i] : 0) : a.resp_lens[i - a.n_groups];
-        return (int)max((int64_t)0, min((int64_t)n, cap));
+        return i32x2{a.rep * (prompt ? starts[i + 1] - starts[i] : 1), n < 0 ? -1 : (int)min((int64_t)n, cap)};
     }
     template <bool F32> __device__ __forceinline__ ListShape shape(int i) const {
+        const i32x2 x = held ? held[i] : read(i);
         ListShape s;
-        s.len = lens ? lens[i] : length(i);
-        s.rows = a.rep * (i < a.n_groups ? starts[i + 1] - starts[i] : 1);
-        s.tiles = s.rows > 0 ? (int)(((unsigned)s.len + 31u) >> 5) : 0;
+        s.rows = x[0];
+        s.len = x[1];
+        s.tiles = s.rows > 0 && s.len > 0 ? (int)(((unsigned)s.len + 31u) >> 5) : 0;
         s.shared = !F32 && s.rows > SOLO_ROWS;
-        s.blocks = 1;                        // (an unsigned division is some twenty instructions: only where there is more than one block)
+        s.blocks = 1;                        // (a division is some twenty instructions: only where there is more than one block)
         const int per = s.shared ? 64 * a.nc : SOLO_ROWS;
         if (s.rows > per) s.blocks = (int)((unsigned)(s.rows + per - 1) / (unsigned)per);
         return s;
@@ -112,22 +114,39 @@ __device__ __forceinline__ int chunk_for(int64_t total, int places, int unit) {
 }
 __device__ __forceinline__ int chunks_of(int tiles, int chunk) { return tiles <= chunk ? tiles > 0 : (int)((unsigned)(tiles + chunk - 1) / (unsigned)chunk); }
 
-// Every wave makes the plan by itself: a lane adds up its share of the lists, then the lanes their sums.  Pieces of shared lists come
-// first, one per workgroup, then those of single waves, four per workgroup.  The chunk of either kind follows from the tiles (row
-// blocks counted) per place, the places being dealt by tiles, so there are no more pieces than PLAN_WGS (PLAN_SOLO) and one per
-// list, block and kv head.  (tile_shift: tiles are added up in units that keep their sum within 31 bits, rounded up.)
+// The piece of this wave (of a shared list: of the workgroup).  Every workgroup makes the whole plan: a thread adds up its share of
+// the lists, which lie in LDS meanwhile (n_held of them fit), the workgroup their sums.  Pieces of shared lists come first, one per workgroup, then those of
+// single waves, four per workgroup.  The chunk of either kind follows from the tiles (row blocks counted) per place, the places being
+// dealt by tiles, so there are no more pieces than places and one per list, block and kv head.
+// (tile_shift: tiles are added up in units that keep their sum within 31 bits, rounded up.)
 template <bool F32>
-__device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, Piece& p, ListShape& shape) {
-    const DecodeArgs& a = ls.a;
-    const int n = a.n_groups + a.n_seqs, per = (n + 63) >> 6, i0 = min(n, lane * per), i1 = min(n, i0 + per);
+__device__ __forceinline__ bool find_piece(const TabArg& starts, const DecodeArgs& a, i32x2* held, int n_held, PlanShare& share, int wave, int lane, Piece& p) {
+    const int n = a.n_groups + a.n_seqs;
+    const Lists ls{table_of(starts), n <= n_held ? held : nullptr, a};
+    if (ls.held) {
+        for (int i = threadIdx.x; i < n; i += 256) held[i] = ls.read(i);
+        __syncthreads();
+    }
+    const int per = (n + 255) >> 8, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
     int shared_tiles = 0, solo_tiles = 0;
     for (int i = i0; i < i1; ++i) {
         const ListShape s = ls.shape<F32>(i);
         const int t = (int)(((int64_t)s.tiles * s.blocks + (1 << a.tile_shift) - 1) >> a.tile_shift);
         (s.shared ? shared_tiles : solo_tiles) += t;
     }
-    auto all = [](int x) { return __builtin_amdgcn_readlane(scan64(x), 63); };
-    const int64_t t_shared = ((int64_t)all(shared_tiles) << a.tile_shift) * a.Hkv, t_solo = ((int64_t)all(solo_tiles) << a.tile_shift) * a.Hkv;
+    auto over_waves = [&](int k, int& before, int& all) {      // of a sum that each wave has left in share.sums[.][k]
+        const int s0 = share.sums[0][k], s1 = share.sums[1][k], s2 = share.sums[2][k], s3 = share.sums[3][k];
+        before = (wave > 0 ? s0 : 0) + (wave > 1 ? s1 : 0) + (wave > 2 ? s2 : 0);
+        all = s0 + s1 + s2 + s3;
+    };
+    shared_tiles = scan64(shared_tiles);
+    solo_tiles = scan64(solo_tiles);
+    if (lane == 63) { share.sums[wave][0] = shared_tiles; share.sums[wave][1] = solo_tiles; }
+    __syncthreads();
+    int before, sum_shared, sum_solo;
+    over_waves(0, before, sum_shared);
+    over_waves(1, before, sum_solo);
+    const int64_t t_shared = ((int64_t)sum_shared << a.tile_shift) * a.Hkv, t_solo = ((int64_t)sum_solo << a.tile_shift) * a.Hkv;
     int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * ((float)t_shared / (float)(t_shared + t_solo)))) : 0;
     if (t_solo > 0) shared_wgs = min(shared_wgs, PLAN_WGS - 1);
     const int chunk_shared = shared_wgs ? chunk_for(t_shared, shared_wgs, 2) : 2;          // whole stages of 64 keys
@@ -139,48 +158,46 @@ __device__ __forceinline__ bool find_piece(const Lists& ls, int wave, int lane, 
         (s.shared ? n_shared : n_solo) += chunks * s.blocks * a.Hkv;
         rows += chunks * a.Hkv * s.rows;
     }
-    const int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
-    if (blockIdx.x == 0 && wave == 0) {         // what the join needs to know of each list
-        int base = to_rows - rows;
+    int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
+    __syncthreads();
+    if (lane == 63) { share.sums[wave][0] = to_shared; share.sums[wave][1] = to_solo; share.sums[wave][2] = to_rows; }
+    __syncthreads();
+    int all_shared, all_solo, all_rows;
+    over_waves(0, before, all_shared); to_shared += before;
+    over_waves(1, before, all_solo); to_solo += before;
+    over_waves(2, before, all_rows); to_rows += before;
+    const bool shared = (int)blockIdx.x < all_shared;
+    const int first = shared ? (int)blockIdx.x : ((int)blockIdx.x - all_shared) * 4, many = shared ? 1 : 4;      // this workgroup's pieces
+    const int to = shared ? to_shared : to_solo, from = to - (shared ? n_shared : n_solo);
+    const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know of each list
+    if (tells || (from < first + many && to > first)) {
+        int at = from, base = to_rows - rows;
         for (int i = i0; i < i1; ++i) {
             const ListShape s = ls.shape<F32>(i);
-            const int chunks = chunks_of(s.tiles, s.shared ? chunk_shared : chunk_solo);
-            const bool out = i >= a.n_groups && a.resp_lens[i - a.n_groups] < 0;
-            a.desc[i] = int2{base, out ? -1 : chunks};
+            const int chunks = chunks_of(s.tiles, s.shared ? chunk_shared : chunk_solo), count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
+            for (int k = max(at, first); k < min(at + count, first + many); ++k) {
+                share.list[k - first] = i; share.left[k - first] = k - at; share.base[k - first] = base;
+            }
+            if (tells) a.desc[i] = int2{base, i >= a.n_groups && s.len < 0 ? -1 : chunks};
+            at += count;
             base += chunks * a.Hkv * s.rows;
         }
     }
-    const int all_shared = __builtin_amdgcn_readlane(to_shared, 63), all_solo = __builtin_amdgcn_readlane(to_solo, 63);
-    const bool shared = (int)blockIdx.x < all_shared;
-    const int index = shared ? (int)blockIdx.x : ((int)blockIdx.x - all_shared) * 4 + wave;
-    if (!shared && index >= all_solo) return false;
-    const int to = shared ? to_shared : to_solo, own = shared ? n_shared : n_solo;
-    const uint64_t here = __builtin_amdgcn_ballot_w64(index >= to - own && index < to);
-    const int src = __ffsll((unsigned long long)here) - 1;                  // the lane whose lists hold the piece
-    int left = index - __builtin_amdgcn_readlane(to - own, src), base = __builtin_amdgcn_readlane(to_rows - rows, src);
-    const int j1 = min(n, (src + 1) * per);
-    p = Piece{};
-    shape = ListShape{};
-    for (int i = src * per; i < j1; ++i) {
-        const ListShape s = ls.shape<F32>(i);
-        const int ct = s.shared ? chunk_shared : chunk_solo, chunks = chunks_of(s.tiles, ct), count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
-        if (left < count) {
-            p.list = i; p.base = base; p.chunk_tiles = ct;
-            shape = s;
-            break;
-        }
-        left -= count;
-        base += chunks * a.Hkv * s.rows;
-    }
-    // the same in every lane, which the compiler does not see
-    auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
-    scalar(p.list); scalar(p.base); scalar(p.chunk_tiles); scalar(left);
-    scalar(shape.rows); scalar(shape.len); scalar(shape.tiles); scalar(shape.blocks);
-    shape.shared = shared;
+    __syncthreads();
+    if (!shared && first + wave >= all_solo) return false;
+    const int slot = shared ? 0 : wave;
+    auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };      // the same in every lane, which the compiler does not see
+    p.list = scalar(share.list[slot]);
+    p.base = scalar(share.base[slot]);
+    const ListShape s = ls.shape<F32>(p.list);
+    p.rows = scalar(s.rows); p.len = scalar(s.len); p.blocks = scalar(s.blocks);
+    p.shared = shared;
+    p.chunk_tiles = scalar(shared ? chunk_shared : chunk_solo);
     unsigned rest;
-    left = (int)divmod((unsigned)left, a.kv_heads, rest);
+    int left = (int)divmod((unsigned)scalar(share.left[slot]), a.kv_heads, rest);
     p.kvh = (int)rest;
-    if (shape.blocks > 1) { p.block = left % shape.blocks; left /= shape.blocks; }
+    p.block = 0;
+    if (p.blocks > 1) { p.block = left % p.blocks; left /= p.blocks; }
     p.chunk = left;
     return true;
 }
@@ -387,33 +404,21 @@ __device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArg
     }
 }
 
-// Lengths of all lists to LDS, where the plan reads them up to four times
-__device__ __forceinline__ Lists read_lists(const TabArg& starts, const DecodeArgs& a, int* lds) {
-    const int n = a.n_groups + a.n_seqs;
-    Lists ls{table_of(starts), n <= LENS_IN_LDS ? lds : nullptr, a};
-    if (ls.lens) {
-        for (int i = threadIdx.x; i < n; i += 256) lds[i] = ls.length(i);
-        __syncthreads();
-    }
-    return ls;
-}
-
 template <int D, int NC>
 __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArgs a) {
     constexpr int KEYS16 = 32 * D;               // bytes of 16 keys
     __shared__ __attribute__((aligned(1024))) char lds[16 * KEYS16];
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
-    const Lists ls = read_lists(starts, a, reinterpret_cast<int*>(lds));
+    __shared__ PlanShare share;
     Piece p;
-    ListShape shape;
-    const bool has = find_piece<false>(ls, w, l, p, shape);
-    __syncthreads();                             // the lengths' place is free
+    const bool has = find_piece<false>(starts, a, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l, p);
+    __syncthreads();                             // the lists' place is free
     if (!has) return;
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
-    const int len = shape.len, key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
-    PieceRows pr{prompt ? ls.starts[p.list] : own, a.rep, shape.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * shape.rows};
+    const int key0 = p.chunk * p.chunk_tiles * 32, key1 = (int)min((unsigned)p.len, (unsigned)key0 + 32u * p.chunk_tiles);
+    PieceRows pr{prompt ? table_of(starts)[p.list] : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
     pages.load(key0 >> a.log_page);
     const Copier<D> copy(l);
@@ -430,10 +435,10 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     const __bf16* const q = (const __bf16*)a.q;
     const unsigned buf = lds_address(lds);
 
-    if (!shape.shared) {
+    if (!p.shared) {
         // one wave: K and V of 32 keys in turn, the next K copied while the weights and the second product run, the next V under the next scores
         Rows<D, 2> r;
-        const int row0 = p.block * SOLO_ROWS, tiles = min(2, (shape.rows - row0 + 15) >> 4);
+        const int row0 = p.block * SOLO_ROWS, tiles = min(2, (p.rows - row0 + 15) >> 4);
         load_rows(r, q, pr, row0, tiles, l);
         r.clear(a.m_none);
         const unsigned kb = buf + w * 4 * KEYS16, vb = kb + 2 * KEYS16;
@@ -467,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     } else {
         // four waves: 64 keys of K and V in one half of LDS while the next 64 are copied into the other, a wave copying 16 keys of each
         Rows<D, NC> r;
-        const int all = (shape.rows + 15) >> 4, per = (all + shape.blocks - 1) / shape.blocks, first = p.block * per, n = min(per, all - first);
+        const int all = (p.rows + 15) >> 4, per = (all + p.blocks - 1) / p.blocks, first = p.block * per, n = min(per, all - first);
         const int t0 = first + (w * n >> 2), tiles = ((w + 1) * n >> 2) - (w * n >> 2), row0 = 16 * t0;
         load_rows(r, q, pr, row0, tiles, l);
         r.clear(a.m_none);
@@ -515,21 +520,20 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
 // tile (h, e) is element 64 h + 4 m + e, so that V is read in pieces of 16 bytes as well.
 template <int D>
 __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, DecodeArgs a) {
-    __shared__ int lens[LENS_IN_LDS];
+    __shared__ i32x2 lists[4096];
+    __shared__ PlanShare share;
     constexpr int NC = SOLO_ROWS / 16, HALVES = D / 64;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, m16 = l & 15, j = l >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
-    const Lists ls = read_lists(starts, a, lens);
     Piece p;
-    ListShape shape;
-    if (!find_piece<true>(ls, w, l, p, shape)) return;
+    if (!find_piece<true>(starts, a, lists, 4096, share, w, l, p)) return;
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
-    const int len = shape.len, key0 = p.chunk * p.chunk_tiles * 32, key1 = min(len, key0 + p.chunk_tiles * 32);
-    PieceRows pr{prompt ? ls.starts[p.list] : own, a.rep, shape.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * shape.rows};
+    const int key0 = p.chunk * p.chunk_tiles * 32, key1 = (int)min((unsigned)p.len, (unsigned)key0 + 32u * p.chunk_tiles);
+    PieceRows pr{prompt ? table_of(starts)[p.list] : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
     pages.load(key0 >> a.log_page);
-    const int row0 = p.block * SOLO_ROWS, tiles = min(NC, (shape.rows - row0 + 15) >> 4);
+    const int row0 = p.block * SOLO_ROWS, tiles = min(NC, (p.rows - row0 + 15) >> 4);
     float q[NC][D / 4];
     f32x4 o[NC][HALVES][4];
     float m[NC], sum[NC];
@@ -704,7 +708,6 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     a.desc = (int2*)partials;
     a.stats = (float*)((char*)partials + desc_bytes(n_groups, n_seqs));
     a.sums = a.stats + up256((size_t)most_rows(n_seqs, Hq, a.rep) * 16) / 4;
-    // pieces at most: the plan's places and one per list, block and kv head
     int64_t shared = 0, solo = 0;
     int widest = 0;
     auto rows_of = [&](int g) { return (int64_t)a.rep * (Gs ? Gs[g] : 1); };
@@ -723,13 +726,19 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
                             ((double)n_seqs * a.rep / SOLO_ROWS + 1) + n_groups + n_seqs;
         while (most / (double)((int64_t)1 << a.tile_shift) + n_groups + n_seqs > 2e9) ++a.tile_shift;
     }
-    auto count = [&](int64_t rows, int64_t lists) {
-        if (rows > SOLO_ROWS && !cache.f32) shared += lists * ((rows + 64 * a.nc - 1) / (64 * a.nc));
-        else solo += lists * ((rows + SOLO_ROWS - 1) / SOLO_ROWS);
+    // the plan's places and one piece per list, block and kv head, or a piece per tile (stage of two) that the tables have room for
+    int64_t tiles_shared = 0, tiles_solo = 0;
+    auto count = [&](int64_t rows, int64_t lists, int64_t width) {
+        const int64_t tiles = (((width << a.log_page) + 31) >> 5) < ((int64_t)1 << 26) ? ((width << a.log_page) + 31) >> 5 : (int64_t)1 << 26;
+        const bool sh = rows > SOLO_ROWS && !cache.f32;
+        const int64_t blocks = lists * (sh ? (rows + 64 * a.nc - 1) / (64 * a.nc) : (rows + SOLO_ROWS - 1) / SOLO_ROWS);
+        (sh ? shared : solo) += blocks;
+        (sh ? tiles_shared : tiles_solo) += blocks * (sh ? (tiles + 1) / 2 : tiles);
     };
-    if (prompts) for (int g = 0; g < n_groups; ++g) count(rows_of(g), 1);
-    count(a.rep, n_seqs);
-    const int64_t grid = (shared ? PLAN_WGS + shared * a.Hkv : 0) + (solo ? PLAN_WGS + (solo * a.Hkv + 3) / 4 : 0);
+    if (prompts) for (int g = 0; g < n_groups; ++g) count(rows_of(g), 1, prompt_width);
+    count(a.rep, n_seqs, resp_width);
+    int64_t grid = PLAN_WGS + shared * a.Hkv + (solo * a.Hkv + 3) / 4 + 1;
+    grid = std::max<int64_t>(1, std::min(grid, tiles_shared * a.Hkv + (tiles_solo * a.Hkv + 3) / 4));
     auto launch = [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         if (cache.f32) hipLaunchKernelGGL((decode_f32_kernel<D>), dim3((unsigned)grid), dim3(256), 0, s, starts, a);
