@@ -31,9 +31,12 @@ struct DecodeArgs {
     const char* k_cache; const char* v_cache;
     const int* prompt_tables; const int* prompt_lens; const int* resp_tables; const int* resp_lens;
     int64_t prompt_width, resp_width;
+    int prompt_cap, resp_cap;              // tokens that a table holds (at most 2^31 - 1)
+    int members;                           // sequences of each group, 0: of several sizes
+    Div group_size, block_rows;            // of `members`, of the rows of a shared piece
     int n_pages, n_groups, n_seqs, Hq, Hkv, rep, log_page;
     int nc, tile_shift;                    // row tiles per wave of a shared piece; see find_piece()
-    Div kv_heads;
+    Div kv_heads, q_heads, heads_each;     // of Hkv, Hq, rep
     float c, m_none;                       // softmax_scale * log2(e); reference point of a row that has not seen a key
     uint32_t* tag;
     int2* desc;                            // per list: first row of its sums, chunks (-1: a sequence that takes no part)
@@ -81,58 +84,70 @@ struct Piece { int list, chunk, kvh, block, base, chunk_tiles, rows, len, blocks
 struct PlanShare { int sums[4][3]; int left[4], list[4], base[4]; };     // of the waves of a workgroup; their pieces
 
 struct Lists {
-    const int* starts;                       // first sequence of each group
+    const int* starts;                       // first sequence of each group, where groups are of several sizes
     const i32x2* held;                       // rows and length of each list in LDS, or nullptr
     const DecodeArgs& a;
     __device__ __forceinline__ i32x2 read(int i) const {
         const bool prompt = i < a.n_groups;
-        const int64_t cap = (prompt ? a.prompt_width : a.resp_width) << a.log_page;
-        const int n = prompt ? (a.prompt_lens ? a.prompt_lens[i] : 0) : a.resp_lens[i - a.n_groups];
-        return i32x2{a.rep * (prompt ? starts[i + 1] - starts[i] : 1), n < 0 ? -1 : (int)min((int64_t)n, cap)};
+        const int prompt_cap = a.prompt_cap, resp_cap = a.resp_cap;
+        const int* const prompt_lens = a.prompt_lens;
+        const int* const resp_lens = a.resp_lens - a.n_groups;
+        const int n = prompt && !prompt_cap ? 0 : (prompt ? prompt_lens : resp_lens)[i];
+        int members = 1;
+        if (prompt) members = a.members ? a.members : starts[i + 1] - starts[i];
+        return i32x2{a.rep * members, min(max(n, -1), prompt ? prompt_cap : resp_cap)};
     }
-    template <bool F32> __device__ __forceinline__ ListShape shape(int i) const {
-        const i32x2 x = held ? held[i] : read(i);
+    template <bool F32> __device__ __forceinline__ ListShape shape(i32x2 x) const {
         ListShape s;
         s.rows = x[0];
         s.len = x[1];
         s.tiles = s.rows > 0 && s.len > 0 ? (int)(((unsigned)s.len + 31u) >> 5) : 0;
         s.shared = !F32 && s.rows > SOLO_ROWS;
-        s.blocks = 1;                        // (a division is some twenty instructions: only where there is more than one block)
-        const int per = s.shared ? 64 * a.nc : SOLO_ROWS;
-        if (s.rows > per) s.blocks = (int)((unsigned)(s.rows + per - 1) / (unsigned)per);
+        unsigned rest;
+        s.blocks = s.shared ? (int)divmod((unsigned)(s.rows - 1), a.block_rows, rest) + 1 : (s.rows + SOLO_ROWS - 1) / SOLO_ROWS;
         return s;
+    }
+    template <bool F32> __device__ __forceinline__ ListShape shape(int i) const { return shape<F32>(held ? held[i] : read(i)); }
+};
+
+// A chunk and its reciprocal.  Whole numbers: the least chunk of `unit` tiles with chunk * places >= total.  (The quotients are below the
+// number of places, a few thousand, so that a float is off by one at most.)
+struct Chunk {
+    int tiles; float inv;
+    __device__ __forceinline__ Chunk(int64_t total, int places, int unit) {
+        const int step = places * unit;
+        int c = (int)fminf((float)total * __builtin_amdgcn_rcpf((float)step), 1e8f);
+        c += (int64_t)c * step < total;
+        c += (int64_t)c * step < total;
+        tiles = max(c, 1) * unit;
+        inv = __builtin_amdgcn_rcpf((float)tiles);
+    }
+    __device__ __forceinline__ int of(int n) const {       // chunks of n tiles
+        int c = (int)((float)n * inv);
+        c -= c > 0 && (int64_t)c * tiles >= n;
+        c += (int64_t)c * tiles < n;
+        return c + ((int64_t)c * tiles < n);
     }
 };
 
-// the least chunk, a multiple of `unit`, with chunk * places >= total
-__device__ __forceinline__ int chunk_for(int64_t total, int places, int unit) {
-    const int64_t step = (int64_t)places * unit;
-    int64_t c = (int64_t)((float)total / (float)step);
-    while (c * step < total) ++c;
-    while (c > 1 && (c - 1) * step >= total) --c;
-    return (int)min(max(c, (int64_t)1) * unit, (int64_t)1 << 28);
-}
-__device__ __forceinline__ int chunks_of(int tiles, int chunk) { return tiles <= chunk ? tiles > 0 : (int)((unsigned)(tiles + chunk - 1) / (unsigned)chunk); }
-
-// The piece of this wave (of a shared list: of the workgroup).  Every workgroup makes the whole plan: a thread adds up its share of
-// the lists, which lie in LDS meanwhile (n_held of them fit), the workgroup their sums.  Pieces of shared lists come first, one per workgroup, then those of
+// The piece of this wave (of a shared list: of the workgroup).  Every workgroup makes the whole plan: its threads add up the tiles of
+// all lists, leaving them in LDS (n_held of them fit).  Pieces of shared lists come first, one per workgroup, then those of
 // single waves, four per workgroup.  The chunk of either kind follows from the tiles (row blocks counted) per place, the places being
 // dealt by tiles, so there are no more pieces than places and one per list, block and kv head.
 // (tile_shift: tiles are added up in units that keep their sum within 31 bits, rounded up.)
+// Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time.
 template <bool F32>
 __device__ __forceinline__ bool find_piece(const TabArg& starts, const DecodeArgs& a, i32x2* held, int n_held, PlanShare& share, int wave, int lane, Piece& p) {
     const int n = a.n_groups + a.n_seqs;
     const Lists ls{table_of(starts), n <= n_held ? held : nullptr, a};
-    if (ls.held) {
-        for (int i = threadIdx.x; i < n; i += 256) held[i] = ls.read(i);
-        __syncthreads();
-    }
-    const int per = (n + 255) >> 8, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
     int shared_tiles = 0, solo_tiles = 0;
-    for (int i = i0; i < i1; ++i) {
-        const ListShape s = ls.shape<F32>(i);
-        const int t = (int)(((int64_t)s.tiles * s.blocks + (1 << a.tile_shift) - 1) >> a.tile_shift);
-        (s.shared ? shared_tiles : solo_tiles) += t;
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const i32x2 x = ls.read(i);
+        if (ls.held) held[i] = x;
+        const ListShape s = ls.shape<F32>(x);
+        const int t = ((s.tiles + (1 << a.tile_shift) - 1) >> a.tile_shift) * s.blocks;
+        shared_tiles += s.shared ? t : 0;
+        solo_tiles += s.shared ? 0 : t;
     }
     auto over_waves = [&](int k, int& before, int& all) {      // of a sum that each wave has left in share.sums[.][k]
         const int s0 = share.sums[0][k], s1 = share.sums[1][k], s2 = share.sums[2][k], s3 = share.sums[3][k];
@@ -147,15 +162,21 @@ __device__ __forceinline__ bool find_piece(const TabArg& starts, const DecodeArg
     over_waves(0, before, sum_shared);
     over_waves(1, before, sum_solo);
     const int64_t t_shared = ((int64_t)sum_shared << a.tile_shift) * a.Hkv, t_solo = ((int64_t)sum_solo << a.tile_shift) * a.Hkv;
-    int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * ((float)t_shared / (float)(t_shared + t_solo)))) : 0;
+    int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * ((float)t_shared * __builtin_amdgcn_rcpf((float)(t_shared + t_solo))))) : 0;
     if (t_solo > 0) shared_wgs = min(shared_wgs, PLAN_WGS - 1);
-    const int chunk_shared = shared_wgs ? chunk_for(t_shared, shared_wgs, 2) : 2;          // whole stages of 64 keys
-    const int chunk_solo = t_solo > 0 ? chunk_for(t_solo, 4 * (PLAN_WGS - shared_wgs), 1) : 1;
+    const Chunk chunk_shared(t_shared, max(1, min(shared_wgs, PLAN_WGS)), 2), chunk_solo(t_solo, 4 * max(1, PLAN_WGS - shared_wgs), 1);      // shared: whole stages of 64 keys
+    auto pick = [&](bool shared) {
+        Chunk c = chunk_solo;
+        if (shared) { c.tiles = chunk_shared.tiles; c.inv = chunk_shared.inv; }
+        return c;
+    };
+    const int per = (n + 255) >> 8, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
     int n_shared = 0, n_solo = 0, rows = 0;
     for (int i = i0; i < i1; ++i) {
         const ListShape s = ls.shape<F32>(i);
-        const int chunks = chunks_of(s.tiles, s.shared ? chunk_shared : chunk_solo);
-        (s.shared ? n_shared : n_solo) += chunks * s.blocks * a.Hkv;
+        const int chunks = pick(s.shared).of(s.tiles), count = chunks * s.blocks * a.Hkv;
+        n_shared += s.shared ? count : 0;
+        n_solo += s.shared ? 0 : count;
         rows += chunks * a.Hkv * s.rows;
     }
     int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
@@ -174,7 +195,7 @@ __device__ __forceinline__ bool find_piece(const TabArg& starts, const DecodeArg
         int at = from, base = to_rows - rows;
         for (int i = i0; i < i1; ++i) {
             const ListShape s = ls.shape<F32>(i);
-            const int chunks = chunks_of(s.tiles, s.shared ? chunk_shared : chunk_solo), count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
+            const int chunks = pick(s.shared).of(s.tiles), count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
             for (int k = max(at, first); k < min(at + count, first + many); ++k) {
                 share.list[k - first] = i; share.left[k - first] = k - at; share.base[k - first] = base;
             }
@@ -192,7 +213,7 @@ __device__ __forceinline__ bool find_piece(const TabArg& starts, const DecodeArg
     const ListShape s = ls.shape<F32>(p.list);
     p.rows = scalar(s.rows); p.len = scalar(s.len); p.blocks = scalar(s.blocks);
     p.shared = shared;
-    p.chunk_tiles = scalar(shared ? chunk_shared : chunk_solo);
+    p.chunk_tiles = scalar(shared ? chunk_shared.tiles : chunk_solo.tiles);
     unsigned rest;
     int left = (int)divmod((unsigned)scalar(share.left[slot]), a.kv_heads, rest);
     p.kvh = (int)rest;
@@ -372,9 +393,11 @@ struct Copier {
 struct PieceRows {
     int seq0, rep, rows, Hq, kvh;
     int64_t base;                       // of row 0 among the rows of sums
+    Div heads_each;
     __device__ __forceinline__ int64_t q_row(int r) const {        // row of q and o
-        const int member = r / rep;
-        return (int64_t)(seq0 + member) * Hq + kvh * rep + (r - member * rep);
+        unsigned hr;
+        const int member = (int)divmod((unsigned)r, heads_each, hr);
+        return (int64_t)(seq0 + member) * Hq + kvh * rep + (int)hr;
     }
 };
 
@@ -418,7 +441,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
     const int key0 = p.chunk * p.chunk_tiles * 32, key1 = (int)min((unsigned)p.len, (unsigned)key0 + 32u * p.chunk_tiles);
-    PieceRows pr{prompt ? table_of(starts)[p.list] : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows};
+    PieceRows pr{prompt ? (a.members ? p.list * a.members : table_of(starts)[p.list]) : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows, a.heads_each};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
     pages.load(key0 >> a.log_page);
     const Copier<D> copy(l);
@@ -530,7 +553,7 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, Decod
     const bool prompt = p.list < a.n_groups;
     const int own = p.list - a.n_groups;
     const int key0 = p.chunk * p.chunk_tiles * 32, key1 = (int)min((unsigned)p.len, (unsigned)key0 + 32u * p.chunk_tiles);
-    PieceRows pr{prompt ? table_of(starts)[p.list] : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows};
+    PieceRows pr{prompt ? (a.members ? p.list * a.members : table_of(starts)[p.list]) : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows, a.heads_each};
     Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
     pages.load(key0 >> a.log_page);
     const int row0 = p.block * SOLO_ROWS, tiles = min(NC, (p.rows - row0 + 15) >> 4);
@@ -622,14 +645,26 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
     const int l = threadIdx.x & 63, mine = l / LANES, e0 = 4 * (l % LANES);
     const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (item >= (int64_t)a.n_seqs * a.Hq) return;
-    const int seq = (int)(item / a.Hq), h = (int)(item - (int64_t)seq * a.Hq), kvh = h / a.rep, hr = h - kvh * a.rep;
-    int g = 0, hi = a.n_groups;
-    while (hi - g > 1) { const int mid = (g + hi) >> 1; if (w[mid] <= seq) g = mid; else hi = mid; }
+    unsigned in_seq;
+    const int seq = (int)divmod((unsigned)item, a.q_heads, in_seq), h = (int)in_seq;
+    unsigned hr;
+    const int kvh = (int)divmod((unsigned)h, a.heads_each, hr);
+    int g = 0, first, members = a.members;
+    if (members) {
+        unsigned rest;
+        g = (int)divmod((unsigned)seq, a.group_size, rest);
+        first = seq - (int)rest;
+    } else {
+        int hi = a.n_groups;
+        while (hi - g > 1) { const int mid = (g + hi) >> 1; if (w[mid] <= seq) g = mid; else hi = mid; }
+        first = w[g];
+        members = w[g + 1] - first;
+    }
     int2 dp = a.desc[g];
     const int2 dr = a.desc[a.n_groups + seq];
     if (dr.y < 0) dp.y = 0;
-    const int prompt_rows = (w[g + 1] - w[g]) * a.rep;
-    const int64_t base_p = dp.x + (int64_t)kvh * prompt_rows + (seq - w[g]) * a.rep + hr, base_r = dr.x + (int64_t)kvh * a.rep + hr;
+    const int prompt_rows = members * a.rep;
+    const int64_t base_p = dp.x + (int64_t)kvh * prompt_rows + (seq - first) * a.rep + hr, base_r = dr.x + (int64_t)kvh * a.rep + hr;
     const int n = dp.y + max(dr.y, 0);
     auto row_of = [&](int i) { return i < dp.y ? base_p + (int64_t)i * (a.Hkv * prompt_rows) : base_r + (int64_t)(i - dp.y) * (a.Hkv * a.rep); };
     float M = a.m_none, L = 0.f, LR = 0.f;
@@ -721,6 +756,14 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     if (a.rep > SOLO_ROWS && !cache.f32) widest = std::max(widest, per_wave(a.rep));
     a.nc = std::max(1, widest);
     a.kv_heads = make_div(a.Hkv);
+    a.q_heads = make_div(Hq);
+    a.heads_each = make_div(a.rep);
+    a.block_rows = make_div(64 * a.nc);
+    a.prompt_cap = (int)std::min<int64_t>((int64_t)prompt_width << a.log_page, 0x7fffffff);
+    a.resp_cap = (int)std::min<int64_t>((int64_t)resp_width << a.log_page, 0x7fffffff);
+    a.members = Gs ? Gs[0] : 1;
+    for (int g = 1; Gs && g < n_groups; ++g) if (Gs[g] != Gs[0]) a.members = 0;
+    a.group_size = make_div(std::max(1, a.members));
     {   // tiles at most
         const double most = ((double)n_groups * prompt_width + (double)n_seqs * resp_width) * (1 << a.log_page) / 32 *
                             ((double)n_seqs * a.rep / SOLO_ROWS + 1) + n_groups + n_seqs;
