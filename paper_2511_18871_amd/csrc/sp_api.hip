@@ -755,6 +755,10 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
         return fail(SP_ERR_INVALID_ARG, "prompt_tables, prompt_lens and prompt_width, and resp_tables and resp_width, go together; resp_lens is needed");
     if (off4(prompt_tables) || off4(prompt_lens) || off4(resp_tables) || off4(resp_lens) || off4(lse))
         return fail(SP_ERR_INVALID_ARG, "a 32-bit array is not 4-byte aligned");
+    if ((int64_t)n_seqs * n_q_heads > 0x7fffffffLL ||
+        sp::decode_units(n_groups, n_seqs, n_q_heads, c.n_kv_heads, (int64_t)prompt_width << c.log_page, (int64_t)resp_width << c.log_page, Gs) > 2e9)
+        return fail(SP_ERR_INVALID_ARG, "%d sequences of %d heads with tables of %d and %d pages: more than one call serves", n_seqs, n_q_heads,
+                    prompt_width, resp_width);
     const size_t need = sp_attn_decode_workspace_bytes(n_groups, n_seqs, n_q_heads, c.n_kv_heads, c.head_dim, cache->dtype);
     if (!workspace || misaligned(workspace) || workspace_bytes < need)
         return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);

@@ -5,14 +5,15 @@
 //
 // Bound: the keys and values, each read once.  A LIST is what is walked together: the prompt of a group, seen by its G rep rows of
 // each kv head (rep = n_q_heads / n_kv_heads; row r is q head r % rep of the group's sequence r / rep), or the response of a
-// sequence, seen by its rep rows.  Lists are cut into chunks of keys; a chunk leaves unnormalised sums (m, l, sum p v) of its rows in the
-// workspace, and the join kernel adds up those of a row.  Lengths are on the device, so the cutting happens there: every workgroup
-// adds up the tiles of all lists, derives the chunk that fills the chip, and finds its own piece (Plan).
+// sequence, seen by its rep rows.  The units of keys of all lists lie one behind the other (list by list, in it block of rows by
+// block, kv head by kv head: a SEGMENT each), and every worker takes an equal run of them, across segments: no worker waits for a
+// longer one.  Where a worker leaves a segment it leaves unnormalised sums (m, l, sum p v) of its rows in the workspace; the join kernel adds up
+// those of a row.  Lengths are on the device, so the dealing happens there, by every workgroup for itself.
 //
 // Products on matrix instructions of 16 x 16: S^T = K Q^T (keys x rows) leaves a lane with scores of one row, four keys in turn, and
 // these are, rounded, the operand of O^T += V^T P^T as they stand, if the keys of V are taken in the same order.
-//   a list of at most 32 rows   a wave takes a piece by itself: 32 keys at a time through 16 KB of LDS of its own, no barriers
-//   more rows                   the four waves of a workgroup share 64 keys at a time and have up to 16 NC rows each
+//   a list of at most 32 rows   the worker is a wave: units of 32 keys through 16 KB of LDS of its own, no barriers
+//   more rows                   the worker is a workgroup: its four waves share units of 64 keys and have up to 16 NC rows each
 #include "sp_common.hpp"
 #include "sp_launch.hpp"
 #include <algorithm>
@@ -21,10 +22,13 @@
 namespace sp {
 namespace {
 
-constexpr int SOLO_ROWS = 32;              // rows of a list that a wave takes by itself
+#define SP_INLINE __attribute__((always_inline))      // lambdas: what they refer to has to stay in registers
+
+constexpr int SOLO_ROWS = 32;              // rows of a segment that a wave takes by itself
 constexpr int MAX_NC = 3;                  // row tiles of 16 of a wave that shares its keys: 192 rows to a workgroup
-constexpr int PLAN_WGS = 512;              // workgroups that the pieces are made for: two to a CU
-constexpr int PLAN_SOLO = 4 * PLAN_WGS;    // pieces of single waves, at most, that the chunk is made for
+constexpr int PLAN_WGS = 512;              // workgroups that the units are dealt to: two to a CU
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct DecodeArgs {
     const void* q; void* o; float* lse;
@@ -33,14 +37,19 @@ struct DecodeArgs {
     int64_t prompt_width, resp_width;
     int prompt_cap, resp_cap;              // tokens that a table holds (at most 2^31 - 1)
     int members;                           // sequences of each group, 0: of several sizes
-    Div group_size, block_rows;            // of `members`, of the rows of a shared piece
     int n_pages, n_groups, n_seqs, Hq, Hkv, rep, log_page;
-    int nc, tile_shift;                    // row tiles per wave of a shared piece; see find_piece()
+    int nc;                                // row tiles per wave of a shared segment
+    float shared_cost;                     // of a shared unit, against a solo one
+    Div group_size, block_rows;            // of `members`, of the rows of a shared segment (64 nc)
     Div kv_heads, q_heads, heads_each;     // of Hkv, Hq, rep
     float c, m_none;                       // softmax_scale * log2(e); reference point of a row that has not seen a key
     uint32_t* tag;
-    int2* desc;                            // per list: first row of its sums, chunks (-1: a sequence that takes no part)
-    float* stats;                          // per row of sums: m, l, l of the rounded weights, 0
+    i32x4* desc;                           // [0]: units of a worker, shared and solo; [1 + i], of list i: units ahead of it among its kind,
+                                           // units of a segment, blocks ahead of it among its kind, 1 for a sequence that takes no part
+    // Slots of sums.  Worker w's sums of segment s (both counted within their kind) lie in slot w + s: either grows by one at a time.
+    int shared_rows, prompt_rows, resp_rows;                 // rows of a slot of shared lists, and of solo prompts and responses
+    int64_t prompt_base, resp_base;                          // first row of the solo prompts' slots, of the responses'
+    float* stats;                          // per row of a slot: m, l
     float* sums;                           // per row: sum p v
 };
 
@@ -79,15 +88,15 @@ __device__ __forceinline__ float wave_sum(float x) {
     return quad_sum(x);
 }
 
-struct ListShape { int rows, len, tiles, blocks; bool shared; };      // tiles of 32 keys; blocks of rows that a piece holds
-struct Piece { int list, chunk, kvh, block, base, chunk_tiles, rows, len, blocks; bool shared; };
-struct PlanShare { int sums[4][3]; int left[4], list[4], base[4]; };     // of the waves of a workgroup; their pieces
+struct ListShape { int rows, len, units, blocks; bool shared; };      // units of keys of a segment; blocks of rows
+struct PlanShare { int sums[4][4]; int list[4], at[4], ord[4], rows[4], len[4]; };      // of the waves of a workgroup; where their runs start
 
+// KIND 0: all lists are solo, 1: shared ones too
+template <int KIND>
 struct Lists {
     const int* starts;                       // first sequence of each group, where groups are of several sizes
-    const i32x2* held;                       // rows and length of each list in LDS, or nullptr
     const DecodeArgs& a;
-    __device__ __forceinline__ i32x2 read(int i) const {
+    __device__ __forceinline__ i32x2 read(int i) const {      // rows and length, -1: takes no part
         const bool prompt = i < a.n_groups;
         const int prompt_cap = a.prompt_cap, resp_cap = a.resp_cap;
         const int* const prompt_lens = a.prompt_lens;
@@ -97,131 +106,194 @@ struct Lists {
         if (prompt) members = a.members ? a.members : starts[i + 1] - starts[i];
         return i32x2{a.rep * members, min(max(n, -1), prompt ? prompt_cap : resp_cap)};
     }
-    template <bool F32> __device__ __forceinline__ ListShape shape(i32x2 x) const {
+    __device__ __forceinline__ ListShape shape(i32x2 x) const {
         ListShape s;
         s.rows = x[0];
         s.len = x[1];
-        s.tiles = s.rows > 0 && s.len > 0 ? (int)(((unsigned)s.len + 31u) >> 5) : 0;
-        s.shared = !F32 && s.rows > SOLO_ROWS;
+        s.shared = KIND && s.rows > SOLO_ROWS;
+        s.units = s.rows > 0 && s.len > 0 ? (int)(((unsigned)s.len + (s.shared ? 63u : 31u)) >> (s.shared ? 6 : 5)) : 0;
         unsigned rest;
         s.blocks = s.shared ? (int)divmod((unsigned)(s.rows - 1), a.block_rows, rest) + 1 : (s.rows + SOLO_ROWS - 1) / SOLO_ROWS;
         return s;
     }
-    template <bool F32> __device__ __forceinline__ ListShape shape(int i) const { return shape<F32>(held ? held[i] : read(i)); }
+    __device__ __forceinline__ int first_seq(int i) const { return i >= a.n_groups ? i - a.n_groups : a.members ? i * a.members : starts[i]; }
 };
 
-// A chunk and its reciprocal.  Whole numbers: the least chunk of `unit` tiles with chunk * places >= total.  (The quotients are below the
-// number of places, a few thousand, so that a float is off by one at most.)
-struct Chunk {
-    int tiles; float inv;
-    __device__ __forceinline__ Chunk(int64_t total, int places, int unit) {
-        const int step = places * unit;
-        int c = (int)fminf((float)total * __builtin_amdgcn_rcpf((float)step), 1e8f);
-        c += (int64_t)c * step < total;
-        c += (int64_t)c * step < total;
-        tiles = max(c, 1) * unit;
-        inv = __builtin_amdgcn_rcpf((float)tiles);
-    }
-    __device__ __forceinline__ int of(int n) const {       // chunks of n tiles
-        int c = (int)((float)n * inv);
-        c -= c > 0 && (int64_t)c * tiles >= n;
-        c += (int64_t)c * tiles < n;
-        return c + ((int64_t)c * tiles < n);
-    }
-};
+// ceil(total / places), total < 2^31, from a float quotient that is no more than one (for large ones 2^-20 of it) low
+__device__ __forceinline__ int per_place(int total, int places) {
+    int c = max(1, (int)((float)total * __builtin_amdgcn_rcpf((float)places) * 0.999999f));
+#pragma unroll 1
+    while ((int64_t)c * places < total) ++c;
+    return c;
+}
 
-// The piece of this wave (of a shared list: of the workgroup).  Every workgroup makes the whole plan: its threads add up the tiles of
-// all lists, leaving them in LDS (n_held of them fit).  Pieces of shared lists come first, one per workgroup, then those of
-// single waves, four per workgroup.  The chunk of either kind follows from the tiles (row blocks counted) per place, the places being
-// dealt by tiles, so there are no more pieces than places and one per list, block and kv head.
-// (tile_shift: tiles are added up in units that keep their sum within 31 bits, rounded up.)
+// What a worker does: `left` units from unit `at` of a list on (counted over the list's segments).
+struct Work { bool shared; int worker, list, at, ord, left; i32x2 list_is; };
+
+// Every workgroup makes the whole plan: a thread adds up the units of its share of the lists (MANY: more lists than threads; they lie in LDS meanwhile
+// if there are no more than n_held), the workgroup their sums.  Places are dealt by cost: a segment costs, for its rows and its sums, what
+// one and a half of its units (shared) or one (solo) cost, and a shared unit what shared_cost solo ones do.  Workgroups of shared lists come first.
 // Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time.
-template <bool F32>
-__device__ __forceinline__ bool find_piece(const TabArg& starts, const DecodeArgs& a, i32x2* held, int n_held, PlanShare& share, int wave, int lane, Piece& p) {
-    const int n = a.n_groups + a.n_seqs;
-    const Lists ls{table_of(starts), n <= n_held ? held : nullptr, a};
-    int shared_tiles = 0, solo_tiles = 0;
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const i32x2 x = ls.read(i);
-        if (ls.held) held[i] = x;
-        const ListShape s = ls.shape<F32>(x);
-        const int t = ((s.tiles + (1 << a.tile_shift) - 1) >> a.tile_shift) * s.blocks;
-        shared_tiles += s.shared ? t : 0;
-        solo_tiles += s.shared ? 0 : t;
+template <int KIND, bool MANY>
+__device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, int n_held, PlanShare& share, int wave, int lane) {
+    constexpr int SUMS = KIND ? 4 : 2;       // solo units and blocks, shared units and blocks
+    const DecodeArgs& a = ls.a;
+    const int n = a.n_groups + a.n_seqs, per = MANY ? (n + 255) >> 8 : 1, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
+    i32x2 mine{0, 0};
+    const bool in_lds = MANY && n <= n_held;
+    if constexpr (!MANY) {
+        if (i0 < n) mine = ls.read(i0);
+    } else if (in_lds) {
+        for (int i = threadIdx.x; i < n; i += 256 * 4) {      // four reads in flight
+            i32x2 x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) if (i + 256 * u < n) x[u] = ls.read(i + 256 * u);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) if (i + 256 * u < n) held[i + 256 * u] = x[u];
+        }
+        __syncthreads();
     }
-    auto over_waves = [&](int k, int& before, int& all) {      // of a sum that each wave has left in share.sums[.][k]
-        const int s0 = share.sums[0][k], s1 = share.sums[1][k], s2 = share.sums[2][k], s3 = share.sums[3][k];
-        before = (wave > 0 ? s0 : 0) + (wave > 1 ? s1 : 0) + (wave > 2 ? s2 : 0);
-        all = s0 + s1 + s2 + s3;
+    auto list_of = [&](int i) SP_INLINE { return !MANY ? mine : in_lds ? held[i] : ls.read(i); };
+    int own[SUMS] = {}, to[SUMS], all[SUMS];
+    auto add = [&](int (&sum)[SUMS], const ListShape& s) SP_INLINE {
+        sum[0] += s.shared ? 0 : s.units * s.blocks;
+        sum[1] += s.shared ? 0 : s.blocks;
+        if constexpr (KIND) {
+            sum[2] += s.shared ? s.units * s.blocks : 0;
+            sum[3] += s.shared ? s.blocks : 0;
+        }
     };
-    shared_tiles = scan64(shared_tiles);
-    solo_tiles = scan64(solo_tiles);
-    if (lane == 63) { share.sums[wave][0] = shared_tiles; share.sums[wave][1] = solo_tiles; }
-    __syncthreads();
-    int before, sum_shared, sum_solo;
-    over_waves(0, before, sum_shared);
-    over_waves(1, before, sum_solo);
-    const int64_t t_shared = ((int64_t)sum_shared << a.tile_shift) * a.Hkv, t_solo = ((int64_t)sum_solo << a.tile_shift) * a.Hkv;
-    int shared_wgs = t_shared > 0 ? max(1, (int)(PLAN_WGS * ((float)t_shared * __builtin_amdgcn_rcpf((float)(t_shared + t_solo))))) : 0;
-    if (t_solo > 0) shared_wgs = min(shared_wgs, PLAN_WGS - 1);
-    const Chunk chunk_shared(t_shared, max(1, min(shared_wgs, PLAN_WGS)), 2), chunk_solo(t_solo, 4 * max(1, PLAN_WGS - shared_wgs), 1);      // shared: whole stages of 64 keys
-    auto pick = [&](bool shared) {
-        Chunk c = chunk_solo;
-        if (shared) { c.tiles = chunk_shared.tiles; c.inv = chunk_shared.inv; }
-        return c;
-    };
-    const int per = (n + 255) >> 8, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
-    int n_shared = 0, n_solo = 0, rows = 0;
-    for (int i = i0; i < i1; ++i) {
-        const ListShape s = ls.shape<F32>(i);
-        const int chunks = pick(s.shared).of(s.tiles), count = chunks * s.blocks * a.Hkv;
-        n_shared += s.shared ? count : 0;
-        n_solo += s.shared ? 0 : count;
-        rows += chunks * a.Hkv * s.rows;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) add(own, ls.shape(list_of(i)));
+#pragma unroll
+    for (int k = 0; k < SUMS; ++k) {
+        to[k] = scan64(own[k]);
+        if (lane == 63) share.sums[wave][k] = to[k];
     }
-    int to_shared = scan64(n_shared), to_solo = scan64(n_solo), to_rows = scan64(rows);
     __syncthreads();
-    if (lane == 63) { share.sums[wave][0] = to_shared; share.sums[wave][1] = to_solo; share.sums[wave][2] = to_rows; }
-    __syncthreads();
-    int all_shared, all_solo, all_rows;
-    over_waves(0, before, all_shared); to_shared += before;
-    over_waves(1, before, all_solo); to_solo += before;
-    over_waves(2, before, all_rows); to_rows += before;
-    const bool shared = (int)blockIdx.x < all_shared;
-    const int first = shared ? (int)blockIdx.x : ((int)blockIdx.x - all_shared) * 4, many = shared ? 1 : 4;      // this workgroup's pieces
-    const int to = shared ? to_shared : to_solo, from = to - (shared ? n_shared : n_solo);
-    const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know of each list
-    if (tells || (from < first + many && to > first)) {
-        int at = from, base = to_rows - rows;
-        for (int i = i0; i < i1; ++i) {
-            const ListShape s = ls.shape<F32>(i);
-            const int chunks = pick(s.shared).of(s.tiles), count = s.shared == shared ? chunks * s.blocks * a.Hkv : 0;
-            for (int k = max(at, first); k < min(at + count, first + many); ++k) {
-                share.list[k - first] = i; share.left[k - first] = k - at; share.base[k - first] = base;
-            }
-            if (tells) a.desc[i] = int2{base, i >= a.n_groups && s.len < 0 ? -1 : chunks};
-            at += count;
-            base += chunks * a.Hkv * s.rows;
+#pragma unroll
+    for (int k = 0; k < SUMS; ++k) {
+        all[k] = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) { const int x = share.sums[w][k]; to[k] += w < wave ? x : 0; all[k] += x; }
+        all[k] *= a.Hkv;
+    }
+    int used = 0, shared_run = 1, solo_run = 1;
+    bool shared = false;
+    if constexpr (KIND) {
+        if (all[2] > 0) {
+            const float cost = a.shared_cost * ((float)all[2] + 1.5f * (float)all[3]), solo = (float)all[0] + (float)all[1];
+            int wgs = (int)(PLAN_WGS * (cost * __builtin_amdgcn_rcpf(cost + solo)));
+            wgs = max(1, min(wgs, all[0] > 0 ? PLAN_WGS - 1 : PLAN_WGS));
+            shared_run = per_place(all[2], wgs);
+            used = per_place(all[2], shared_run);
+            shared = (int)blockIdx.x < used;
         }
     }
+    if (all[0] > 0) solo_run = per_place(all[0], 4 * (PLAN_WGS - used));
+    // this workgroup's runs start at `first` and multiples of the run behind it
+    const int run = shared ? shared_run : solo_run, many = shared ? 1 : 4;
+    const int64_t first = shared ? (int64_t)blockIdx.x * run : ((int64_t)blockIdx.x - used) * 4 * run;
+    const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know
+    const int64_t through = (int64_t)(KIND && shared ? to[SUMS - 2] : to[0]) * a.Hkv, ahead = through - (int64_t)(KIND && shared ? own[SUMS - 2] : own[0]) * a.Hkv;
+    if (tells || (ahead < first + (int64_t)many * run && through > first)) {
+        int at[SUMS];
+#pragma unroll
+        for (int k = 0; k < SUMS; ++k) at[k] = to[k] - own[k];
+#pragma unroll 1
+        for (int i = i0; i < i1; ++i) {
+            const i32x2 x = list_of(i);
+            const ListShape s = ls.shape(x);
+            const int units = s.shared ? at[SUMS - 2] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1];
+            const int64_t from = (int64_t)units * a.Hkv, end = from + (int64_t)s.units * s.blocks * a.Hkv;
+            if (s.shared == shared)
+#pragma unroll 1
+                for (int k = 0; k < many; ++k) {
+                    const int64_t pos = first + (int64_t)k * run;
+                    if (pos >= from && pos < end) {
+                        share.list[k] = i; share.at[k] = (int)(pos - from); share.ord[k] = blocks;
+                        share.rows[k] = x[0]; share.len[k] = x[1];
+                    }
+                }
+            if (tells) a.desc[1 + i] = i32x4{units, s.units, blocks, s.len < 0};
+            add(at, s);
+        }
+        if (tells && threadIdx.x == 0) a.desc[0] = i32x4{shared_run, solo_run, 0, 0};
+    }
     __syncthreads();
-    if (!shared && first + wave >= all_solo) return false;
+    auto scalar = [](int x) SP_INLINE { return __builtin_amdgcn_readfirstlane(x); };      // the same in every lane, which the compiler does not see
     const int slot = shared ? 0 : wave;
-    auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };      // the same in every lane, which the compiler does not see
-    p.list = scalar(share.list[slot]);
-    p.base = scalar(share.base[slot]);
-    const ListShape s = ls.shape<F32>(p.list);
-    p.rows = scalar(s.rows); p.len = scalar(s.len); p.blocks = scalar(s.blocks);
-    p.shared = shared;
-    p.chunk_tiles = scalar(shared ? chunk_shared.tiles : chunk_solo.tiles);
-    unsigned rest;
-    int left = (int)divmod((unsigned)scalar(share.left[slot]), a.kv_heads, rest);
-    p.kvh = (int)rest;
-    p.block = 0;
-    if (p.blocks > 1) { p.block = left % p.blocks; left /= p.blocks; }
-    p.chunk = left;
-    return true;
+    const int64_t pos = first + (int64_t)slot * run, rest = (KIND && shared ? all[SUMS - 2] : all[0]) - pos;
+    Work work;
+    work.shared = shared;
+    work.left = rest > 0 ? scalar((int)min((int64_t)run, rest)) : 0;
+    work.worker = scalar(shared ? (int)blockIdx.x : ((int)blockIdx.x - used) * 4 + wave);
+    work.list = scalar(share.list[slot]);
+    work.at = scalar(share.at[slot]);
+    work.ord = scalar(share.ord[slot]);
+    work.list_is = i32x2{share.rows[slot], share.len[slot]};
+    return work;
 }
+
+// A place among the units: of list `list` segment `seg` (block * n_kv_heads + kv head), unit `t`
+template <int KIND>
+struct Cursor {
+    const Lists<KIND>& ls;
+    const bool shared;
+    int list, seg, t, units, segs, rows, len, blocks, ord;
+    __device__ __forceinline__ Cursor(const Lists<KIND>& l, const Work& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
+        load(w.list_is);
+        seg = (int)((float)w.at * __builtin_amdgcn_rcpf((float)units));        // off by one at most, or low by 2^-22 of it
+        seg = __builtin_amdgcn_readfirstlane(seg);
+        if ((int64_t)seg * units > w.at) --seg;
+#pragma unroll 1
+        while ((int64_t)(seg + 1) * units <= w.at) ++seg;
+        t = w.at - seg * units;
+    }
+    __device__ __forceinline__ bool load(i32x2 x) {
+        const ListShape s = ls.shape(x);
+        auto scalar = [](int x) SP_INLINE { return __builtin_amdgcn_readfirstlane(x); };
+        rows = scalar(s.rows); len = scalar(s.len); units = scalar(s.units); blocks = scalar(s.blocks);
+        segs = blocks * ls.a.Hkv;
+        return s.shared == shared;
+    }
+    // the next unit; there is one
+    __device__ __forceinline__ void next() {
+        if (++t < units) return;
+        t = 0;
+        if (++seg < segs) return;
+        seg = 0;
+        ord += blocks;
+        do {
+            ++list;
+            if (load(ls.read(list))) { if (units > 0) return; ord += blocks; }
+        } while (list < ls.a.n_groups + ls.a.n_seqs - 1);
+    }
+};
+
+// Rows of a segment: where they come from, and the slot that they go to
+struct SegmentRows {
+    int seq0, rep, row0, rows, Hq, kvh, block;          // rows row0 ... row0 + rows - 1 of the list
+    int64_t base;                                // of row0 among the rows of sums
+    Div heads_each;
+    template <int KIND> __device__ __forceinline__ SegmentRows(const Cursor<KIND>& c, const DecodeArgs& a, int worker) {
+        unsigned k;
+        block = c.blocks > 1 ? (int)divmod((unsigned)c.seg, a.kv_heads, k) : 0;
+        kvh = c.blocks > 1 ? (int)k : c.seg;
+        const int per = c.shared ? 16 * (((((c.rows + 15) >> 4)) + c.blocks - 1) / c.blocks) : SOLO_ROWS;
+        row0 = block * per;
+        rows = min(per, c.rows - row0);
+        seq0 = c.ls.first_seq(c.list);
+        rep = a.rep; Hq = a.Hq; heads_each = a.heads_each;
+        const int64_t slot = (int64_t)worker + (int64_t)c.ord * a.Hkv + c.seg;
+        base = c.shared ? slot * a.shared_rows : c.list < a.n_groups ? a.prompt_base + slot * a.prompt_rows : a.resp_base + slot * a.resp_rows;
+    }
+    __device__ __forceinline__ int64_t q_row(int r) const {        // row of q and o
+        unsigned hr;
+        const int member = (int)divmod((unsigned)(row0 + r), heads_each, hr);
+        return (int64_t)(seq0 + member) * Hq + kvh * rep + (int)hr;
+    }
+};
 
 // ---- rows of a wave ---------------------------------------------------------------------------------------
 
@@ -235,13 +307,14 @@ template <int D> __device__ __forceinline__ int kv_off(int row, int granule) { r
 
 template <int D, int NC>
 struct Rows {
+    static_assert(NC <= 4, "one element of m and l per tile");
     f32x4 o[NC][D / 16];       // lane: row l % 16 of tile c, elements 16 dt + 4 (l / 16) + i
-    float m[NC], l[NC], lr[NC];
+    f32x4 m, l;                // (vectors: arrays of these ended up in LDS)
     bf16x8 q[NC][D / 32];
     __device__ __forceinline__ void clear(float m_none) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            m[c] = m_none; l[c] = 0.f; lr[c] = 0.f;
+            m[c] = m_none; l[c] = 0.f;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) o[c][dt] = f32x4{0, 0, 0, 0};
         }
@@ -287,8 +360,8 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
     }
 }
 
-// Weights of 32 keys from their scores, rounded to bf16 as the second product needs them: the rounding of a weight, 2^-9 at most
-// of it, is like that of o itself, and the sum that divides o is of the rounded ones (lr).
+// Weights of 32 keys from their scores, rounded to bf16 as the second product needs them: a rounding of 2^-9 of the weight at most, like
+// that of o itself, and of either sign.  Their sum is of the unrounded ones.
 template <int D, int NC>
 __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, int tiles, bf16x8 (&p)[NC]) {
 #pragma unroll
@@ -298,7 +371,7 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
         mx = quad_max(mx);
         if (__builtin_amdgcn_ballot_w64(mx > r.m[c]) != 0) {
             const float mn = fmaxf(r.m[c], mx), alpha = __builtin_amdgcn_exp2f((r.m[c] - mn) * c2);
-            r.l[c] *= alpha; r.lr[c] *= alpha;
+            r.l[c] *= alpha;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt)
 #pragma unroll
@@ -306,17 +379,14 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
             r.m[c] = mn;
         }
         const float mc = r.m[c] * c2;
-        float sum = 0.f, rounded = 0.f;
+        float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e >> 2][e & 3], c2, -mc));
             sum += x;
             p[c][e] = (__bf16)x;
         }
-        const bf16x8 one = {(__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f};
-        rounded = dot8(p[c], one, 0.f);
         r.l[c] += sum;
-        r.lr[c] += rounded;
     }
 }
 
@@ -343,7 +413,7 @@ __device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf1
 struct Pages {
     const int* table; int width, first, held, lane;
     __device__ __forceinline__ int at(int page) {
-        if (page - first >= 64) load(page);
+        if ((unsigned)(page - first) >= 64u) load(page);
         return __builtin_amdgcn_readlane(held, page - first);
     }
     __device__ __forceinline__ void load(int page) {
@@ -375,6 +445,7 @@ struct Copier {
     // `valid` of the 16 rows at `src` (negative or zero: none) to LDS address `dst`; rows that are not there read as zero, whatever memory holds
     __device__ __forceinline__ void rows16(uint64_t src, int valid, unsigned dst) const {
         src = uniform64(src);
+        dst = __builtin_amdgcn_readfirstlane(dst);
         valid = __builtin_amdgcn_readfirstlane(valid);
         if (valid >= 16) {
 #pragma unroll
@@ -389,20 +460,8 @@ struct Copier {
     }
 };
 
-// Where the rows of a piece come from and go to
-struct PieceRows {
-    int seq0, rep, rows, Hq, kvh;
-    int64_t base;                       // of row 0 among the rows of sums
-    Div heads_each;
-    __device__ __forceinline__ int64_t q_row(int r) const {        // row of q and o
-        unsigned hr;
-        const int member = (int)divmod((unsigned)r, heads_each, hr);
-        return (int64_t)(seq0 + member) * Hq + kvh * rep + (int)hr;
-    }
-};
-
 template <int D, int NC>
-__device__ __forceinline__ void load_rows(Rows<D, NC>& r, const __bf16* q, const PieceRows& pr, int row0, int tiles, int l) {
+__device__ __forceinline__ void load_rows(Rows<D, NC>& r, const __bf16* q, const SegmentRows& pr, int row0, int tiles, int l) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int row = row0 + 16 * c + (l & 15);
@@ -414,222 +473,274 @@ __device__ __forceinline__ void load_rows(Rows<D, NC>& r, const __bf16* q, const
 }
 
 template <int D, int NC>
-__device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArgs& a, const PieceRows& pr, int row0, int tiles, int l) {
+__device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArgs& a, const SegmentRows& pr, int row0, int tiles, int l) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int row = row0 + 16 * c + (l & 15);
-        const float lt = quad_sum(r.l[c]), lrt = quad_sum(r.lr[c]);
+        const float lt = quad_sum(r.l[c]);
         if (c >= tiles || row >= pr.rows) continue;
         float* const out = a.sums + (pr.base + row) * D + 4 * (l >> 4);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(out + 16 * dt) = r.o[c][dt];
-        if (l < 16) *reinterpret_cast<f32x4*>(a.stats + (pr.base + row) * 4) = f32x4{r.m[c], lt, lrt, 0.f};
+        if (l < 16) *reinterpret_cast<f32x2*>(a.stats + (pr.base + row) * 2) = f32x2{r.m[c], lt};
     }
 }
 
-template <int D, int NC>
+// NC = 0: no list is shared
+template <int D, int NC, bool MANY>
 __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArgs a) {
-    constexpr int KEYS16 = 32 * D;               // bytes of 16 keys
+    constexpr int KEYS16 = 32 * D, KIND = NC > 0;       // bytes of 16 keys
     __shared__ __attribute__((aligned(1024))) char lds[16 * KEYS16];
+    __shared__ PlanShare share;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
-    __shared__ PlanShare share;
-    Piece p;
-    const bool has = find_piece<false>(starts, a, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l, p);
+    const Lists<KIND> ls{table_of(starts), a};
+    Work work = find_work<KIND, MANY>(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
     __syncthreads();                             // the lists' place is free
-    if (!has) return;
-    const bool prompt = p.list < a.n_groups;
-    const int own = p.list - a.n_groups;
-    const int key0 = p.chunk * p.chunk_tiles * 32, key1 = (int)min((unsigned)p.len, (unsigned)key0 + 32u * p.chunk_tiles);
-    PieceRows pr{prompt ? (a.members ? p.list * a.members : table_of(starts)[p.list]) : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows, a.heads_each};
-    Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
-    pages.load(key0 >> a.log_page);
+    if (work.left == 0) return;
+    Cursor<KIND> at(ls, work);
+    auto kv_head = [&]() SP_INLINE {
+        unsigned k = (unsigned)at.seg;
+        if (KIND && at.blocks > 1) divmod((unsigned)at.seg, a.kv_heads, k);
+        return (int)k;
+    };
+    int kvh = kv_head();
+    Pages pages;
+    pages.lane = l;
+    auto table_of_list = [&]() SP_INLINE {
+        const bool prompt = at.list < a.n_groups;
+        pages.table = prompt ? a.prompt_tables + at.list * a.prompt_width : a.resp_tables + (at.list - a.n_groups) * a.resp_width;
+        pages.width = (int)(prompt ? a.prompt_width : a.resp_width);
+    };
+    auto next = [&]() SP_INLINE {
+        const int list = at.list, seg = at.seg;
+        at.next();
+        if (at.list != list) { table_of_list(); pages.load(0); }
+        if (at.seg != seg || at.list != list) kvh = kv_head();
+    };
+    table_of_list();
     const Copier<D> copy(l);
     const uint64_t kc = uniform64((uint64_t)(uintptr_t)a.k_cache), vc = uniform64((uint64_t)(uintptr_t)a.v_cache);
     // byte offset of 16 keys in either cache and how many of them there are
-    auto locate = [&](int key, uint64_t& at, int& valid) {
-        valid = min(16, key1 - key);
-        at = 0;
+    auto locate = [&](int key, uint64_t& off, int& valid) SP_INLINE {
+        valid = min(16, at.len - key);
+        off = 0;
         if (valid <= 0) return;
         const int page = __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page));
         if (page < 0 || page >= a.n_pages) { valid = 0; return; }
-        at = ((((uint64_t)(unsigned)page * a.Hkv + p.kvh) << a.log_page) + (key & ((1 << a.log_page) - 1))) * (2 * D);
+        off = ((((uint64_t)(unsigned)page * a.Hkv + kvh) << a.log_page) + (key & ((1 << a.log_page) - 1))) * (2 * D);
     };
     const __bf16* const q = (const __bf16*)a.q;
     const unsigned buf = lds_address(lds);
 
-    if (!p.shared) {
-        // one wave: K and V of 32 keys in turn, the next K copied while the weights and the second product run, the next V under the next scores
+    if (!KIND || !work.shared) {
+        // One wave: K and V of a unit in turn.  The next K is copied while the weights and the second product run, the next V under the
+        // next scores, also from segment to segment.
         Rows<D, 2> r;
-        const int row0 = p.block * SOLO_ROWS, tiles = min(2, (p.rows - row0 + 15) >> 4);
-        load_rows(r, q, pr, row0, tiles, l);
-        r.clear(a.m_none);
         const unsigned kb = buf + w * 4 * KEYS16, vb = kb + 2 * KEYS16;
-        uint64_t at[2];
+        uint64_t off[2];
         int valid[2];
-        auto fetch = [&](int key) { locate(key, at[0], valid[0]); locate(key + 16, at[1], valid[1]); };
-        auto issue = [&](uint64_t cache, unsigned dst) {
-            copy.rows16(cache + at[0], valid[0], dst);
-            copy.rows16(cache + at[1], valid[1], dst + KEYS16);
+        auto fetch = [&]() SP_INLINE {
+            locate(32 * at.t, off[0], valid[0]);
+            locate(32 * at.t + 16, off[1], valid[1]);
+        };
+        auto issue = [&](uint64_t cache, unsigned dst) SP_INLINE {
+            copy.rows16(cache + off[0], valid[0], dst);
+            copy.rows16(cache + off[1], valid[1], dst + KEYS16);
         };
         constexpr int N = 2 * Copier<D>::COPIES;
-        fetch(key0);
+        pages.load(32 * at.t >> a.log_page);
+        fetch();
         issue(kc, kb);
         issue(vc, vb);
-        for (int key = key0; key < key1; key += 32) {
-            const unsigned bits = low_bits(valid[0]) | low_bits(valid[1]) << 16;
-            const bool more = key + 32 < key1;
-            f32x4 s[2][2];
-            bf16x8 pw[2];
-            wait_copies<N>();
-            scores(r, kb, bits, tiles, l, s);
-            wait_lds();
-            if (more) { fetch(key + 32); issue(kc, kb); }
-            weights(r, s, a.c, tiles, pw);
-            if (more) wait_copies<N>(); else wait_copies<0>();
-            add_values(r, vb, pw, tiles, l);
-            wait_lds();
-            if (more) issue(vc, vb);
+        while (true) {
+            SegmentRows seg(at, a, work.worker);
+            const int tiles = (seg.rows + 15) >> 4;
+            load_rows(r, q, seg, 0, tiles, l);
+            r.clear(a.m_none);
+            bool more = true, same = true;
+            while (same) {
+                const unsigned bits = low_bits(valid[0]) | low_bits(valid[1]) << 16;
+                f32x4 s[2][2];
+                bf16x8 pw[2];
+                wait_copies<N>();
+                scores(r, kb, bits, tiles, l, s);
+                wait_lds();
+                same = at.t + 1 < at.units;
+                more = --work.left > 0;
+                same = same && more;
+                if (more) {
+                    next();
+                    fetch();
+                    issue(kc, kb);
+                }
+                weights(r, s, a.c, tiles, pw);
+                if (more) wait_copies<N>(); else wait_copies<0>();
+                add_values(r, vb, pw, tiles, l);
+                wait_lds();
+                if (more) issue(vc, vb);
+            }
+            store_rows(r, a, seg, 0, tiles, l);
+            if (!more) return;
         }
-        store_rows(r, a, pr, row0, tiles, l);
-    } else {
-        // four waves: 64 keys of K and V in one half of LDS while the next 64 are copied into the other, a wave copying 16 keys of each
+    } else if constexpr (KIND) {
+        // Four waves: a unit of K and V in one half of LDS while the next is copied into the other, a wave copying 16 keys of each,
+        // also from segment to segment.
         Rows<D, NC> r;
-        const int all = (p.rows + 15) >> 4, per = (all + p.blocks - 1) / p.blocks, first = p.block * per, n = min(per, all - first);
-        const int t0 = first + (w * n >> 2), tiles = ((w + 1) * n >> 2) - (w * n >> 2), row0 = 16 * t0;
-        load_rows(r, q, pr, row0, tiles, l);
-        r.clear(a.m_none);
-        uint64_t at;
+        unsigned half = 0;
+        const int odd = blockIdx.x & 256 ? 2 : 0;      // of two workgroups of a CU one begins with the larger share of uneven row tiles
         int valid[4];
-        auto issue = [&](int key, unsigned dst) {
-            uint64_t mine = 0;
+        auto issue = [&](unsigned dst) SP_INLINE {
+            uint64_t mine = 0, off;
             int v_mine = 0;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                locate(key + 16 * h, at, valid[h]);
-                if (h == w) { mine = at; v_mine = valid[h]; }
+                locate(64 * at.t + 16 * h, off, valid[h]);
+                if (h == w) { mine = off; v_mine = valid[h]; }
             }
             copy.rows16(kc + mine, v_mine, dst + w * KEYS16);
             copy.rows16(vc + mine, v_mine, dst + (4 + w) * KEYS16);
         };
-        unsigned half = 0;
-        issue(key0, buf);
-        for (int key = key0; key < key1; key += 64) {
-            const unsigned lo = low_bits(valid[0]) | low_bits(valid[1]) << 16, hi = low_bits(valid[2]) | low_bits(valid[3]) << 16;
-            wait_copies<0>();
-            __syncthreads();
-            const unsigned kb = buf + half * 8 * KEYS16, vb = kb + 4 * KEYS16;
-            half ^= 1;
-            if (key + 64 < key1) issue(key + 64, buf + half * 8 * KEYS16);
-            if (tiles > 0) {
+        pages.load(64 * at.t >> a.log_page);
+        issue(buf);
+        while (true) {
+            SegmentRows seg(at, a, work.worker);
+            const int n = (seg.rows + 15) >> 4, t0 = (w * n + odd) >> 2, tiles = ((w + 1) * n + odd >> 2) - t0;
+            load_rows(r, q, seg, 16 * t0, tiles, l);
+            r.clear(a.m_none);
+            bool more = true, same = true;
+            while (same) {
+                const unsigned lo = low_bits(valid[0]) | low_bits(valid[1]) << 16, hi = low_bits(valid[2]) | low_bits(valid[3]) << 16;
+                wait_copies<0>();
+                __syncthreads();
+                const unsigned kb = buf + half * 8 * KEYS16, vb = kb + 4 * KEYS16;
+                half ^= 1;
+                more = --work.left > 0;
+                same = more && at.t + 1 < at.units;
+                if (more) { next(); issue(buf + half * 8 * KEYS16); }
+                if (tiles > 0) {
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    f32x4 s[NC][2];
-                    bf16x8 pw[NC];
-                    scores(r, kb + 2 * h * KEYS16, h ? hi : lo, tiles, l, s);
-                    weights(r, s, a.c, tiles, pw);
-                    add_values(r, vb + 2 * h * KEYS16, pw, tiles, l);
+                    for (int h = 0; h < 2; ++h) {
+                        f32x4 s[NC][2];
+                        bf16x8 pw[NC];
+                        scores(r, kb + 2 * h * KEYS16, h ? hi : lo, tiles, l, s);
+                        weights(r, s, a.c, tiles, pw);
+                        add_values(r, vb + 2 * h * KEYS16, pw, tiles, l);
+                    }
                 }
             }
+            store_rows(r, a, seg, 16 * t0, tiles, l);
+            if (!more) return;
         }
-        store_rows(r, a, pr, row0, tiles, l);
     }
 }
 
-// ---- float32: the same pieces, all of single waves, K and V read straight into the operands' registers ------------------------------
+// ---- float32: all workers are waves, K and V are read straight into the operands' registers ------------------------------
 
 // Products on float32 matrix instructions of 16 x 16 x 4.  S^T: lane group j = l / 16 contracts elements [j D / 4, (j + 1) D / 4) of its key, so
 // that it reads them in pieces of 16 bytes.  O^T += V^T P^T: step i contracts keys 4 j + i, whose weight is score i of the lane, and row m of
 // tile (h, e) is element 64 h + 4 m + e, so that V is read in pieces of 16 bytes as well.
-template <int D>
+template <int D, bool MANY>
 __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, DecodeArgs a) {
     __shared__ i32x2 lists[4096];
     __shared__ PlanShare share;
     constexpr int NC = SOLO_ROWS / 16, HALVES = D / 64;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, m16 = l & 15, j = l >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
-    Piece p;
-    if (!find_piece<true>(starts, a, lists, 4096, share, w, l, p)) return;
-    const bool prompt = p.list < a.n_groups;
-    const int own = p.list - a.n_groups;
-    const int key0 = p.chunk * p.chunk_tiles * 32, key1 = (int)min((unsigned)p.len, (unsigned)key0 + 32u * p.chunk_tiles);
-    PieceRows pr{prompt ? (a.members ? p.list * a.members : table_of(starts)[p.list]) : own, a.rep, p.rows, a.Hq, p.kvh, p.base + ((int64_t)p.chunk * a.Hkv + p.kvh) * p.rows, a.heads_each};
-    Pages pages{prompt ? a.prompt_tables + p.list * a.prompt_width : a.resp_tables + own * a.resp_width, (int)(prompt ? a.prompt_width : a.resp_width), 0, 0, l};
-    pages.load(key0 >> a.log_page);
-    const int row0 = p.block * SOLO_ROWS, tiles = min(NC, (p.rows - row0 + 15) >> 4);
-    float q[NC][D / 4];
-    f32x4 o[NC][HALVES][4];
-    float m[NC], sum[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int row = row0 + 16 * c + m16;
-        const float* const src = (const float*)a.q + pr.q_row(c < tiles && row < pr.rows ? row : 0) * D + j * (D / 4);
-#pragma unroll
-        for (int e = 0; e < D / 4; e += 4) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(src + e);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[c][e + i] = x[i];
-        }
-        m[c] = a.m_none; sum[c] = 0.f;
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][h][e] = f32x4{0, 0, 0, 0};
-    }
-    for (int key = key0; key < key1; key += 16) {
-        int valid = min(16, key1 - key);
-        const int page = pages.at(key >> a.log_page);
-        if (page < 0 || page >= a.n_pages) continue;
-        const int64_t row = ((((int64_t)page * a.Hkv + p.kvh) << a.log_page) + (key & ((1 << a.log_page) - 1)));
-        // keys behind the last one read the first one's row and are masked
-        const float* const kp = (const float*)a.k_cache + (row + (m16 < valid ? m16 : 0)) * D + j * (D / 4);
-        f32x4 k[D / 16], v[4][HALVES];
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) k[e] = *reinterpret_cast<const f32x4*>(kp + 4 * e);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float* const vp = (const float*)a.v_cache + (row + (4 * j + i < valid ? 4 * j + i : 0)) * D + 4 * m16;
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) v[i][h] = *reinterpret_cast<const f32x4*>(vp + 64 * h);
-        }
+    const Lists<0> ls{table_of(starts), a};
+    Work work = find_work<0, MANY>(ls, lists, 4096, share, w, l);
+    if (work.left == 0) return;
+    Cursor<0> at(ls, work);
+    Pages pages;
+    pages.lane = l;
+    while (true) {
+        SegmentRows seg(at, a, work.worker);
+        const bool prompt = at.list < a.n_groups;
+        pages.table = prompt ? a.prompt_tables + at.list * a.prompt_width : a.resp_tables + (at.list - a.n_groups) * a.resp_width;
+        pages.width = (int)(prompt ? a.prompt_width : a.resp_width);
+        const int run = min(work.left, at.units - at.t), key0 = 32 * at.t, key1 = (int)min((unsigned)at.len, 32u * (unsigned)(at.t + run));
+        pages.load(key0 >> a.log_page);
+        const int tiles = (seg.rows + 15) >> 4;
+        float q[NC][D / 4];
+        f32x4 o[NC][HALVES][4];
+        float m[NC], sum[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            if (c > 0 && c >= tiles) continue;
-            f32x4 s = {0, 0, 0, 0};
+            const int row = 16 * c + m16;
+            const float* const src = (const float*)a.q + seg.q_row(row < seg.rows ? row : 0) * D + j * (D / 4);
 #pragma unroll
-            for (int e = 0; e < D / 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e >> 2][e & 3], q[c][e], s, 0, 0, 0);
-            if (valid < 16)
+            for (int e = 0; e < D / 4; e += 4) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(src + e);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = 4 * j + i < valid ? s[i] : -INFINITY;
-            const float mn = fmaxf(m[c], quad_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])))), alpha = __builtin_amdgcn_exp2f((m[c] - mn) * a.c);
-            m[c] = mn;
-            float part = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { s[i] = __builtin_amdgcn_exp2f((s[i] - mn) * a.c); part += s[i]; }
-            sum[c] = sum[c] * alpha + part;
+                for (int i = 0; i < 4; ++i) q[c][e + i] = x[i];
+            }
+            m[c] = a.m_none; sum[c] = 0.f;
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[c][h][e][i] *= alpha;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[c][h][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][h][e], s[i], o[c][h][e], 0, 0, 0);
-                }
+                for (int e = 0; e < 4; ++e) o[c][h][e] = f32x4{0, 0, 0, 0};
         }
-    }
+        for (int key = key0; key < key1; key += 16) {
+            const int valid = min(16, key1 - key), page = __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page));
+            if (page < 0 || page >= a.n_pages) continue;
+            const int64_t row = ((((int64_t)page * a.Hkv + seg.kvh) << a.log_page) + (key & ((1 << a.log_page) - 1)));
+            // keys behind the last one read the first one's row; their scores are masked, and their values taken for zero
+            const float* const kp = (const float*)a.k_cache + (row + (m16 < valid ? m16 : 0)) * D + j * (D / 4);
+            f32x4 k[D / 16], v[4][HALVES];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int row = row0 + 16 * c + m16;
-        const float lt = quad_sum(sum[c]);
-        if (c >= tiles || row >= pr.rows) continue;
-        float* const out = a.sums + (pr.base + row) * D + 16 * j;
+            for (int e = 0; e < D / 16; ++e) k[e] = *reinterpret_cast<const f32x4*>(kp + 4 * e);
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
+            for (int i = 0; i < 4; ++i) {
+                const float* const vp = (const float*)a.v_cache + (row + (4 * j + i < valid ? 4 * j + i : 0)) * D + 4 * m16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4*>(out + 64 * h + 4 * i) = f32x4{o[c][h][0][i], o[c][h][1][i], o[c][h][2][i], o[c][h][3][i]};
-        if (j == 0) *reinterpret_cast<f32x4*>(a.stats + (pr.base + row) * 4) = f32x4{m[c], lt, lt, 0.f};
+                for (int h = 0; h < HALVES; ++h) v[i][h] = *reinterpret_cast<const f32x4*>(vp + 64 * h);
+                if (valid < 16 && 4 * j + i >= valid)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) v[i][h] = f32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                if (c > 0 && c >= tiles) continue;
+                f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < D / 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e >> 2][e & 3], q[c][e], s, 0, 0, 0);
+                if (valid < 16)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[i] = 4 * j + i < valid ? s[i] : -INFINITY;
+                const float mn = fmaxf(m[c], quad_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])))), alpha = __builtin_amdgcn_exp2f((m[c] - mn) * a.c);
+                m[c] = mn;
+                float part = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { s[i] = __builtin_amdgcn_exp2f((s[i] - mn) * a.c); part += s[i]; }
+                sum[c] = sum[c] * alpha + part;
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[c][h][e][i] *= alpha;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[c][h][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][h][e], s[i], o[c][h][e], 0, 0, 0);
+                    }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int row = 16 * c + m16;
+            const float lt = quad_sum(sum[c]);
+            if (row >= seg.rows) continue;
+            float* const out = a.sums + (seg.base + row) * D + 16 * j;
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(out + 64 * h + 4 * i) = f32x4{o[c][h][0][i], o[c][h][1][i], o[c][h][2][i], o[c][h][3][i]};
+            if (j == 0) *reinterpret_cast<f32x2*>(a.stats + (seg.base + row) * 2) = f32x2{m[c], lt};
+        }
+        work.left -= run;
+        if (work.left == 0) return;
+        at.t += run - 1;
+        at.next();
     }
 }
 
@@ -660,19 +771,37 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
         first = w[g];
         members = w[g + 1] - first;
     }
-    int2 dp = a.desc[g];
-    const int2 dr = a.desc[a.n_groups + seq];
-    if (dr.y < 0) dp.y = 0;
-    const int prompt_rows = members * a.rep;
-    const int64_t base_p = dp.x + (int64_t)kvh * prompt_rows + (seq - first) * a.rep + hr, base_r = dr.x + (int64_t)kvh * a.rep + hr;
-    const int n = dp.y + max(dr.y, 0);
-    auto row_of = [&](int i) { return i < dp.y ? base_p + (int64_t)i * (a.Hkv * prompt_rows) : base_r + (int64_t)(i - dp.y) * (a.Hkv * a.rep); };
-    float M = a.m_none, L = 0.f, LR = 0.f;
+    const i32x4 run = a.desc[0], dp = a.desc[1 + g], dr = a.desc[1 + a.n_groups + seq];
+    // consecutive slots: those of the workers that had units of this row's segment, from the first one's on
+    auto slots = [&](const i32x4& d, int rows, int row, bool prompt, int64_t& first_row, int& stride) {
+        const bool shared = sizeof(T) == 2 && rows > SOLO_ROWS;
+        int per = SOLO_ROWS;
+        if (shared) {
+            unsigned rest;
+            const int blocks = (int)divmod((unsigned)(rows - 1), a.block_rows, rest) + 1;
+            per = 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
+        }
+        const int block = rows > per ? row / per : 0, segment = block * a.Hkv + kvh, each = shared ? run[0] : run[1];
+        const unsigned from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[1];
+        const unsigned worker0 = from / (unsigned)each, worker1 = (from + d[1] - 1) / (unsigned)each;
+        stride = shared ? a.shared_rows : prompt ? a.prompt_rows : a.resp_rows;
+        first_row = (shared ? 0 : prompt ? a.prompt_base : a.resp_base) + ((int64_t)worker0 + (int64_t)d[2] * a.Hkv + segment) * stride + row - block * per;
+        return (int)(worker1 - worker0) + 1;
+    };
+    int64_t base_p = 0, base_r = 0;
+    int stride_p = 0, stride_r = 0, n_p = 0, n = 0;
+    if (!dr[3]) {
+        if (dp[1] > 0) n_p = slots(dp, members * a.rep, (seq - first) * a.rep + (int)hr, true, base_p, stride_p);
+        n = n_p + (dr[1] > 0 ? slots(dr, a.rep, (int)hr, false, base_r, stride_r) : 0);
+    }
+    auto row_of = [&](int i) { return i < n_p ? base_p + (int64_t)i * stride_p : base_r + (int64_t)(i - n_p) * stride_r; };
+    float M = a.m_none, L = 0.f;
     f32x4 acc = {0, 0, 0, 0};
     for (int i0 = 0; i0 < n; i0 += 64) {
         const int count = min(64, n - i0);
-        f32x4 st = {a.m_none, 0.f, 0.f, 0.f}, x[DEPTH];
-        if (l < count) st = *reinterpret_cast<const f32x4*>(a.stats + row_of(i0 + l) * 4);
+        f32x2 st = {a.m_none, 0.f};
+        f32x4 x[DEPTH];
+        if (l < count) st = *reinterpret_cast<const f32x2*>(a.stats + row_of(i0 + l) * 2);
         auto fetch = [&](int i) {
 #pragma unroll
             for (int u = 0; u < DEPTH; ++u) {
@@ -685,7 +814,6 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
         const float mn = fmaxf(M, wave_max(st[0])), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
         M = mn;
         L = L * alpha + wt * st[1];            // lanes hold their chunks' shares of the sums
-        LR = LR * alpha + wt * st[2];
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] *= alpha;
         for (int i = 0; i < count; i += DEPTH * AT_ONCE) {
@@ -699,12 +827,11 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
         }
     }
     L = wave_sum(L);
-    LR = wave_sum(LR);
 #pragma unroll
     for (int o = 32; o >= LANES; o >>= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
-    const float inv = L > 0.f ? 1.f / LR : 0.f;
+    const float inv = L > 0.f ? 1.f / L : 0.f;
     if (mine == 0) {
         typedef T out4 __attribute__((ext_vector_type(4)));
         out4 y;
@@ -715,18 +842,37 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
     if (l == 0) a.lse[(int64_t)h * a.n_seqs + seq] = L > 0.f ? M * (a.c * LN2) + __logf(L) : -INFINITY;
 }
 
-int64_t most_rows(int n_seqs, int Hq, int rep) {       // rows of sums: a chunk more than the plan's places per list
-    const int64_t in_group = (int64_t)n_seqs * rep;
-    return PLAN_WGS * std::min<int64_t>(64 * MAX_NC, in_group) + PLAN_SOLO * std::min<int64_t>(SOLO_ROWS, in_group) + 2 * (int64_t)n_seqs * Hq;
-}
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-size_t desc_bytes(int n_groups, int n_seqs) { return up256(((size_t)n_groups + n_seqs) * sizeof(int2)); }
+size_t desc_bytes(int n_groups, int n_seqs) { return up256(((size_t)n_groups + n_seqs + 1) * sizeof(i32x4)); }
+
+// Rows of slots at most, whatever the groups' sizes: a slot per worker and one per segment of each kind.  Shared: a list of r rows has at
+// most r / (64 nc) + 1 blocks of 64 nc <= 192 rows.
+struct SlotRows { int64_t shared, prompts, responses; };
+SlotRows slot_rows(int64_t n_groups, int64_t n_seqs, int64_t Hq, int64_t Hkv) {
+    const int64_t rep = Hq / Hkv, all = n_seqs * rep, widest = std::min<int64_t>(64 * MAX_NC, (std::max(all, rep) + 63) / 64 * 64);
+    const int64_t prompt_blocks = n_groups + all / SOLO_ROWS, resp_blocks = n_seqs * ((rep + SOLO_ROWS - 1) / SOLO_ROWS);
+    SlotRows s;
+    s.shared = all > SOLO_ROWS ? PLAN_WGS * widest + Hkv * (all + std::min(n_groups, all / (SOLO_ROWS + 1) + 1) * widest) : 0;
+    if (rep > SOLO_ROWS) s.shared += Hkv * (all + n_seqs * widest);
+    s.prompts = (4 * PLAN_WGS + Hkv * prompt_blocks) * std::min<int64_t>(SOLO_ROWS, all);
+    s.responses = (4 * PLAN_WGS + Hkv * (prompt_blocks + resp_blocks)) * std::min<int64_t>(SOLO_ROWS, rep);
+    return s;
+}
 
 }  // namespace
 
 size_t decode_partial_bytes(int n_groups, int n_seqs, int Hq, int Hkv, int d) {
-    const size_t rows = (size_t)most_rows(n_seqs, Hq, Hq / Hkv);
-    return desc_bytes(n_groups, n_seqs) + up256(rows * 16) + up256(rows * d * 4);
+    const SlotRows s = slot_rows(n_groups, n_seqs, Hq, Hkv);
+    const size_t rows = (size_t)(s.shared + s.prompts + s.responses);
+    return desc_bytes(n_groups, n_seqs) + up256(rows * 8) + up256(rows * d * 4);
+}
+
+// units of all segments that the tables have room for
+double decode_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_tokens, int64_t resp_tokens, const int32_t* Gs) {
+    const double rep = Hq / Hkv;
+    double units = 0;
+    for (int g = 0; g < n_groups; ++g) units += ((double)prompt_tokens / 32 + 1) * ((Gs ? Gs[g] : 1) * rep / SOLO_ROWS + 1);
+    return (units + ((double)resp_tokens / 32 + 1) * n_seqs * (rep / SOLO_ROWS + 1)) * Hkv;
 }
 
 hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, const TabArg& starts,
@@ -740,21 +886,39 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     a.c = scale * LOG2E;
     a.m_none = -3.4e38f / fmaxf(1.f, a.c);
     a.tag = tag;
-    a.desc = (int2*)partials;
+    const SlotRows slots = slot_rows(n_groups, n_seqs, Hq, a.Hkv);
+    a.desc = (i32x4*)partials;
     a.stats = (float*)((char*)partials + desc_bytes(n_groups, n_seqs));
-    a.sums = a.stats + up256((size_t)most_rows(n_seqs, Hq, a.rep) * 16) / 4;
-    int64_t shared = 0, solo = 0;
-    int widest = 0;
-    auto rows_of = [&](int g) { return (int64_t)a.rep * (Gs ? Gs[g] : 1); };
-    auto per_wave = [](int64_t rows) {      // row tiles per wave if the rows are dealt to as few workgroups as can hold them
-        const int64_t tiles = (rows + 15) / 16, blocks = (tiles + 4 * MAX_NC - 1) / (4 * MAX_NC), per = (tiles + blocks - 1) / blocks;
-        return (int)((per + 3) / 4);
-    };
+    a.sums = a.stats + up256((size_t)(slots.shared + slots.prompts + slots.responses) * 8) / 4;
+    a.prompt_base = slots.shared;
+    a.resp_base = slots.shared + slots.prompts;
+    // row tiles per wave if the rows of a shared list are dealt to as few workgroups as can hold them
     const bool prompts = prompt_width > 0;
-    for (int g = 0; g < n_groups; ++g)
-        if (prompts && rows_of(g) > SOLO_ROWS && !cache.f32) widest = std::max(widest, per_wave(rows_of(g)));
-    if (a.rep > SOLO_ROWS && !cache.f32) widest = std::max(widest, per_wave(a.rep));
-    a.nc = std::max(1, widest);
+    auto rows_of = [&](int g) { return (int64_t)a.rep * (Gs ? Gs[g] : 1); };
+    a.nc = 1;
+    auto widen = [&](int64_t rows) {
+        if (rows <= SOLO_ROWS || cache.f32) return;
+        const int64_t tiles = (rows + 15) / 16, blocks = (tiles + 4 * MAX_NC - 1) / (4 * MAX_NC), per = (tiles + blocks - 1) / blocks;
+        a.nc = std::max(a.nc, (int)((per + 3) / 4));
+    };
+    for (int g = 0; prompts && g < n_groups; ++g) widen(rows_of(g));
+    widen(a.rep);
+    // rows of a slot, and workgroups: as many as units that the tables have room for, or as the units are dealt to
+    double units_shared = 0, units_solo = 0;
+    auto count = [&](int64_t rows, int64_t lists, double tokens, int& solo_rows) {
+        if (rows > SOLO_ROWS && !cache.f32) {
+            const int64_t tiles = (rows + 15) / 16, blocks = (rows + 64 * a.nc - 1) / (64 * a.nc);
+            a.shared_rows = std::max(a.shared_rows, (int)(16 * ((tiles + blocks - 1) / blocks)));
+            units_shared += (double)lists * blocks * (tokens / 64 + 1) * a.Hkv;
+        } else {
+            solo_rows = std::max(solo_rows, (int)std::min<int64_t>(rows, SOLO_ROWS));
+            units_solo += (double)lists * ((rows + SOLO_ROWS - 1) / SOLO_ROWS) * (tokens / 32 + 1) * a.Hkv;
+        }
+    };
+    for (int g = 0; prompts && g < n_groups; ++g) count(rows_of(g), 1, (double)prompt_width * (1 << a.log_page), a.prompt_rows);
+    count(a.rep, n_seqs, (double)resp_width * (1 << a.log_page), a.resp_rows);
+    const unsigned grid = (unsigned)std::min<double>(PLAN_WGS, units_shared + units_solo / 4 + 1);
+    a.shared_cost = a.nc == 1 ? 3.f : a.nc == 2 ? 4.f : 5.5f;
     a.kv_heads = make_div(a.Hkv);
     a.q_heads = make_div(Hq);
     a.heads_each = make_div(a.rep);
@@ -764,30 +928,18 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     a.members = Gs ? Gs[0] : 1;
     for (int g = 1; Gs && g < n_groups; ++g) if (Gs[g] != Gs[0]) a.members = 0;
     a.group_size = make_div(std::max(1, a.members));
-    {   // tiles at most
-        const double most = ((double)n_groups * prompt_width + (double)n_seqs * resp_width) * (1 << a.log_page) / 32 *
-                            ((double)n_seqs * a.rep / SOLO_ROWS + 1) + n_groups + n_seqs;
-        while (most / (double)((int64_t)1 << a.tile_shift) + n_groups + n_seqs > 2e9) ++a.tile_shift;
-    }
-    // the plan's places and one piece per list, block and kv head, or a piece per tile (stage of two) that the tables have room for
-    int64_t tiles_shared = 0, tiles_solo = 0;
-    auto count = [&](int64_t rows, int64_t lists, int64_t width) {
-        const int64_t tiles = (((width << a.log_page) + 31) >> 5) < ((int64_t)1 << 26) ? ((width << a.log_page) + 31) >> 5 : (int64_t)1 << 26;
-        const bool sh = rows > SOLO_ROWS && !cache.f32;
-        const int64_t blocks = lists * (sh ? (rows + 64 * a.nc - 1) / (64 * a.nc) : (rows + SOLO_ROWS - 1) / SOLO_ROWS);
-        (sh ? shared : solo) += blocks;
-        (sh ? tiles_shared : tiles_solo) += blocks * (sh ? (tiles + 1) / 2 : tiles);
-    };
-    if (prompts) for (int g = 0; g < n_groups; ++g) count(rows_of(g), 1, prompt_width);
-    count(a.rep, n_seqs, resp_width);
-    int64_t grid = PLAN_WGS + shared * a.Hkv + (solo * a.Hkv + 3) / 4 + 1;
-    grid = std::max<int64_t>(1, std::min(grid, tiles_shared * a.Hkv + (tiles_solo * a.Hkv + 3) / 4));
     auto launch = [&](auto dim) {
         constexpr int D = decltype(dim)::value;
-        if (cache.f32) hipLaunchKernelGGL((decode_f32_kernel<D>), dim3((unsigned)grid), dim3(256), 0, s, starts, a);
-        else if (a.nc == 1) hipLaunchKernelGGL((decode_kernel<D, 1>), dim3((unsigned)grid), dim3(256), 0, s, starts, a);
-        else if (a.nc == 2) hipLaunchKernelGGL((decode_kernel<D, 2>), dim3((unsigned)grid), dim3(256), 0, s, starts, a);
-        else hipLaunchKernelGGL((decode_kernel<D, 3>), dim3((unsigned)grid), dim3(256), 0, s, starts, a);
+        auto with_lists = [&](auto many) {
+            constexpr bool MANY = decltype(many)::value;
+            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, starts, a); };
+            if (cache.f32) with(decode_f32_kernel<D, MANY>);
+            else if (units_shared == 0) with(decode_kernel<D, 0, MANY>);
+            else if (a.nc == 1) with(decode_kernel<D, 1, MANY>);
+            else if (a.nc == 2) with(decode_kernel<D, 2, MANY>);
+            else with(decode_kernel<D, 3, MANY>);
+        };
+        if (n_groups + n_seqs > 256) with_lists(std::true_type{}); else with_lists(std::false_type{});
         const unsigned joins = (unsigned)(((int64_t)n_seqs * Hq + 3) / 4);
         if (cache.f32) hipLaunchKernelGGL((decode_join_kernel<float, D>), dim3(joins), dim3(256), 0, s, starts, a);
         else hipLaunchKernelGGL((decode_join_kernel<__bf16, D>), dim3(joins), dim3(256), 0, s, starts, a);

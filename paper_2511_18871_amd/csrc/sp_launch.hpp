@@ -363,6 +363,7 @@ hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, 
 
 // starts: first sequence of each group, one past the last behind them.  partials: decode_partial_bytes() bytes.
 size_t decode_partial_bytes(int n_groups, int n_seqs, int Hq, int Hkv, int d);
+double decode_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_tokens, int64_t resp_tokens, const int32_t* Gs);
 hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, const TabArg& starts,
                          const int* prompt_tables, int prompt_width, const int* prompt_lens, const int* resp_tables, int resp_width,
                          const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s);

@@ -175,14 +175,14 @@ def test_reserve_of_a_forward_is_given_up():
     torch.manual_seed(0)
     T, hq, hkv, d = 70, 4, 2, 128
     q, k, v, do = (torch.randn(T, h, d, device="cuda").bfloat16() for h in (hq, hkv, hkv, hq))
-    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
     o, lse = B.sp_attn_fwd(q, k, v, 50, [20], 0.1, workspace=ws)
     with_reserve = B.sp_attn_bwd(q, k, v, o, lse, do, 50, [20], 0.1, workspace=ws)
     o, lse = B.sp_attn_fwd(q, k, v, 50, [20], 0.1, workspace=ws)
     cache_k = torch.randn(4, hkv, 64, d, device="cuda").bfloat16()
     B.sp_attn_decode(B.KvCache(cache_k, cache_k), q[:1], None, None, None, dev32([[0, 1]]), dev32([100]), 0.1, workspace=ws)
     without = B.sp_attn_bwd(q, k, v, o, lse, do, 50, [20], 0.1, workspace=ws)
-    fresh = B.sp_attn_bwd(q, k, v, o, lse, do, 50, [20], 0.1, workspace=torch.empty(1 << 22, dtype=torch.uint8, device="cuda"))
+    fresh = B.sp_attn_bwd(q, k, v, o, lse, do, 50, [20], 0.1, workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(without, fresh))
     assert not all(torch.equal(a, b) for a, b in zip(with_reserve, fresh))
