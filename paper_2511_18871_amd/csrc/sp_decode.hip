@@ -44,8 +44,8 @@ struct DecodeArgs {
     Div kv_heads, q_heads, heads_each;     // of Hkv, Hq, rep
     float c, m_none;                       // softmax_scale * log2(e); reference point of a row that has not seen a key
     uint32_t* tag;
-    i32x4* desc;                           // [0]: units of a worker, shared and solo; [1 + i], of list i: units ahead of it among its kind,
-                                           // units of a segment, blocks ahead of it among its kind, 1 for a sequence that takes no part
+    i32x4* desc;                           // [0]: units of a worker, shared and solo; [1 + i], of list i: room ahead of it among its kind, units
+                                           // of a segment, blocks ahead of it among its kind, room of a segment (-1: takes no part)
     // Slots of sums.  Worker w's sums of segment s (both counted within their kind) lie in slot w + s: either grows by one at a time.
     int shared_rows, prompt_rows, resp_rows;                 // rows of a slot of shared lists, and of solo prompts and responses
     int64_t prompt_base, resp_base;                          // first row of the solo prompts' slots, of the responses'
@@ -89,7 +89,7 @@ __device__ __forceinline__ float wave_sum(float x) {
 }
 
 struct ListShape { int rows, len, units, blocks; bool shared; };      // units of keys of a segment; blocks of rows
-struct PlanShare { int sums[4][4]; int list[4], at[4], ord[4], rows[4], len[4]; };      // of the waves of a workgroup; where their runs start
+struct PlanShare { int sums[4][4]; int list[4], at[4], ord[4], rows[4], len[4], room[4]; };      // of the waves of a workgroup; where their runs start
 
 // KIND 0: all lists are solo, 1: shared ones too
 template <int KIND>
@@ -127,8 +127,11 @@ __device__ __forceinline__ int per_place(int total, int places) {
     return c;
 }
 
+// units of room that a segment has among those of its kind
+__device__ __forceinline__ int room_of(int units, int run, bool aligned) { return aligned && units > 0 ? per_place(units, run) * run : units; }
+
 // What a worker does: `left` units from unit `at` of a list on (counted over the list's segments).
-struct Work { bool shared; int worker, list, at, ord, left; i32x2 list_is; };
+struct Work { bool shared; int worker, list, at, ord, left, room; i32x2 list_is; };
 
 // Every workgroup makes the whole plan: a thread adds up the units of its share of the lists (MANY: more lists than threads; they lie in LDS meanwhile
 // if there are no more than n_held), the workgroup their sums.  Places are dealt by cost: a segment costs, for its rows and its sums, what
@@ -155,16 +158,19 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
     }
     auto list_of = [&](int i) SP_INLINE { return !MANY ? mine : in_lds ? held[i] : ls.read(i); };
     int own[SUMS] = {}, to[SUMS], all[SUMS];
-    auto add = [&](int (&sum)[SUMS], const ListShape& s) SP_INLINE {
-        sum[0] += s.shared ? 0 : s.units * s.blocks;
+    auto add = [&](int (&sum)[SUMS], const ListShape& s, int room) SP_INLINE {
+        sum[0] += s.shared ? 0 : room * s.blocks;
         sum[1] += s.shared ? 0 : s.blocks;
         if constexpr (KIND) {
-            sum[2] += s.shared ? s.units * s.blocks : 0;
+            sum[2] += s.shared ? room * s.blocks : 0;
             sum[3] += s.shared ? s.blocks : 0;
         }
     };
 #pragma unroll 1
-    for (int i = i0; i < i1; ++i) add(own, ls.shape(list_of(i)));
+    for (int i = i0; i < i1; ++i) {
+        const ListShape s = ls.shape(list_of(i));
+        add(own, s, s.units);
+    }
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) {
         to[k] = scan64(own[k]);
@@ -179,13 +185,33 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
         all[k] *= a.Hkv;
     }
     int used = 0, shared_run = 1, solo_run = 1;
-    bool shared = false;
+    bool shared = false, aligned = false;
     if constexpr (KIND) {
         if (all[2] > 0) {
             const float cost = a.shared_cost * ((float)all[2] + 1.5f * (float)all[3]), solo = (float)all[0] + (float)all[1];
             int wgs = (int)(PLAN_WGS * (cost * __builtin_amdgcn_rcpf(cost + solo)));
             wgs = max(1, min(wgs, all[0] > 0 ? PLAN_WGS - 1 : PLAN_WGS));
-            shared_run = per_place(all[2], wgs);
+            // A worker that passes from one segment to another takes longer; where segments are long against the run, each is dealt to workers of
+            // its own, in room that is a multiple of the run (16K prompt with 32 answers: ... us against ...).
+            aligned = 4 * (int64_t)all[3] <= wgs;
+            shared_run = per_place(all[2], aligned ? wgs - all[3] : wgs);
+            if (aligned) {
+                int room = 0;
+#pragma unroll 1
+                for (int i = i0; i < i1; ++i) {
+                    const ListShape s = ls.shape(list_of(i));
+                    room += s.shared ? room_of(s.units, shared_run, true) * s.blocks : 0;
+                }
+                own[2] = room;
+                to[2] = scan64(room);
+                __syncthreads();
+                if (lane == 63) share.sums[wave][2] = to[2];
+                __syncthreads();
+                all[2] = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) { const int x = share.sums[w][2]; to[2] += w < wave ? x : 0; all[2] += x; }
+                all[2] *= a.Hkv;
+            }
             used = per_place(all[2], shared_run);
             shared = (int)blockIdx.x < used;
         }
@@ -205,18 +231,19 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
             const i32x2 x = list_of(i);
             const ListShape s = ls.shape(x);
             const int units = s.shared ? at[SUMS - 2] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1];
-            const int64_t from = (int64_t)units * a.Hkv, end = from + (int64_t)s.units * s.blocks * a.Hkv;
+            const int room = room_of(s.units, shared_run, s.shared && aligned);
+            const int64_t from = (int64_t)units * a.Hkv, end = from + (int64_t)room * s.blocks * a.Hkv;
             if (s.shared == shared)
 #pragma unroll 1
                 for (int k = 0; k < many; ++k) {
                     const int64_t pos = first + (int64_t)k * run;
                     if (pos >= from && pos < end) {
                         share.list[k] = i; share.at[k] = (int)(pos - from); share.ord[k] = blocks;
-                        share.rows[k] = x[0]; share.len[k] = x[1];
+                        share.rows[k] = x[0]; share.len[k] = x[1]; share.room[k] = room;
                     }
                 }
-            if (tells) a.desc[1 + i] = i32x4{units, s.units, blocks, s.len < 0};
-            add(at, s);
+            if (tells) a.desc[1 + i] = i32x4{units, s.units, blocks, s.len < 0 ? -1 : room};
+            add(at, s, room);
         }
         if (tells && threadIdx.x == 0) a.desc[0] = i32x4{shared_run, solo_run, 0, 0};
     }
@@ -232,6 +259,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
     work.at = scalar(share.at[slot]);
     work.ord = scalar(share.ord[slot]);
     work.list_is = i32x2{share.rows[slot], share.len[slot]};
+    work.room = scalar(share.room[slot]);
     return work;
 }
 
@@ -241,14 +269,15 @@ struct Cursor {
     const Lists<KIND>& ls;
     const bool shared;
     int list, seg, t, units, segs, rows, len, blocks, ord;
-    __device__ __forceinline__ Cursor(const Lists<KIND>& l, const Work& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
+    __device__ __forceinline__ Cursor(const Lists<KIND>& l, Work& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
         load(w.list_is);
-        seg = (int)((float)w.at * __builtin_amdgcn_rcpf((float)units));        // off by one at most, or low by 2^-22 of it
+        seg = (int)((float)w.at * __builtin_amdgcn_rcpf((float)w.room));        // off by one at most, or low by 2^-22 of it
         seg = __builtin_amdgcn_readfirstlane(seg);
-        if ((int64_t)seg * units > w.at) --seg;
+        if ((int64_t)seg * w.room > w.at) --seg;
 #pragma unroll 1
-        while ((int64_t)(seg + 1) * units <= w.at) ++seg;
-        t = w.at - seg * units;
+        while ((int64_t)(seg + 1) * w.room <= w.at) ++seg;
+        t = w.at - seg * w.room;
+        if (w.room > units) w.left = min(w.left, units - t);        // a run of the segment's own, the last one shorter
     }
     __device__ __forceinline__ bool load(i32x2 x) {
         const ListShape s = ls.shape(x);
@@ -331,10 +360,12 @@ template <int N> __device__ __forceinline__ void wait_copies() {
     else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
 }
 
+// (All NC row tiles that a wave has room for are computed, also where it has fewer: branches between them kept the reads from LDS from
+// running ahead of the products, and branches around them cost registers.)
 // Scores of 32 keys at LDS address `k`, keys not in `bits` masked: s[c][kt][i] is key 16 kt + 4 (l / 16) + i of row l % 16 of tile c
 // (an operand's granule is its first one's with a constant xored in, which leaves the address of the first in a register only)
 template <int D, int NC>
-__device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigned bits, int tiles, int l, f32x4 (&s)[NC][2]) {
+__device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigned bits, int l, f32x4 (&s)[NC][2]) {
     const unsigned at = k + kv_off<D>(l & 15, l >> 4);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -343,7 +374,6 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
         for (int ks = 0; ks < D / 32; ++ks) a[ks] = lds_at_row8((at ^ (ks << 6)) + kt * (32 * D));
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            if (c > 0 && c >= tiles) continue;
             s[c][kt] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) s[c][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[ks], r.q[c][ks], s[c][kt], 0, 0, 0);
@@ -363,10 +393,9 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
 // Weights of 32 keys from their scores, rounded to bf16 as the second product needs them: a rounding of 2^-9 of the weight at most, like
 // that of o itself, and of either sign.  Their sum is of the unrounded ones.
 template <int D, int NC>
-__device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, int tiles, bf16x8 (&p)[NC]) {
+__device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, bf16x8 (&p)[NC]) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        if (c > 0 && c >= tiles) continue;
         float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])), fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3])));
         mx = quad_max(mx);
         if (__builtin_amdgcn_ballot_w64(mx > r.m[c]) != 0) {
@@ -392,7 +421,7 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
 
 // O^T += V^T P^T over 32 keys at LDS address `v`
 template <int D, int NC>
-__device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf16x8 (&p)[NC], int tiles, int l) {
+__device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf16x8 (&p)[NC], int l) {
     const unsigned at = v + kv_off<D>(4 * (l >> 4) + ((l & 15) >> 2), (l & 3) >> 1) + ((l & 1) << 3);
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
@@ -403,22 +432,23 @@ __device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf1
         const bf16x8 a = cat4(half[0], half[1]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            if (c > 0 && c >= tiles) continue;
             r.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[c], r.o[c][dt], 0, 0, 0);
         }
     }
 }
 
-// Pages of a list's keys: a lane holds one of 64 page numbers, from page `first` on
+// Pages of a list's keys: a lane holds one of 64 page numbers, from page `first` on; `bad`: some of them are none of the cache's
 struct Pages {
-    const int* table; int width, first, held, lane;
+    const int* table; int width, n_pages, first, held, lane; bool bad;
     __device__ __forceinline__ int at(int page) {
-        if ((unsigned)(page - first) >= 64u) load(page);
+        need(page);
         return __builtin_amdgcn_readlane(held, page - first);
     }
+    __device__ __forceinline__ void need(int page) { if ((unsigned)(page - first) >= 64u) load(page); }
     __device__ __forceinline__ void load(int page) {
         first = page;
         held = page + lane < width ? table[page + lane] : -1;
+        bad = __builtin_amdgcn_ballot_w64((unsigned)held >= (unsigned)n_pages) != 0;
     }
 };
 
@@ -486,8 +516,8 @@ __device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArg
     }
 }
 
-// NC = 0: no list is shared
-template <int D, int NC, bool MANY>
+// NC: row tiles of a wave in a shared segment, 0: no list is shared.  NS: in a solo one.
+template <int D, int NC, int NS, bool MANY>
 __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArgs a) {
     constexpr int KEYS16 = 32 * D, KIND = NC > 0;       // bytes of 16 keys
     __shared__ __attribute__((aligned(1024))) char lds[16 * KEYS16];
@@ -507,28 +537,40 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     int kvh = kv_head();
     Pages pages;
     pages.lane = l;
+    pages.n_pages = a.n_pages;
     auto table_of_list = [&]() SP_INLINE {
         const bool prompt = at.list < a.n_groups;
         pages.table = prompt ? a.prompt_tables + at.list * a.prompt_width : a.resp_tables + (at.list - a.n_groups) * a.resp_width;
         pages.width = (int)(prompt ? a.prompt_width : a.resp_width);
     };
     auto next = [&]() SP_INLINE {
-        const int list = at.list, seg = at.seg;
+        const int list = at.list;
         at.next();
         if (at.list != list) { table_of_list(); pages.load(0); }
-        if (at.seg != seg || at.list != list) kvh = kv_head();
+        if (at.t == 0) kvh = kv_head();
     };
     table_of_list();
     const Copier<D> copy(l);
     const uint64_t kc = uniform64((uint64_t)(uintptr_t)a.k_cache), vc = uniform64((uint64_t)(uintptr_t)a.v_cache);
-    // byte offset of 16 keys in either cache and how many of them there are
+    // byte offset of a key's row in either cache, for a page of the cache
+    auto offset = [&](int key, int page) SP_INLINE {
+        return ((((uint64_t)(unsigned)page * a.Hkv + kvh) << a.log_page) + (key & ((1 << a.log_page) - 1))) * (2 * D);
+    };
+    // the same of 16 keys, and how many of them there are
     auto locate = [&](int key, uint64_t& off, int& valid) SP_INLINE {
         valid = min(16, at.len - key);
         off = 0;
         if (valid <= 0) return;
         const int page = __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page));
-        if (page < 0 || page >= a.n_pages) { valid = 0; return; }
-        off = ((((uint64_t)(unsigned)page * a.Hkv + kvh) << a.log_page) + (key & ((1 << a.log_page) - 1))) * (2 * D);
+        if ((unsigned)page >= (unsigned)a.n_pages) { valid = 0; return; }
+        off = offset(key, page);
+    };
+    // whether all of `count` keys are there (the pages held include the last one's; if any of those held is none, it is looked at in turn)
+    auto whole = [&](int key, int count) SP_INLINE {
+        if (key + count > at.len) return false;
+        pages.need(key >> a.log_page);
+        pages.need(key + count - 1 >> a.log_page);
+        return !pages.bad && (unsigned)((key >> a.log_page) - pages.first) < 64u;
     };
     const __bf16* const q = (const __bf16*)a.q;
     const unsigned buf = lds_address(lds);
@@ -536,13 +578,20 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     if (!KIND || !work.shared) {
         // One wave: K and V of a unit in turn.  The next K is copied while the weights and the second product run, the next V under the
         // next scores, also from segment to segment.
-        Rows<D, 2> r;
+        Rows<D, NS> r;
         const unsigned kb = buf + w * 4 * KEYS16, vb = kb + 2 * KEYS16;
         uint64_t off[2];
         int valid[2];
         auto fetch = [&]() SP_INLINE {
-            locate(32 * at.t, off[0], valid[0]);
-            locate(32 * at.t + 16, off[1], valid[1]);
+            const int key = 32 * at.t;
+            if (whole(key, 32)) {
+                valid[0] = valid[1] = 16;
+                off[0] = offset(key, __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page)));
+                off[1] = a.log_page > 4 ? off[0] + KEYS16 : offset(key + 16, __builtin_amdgcn_readfirstlane(pages.at(key + 16 >> a.log_page)));
+            } else {
+                locate(key, off[0], valid[0]);
+                locate(key + 16, off[1], valid[1]);
+            }
         };
         auto issue = [&](uint64_t cache, unsigned dst) SP_INLINE {
             copy.rows16(cache + off[0], valid[0], dst);
@@ -561,22 +610,17 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
             bool more = true, same = true;
             while (same) {
                 const unsigned bits = low_bits(valid[0]) | low_bits(valid[1]) << 16;
-                f32x4 s[2][2];
-                bf16x8 pw[2];
+                f32x4 s[NS][2];
+                bf16x8 pw[NS];
                 wait_copies<N>();
-                scores(r, kb, bits, tiles, l, s);
+                scores(r, kb, bits, l, s);
                 wait_lds();
-                same = at.t + 1 < at.units;
                 more = --work.left > 0;
-                same = same && more;
-                if (more) {
-                    next();
-                    fetch();
-                    issue(kc, kb);
-                }
-                weights(r, s, a.c, tiles, pw);
+                same = more && at.t + 1 < at.units;
+                if (more) { next(); fetch(); issue(kc, kb); }
+                weights(r, s, a.c, pw);
                 if (more) wait_copies<N>(); else wait_copies<0>();
-                add_values(r, vb, pw, tiles, l);
+                add_values(r, vb, pw, l);
                 wait_lds();
                 if (more) issue(vc, vb);
             }
@@ -588,29 +632,38 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
         // also from segment to segment.
         Rows<D, NC> r;
         unsigned half = 0;
-        const int odd = blockIdx.x & 256 ? 2 : 0;      // of two workgroups of a CU one begins with the larger share of uneven row tiles
-        int valid[4];
+        unsigned lo = 0, hi = 0;               // which of the next unit's keys there are
         auto issue = [&](unsigned dst) SP_INLINE {
-            uint64_t mine = 0, off;
-            int v_mine = 0;
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                locate(64 * at.t + 16 * h, off, valid[h]);
-                if (h == w) { mine = off; v_mine = valid[h]; }
+            uint64_t mine = 0;
+            int valid = 16;
+            lo = hi = 0xffffffffu;
+            const int key = 64 * at.t;
+            if (whole(key, 64)) {
+                mine = offset(key + 16 * w, __builtin_amdgcn_readfirstlane(pages.at(key + 16 * w >> a.log_page)));
+            } else {
+                lo = hi = 0;
+#pragma unroll 1
+                for (int h = 0; h < 4; ++h) {
+                    uint64_t off;
+                    int v;
+                    locate(key + 16 * h, off, v);
+                    if (h == w) { mine = off; valid = v; }
+                    (h < 2 ? lo : hi) |= low_bits(v) << (16 * (h & 1));
+                }
             }
-            copy.rows16(kc + mine, v_mine, dst + w * KEYS16);
-            copy.rows16(vc + mine, v_mine, dst + (4 + w) * KEYS16);
+            copy.rows16(kc + mine, valid, dst + w * KEYS16);
+            copy.rows16(vc + mine, valid, dst + (4 + w) * KEYS16);
         };
         pages.load(64 * at.t >> a.log_page);
         issue(buf);
         while (true) {
             SegmentRows seg(at, a, work.worker);
-            const int n = (seg.rows + 15) >> 4, t0 = (w * n + odd) >> 2, tiles = ((w + 1) * n + odd >> 2) - t0;
+            const int n = (seg.rows + 15) >> 4, t0 = w * n >> 2, tiles = ((w + 1) * n >> 2) - t0;
             load_rows(r, q, seg, 16 * t0, tiles, l);
             r.clear(a.m_none);
             bool more = true, same = true;
             while (same) {
-                const unsigned lo = low_bits(valid[0]) | low_bits(valid[1]) << 16, hi = low_bits(valid[2]) | low_bits(valid[3]) << 16;
+                const unsigned here[2] = {lo, hi};
                 wait_copies<0>();
                 __syncthreads();
                 const unsigned kb = buf + half * 8 * KEYS16, vb = kb + 4 * KEYS16;
@@ -618,15 +671,13 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
                 more = --work.left > 0;
                 same = more && at.t + 1 < at.units;
                 if (more) { next(); issue(buf + half * 8 * KEYS16); }
-                if (tiles > 0) {
 #pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        f32x4 s[NC][2];
-                        bf16x8 pw[NC];
-                        scores(r, kb + 2 * h * KEYS16, h ? hi : lo, tiles, l, s);
-                        weights(r, s, a.c, tiles, pw);
-                        add_values(r, vb + 2 * h * KEYS16, pw, tiles, l);
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    f32x4 s[NC][2];
+                    bf16x8 pw[NC];
+                    scores(r, kb + 2 * h * KEYS16, h ? here[1] : here[0], l, s);
+                    weights(r, s, a.c, pw);
+                    add_values(r, vb + 2 * h * KEYS16, pw, l);
                 }
             }
             store_rows(r, a, seg, 16 * t0, tiles, l);
@@ -782,7 +833,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
             per = 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
         }
         const int block = rows > per ? row / per : 0, segment = block * a.Hkv + kvh, each = shared ? run[0] : run[1];
-        const unsigned from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[1];
+        const unsigned from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[3];
         const unsigned worker0 = from / (unsigned)each, worker1 = (from + d[1] - 1) / (unsigned)each;
         stride = shared ? a.shared_rows : prompt ? a.prompt_rows : a.resp_rows;
         first_row = (shared ? 0 : prompt ? a.prompt_base : a.resp_base) + ((int64_t)worker0 + (int64_t)d[2] * a.Hkv + segment) * stride + row - block * per;
@@ -790,7 +841,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeA
     };
     int64_t base_p = 0, base_r = 0;
     int stride_p = 0, stride_r = 0, n_p = 0, n = 0;
-    if (!dr[3]) {
+    if (dr[3] >= 0) {
         if (dp[1] > 0) n_p = slots(dp, members * a.rep, (seq - first) * a.rep + (int)hr, true, base_p, stride_p);
         n = n_p + (dr[1] > 0 ? slots(dr, a.rep, (int)hr, false, base_r, stride_r) : 0);
     }
@@ -933,11 +984,16 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
         auto with_lists = [&](auto many) {
             constexpr bool MANY = decltype(many)::value;
             auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, starts, a); };
+            auto with_solo = [&](auto ns) {
+                constexpr int NS = decltype(ns)::value;
+                if (units_shared == 0) with(decode_kernel<D, 0, NS, MANY>);
+                else if (a.nc == 1) with(decode_kernel<D, 1, NS, MANY>);
+                else if (a.nc == 2) with(decode_kernel<D, 2, NS, MANY>);
+                else with(decode_kernel<D, 3, NS, MANY>);
+            };
             if (cache.f32) with(decode_f32_kernel<D, MANY>);
-            else if (units_shared == 0) with(decode_kernel<D, 0, MANY>);
-            else if (a.nc == 1) with(decode_kernel<D, 1, MANY>);
-            else if (a.nc == 2) with(decode_kernel<D, 2, MANY>);
-            else with(decode_kernel<D, 3, MANY>);
+            else if (std::max(a.prompt_rows, a.resp_rows) <= 16) with_solo(std::integral_constant<int, 1>{});
+            else with_solo(std::integral_constant<int, 2>{});
         };
         if (n_groups + n_seqs > 256) with_lists(std::true_type{}); else with_lists(std::false_type{});
         const unsigned joins = (unsigned)(((int64_t)n_seqs * Hq + 3) / 4);
