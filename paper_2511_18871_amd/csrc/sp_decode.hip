@@ -390,15 +390,30 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
     }
 }
 
-// Weights of 32 keys from their scores, rounded to bf16 as the second product needs them: a rounding of 2^-9 of the weight at most, like
+// Weights of 32 keys from their scores, rounded to bf16 as the second product needs them: a rounding of 2^-8 of the weight at most, like
 // that of o itself, and of either sign.  Their sum is of the unrounded ones.
+// They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
+// range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key, or to NaN) does the wave
+// take the rows' maxima for new references, scale what it has and take the weights again.  (With the maximum of every 32 keys, 128 rows and short runs
+// rescaled nearly every time: 110 instructions a tile instead of 30.)
 template <int D, int NC>
 __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, bf16x8 (&p)[NC]) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])), fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3])));
-        mx = quad_max(mx);
-        if (__builtin_amdgcn_ballot_w64(mx > r.m[c]) != 0) {
+        float sum;
+        auto take = [&](float mc) SP_INLINE {
+            sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e >> 2][e & 3], c2, -mc));
+                sum += x;
+                p[c][e] = (__bf16)x;
+            }
+        };
+        take(r.m[c] * c2);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= 16384.f)) != 0, 0)) {
+            float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])), fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3])));
+            mx = quad_max(mx);
             const float mn = fmaxf(r.m[c], mx), alpha = __builtin_amdgcn_exp2f((r.m[c] - mn) * c2);
             r.l[c] *= alpha;
 #pragma unroll
@@ -406,14 +421,7 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r.o[c][dt][i] *= alpha;
             r.m[c] = mn;
-        }
-        const float mc = r.m[c] * c2;
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e >> 2][e & 3], c2, -mc));
-            sum += x;
-            p[c][e] = (__bf16)x;
+            take(mn * c2);
         }
         r.l[c] += sum;
     }
