@@ -119,34 +119,97 @@ struct Lists {
     __device__ __forceinline__ int first_seq(int i) const { return i >= a.n_groups ? i - a.n_groups : a.members ? i * a.members : starts[i]; }
 };
 
-// ceil(total / places), total < 2^31, from a float quotient that is no more than one (for large ones 2^-20 of it) low
-__device__ __forceinline__ int per_place(int total, int places) {
-    int c = max(1, (int)((float)total * __builtin_amdgcn_rcpf((float)places) * 0.999999f));
-#pragma unroll 1
-    while ((int64_t)c * places < total) ++c;
-    return c;
+// ceil(total / places), total < 2^31, places > 0: a float quotient that is low by 2^-20 at most, what it leaves divided in the same way, and
+// what that leaves, which is below two places
+__device__ __forceinline__ unsigned per_place(unsigned total, unsigned places) {
+    const float inv = __builtin_amdgcn_rcpf((float)places) * 0.999999f;
+    unsigned c = (unsigned)((float)total * inv);
+    c += (unsigned)((float)(total - c * places) * inv);
+    c += c * places < total;
+    c += c * places < total;
+    return max(c, 1u);
 }
-
 // units of room that a segment has among those of its kind
-__device__ __forceinline__ int room_of(int units, int run, bool aligned) { return aligned && units > 0 ? per_place(units, run) * run : units; }
+__device__ __forceinline__ int room_of(int units, unsigned run, bool aligned) { return aligned && units > 0 ? (int)(per_place(units, run) * run) : units; }
 
 // What a worker does: `left` units from unit `at` of a list on (counted over the list's segments).
 struct Work { bool shared; int worker, list, at, ord, left, room; i32x2 list_is; };
 
-// Every workgroup makes the whole plan: a thread adds up the units of its share of the lists (MANY: more lists than threads; they lie in LDS meanwhile
-// if there are no more than n_held), the workgroup their sums.  Places are dealt by cost: a segment costs, for its rows and its sums, what
-// one and a half of its units (shared) or one (solo) cost, and a shared unit what shared_cost solo ones do.  Workgroups of shared lists come first.
-// Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time.
-template <int KIND, bool MANY>
+// The runs of either kind, from the units and segments of all lists.  Places are dealt by cost: a segment costs, for its rows and its sums, what one and a half of its
+// units (shared) or one (solo) cost, and a shared unit what shared_cost solo ones do.  A worker that passes from one segment to another takes
+// longer; where shared segments are long against the run, each is dealt to workers of its own, in room that is a multiple of the run (`aligned`).
+struct Runs { unsigned shared_run, solo_run, used; bool aligned; };      // used: workgroups of shared segments
+template <int KIND>
+__device__ __forceinline__ void shared_runs(const DecodeArgs& a, unsigned solo, unsigned solo_segs, unsigned shared, unsigned segs, Runs& r) {
+    r = Runs{1, 1, 0, false};
+    if constexpr (KIND) {
+        if (shared == 0) return;
+        const float cost = a.shared_cost * ((float)shared + 1.5f * (float)segs);
+        int wgs = (int)(PLAN_WGS * (cost * __builtin_amdgcn_rcpf(cost + (float)solo + (float)solo_segs)));
+        wgs = max(1, min(wgs, solo ? PLAN_WGS - 1 : PLAN_WGS));
+        r.aligned = 4 * segs <= (unsigned)wgs;
+        r.shared_run = per_place(shared, r.aligned ? wgs - segs : wgs);
+    }
+}
+
+// Every workgroup makes the whole plan.  Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time, and
+// takes a cycle a byte.
+// Up to 64 lists: a wave by itself, a list to a lane.
+template <int KIND>
+__device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND>& ls, int wave, int lane) {
+    const DecodeArgs& a = ls.a;
+    const int n = a.n_groups + a.n_seqs;
+    const bool there = lane < n;
+    i32x2 mine{0, 0};
+    if (there) mine = ls.read(lane);
+    const ListShape s = ls.shape(mine);
+    auto last = [](int x) SP_INLINE { return (unsigned)__builtin_amdgcn_readlane(x, 63); };
+    const int solo_units = s.shared ? 0 : s.units * s.blocks, solo_blocks = s.shared ? 0 : s.blocks;
+    const int to_solo = scan64(solo_units), ord_solo = scan64(solo_blocks);
+    const unsigned solo = last(to_solo) * a.Hkv;
+    int room = s.units, units = solo_units, to = to_solo, ord = ord_solo - solo_blocks;
+    unsigned shared_room = 0;
+    Runs runs{1, 1, 0, false};
+    if constexpr (KIND) {
+        const int shared_units = s.shared ? s.units * s.blocks : 0, shared_blocks = s.shared ? s.blocks : 0;
+        const int ord_shared = scan64(shared_blocks);
+        shared_runs<KIND>(a, solo, last(ord_solo) * a.Hkv, last(scan64(shared_units)) * a.Hkv, last(ord_shared) * a.Hkv, runs);
+        if (s.shared) { room = room_of(s.units, runs.shared_run, runs.aligned); units = room * s.blocks; ord = ord_shared - shared_blocks; }
+        const int to_shared = scan64(s.shared ? units : 0);
+        if (s.shared) to = to_shared;
+        shared_room = last(to_shared) * a.Hkv;
+        if (shared_room) runs.used = per_place(shared_room, runs.shared_run);
+    }
+    if (solo) runs.solo_run = per_place(solo, 4 * (PLAN_WGS - runs.used));
+    if (blockIdx.x == 0 && wave == 0) {          // what the join needs to know
+        if (there) a.desc[1 + lane] = i32x4{to - units, s.units, ord, s.len < 0 ? -1 : room};
+        if (lane == 0) a.desc[0] = i32x4{(int)runs.shared_run, (int)runs.solo_run, 0, 0};
+    }
+    Work work;
+    work.shared = blockIdx.x < runs.used;
+    work.worker = work.shared ? (int)blockIdx.x : (int)(blockIdx.x - runs.used) * 4 + wave;
+    const unsigned run = work.shared ? runs.shared_run : runs.solo_run, all = work.shared ? shared_room : solo, pos = (unsigned)work.worker * run;
+    // (through a lane read: without it the compiler left the comparison out and took the difference, wrapped, as it was)
+    work.left = pos < all ? __builtin_amdgcn_readfirstlane((int)min(run, all - pos)) : 0;
+    const unsigned from = (unsigned)(to - units) * a.Hkv, end = (unsigned)to * a.Hkv;
+    const int src = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(s.shared == work.shared && pos >= from && pos < end)) - 1;
+    auto of = [&](int x) SP_INLINE { return __builtin_amdgcn_readlane(x, src & 63); };
+    work.list = src & 63;
+    work.at = (int)(pos - (unsigned)of((int)from));
+    work.ord = of(ord);
+    work.room = of(room);
+    work.list_is = i32x2{of(mine[0]), of(mine[1])};
+    return work;
+}
+
+// More lists: a thread adds up the units of its share of them (they lie in LDS meanwhile, if there are no more than n_held), the workgroup their sums.
+template <int KIND>
 __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, int n_held, PlanShare& share, int wave, int lane) {
     constexpr int SUMS = KIND ? 4 : 2;       // solo units and blocks, shared units and blocks
     const DecodeArgs& a = ls.a;
-    const int n = a.n_groups + a.n_seqs, per = MANY ? (n + 255) >> 8 : 1, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
-    i32x2 mine{0, 0};
-    const bool in_lds = MANY && n <= n_held;
-    if constexpr (!MANY) {
-        if (i0 < n) mine = ls.read(i0);
-    } else if (in_lds) {
+    const int n = a.n_groups + a.n_seqs, per = (n + 255) >> 8, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
+    const bool in_lds = n <= n_held;
+    if (in_lds) {
         for (int i = threadIdx.x; i < n; i += 256 * 4) {      // four reads in flight
             i32x2 x[4];
 #pragma unroll
@@ -156,8 +219,9 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
         }
         __syncthreads();
     }
-    auto list_of = [&](int i) SP_INLINE { return !MANY ? mine : in_lds ? held[i] : ls.read(i); };
-    int own[SUMS] = {}, to[SUMS], all[SUMS];
+    auto list_of = [&](int i) SP_INLINE { return in_lds ? held[i] : ls.read(i); };
+    int own[SUMS] = {}, to[SUMS];
+    unsigned all[SUMS];
     auto add = [&](int (&sum)[SUMS], const ListShape& s, int room) SP_INLINE {
         sum[0] += s.shared ? 0 : room * s.blocks;
         sum[1] += s.shared ? 0 : s.blocks;
@@ -166,63 +230,46 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
             sum[3] += s.shared ? s.blocks : 0;
         }
     };
+    auto over_waves = [&](int k) SP_INLINE {       // to[k], inclusive, and all[k] from own[k]
+        to[k] = scan64(own[k]);
+        __syncthreads();
+        if (lane == 63) share.sums[wave][k] = to[k];
+        __syncthreads();
+        unsigned sum = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) { const int x = share.sums[w][k]; to[k] += w < wave ? x : 0; sum += x; }
+        all[k] = sum * a.Hkv;
+    };
 #pragma unroll 1
     for (int i = i0; i < i1; ++i) {
         const ListShape s = ls.shape(list_of(i));
         add(own, s, s.units);
     }
 #pragma unroll
-    for (int k = 0; k < SUMS; ++k) {
-        to[k] = scan64(own[k]);
-        if (lane == 63) share.sums[wave][k] = to[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < SUMS; ++k) {
-        all[k] = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) { const int x = share.sums[w][k]; to[k] += w < wave ? x : 0; all[k] += x; }
-        all[k] *= a.Hkv;
-    }
-    int used = 0, shared_run = 1, solo_run = 1;
-    bool shared = false, aligned = false;
+    for (int k = 0; k < SUMS; ++k) over_waves(k);
+    Runs runs{1, 1, 0, false};
     if constexpr (KIND) {
-        if (all[2] > 0) {
-            const float cost = a.shared_cost * ((float)all[2] + 1.5f * (float)all[3]), solo = (float)all[0] + (float)all[1];
-            int wgs = (int)(PLAN_WGS * (cost * __builtin_amdgcn_rcpf(cost + solo)));
-            wgs = max(1, min(wgs, all[0] > 0 ? PLAN_WGS - 1 : PLAN_WGS));
-            // A worker that passes from one segment to another takes longer; where segments are long against the run, each is dealt to workers of
-            // its own, in room that is a multiple of the run (16K prompt with 32 answers: ... us against ...).
-            aligned = 4 * (int64_t)all[3] <= wgs;
-            shared_run = per_place(all[2], aligned ? wgs - all[3] : wgs);
-            if (aligned) {
-                int room = 0;
+        shared_runs<KIND>(a, all[0], all[1], all[SUMS - 2], all[SUMS - 1], runs);
+        if (runs.aligned) {
+            own[SUMS - 2] = 0;
 #pragma unroll 1
-                for (int i = i0; i < i1; ++i) {
-                    const ListShape s = ls.shape(list_of(i));
-                    room += s.shared ? room_of(s.units, shared_run, true) * s.blocks : 0;
-                }
-                own[2] = room;
-                to[2] = scan64(room);
-                __syncthreads();
-                if (lane == 63) share.sums[wave][2] = to[2];
-                __syncthreads();
-                all[2] = 0;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) { const int x = share.sums[w][2]; to[2] += w < wave ? x : 0; all[2] += x; }
-                all[2] *= a.Hkv;
+            for (int i = i0; i < i1; ++i) {
+                const ListShape s = ls.shape(list_of(i));
+                own[SUMS - 2] += s.shared ? room_of(s.units, runs.shared_run, true) * s.blocks : 0;
             }
-            used = per_place(all[2], shared_run);
-            shared = (int)blockIdx.x < used;
+            over_waves(SUMS - 2);
         }
+        if (all[SUMS - 2]) runs.used = per_place(all[SUMS - 2], runs.shared_run);
     }
-    if (all[0] > 0) solo_run = per_place(all[0], 4 * (PLAN_WGS - used));
+    if (all[0]) runs.solo_run = per_place(all[0], 4 * (PLAN_WGS - runs.used));
     // this workgroup's runs start at `first` and multiples of the run behind it
-    const int run = shared ? shared_run : solo_run, many = shared ? 1 : 4;
-    const int64_t first = shared ? (int64_t)blockIdx.x * run : ((int64_t)blockIdx.x - used) * 4 * run;
+    Work work;
+    const bool shared = work.shared = blockIdx.x < runs.used;
+    const unsigned run = shared ? runs.shared_run : runs.solo_run, many = shared ? 1 : 4, first = (shared ? blockIdx.x : 4 * (blockIdx.x - runs.used)) * run;
     const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know
-    const int64_t through = (int64_t)(KIND && shared ? to[SUMS - 2] : to[0]) * a.Hkv, ahead = through - (int64_t)(KIND && shared ? own[SUMS - 2] : own[0]) * a.Hkv;
-    if (tells || (ahead < first + (int64_t)many * run && through > first)) {
+    const int mine = KIND && shared ? SUMS - 2 : 0;
+    const unsigned through = (unsigned)(mine ? to[SUMS - 2] : to[0]) * a.Hkv, ahead = through - (unsigned)(mine ? own[SUMS - 2] : own[0]) * a.Hkv;
+    if (tells || (ahead < first + many * run && through > first)) {
         int at[SUMS];
 #pragma unroll
         for (int k = 0; k < SUMS; ++k) at[k] = to[k] - own[k];
@@ -230,13 +277,12 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
         for (int i = i0; i < i1; ++i) {
             const i32x2 x = list_of(i);
             const ListShape s = ls.shape(x);
-            const int units = s.shared ? at[SUMS - 2] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1];
-            const int room = room_of(s.units, shared_run, s.shared && aligned);
-            const int64_t from = (int64_t)units * a.Hkv, end = from + (int64_t)room * s.blocks * a.Hkv;
+            const int units = s.shared ? at[SUMS - 2] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1], room = room_of(s.units, runs.shared_run, s.shared && runs.aligned);
+            const unsigned from = (unsigned)units * a.Hkv, end = from + (unsigned)(room * s.blocks) * a.Hkv;
             if (s.shared == shared)
 #pragma unroll 1
-                for (int k = 0; k < many; ++k) {
-                    const int64_t pos = first + (int64_t)k * run;
+                for (unsigned k = 0; k < many; ++k) {
+                    const unsigned pos = first + k * run;
                     if (pos >= from && pos < end) {
                         share.list[k] = i; share.at[k] = (int)(pos - from); share.ord[k] = blocks;
                         share.rows[k] = x[0]; share.len[k] = x[1]; share.room[k] = room;
@@ -245,21 +291,19 @@ __device__ __forceinline__ Work find_work(const Lists<KIND>& ls, i32x2* held, in
             if (tells) a.desc[1 + i] = i32x4{units, s.units, blocks, s.len < 0 ? -1 : room};
             add(at, s, room);
         }
-        if (tells && threadIdx.x == 0) a.desc[0] = i32x4{shared_run, solo_run, 0, 0};
+        if (tells && threadIdx.x == 0) a.desc[0] = i32x4{(int)runs.shared_run, (int)runs.solo_run, 0, 0};
     }
     __syncthreads();
     auto scalar = [](int x) SP_INLINE { return __builtin_amdgcn_readfirstlane(x); };      // the same in every lane, which the compiler does not see
     const int slot = shared ? 0 : wave;
-    const int64_t pos = first + (int64_t)slot * run, rest = (KIND && shared ? all[SUMS - 2] : all[0]) - pos;
-    Work work;
-    work.shared = shared;
-    work.left = rest > 0 ? scalar((int)min((int64_t)run, rest)) : 0;
-    work.worker = scalar(shared ? (int)blockIdx.x : ((int)blockIdx.x - used) * 4 + wave);
+    const unsigned pos = first + slot * run, end = mine ? all[SUMS - 2] : all[0];
+    work.left = pos < end ? scalar((int)min(run, end - pos)) : 0;
+    work.worker = scalar(shared ? (int)blockIdx.x : (int)(blockIdx.x - runs.used) * 4 + wave);
     work.list = scalar(share.list[slot]);
     work.at = scalar(share.at[slot]);
     work.ord = scalar(share.ord[slot]);
-    work.list_is = i32x2{share.rows[slot], share.len[slot]};
     work.room = scalar(share.room[slot]);
+    work.list_is = i32x2{share.rows[slot], share.len[slot]};
     return work;
 }
 
@@ -271,11 +315,10 @@ struct Cursor {
     int list, seg, t, units, segs, rows, len, blocks, ord;
     __device__ __forceinline__ Cursor(const Lists<KIND>& l, Work& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
         load(w.list_is);
-        seg = (int)((float)w.at * __builtin_amdgcn_rcpf((float)w.room));        // off by one at most, or low by 2^-22 of it
+        seg = (int)((float)w.at * __builtin_amdgcn_rcpf((float)w.room));        // off by one at most: there are some thousand segments
         seg = __builtin_amdgcn_readfirstlane(seg);
-        if ((int64_t)seg * w.room > w.at) --seg;
-#pragma unroll 1
-        while ((int64_t)(seg + 1) * w.room <= w.at) ++seg;
+        seg -= seg * w.room > w.at;
+        seg += (unsigned)(seg + 1) * w.room <= (unsigned)w.at;
         t = w.at - seg * w.room;
         if (w.room > units) w.left = min(w.left, units - t);        // a run of the segment's own, the last one shorter
     }
@@ -533,8 +576,13 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<KIND> ls{table_of(starts), a};
-    Work work = find_work<KIND, MANY>(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
-    __syncthreads();                             // the lists' place is free
+    Work work;
+    if constexpr (MANY) {
+        work = find_work<KIND>(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
+        __syncthreads();                             // the lists' place is free
+    } else {
+        work = find_work_in_lanes<KIND>(ls, w, l);
+    }
     if (work.left == 0) return;
     Cursor<KIND> at(ls, work);
     auto kv_head = [&]() SP_INLINE {
@@ -707,7 +755,8 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, Decod
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, m16 = l & 15, j = l >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<0> ls{table_of(starts), a};
-    Work work = find_work<0, MANY>(ls, lists, 4096, share, w, l);
+    Work work;
+    if constexpr (MANY) work = find_work<0>(ls, lists, 4096, share, w, l); else work = find_work_in_lanes<0>(ls, w, l);
     if (work.left == 0) return;
     Cursor<0> at(ls, work);
     Pages pages;
@@ -1003,7 +1052,7 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
             else if (std::max(a.prompt_rows, a.resp_rows) <= 16) with_solo(std::integral_constant<int, 1>{});
             else with_solo(std::integral_constant<int, 2>{});
         };
-        if (n_groups + n_seqs > 256) with_lists(std::true_type{}); else with_lists(std::false_type{});
+        if (n_groups + n_seqs > 64) with_lists(std::true_type{}); else with_lists(std::false_type{});
         const unsigned joins = (unsigned)(((int64_t)n_seqs * Hq + 3) / 4);
         if (cache.f32) hipLaunchKernelGGL((decode_join_kernel<float, D>), dim3(joins), dim3(256), 0, s, starts, a);
         else hipLaunchKernelGGL((decode_join_kernel<__bf16, D>), dim3(joins), dim3(256), 0, s, starts, a);
