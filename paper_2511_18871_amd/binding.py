@@ -578,36 +578,35 @@ def _refuse(message: str):
     raise SpAttnError(SP_ERR_INVALID_ARG, message)
 
 
-def _tensor(name, t, dtype, shape, device, contiguous=True):
-    """Checks what the library cannot see behind a pointer.  A None in `shape` stands for any size."""
-    if t.dtype != dtype or t.device != device or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        _refuse(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {shape} on {device}")
-    if contiguous and not t.is_contiguous():
-        _refuse(f"{name} is not contiguous")
+def _is(t, dtype, shape, index) -> bool:
+    """Whether t is what a kernel takes its pointer for.  `index`: of the GPU, -1 for host memory."""
+    return t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()
 
 
-class _on:
-    """The device and stream on which a call allocates and enqueues: those of its tensors, or the caller's stream."""
+def _need(name, t, dtype, shape, index):
+    if not _is(t, dtype, shape, index):
+        _refuse(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
+                f"expected {dtype} {tuple(shape)} on {'the host' if index < 0 else f'cuda:{index}'}, contiguous")
 
-    def __init__(self, device, stream):
-        self.switch = None
-        if device.type != "cuda":
-            _refuse(f"the tensors are on {device}, not on a GPU")
-        if stream is not None:
-            if stream.device != device:
-                _refuse(f"the stream is on {stream.device}, the tensors are on {device}")
-            self.switch = torch.cuda.stream(stream)
-        elif device.index != torch.cuda.current_device():
-            self.switch = torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.switch is not None:
-            self.switch.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def __exit__(self, *error):
-        if self.switch is not None:
-            self.switch.__exit__(*error)
+
+def _placed(f):
+    """Runs f(raw stream, ...) on the device of its tensors (`index`) and on the caller's stream, so that what it allocates belongs there."""
+    def run(index, stream, *args):
+        if index < 0:
+            _refuse("the tensors are not on a GPU")
+        if stream is None:
+            if index == torch.cuda.current_device():
+                return f(_raw_stream(index), *args)
+            with torch.cuda.device(index):
+                return f(_raw_stream(index), *args)
+        if stream.device_index != index:
+            _refuse(f"the stream is on cuda:{stream.device_index}, the tensors are on cuda:{index}")
+        with torch.cuda.stream(stream):
+            return f(stream.cuda_stream, *args)
+    return run
 
 
 class KvCache:
@@ -616,8 +615,9 @@ class KvCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         if k.dim() != 4:
             _refuse(f"k: {tuple(k.shape)}, expected [n_pages, n_kv_heads, page_size, head_dim]")
-        _tensor("k", k, k.dtype, k.shape, k.device)
-        _tensor("v", v, k.dtype, k.shape, k.device)
+        self.index = k.get_device()
+        _need("k", k, k.dtype, k.shape, self.index)
+        _need("v", v, k.dtype, k.shape, self.index)
         self.k, self.v = k, v
         self.dtype, self.device = k.dtype, k.device
         n_pages, self.n_kv_heads, page_size, self.head_dim = k.shape
@@ -631,27 +631,31 @@ class LogitRules:
 
     def __init__(self, repetition: float = 1.0, presence: float = 0.0, frequency: float = 0.0, temperature: float = 1.0, bias=None):
         if bias is not None:
-            _tensor("bias", bias, torch.float32, (None,), bias.device)
+            if bias.dim() != 1:
+                _refuse(f"bias: {tuple(bias.shape)}, expected [vocab]")
+            _need("bias", bias, torch.float32, bias.shape, bias.get_device())
         self.bias = bias
         self._struct = _LogitRulesStruct(repetition, presence, frequency, temperature, None if bias is None else bias.data_ptr())
         self._ref = ctypes.pointer(self._struct)
 
-    def _fits(self, vocab, device):
+    def _fits(self, vocab, index):
         if self.bias is not None:
-            _tensor("bias", self.bias, torch.float32, (vocab,), device)
+            _need("bias", self.bias, torch.float32, (vocab,), index)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _token_rows(name, t, cache, heads):
-    """Tokens of `heads` heads with any stride from token to token; returns that stride."""
+def _token_stride(name, t, cache, heads) -> int:
+    """Elements from token to token of [T, heads, d], whose heads are contiguous within a token."""
     d = cache.head_dim
-    _tensor(name, t, cache.dtype, (None, heads, d), cache.device, contiguous=False)
-    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+    if t.dtype is not cache.dtype or t.get_device() != cache.index or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        _refuse(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {cache.dtype} [tokens, {heads}, {d}] on {cache.device}")
+    at, head, one = t.stride()
+    if t.shape[0] and (one != 1 or (heads > 1 and head != d)):
         _refuse(f"{name}: the heads of a token are not contiguous (strides {t.stride()})")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return at if t.shape[0] > 1 else heads * d
 
 
 def sp_attn_cache_append(cache: KvCache, k, v, tables, lens, rope_base: float, q=None, new_lens: Optional[Sequence[int]] = None,
@@ -660,41 +664,46 @@ def sp_attn_cache_append(cache: KvCache, k, v, tables, lens, rope_base: float, q
     (host integers; None: one each), which become its tokens lens[s], lens[s] + 1, ... in the pages tables[s].  q [T, n_q_heads, d] is rotated
     along (into q_out), and the rotated keys also go to k_out where that is given.  k, v and q may be parts of one
     projection's output.  Returns (q_out, lens_out); q_out is None without q."""
-    lib = load_library()
-    dev, hkv = cache.device, cache.n_kv_heads
-    ks, vs = _token_rows("k", k, cache, hkv), _token_rows("v", v, cache, hkv)
+    index, hkv, d, int32 = cache.index, cache.n_kv_heads, cache.head_dim, torch.int32
+    ks, vs = _token_stride("k", k, cache, hkv), _token_stride("v", v, cache, hkv)
     T, n_seqs = k.shape[0], lens.shape[0]
-    counts = None if new_lens is None else _i32(new_lens)
     if v.shape[0] != T or T != (n_seqs if new_lens is None else sum(new_lens)) or (new_lens is not None and len(new_lens) != n_seqs):
         _refuse(f"{T} keys, {v.shape[0]} values and {n_seqs} sequences do not fit the new tokens")
-    _tensor("lens", lens, torch.int32, (n_seqs,), dev)
-    _tensor("tables", tables, torch.int32, (n_seqs, None), dev)
+    _need("lens", lens, int32, (n_seqs,), index)
+    if tables.dim() != 2:
+        _refuse(f"tables: {tuple(tables.shape)}, expected [sequences, pages]")
+    _need("tables", tables, int32, (n_seqs, tables.shape[1]), index)
     if pos_base is not None:
-        _tensor("pos_base", pos_base, torch.int32, (n_seqs,), dev)
+        _need("pos_base", pos_base, int32, (n_seqs,), index)
     hq, qs = 0, 0
     if q is not None:
         hq = q.shape[1]
-        qs = _token_rows("q", q, cache, hq)
+        qs = _token_stride("q", q, cache, hq)
         if q.shape[0] != T:
             _refuse(f"q has {q.shape[0]} tokens, k has {T}")
         if q_out is not None:
-            _tensor("q_out", q_out, cache.dtype, (T, hq, cache.head_dim), dev)
+            _need("q_out", q_out, cache.dtype, (T, hq, d), index)
     elif q_out is not None:
         _refuse("q_out without q")
     if k_out is not None:
-        _tensor("k_out", k_out, cache.dtype, (T, hkv, cache.head_dim), dev)
+        _need("k_out", k_out, cache.dtype, (T, hkv, d), index)
     if lens_out is not None:
-        _tensor("lens_out", lens_out, torch.int32, (n_seqs,), dev)
-    with _on(dev, stream) as s:
-        if q is not None and q_out is None:
-            q_out = torch.empty((T, hq, cache.head_dim), dtype=cache.dtype, device=dev)
-        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
-        if T == 0:                     # nothing to store; the pointers of empty tensors are null
-            lens_out.copy_(lens)
-            return q_out, lens_out
-        _check(lib.sp_attn_cache_append(cache._ref, _ptr(q), qs, _ptr(q_out), hq, k.data_ptr(), ks, _ptr(k_out), v.data_ptr(), vs, n_seqs, counts,
-                                        tables.data_ptr(), tables.shape[1], lens.data_ptr(), _ptr(pos_base), lens_out.data_ptr(),
-                                        float(rope_base), s))
+        _need("lens_out", lens_out, int32, (n_seqs,), index)
+    return _append(index, stream, cache, q, qs, q_out, hq, k, ks, k_out, v, vs, n_seqs, new_lens, tables, lens, pos_base, lens_out, rope_base)
+
+
+@_placed
+def _append(raw, cache, q, qs, q_out, hq, k, ks, k_out, v, vs, n_seqs, new_lens, tables, lens, pos_base, lens_out, rope_base):
+    if q is not None and q_out is None:
+        q_out = torch.empty((k.shape[0], hq, cache.head_dim), dtype=cache.dtype, device=cache.device)
+    if lens_out is None:
+        lens_out = torch.empty_like(lens)
+    if k.shape[0] == 0:                    # nothing to store; the pointers of empty tensors are null
+        lens_out.copy_(lens)
+        return q_out, lens_out
+    _check(load_library().sp_attn_cache_append(cache._ref, _ptr(q), qs, _ptr(q_out), hq, k.data_ptr(), ks, _ptr(k_out), v.data_ptr(), vs, n_seqs,
+                                               None if new_lens is None else _i32(new_lens), tables.data_ptr(), tables.shape[1], lens.data_ptr(),
+                                               _ptr(pos_base), lens_out.data_ptr(), rope_base, raw))
     return q_out, lens_out
 
 
@@ -702,14 +711,17 @@ def decode_workspace_bytes(n_groups: int, n_seqs: int, n_q_heads: int, n_kv_head
     return load_library().sp_attn_decode_workspace_bytes(n_groups, n_seqs, n_q_heads, n_kv_heads, head_dim, dtype_code)
 
 
-def _pages_of(name, tables, lens, rows, device):
+def _pages_of(name, tables, lens, rows, index):
     """(pointer, width, pointer of the lengths) of a table, which may be None or have no columns."""
     if lens is not None:
-        _tensor(name + "_lens", lens, torch.int32, (rows,), device)
+        _need(name + "_lens", lens, torch.int32, (rows,), index)
     if tables is None:
         return None, 0, _ptr(lens)
-    _tensor(name + "_tables", tables, torch.int32, (rows, None), device)
-    return (tables.data_ptr() if tables.shape[1] else None), tables.shape[1], _ptr(lens)
+    if tables.dim() != 2:
+        _refuse(f"{name}_tables: {tuple(tables.shape)}, expected [rows, pages]")
+    width = tables.shape[1]
+    _need(name + "_tables", tables, torch.int32, (rows, width), index)
+    return (tables.data_ptr() if width else None), width, _ptr(lens)
 
 
 def sp_attn_decode(cache: KvCache, q, Gs: Optional[Sequence[int]], prompt_tables, prompt_lens, resp_tables, resp_lens, softmax_scale: float,
@@ -717,43 +729,68 @@ def sp_attn_decode(cache: KvCache, q, Gs: Optional[Sequence[int]], prompt_tables
     """Attention of one new token per sequence.  Row s of q [n_seqs, n_q_heads, d] attends to its group's prompt and to the first
     resp_lens[s] tokens of its own.  Gs: sequences of each group (host integers), None: one each.  prompt_tables [n_groups, width] and
     prompt_lens may be None (no shared prompts).  Returns (o, lse [n_q_heads, n_seqs])."""
-    lib = load_library()
-    dev = cache.device
-    _tensor("q", q, cache.dtype, (None, None, cache.head_dim), dev)
+    index = cache.index
+    if q.dim() != 3:
+        _refuse(f"q: {tuple(q.shape)}, expected [sequences, heads, {cache.head_dim}]")
     n_seqs, hq, d = q.shape
+    _need("q", q, cache.dtype, (n_seqs, hq, cache.head_dim), index)
     n_groups = n_seqs if Gs is None else len(Gs)
-    pt, pw, pl = _pages_of("prompt", prompt_tables, prompt_lens, n_groups, dev)
-    rt, rw, rl = _pages_of("resp", resp_tables, resp_lens, n_seqs, dev)
+    prompt = _pages_of("prompt", prompt_tables, prompt_lens, n_groups, index)
+    resp = _pages_of("resp", resp_tables, resp_lens, n_seqs, index)
     if o is not None:
-        _tensor("o", o, cache.dtype, (n_seqs, hq, d), dev)
+        _need("o", o, cache.dtype, (n_seqs, hq, d), index)
     if lse is not None:
-        _tensor("lse", lse, torch.float32, (hq, n_seqs), dev)
-    with _on(dev, stream) as s:
-        o = torch.empty_like(q) if o is None else o
-        lse = torch.empty((hq, n_seqs), dtype=torch.float32, device=dev) if lse is None else lse
-        if workspace is None:
-            need = lib.sp_attn_decode_workspace_bytes(n_groups, n_seqs, hq, cache.n_kv_heads, d, cache.code)
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-        _check(lib.sp_attn_decode(cache._ref, q.data_ptr(), o.data_ptr(), lse.data_ptr(), hq, n_groups, n_seqs, None if Gs is None else _i32(Gs),
-                                  pt, pw, pl if pw else None, rt, rw, rl, softmax_scale, workspace.data_ptr(), workspace.numel(), s))
+        _need("lse", lse, torch.float32, (hq, n_seqs), index)
+    return _decode(index, stream, cache, q, o, lse, hq, n_groups, n_seqs, Gs, prompt, resp, softmax_scale, workspace)
+
+
+@_placed
+def _decode(raw, cache, q, o, lse, hq, n_groups, n_seqs, Gs, prompt, resp, softmax_scale, workspace):
+    lib = load_library()
+    if o is None:
+        o = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((hq, n_seqs), dtype=torch.float32, device=cache.device)
+    if workspace is None:
+        need = lib.sp_attn_decode_workspace_bytes(n_groups, n_seqs, hq, cache.n_kv_heads, cache.head_dim, cache.code)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
+    pt, pw, pl = prompt
+    rt, rw, rl = resp
+    _check(lib.sp_attn_decode(cache._ref, q.data_ptr(), o.data_ptr(), lse.data_ptr(), hq, n_groups, n_seqs, None if Gs is None else _i32(Gs),
+                              pt, pw, pl if pw else None, rt, rw, rl, softmax_scale, workspace.data_ptr(), workspace.numel(), raw))
     return o, lse
 
 
-def _logit_rows(name, t, shape, dtype, device):
-    """Rows of logits with any stride from row to row; returns that stride."""
-    _tensor(name, t, dtype, shape, device, contiguous=False)
+def _logit_stride(name, t, shape, dtype, index) -> int:
+    """Elements from row to row of logits, whose rows are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _refuse(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {tuple(shape)} beside the logits")
     if t.stride(1) != 1 and t.shape[1] > 1:
         _refuse(f"{name}: the elements of a row are not contiguous")
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _mask_rows(mask, rows, device):
+def _mask_rows(mask, rows, index):
     if mask is None:
         return None, 0
-    if mask.dtype not in (torch.int32, torch.uint32):
-        _refuse(f"mask: {mask.dtype}, expected int32 or uint32 words")
-    _tensor("mask", mask, mask.dtype, (rows, None), device)
+    if mask.dtype not in (torch.int32, torch.uint32) or mask.dim() != 2:
+        _refuse(f"mask: {mask.dtype} {tuple(mask.shape)}, expected rows of int32 or uint32 words")
+    _need("mask", mask, mask.dtype, (rows, mask.shape[1]), index)
     return mask.data_ptr(), mask.shape[1]
+
+
+def _history(name, tokens, lens, rows, index):
+    """(pointer, stride, pointer of the lengths) of rows of token ids, which may be missing."""
+    if tokens is None and lens is None:
+        return None, 0, None
+    if tokens is None or lens is None:
+        _refuse(f"{name}_tokens and {name}_lens go together")
+    if tokens.dim() != 2:
+        _refuse(f"{name}_tokens: {tuple(tokens.shape)}, expected [rows, tokens]")
+    stride = tokens.shape[1]
+    _need(name + "_tokens", tokens, torch.int32, (rows, stride), index)
+    _need(name + "_lens", lens, torch.int32, (rows,), index)
+    return (tokens.data_ptr(), stride, lens.data_ptr()) if stride else (None, 0, None)
 
 
 def sp_attn_adjust_logits(logits, rules: LogitRules, Gs: Optional[Sequence[int]], prompt_tokens, prompt_lens, resp_tokens, resp_lens,
@@ -761,47 +798,46 @@ def sp_attn_adjust_logits(logits, rules: LogitRules, Gs: Optional[Sequence[int]]
     """Adjusted logits [n_seqs, vocab] of one row per sequence.  Its history is the first prompt_lens[g] ids of its group's row of
     prompt_tokens [n_groups, .] and the first resp_lens[s] ids of its row of resp_tokens [n_seqs, .] (either pair may be None).  mask [n_seqs, words]:
     bit v % 32 of word v / 32 allows id v.  ``out`` may be logits itself."""
-    lib = load_library()
-    dev = logits.device
+    index = logits.get_device()
     n_seqs, vocab = logits.shape
     n_groups = n_seqs if Gs is None else len(Gs)
-    stride = _logit_rows("logits", logits, (n_seqs, vocab), logits.dtype, dev)
-    rules._fits(vocab, dev)
-    mp, ms = _mask_rows(mask, n_seqs, dev)
+    stride = _logit_stride("logits", logits, logits.shape, logits.dtype, index)
+    out_stride = vocab if out is None else _logit_stride("out", out, logits.shape, logits.dtype, index)
+    rules._fits(vocab, index)
+    rows = _mask_rows(mask, n_seqs, index)
+    prompt, resp = _history("prompt", prompt_tokens, prompt_lens, n_groups, index), _history("resp", resp_tokens, resp_lens, n_seqs, index)
+    return _adjust(index, stream, logits, stride, out, out_stride, rules, rows, n_groups, n_seqs, Gs, prompt, resp)
 
-    def tokens_of(name, tokens, lens, rows):
-        if tokens is None and lens is None:
-            return None, 0, None
-        if tokens is None or lens is None:
-            _refuse(f"{name}_tokens and {name}_lens go together")
-        _tensor(name + "_tokens", tokens, torch.int32, (rows, None), dev)
-        _tensor(name + "_lens", lens, torch.int32, (rows,), dev)
-        return (tokens.data_ptr(), tokens.shape[1], lens.data_ptr()) if tokens.shape[1] else (None, 0, None)
 
-    history = (*tokens_of("prompt", prompt_tokens, prompt_lens, n_groups), *tokens_of("resp", resp_tokens, resp_lens, n_seqs))
-    with _on(dev, stream) as s:
-        out = torch.empty((n_seqs, vocab), dtype=logits.dtype, device=dev) if out is None else out
-        out_stride = _logit_rows("out", out, (n_seqs, vocab), logits.dtype, dev)
-        _check(lib.sp_attn_adjust_logits(logits.data_ptr(), stride, out.data_ptr(), out_stride, vocab, rules._ref, mp, ms, n_groups, n_seqs,
-                                         None if Gs is None else _i32(Gs), *history, _dtype_code(logits), s))
+@_placed
+def _adjust(raw, logits, stride, out, out_stride, rules, mask, n_groups, n_seqs, Gs, prompt, resp):
+    vocab = logits.shape[1]
+    if out is None:
+        out = torch.empty((n_seqs, vocab), dtype=logits.dtype, device=logits.device)
+    _check(load_library().sp_attn_adjust_logits(logits.data_ptr(), stride, out.data_ptr(), out_stride, vocab, rules._ref, *mask, n_groups, n_seqs,
+                                                None if Gs is None else _i32(Gs), *prompt, *resp, _dtype_code(logits), raw))
     return out
 
 
-def _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace):
-    """What the forward and the backward check alike; returns the mask's pointer and stride and the workspace's size where it is to be made."""
-    dev = logits.device
+def _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, mask):
+    """What the forward and the backward check alike; returns the device's index and the mask's pointer and stride."""
+    index = logits.get_device()
     T, V = logits.shape
-    _tensor("logits", logits, logits.dtype, (T, V), dev)
+    _need("logits", logits, logits.dtype, (T, V), index)
     if T != sum(prompt_lens) + sum(resp_lens_flat):
         _refuse(f"logits have {T} rows, the pack has {sum(prompt_lens) + sum(resp_lens_flat)}")
-    _tensor("labels", labels, torch.int32, (T,), dev)
-    _tensor("tokens", tokens, torch.int32, (T,), dev)
-    rules._fits(V, dev)
-    mp, ms = _mask_rows(mask, T, dev)
-    need = 0
-    if workspace is None:
-        need = max(256, load_library().sp_attn_adjusted_logprob_workspace_bytes(T, len(prompt_lens), len(resp_lens_flat), V))
-    return mp, ms, need
+    _need("labels", labels, torch.int32, (T,), index)
+    _need("tokens", tokens, torch.int32, (T,), index)
+    rules._fits(V, index)
+    return index, _mask_rows(mask, T, index)
+
+
+def _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace):
+    if workspace is not None:
+        return workspace
+    T, V = logits.shape
+    need = load_library().sp_attn_adjusted_logprob_workspace_bytes(T, len(prompt_lens), len(resp_lens_flat), V)
+    return torch.empty(max(256, need), dtype=torch.uint8, device=logits.device)
 
 
 def sp_attn_adjusted_logprob_fwd(logits, labels, tokens, rules: LogitRules, prompt_lens: Sequence[int], Gs: Sequence[int],
@@ -809,20 +845,23 @@ def sp_attn_adjusted_logprob_fwd(logits, labels, tokens, rules: LogitRules, prom
     """Log-probability of labels[t] under the adjusted distribution at every response row t of logits [T, V]; tokens [T] are the pack's ids.
     mask [T, words] as in sp_attn_adjust_logits.  Returns (logp, lse); prompt rows keep whatever the output tensors held (zeros when
     allocated here)."""
-    lib = load_library()
-    dev = logits.device
-    mp, ms, need = _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace)
-    T, V = logits.shape
+    index, rows = _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, mask)
     for name, t in (("logp", logp), ("lse", lse)):
         if t is not None:
-            _tensor(name, t, torch.float32, (T,), dev)
-    with _on(dev, stream) as s:
-        logp = torch.zeros(T, dtype=torch.float32, device=dev) if logp is None else logp
-        lse = torch.zeros(T, dtype=torch.float32, device=dev) if lse is None else lse
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
-        _check(lib.sp_attn_adjusted_logprob_fwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), V,
-                                                rules._ref, mp, ms, len(prompt_lens), _i32(prompt_lens), _i32(Gs), _i32(resp_lens_flat),
-                                                _dtype_code(logits), flags, workspace.data_ptr(), workspace.numel(), s))
+            _need(name, t, torch.float32, (logits.shape[0],), index)
+    return _adjusted_fwd(index, stream, logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, rows, flags, logp, lse, workspace)
+
+
+@_placed
+def _adjusted_fwd(raw, logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, flags, logp, lse, workspace):
+    T, V = logits.shape
+    if logp is None or lse is None:
+        zeros = torch.zeros((2, T), dtype=torch.float32, device=logits.device)      # one launch for both
+        logp, lse = zeros[0] if logp is None else logp, zeros[1] if lse is None else lse
+    workspace = _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace)
+    _check(load_library().sp_attn_adjusted_logprob_fwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), V,
+                                                       rules._ref, *mask, len(prompt_lens), _i32(prompt_lens), _i32(Gs), _i32(resp_lens_flat),
+                                                       _dtype_code(logits), flags, workspace.data_ptr(), workspace.numel(), raw))
     return logp, lse
 
 
@@ -830,20 +869,24 @@ def sp_attn_adjusted_logprob_bwd(logits, labels, tokens, lse, g, rules: LogitRul
                                  resp_lens_flat: Sequence[int], mask=None, flags: int = 0, dlogits=None, workspace=None, stream=None):
     """Gradient with respect to the raw logits of sum_t g[t] logp[t], logp of sp_attn_adjusted_logprob_fwd.  Prompt rows of dlogits are zero
     when it is allocated here, otherwise they keep what they held (SP_FLAG_ZERO_PROMPT_ROWS: zero).  ``dlogits`` may be logits itself."""
-    lib = load_library()
-    dev = logits.device
-    mp, ms, need = _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace)
+    index, rows = _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, mask)
     T, V = logits.shape
-    _tensor("lse", lse, torch.float32, (T,), dev)
-    _tensor("g", g, torch.float32, (T,), dev)
+    _need("lse", lse, torch.float32, (T,), index)
+    _need("g", g, torch.float32, (T,), index)
     if dlogits is None:
         flags |= SP_FLAG_ZERO_PROMPT_ROWS
     else:
-        _tensor("dlogits", dlogits, logits.dtype, (T, V), dev)
-    with _on(dev, stream) as s:
-        dlogits = torch.empty_like(logits) if dlogits is None else dlogits
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
-        _check(lib.sp_attn_adjusted_logprob_bwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), lse.data_ptr(), g.data_ptr(),
-                                                dlogits.data_ptr(), V, rules._ref, mp, ms, len(prompt_lens), _i32(prompt_lens), _i32(Gs),
-                                                _i32(resp_lens_flat), _dtype_code(logits), flags, workspace.data_ptr(), workspace.numel(), s))
+        _need("dlogits", dlogits, logits.dtype, (T, V), index)
+    return _adjusted_bwd(index, stream, logits, labels, tokens, lse, g, rules, prompt_lens, Gs, resp_lens_flat, rows, flags, dlogits, workspace)
+
+
+@_placed
+def _adjusted_bwd(raw, logits, labels, tokens, lse, g, rules, prompt_lens, Gs, resp_lens_flat, mask, flags, dlogits, workspace):
+    if dlogits is None:
+        dlogits = torch.empty_like(logits)
+    workspace = _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace)
+    _check(load_library().sp_attn_adjusted_logprob_bwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), lse.data_ptr(), g.data_ptr(),
+                                                       dlogits.data_ptr(), logits.shape[1], rules._ref, *mask, len(prompt_lens), _i32(prompt_lens),
+                                                       _i32(Gs), _i32(resp_lens_flat), _dtype_code(logits), flags, workspace.data_ptr(),
+                                                       workspace.numel(), raw))
     return dlogits

@@ -181,7 +181,7 @@ struct AdjustArgs {
 
 // One workgroup per (sequence, slice).  words[g] = first sequence of the launch's group g, ahead of one word past the last.
 template <typename T, bool HIST>
-__global__ __launch_bounds__(AT) void adjust_kernel(TabArg starts, AdjustArgs a) {
+__global__ __launch_bounds__(AT) void adjust_kernel(SeqArg starts, AdjustArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned lds[];
     const int seq = a.first + blockIdx.y;
     const Slice s = slice_of(blockIdx.x, a.slice_len, a.vocab, lds);
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(AT) void adjust_kernel(TabArg starts, AdjustArgs a)
         clear_counts(s);
         __syncthreads();
         if (a.prompt_tokens) {
-            const int* const w = table_of(starts);
+            const int* const w = words_of(starts);
             int lo = 0, hi = a.n_groups;
             while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (w[mid] <= seq) lo = mid; else hi = mid; }
             const int g = w[a.n_groups + 1] + lo;
@@ -392,12 +392,12 @@ hipError_t launch_adjust_logits(const void* logits, int64_t stride, void* out, i
     const bool hist = uses_history(rules) && (a.prompt_tokens || a.resp_tokens);
     const size_t lds = hist ? (size_t)a.slice_len * 2 : 0;
     // the groups of a launch are a kernel argument, and its rows a grid's second dimension: larger calls are several launches
-    constexpr int MAX_GROUPS = ARG_WORDS - 2, MAX_ROWS = 32768;
+    constexpr int MAX_GROUPS = SEQ_WORDS - 2, MAX_ROWS = 32768;
     int seq = 0, g = 0, left = 0;                        // left: sequences of group g that the launches so far have not served
     while (true) {
         while (g < n_groups && left == 0) { left = Gs ? Gs[g] : 1; if (left == 0) ++g; }
         if (g >= n_groups) break;
-        TabArg starts{};
+        SeqArg starts{};
         const int g0 = g;
         int n = 0, rows = 0;
         while (g < n_groups && n < MAX_GROUPS && rows < MAX_ROWS) {

@@ -764,16 +764,21 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
         return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
     hipStream_t s = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    sp::TabArg starts;
-    try {       // first sequence of each group: a kernel argument, or in the workspace
-        std::vector<int32_t> words((size_t)n_groups + 1, 0);
-        for (int g = 0; g < n_groups; ++g) words[g + 1] = words[g] + (Gs ? Gs[g] : 1);
-        starts = sp::make_tab_arg(words.data(), words.size(), table_of(workspace));
-        if (starts.dev)
+    sp::SeqArg starts{};
+    bool alike = true;          // groups of one size need no table
+    for (int g = 1; Gs && g < n_groups; ++g) alike = alike && Gs[g] == Gs[0];
+    if (!alike && n_groups < sp::SEQ_WORDS) {
+        for (int g = 0; g < n_groups; ++g) starts.words[g + 1] = starts.words[g] + Gs[g];
+    } else if (!alike) {
+        try {
+            std::vector<int32_t> words((size_t)n_groups + 1, 0);
+            for (int g = 0; g < n_groups; ++g) words[g + 1] = words[g] + Gs[g];
+            starts.dev = table_of(workspace);
             e = sp::launch_prepare(words.data(), (int)words.size(), table_of(workspace), (uint32_t*)workspace, sp::ReserveTag{}, sp::TAG_CLEAR, false,
                                    n_groups, n_seqs, 0, 0, sp::Schedule{}, sp::KEYS_AS_PACKED, s);
-    } catch (const std::exception&) {
-        return fail(SP_ERR_INVALID_ARG, "no host memory for %d groups", n_groups);
+        } catch (const std::exception&) {
+            return fail(SP_ERR_INVALID_ARG, "no host memory for %d groups", n_groups);
+        }
     }
     if (e == hipSuccess)
         e = sp::launch_decode(c, q, o, lse, n_q_heads, n_groups, n_seqs, Gs, starts, prompt_tables, prompt_width, prompt_lens, resp_tables, resp_width,

@@ -32,11 +32,11 @@ struct AppendArgs {
 // hold eight pairs each of a head, as in the rotary pass.  The heads of a token are those of q, of k and of v in this order; their
 // rows are loaded ahead of the lookups.  starts.words[i] = first of the launch's new tokens of its sequence i, one past the last behind.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void append_kernel(TabArg starts, AppendFreq f, AppendArgs a) {
+__global__ __launch_bounds__(256) void append_kernel(SeqArg starts, AppendFreq f, AppendArgs a) {
     typedef typename CacheVec8<T>::type V8;
     constexpr int HALF = D / 2, TOKENS = 256 / HALF, LANES = D / 16, UNROLL = 6;
     __shared__ float cs[TOKENS][HALF], sn[TOKENS][HALF];
-    const int* const w = table_of(starts);
+    const int* const w = words_of(starts);
     {   // lengths behind the call
         const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
         if (a.lens_out && n < a.n_seqs) {
@@ -148,10 +148,10 @@ hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, 
     a.width = width; a.log_page = cache.log_page; a.capacity = (int64_t)width << cache.log_page; a.n_pages = cache.n_pages;
     a.one_each = !new_lens; a.Hq = Hq; a.Hkv = cache.n_kv_heads;
     // a launch's token counts are a kernel argument: more sequences than it holds are several launches
-    constexpr int MAX_SEQS = ARG_WORDS - 1;
+    constexpr int MAX_SEQS = SEQ_WORDS - 1;
     int64_t tok = 0;
     for (int seq = 0; seq < n_seqs;) {
-        TabArg starts{};
+        SeqArg starts{};
         int n = 0;
         int64_t tokens = 0;
         if (new_lens) {

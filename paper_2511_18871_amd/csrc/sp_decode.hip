@@ -569,13 +569,13 @@ __device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArg
 
 // NC: row tiles of a wave in a shared segment, 0: no list is shared.  NS: in a solo one.
 template <int D, int NC, int NS, bool MANY>
-__global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArgs a) {
+__global__ __launch_bounds__(256, 2) void decode_kernel(SeqArg starts, DecodeArgs a) {
     constexpr int KEYS16 = 32 * D, KIND = NC > 0;       // bytes of 16 keys
     __shared__ __attribute__((aligned(1024))) char lds[16 * KEYS16];
     __shared__ PlanShare share;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
-    const Lists<KIND> ls{table_of(starts), a};
+    const Lists<KIND> ls{words_of(starts), a};
     Work work;
     if constexpr (MANY) {
         work = find_work<KIND>(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
     auto whole = [&](int key, int count) SP_INLINE {
         if (key + count > at.len) return false;
         pages.need(key >> a.log_page);
-        pages.need(key + count - 1 >> a.log_page);
+        pages.need((key + count - 1) >> a.log_page);
         return !pages.bad && (unsigned)((key >> a.log_page) - pages.first) < 64u;
     };
     const __bf16* const q = (const __bf16*)a.q;
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
             if (whole(key, 32)) {
                 valid[0] = valid[1] = 16;
                 off[0] = offset(key, __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page)));
-                off[1] = a.log_page > 4 ? off[0] + KEYS16 : offset(key + 16, __builtin_amdgcn_readfirstlane(pages.at(key + 16 >> a.log_page)));
+                off[1] = a.log_page > 4 ? off[0] + KEYS16 : offset(key + 16, __builtin_amdgcn_readfirstlane(pages.at((key + 16) >> a.log_page)));
             } else {
                 locate(key, off[0], valid[0]);
                 locate(key + 16, off[1], valid[1]);
@@ -695,7 +695,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
             lo = hi = 0xffffffffu;
             const int key = 64 * at.t;
             if (whole(key, 64)) {
-                mine = offset(key + 16 * w, __builtin_amdgcn_readfirstlane(pages.at(key + 16 * w >> a.log_page)));
+                mine = offset(key + 16 * w, __builtin_amdgcn_readfirstlane(pages.at((key + 16 * w) >> a.log_page)));
             } else {
                 lo = hi = 0;
 #pragma unroll 1
@@ -748,13 +748,13 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(TabArg starts, DecodeArg
 // that it reads them in pieces of 16 bytes.  O^T += V^T P^T: step i contracts keys 4 j + i, whose weight is score i of the lane, and row m of
 // tile (h, e) is element 64 h + 4 m + e, so that V is read in pieces of 16 bytes as well.
 template <int D, bool MANY>
-__global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, DecodeArgs a) {
+__global__ __launch_bounds__(256, 2) void decode_f32_kernel(SeqArg starts, DecodeArgs a) {
     __shared__ i32x2 lists[4096];
     __shared__ PlanShare share;
     constexpr int NC = SOLO_ROWS / 16, HALVES = D / 64;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, m16 = l & 15, j = l >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
-    const Lists<0> ls{table_of(starts), a};
+    const Lists<0> ls{words_of(starts), a};
     Work work;
     if constexpr (MANY) work = find_work<0>(ls, lists, 4096, share, w, l); else work = find_work_in_lanes<0>(ls, w, l);
     if (work.left == 0) return;
@@ -858,9 +858,9 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(TabArg starts, Decod
 // Bound: the latency of three loads that wait for each other (where the sums are, the statistics, the sums); the first sums are
 // therefore asked for with the statistics.  D / 4 lanes hold a row, so that a wave has 4 x 256 / D rows in flight.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void decode_join_kernel(TabArg starts, DecodeArgs a) {
+__global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeArgs a) {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, DEPTH = 4;
-    const int* const w = table_of(starts);
+    const int* const w = words_of(starts);
     const int l = threadIdx.x & 63, mine = l / LANES, e0 = 4 * (l % LANES);
     const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (item >= (int64_t)a.n_seqs * a.Hq) return;
@@ -983,7 +983,7 @@ double decode_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_to
     return (units + ((double)resp_tokens / 32 + 1) * n_seqs * (rep / SOLO_ROWS + 1)) * Hkv;
 }
 
-hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, const TabArg& starts,
+hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, const SeqArg& starts,
                          const int* prompt_tables, int prompt_width, const int* prompt_lens, const int* resp_tables, int resp_width,
                          const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s) {
     DecodeArgs a{};

@@ -355,6 +355,15 @@ int f32_rows(const Problem& p, int kernel);
 // Waves per workgroup (8 or 4) of a dkdv pass that is not split over the q heads (rule and reasons: sp_bwd.hip).
 int dkdv_waves(const Problem& p);
 
+// What the rollout calls know on the host of their sequences, as the FIRST parameter of a kernel: few words, for most steps need none of
+// them and a launch copies all (one sequence's decode call, host: 20.7 us with the table's 768 words).
+constexpr int SEQ_WORDS = 200;
+struct SeqArg { const int* dev; int32_t words[SEQ_WORDS]; };
+__device__ __forceinline__ const int* words_of(const SeqArg& t) {
+    const uint64_t at = t.dev ? (uint64_t)(uintptr_t)t.dev : (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(SeqArg, words);
+    return (const int*)(const __attribute__((address_space(4))) int*)at;
+}
+
 // Paged cache of the rollout calls (sp_kv_cache, its page size as a power of two)
 struct KvCache { void* k; void* v; int64_t n_pages; int log_page, n_kv_heads, head_dim; bool f32; };
 hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, void* q_out, int Hq, const void* k, int64_t k_stride,
@@ -364,7 +373,7 @@ hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, 
 // starts: first sequence of each group, one past the last behind them.  partials: decode_partial_bytes() bytes.
 size_t decode_partial_bytes(int n_groups, int n_seqs, int Hq, int Hkv, int d);
 double decode_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_tokens, int64_t resp_tokens, const int32_t* Gs);
-hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, const TabArg& starts,
+hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, const SeqArg& starts,
                          const int* prompt_tables, int prompt_width, const int* prompt_lens, const int* resp_tables, int resp_width,
                          const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s);
 
