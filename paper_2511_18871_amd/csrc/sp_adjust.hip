@@ -27,24 +27,34 @@ template <typename T> struct Pack8;
 template <> struct Pack8<__bf16> {
     typedef __bf16 vec __attribute__((ext_vector_type(8), aligned(2)));
     vec x;
-    __device__ __forceinline__ void load(const __bf16* p) { x = *reinterpret_cast<const vec*>(p); }
-    __device__ __forceinline__ void store(__bf16* p) const { *reinterpret_cast<vec*>(p) = x; }
+    template <bool PAST> __device__ __forceinline__ void load(const __bf16* p) {
+        if constexpr (PAST) x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
+        else x = *reinterpret_cast<const vec*>(p);
+    }
+    template <bool PAST> __device__ __forceinline__ void store(__bf16* p) const {
+        if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<vec*>(p));
+        else *reinterpret_cast<vec*>(p) = x;
+    }
 };
 template <> struct Pack8<float> {
     typedef float half __attribute__((ext_vector_type(4), aligned(4)));
     typedef float vec __attribute__((ext_vector_type(8)));
     vec x;
-    __device__ __forceinline__ void load(const float* p) {
-        const half a = *reinterpret_cast<const half*>(p), b = *reinterpret_cast<const half*>(p + 4);
+    template <bool PAST> __device__ __forceinline__ void load(const float* p) {
+        const half* const q = reinterpret_cast<const half*>(p);
+        half a, b;
+        if constexpr (PAST) { a = __builtin_nontemporal_load(q); b = __builtin_nontemporal_load(q + 1); }
+        else { a = q[0]; b = q[1]; }
 #pragma unroll
         for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[e + 4] = b[e]; }
     }
-    __device__ __forceinline__ void store(float* p) const {
+    template <bool PAST> __device__ __forceinline__ void store(float* p) const {
+        half* const q = reinterpret_cast<half*>(p);
         half a, b;
 #pragma unroll
         for (int e = 0; e < 4; ++e) { a[e] = x[e]; b[e] = x[e + 4]; }
-        *reinterpret_cast<half*>(p) = a;
-        *reinterpret_cast<half*>(p + 4) = b;
+        if constexpr (PAST) { __builtin_nontemporal_store(a, q); __builtin_nontemporal_store(b, q + 1); }
+        else { q[0] = a; q[1] = b; }
     }
 };
 
@@ -83,70 +93,78 @@ __device__ __forceinline__ void add_generated(const Slice& s, const int* tokens,
     }
 }
 
-// Eight elements of a row after bias, penalties and mask, ahead of the division by the temperature; slope (SLOPE): their
-// derivative with respect to the raw elements, but for the temperature.
+// Eight elements of a row after the bias: penalties and mask, ahead of the division by the temperature; slope (SLOPE): their
+// derivative with respect to the raw elements, but for the temperature and the mask.  An element costs some twelve instructions if it
+// is in the history of any of the wave's rows of eight, else two: few are.
 template <bool SLOPE, bool HIST>
-__device__ __forceinline__ void adjust8(float (&a)[8], float (&slope)[8], const AdjustRules& r, i32x4 counts, unsigned bits) {
+__device__ __forceinline__ void adjust8(float (&a)[8], float (&slope)[8], const AdjustRules& r, i32x4 counts, bool masked, unsigned bits) {
     if constexpr (SLOPE)
 #pragma unroll
         for (int e = 0; e < 8; ++e) slope[e] = 1.f;
     if constexpr (HIST) {
-        if ((counts[0] | counts[1]) | (counts[2] | counts[3])) {       // some of the eight are in the history
+        if (__builtin_amdgcn_ballot_w64(((counts[0] | counts[1]) | (counts[2] | counts[3])) != 0) != 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const unsigned c = ((unsigned)counts[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-                const float f = c ? (a[e] > 0.f ? r.inv_repetition : r.repetition) : 1.f;
-                const float n = (float)(c & 0x7fffu);
-                a[e] = a[e] * f - (n * r.frequency + (n > 0.f ? r.presence : 0.f));
-                if constexpr (SLOPE) slope[e] = f;
+                const unsigned c = e & 1 ? (unsigned)counts[e >> 1] >> 16 : (unsigned)counts[e >> 1] & 0xffffu;
+                if (__builtin_amdgcn_ballot_w64(c != 0) != 0) {
+                    const float f = c ? (a[e] > 0.f ? r.inv_repetition : r.repetition) : 1.f;
+                    const float n = (float)(c & 0x7fffu);
+                    a[e] = a[e] * f - (n * r.frequency + (n > 0.f ? r.presence : 0.f));
+                    if constexpr (SLOPE) slope[e] = f;
+                }
             }
         }
     }
+    if (masked) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const bool off = !(bits >> e & 1);
-        a[e] = off ? -INFINITY : a[e];
-        if constexpr (SLOPE) slope[e] = off ? 0.f : slope[e];
+        for (int e = 0; e < 8; ++e) {
+            const unsigned keep = (unsigned)__builtin_amdgcn_sbfe((int)bits, e, 1);
+            a[e] = __uint_as_float((__float_as_uint(a[e]) & keep) | (0xff800000u & ~keep));
+        }
     }
 }
 
 // Visits the slice of one row in vectors of eight, UNROLL of them in flight per thread: f(values, counts, mask bits, index
-// of the first element within the slice, how many of them there are).
-template <typename T, bool HIST, int UNROLL, typename F>
+// of the first element within the slice, how many of them there are).  PAST: the row is read past the caches.
+template <typename T, bool HIST, bool PAST, int UNROLL, typename F>
 __device__ __forceinline__ void for_vectors(const T* row, const uint8_t* mask, const AdjustRules& r, const Slice& s, F f) {
     const int vecs = s.n / 8;
     const T* const z = row + s.v0;
     const float* const bias = r.bias ? r.bias + s.v0 : nullptr;
     const uint8_t* const bits = mask ? mask + s.v0 / 8 : nullptr;
-    auto one = [&](const Pack8<T>& x, const Pack8<float>& b, unsigned m, int i) {
-        float a[8];
+    auto several = [&](int i, auto count) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value;
+        Pack8<T> x[N];
+        Pack8<float> b[N];
+        unsigned m[N];
+        i32x4 c[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = (float)x.x[e] + b.x[e];
-        i32x4 c{0, 0, 0, 0};
-        if constexpr (HIST) c = reinterpret_cast<const i32x4*>(s.counts)[i];
-        f(a, c, m, 8 * i, 8);
-    };
-    int i = threadIdx.x;
-    for (; i + (UNROLL - 1) * AT < vecs; i += UNROLL * AT) {
-        Pack8<T> x[UNROLL];
-        Pack8<float> b[UNROLL];
-        unsigned m[UNROLL];
+        for (int u = 0; u < N; ++u) x[u].template load<PAST>(z + 8 * (i + u * AT));
+        if (bits)
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            x[u].load(z + 8 * (i + u * AT));
-            if (bias) b[u].load(bias + 8 * (i + u * AT)); else b[u].x = (typename Pack8<float>::vec)(0.f);
-            m[u] = bits ? bits[i + u * AT] : 0xffu;
+            for (int u = 0; u < N; ++u) m[u] = bits[i + u * AT];
+        if (bias)
+#pragma unroll
+            for (int u = 0; u < N; ++u) b[u].template load<false>(bias + 8 * (i + u * AT));
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            c[u] = i32x4{0, 0, 0, 0};
+            if constexpr (HIST) c[u] = reinterpret_cast<const i32x4*>(s.counts)[i + u * AT];
         }
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) one(x[u], b[u], m[u], i + u * AT);
-    }
-    for (; i < vecs; i += AT) {
-        Pack8<T> x;
-        Pack8<float> b;
-        x.load(z + 8 * i);
-        if (bias) b.load(bias + 8 * i); else b.x = (typename Pack8<float>::vec)(0.f);
-        one(x, b, bits ? bits[i] : 0xffu, i);
-    }
+        for (int u = 0; u < N; ++u) {
+            float a[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] = (float)x[u].x[e];
+            if (bias)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] += b[u].x[e];
+            f(a, c[u], bits ? m[u] : 0xffu, 8 * (i + u * AT), 8);
+        }
+    };
+    int i = threadIdx.x;
+    for (; i + (UNROLL - 1) * AT < vecs; i += UNROLL * AT) several(i, std::integral_constant<int, UNROLL>{});
+    for (; i < vecs; i += AT) several(i, std::integral_constant<int, 1>{});
     if (i == vecs && (s.n & 7)) {                       // the vocabulary's last, incomplete vector
         float a[8];
 #pragma unroll
@@ -157,13 +175,13 @@ __device__ __forceinline__ void for_vectors(const T* row, const uint8_t* mask, c
     }
 }
 
-template <typename T>
+template <bool PAST, typename T>
 __device__ __forceinline__ void store8(T* p, const float (&x)[8], int n) {
     if (n == 8) {
         Pack8<T> y;
 #pragma unroll
         for (int e = 0; e < 8; ++e) y.x[e] = (T)x[e];
-        y.store(p);
+        y.template store<PAST>(p);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) if (e < n) p[e] = (T)x[e];
@@ -203,13 +221,13 @@ __global__ __launch_bounds__(AT) void adjust_kernel(SeqArg starts, AdjustArgs a)
         __syncthreads();
     }
     T* const out = (T*)a.out + seq * a.out_stride + s.v0;
-    for_vectors<T, HIST, 2>((const T*)a.logits + seq * a.stride, a.mask ? a.mask + seq * a.mask_stride : nullptr, a.rules, s,
-        [&](float (&x)[8], i32x4 c, unsigned bits, int at, int n) {
+    for_vectors<T, HIST, false, 2>((const T*)a.logits + seq * a.stride, a.mask ? a.mask + seq * a.mask_stride : nullptr, a.rules, s,
+        [&](float (&x)[8], i32x4 c, unsigned bits, int at, int n) __attribute__((always_inline)) {
             float none[8];
-            adjust8<false, HIST>(x, none, a.rules, c, bits);
+            adjust8<false, HIST>(x, none, a.rules, c, a.mask != nullptr, bits);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= a.rules.inv_temperature;
-            store8(out + at, x, n);
+            store8<false>(out + at, x, n);
         });
 }
 
@@ -231,17 +249,23 @@ __device__ __forceinline__ void scaled_merge(float& m, float& s, float m2, float
     s = s * __builtin_amdgcn_exp2f((m - mn) * c) + s2 * __builtin_amdgcn_exp2f((m2 - mn) * c);
     m = mn;
 }
+// over the lanes of a wave
+__device__ __forceinline__ void scaled_wave(float& m, float& s, float c) {
+    const float mn = wave_max(m);
+    s = wave_sum(s * __builtin_amdgcn_exp2f((m - mn) * c));
+    m = mn;
+}
 __device__ __forceinline__ float log_of(float m, float s, float inv_t) { return m * inv_t + __logf(s); }
 // no id allowed: L = -inf, and the log-probability of any label is -inf
 __device__ __forceinline__ float label_logp(float z, float L) { return L == -INFINITY ? -INFINITY : z - L; }
 
-// One workgroup per (slice, run of rows of the pack).
-template <typename T, bool HIST, bool BWD>
+// One workgroup per (slice, run of rows of the pack); the backward takes the last rows first, which the caches still hold from the forward.
+template <typename T, bool HIST, bool BWD, bool PAST>
 __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, LogprobArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned lds[];
     const int* const tab = table_of(table);
     const Slice s = slice_of(blockIdx.x, a.slice_len, a.vocab, lds);
-    const int T_total = tab[1], t0 = blockIdx.y * a.run, t1 = min(t0 + a.run, T_total);
+    const int T_total = tab[1], t0 = (BWD ? gridDim.y - 1 - blockIdx.y : blockIdx.y) * a.run, t1 = min(t0 + a.run, T_total);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const float c = a.rules.inv_temperature * LOG2E;
     if (!BWD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) a.tag[threadIdx.x] = 0u;
@@ -270,7 +294,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             if (BWD && a.zero_prompt) {
                 T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
                 const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) store8(out + 8 * i, zero, min(8, s.n - 8 * i));
+                for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) store8<PAST>(out + 8 * i, zero, min(8, s.n - 8 * i));
             }
             continue;
         }
@@ -282,49 +306,50 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
         }
         const T* const row = (const T*)a.logits + (int64_t)t * a.vocab;
         const uint8_t* const mask = a.mask ? a.mask + t * a.mask_stride : nullptr;
-        const int label = a.labels[t];
+        const unsigned label = (unsigned)a.labels[t] - (unsigned)s.v0;          // within the slice, if below s.n
+        const int label_at = label < (unsigned)s.n ? (int)(label & ~7u) : -1;
         if constexpr (BWD) {
             T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
-            const float L = a.lse[t], g = L == -INFINITY ? 0.f : a.g[t], Lf = L == -INFINITY ? 0.f : L;
-            const float gt = g * a.rules.inv_temperature;
-            for_vectors<T, HIST, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) {
+            const float L = a.lse[t], Lf = L == -INFINITY ? 0.f : L, gt = L == -INFINITY ? 0.f : -a.g[t] * a.rules.inv_temperature;
+            for_vectors<T, HIST, PAST, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float slope[8];
-                adjust8<true, HIST>(x, slope, a.rules, cnt, bits);
+                adjust8<true, HIST>(x, slope, a.rules, cnt, mask != nullptr, bits);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = __builtin_amdgcn_exp2f((x[e] * a.rules.inv_temperature - Lf) * LOG2E);
-                    x[e] = gt * slope[e] * ((s.v0 + at + e == label ? 1.f : 0.f) - p);
-                }
-                store8(out + at, x, n);
+                for (int e = 0; e < 8; ++e)
+                    x[e] = gt * slope[e] * __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.rules.inv_temperature, -Lf) * LOG2E);
+                if (at == label_at)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) if (e == (int)(label & 7) && (bits >> e & 1)) x[e] -= gt * slope[e];
+                store8<PAST>(out + at, x, n);
             });
         } else {
             float m = A_LOWEST, sum = 0.f, z_label = -INFINITY;
-            bool has = false;
-            for_vectors<T, HIST, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) {
+            for_vectors<T, HIST, false, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float none[8];
-                adjust8<false, HIST>(x, none, a.rules, cnt, bits);
-                float mx = x[0];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
-                const float mn = fmaxf(m, mx);
+                adjust8<false, HIST>(x, none, a.rules, cnt, mask != nullptr, bits);
+                // against the reference from earlier elements, which serves as long as the exponentials stay in range
                 float part = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) part += __builtin_amdgcn_exp2f((x[e] - mn) * c);
-                sum = sum * __builtin_amdgcn_exp2f((m - mn) * c) + part;
-                m = mn;
-                const int k = label - s.v0 - at;
-                if (k >= 0 && k < n) {
-                    has = true;
+                for (int e = 0; e < 8; ++e) part += __builtin_amdgcn_exp2f((x[e] - m) * c);
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(part <= 16384.f)) != 0, 0)) {
+                    float mx = x[0];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) if (e == k) z_label = x[e] * a.rules.inv_temperature;
+                    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+                    const float mn = fmaxf(m, mx);
+                    part = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) part += __builtin_amdgcn_exp2f((x[e] - mn) * c);
+                    sum *= __builtin_amdgcn_exp2f((m - mn) * c);
+                    m = mn;
                 }
+                sum += part;
+                if (at == label_at)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) if (e == (int)(label & 7)) z_label = x[e] * a.rules.inv_temperature;
             });
-            for (int o = 32; o >= 1; o >>= 1) {
-                const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(sum, o, 64);
-                scaled_merge(m, sum, m2, s2, c);
-            }
+            scaled_wave(m, sum, c);
             float* const labels_z = a.parts + (int64_t)T_total * a.n_slices * AWAVES * 2;
-            if (has) labels_z[t] = z_label;
+            if (label_at >= 0 && (int)threadIdx.x == (label_at >> 3) % AT) labels_z[t] = z_label;
             if (lane == 0) {
                 float* const p = a.parts + (((int64_t)t * a.n_slices + blockIdx.x) * AWAVES + wave) * 2;
                 p[0] = m;
@@ -348,10 +373,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(TabArg table, const i
         const float* const p = parts + ((int64_t)t * per_row + i) * 2;
         scaled_merge(m, s, p[0], p[1], c);
     }
-    for (int o = 32; o >= 1; o >>= 1) {
-        const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
-        scaled_merge(m, s, m2, s2, c);
-    }
+    scaled_wave(m, s, c);
     if (l == 0) {
         const float L = log_of(m, s, inv_t);
         const int y = labels[t];
@@ -439,11 +461,15 @@ hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labe
     const bool hist = uses_history(rules);
     const size_t lds = hist ? (size_t)a.slice_len * 2 : 0;
     const dim3 grid((unsigned)a.n_slices, (unsigned)((total_tokens + a.run - 1) / a.run));
+    // As the ordinary gradient: one that the Infinity Cache (256 MB) cannot hold is stored past the caches, and then the logits are read past them.
+    const int64_t row = vocab * (f32 ? 4 : 2);
+    const bool past = total_tokens * row > (int64_t)256 << 20 && row >= 8192;
     with_kernel(f32, hist, [&](auto elem, auto with) {
         typedef decltype(elem) T;
         constexpr bool H = decltype(with)::value;
-        if (bwd) hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, true>), grid, dim3(AT), lds, s, tab, a);
-        else hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, false>), grid, dim3(AT), lds, s, tab, a);
+        if (!bwd) hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, false, false>), grid, dim3(AT), lds, s, tab, a);
+        else if (past) hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, true, true>), grid, dim3(AT), lds, s, tab, a);
+        else hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, true, false>), grid, dim3(AT), lds, s, tab, a);
     });
     if (!bwd)
         hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)((total_tokens + 3) / 4)), dim3(256), 0, s, tab, labels, parts, logp, lse,

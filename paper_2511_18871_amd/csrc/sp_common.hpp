@@ -315,6 +315,29 @@ __device__ __forceinline__ float pair_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// maximum and sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48, and over all lanes of a wave; in every lane
+template <int CTRL> __device__ __forceinline__ float rotated16(float x) {
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float quad_max(float x) {
+    x = pair_max(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    x = pair_sum(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, rotated16<0x128>(x)); x = fmaxf(x, rotated16<0x124>(x)); x = fmaxf(x, rotated16<0x122>(x)); x = fmaxf(x, rotated16<0x121>(x));
+    return quad_max(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += rotated16<0x128>(x); x += rotated16<0x124>(x); x += rotated16<0x122>(x); x += rotated16<0x121>(x);
+    return quad_sum(x);
+}
+
 // Asynchronous global -> LDS copy of 16 bytes per lane (global_load_lds_dwordx4): lane i of
 // the wave writes LDS bytes [lds_base + 16*i, +16).  lds_base must be wave-uniform.
 // Written as inline assembly so that the compiler does not place a conservative

@@ -57,7 +57,7 @@ __device__ const i32x4 zero_granule = {0, 0, 0, 0};      // what keys that are n
 
 // ---- the plan --------------------------------------------------------------------------------------------
 
-// over the lanes of a wave: inclusive sums, and the maximum or the sum in every lane
+// inclusive sums over the lanes of a wave
 template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int x) {
     return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
 }
@@ -65,29 +65,6 @@ __device__ __forceinline__ int scan64(int x) {
     x = dpp_add<0x111, 0xf>(x); x = dpp_add<0x112, 0xf>(x); x = dpp_add<0x114, 0xf>(x); x = dpp_add<0x118, 0xf>(x);      // within 16 lanes
     x = dpp_add<0x142, 0xa>(x); return dpp_add<0x143, 0xc>(x);                                                      // across them
 }
-template <int CTRL> __device__ __forceinline__ float rotated16(float x) {
-    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
-}
-// the four lanes l, l ^ 16, l ^ 32, l ^ 48
-__device__ __forceinline__ float quad_max(float x) {
-    x = pair_max(x);
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-    x = pair_sum(x);
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float wave_max(float x) {
-    x = fmaxf(x, rotated16<0x128>(x)); x = fmaxf(x, rotated16<0x124>(x)); x = fmaxf(x, rotated16<0x122>(x)); x = fmaxf(x, rotated16<0x121>(x));
-    return quad_max(x);
-}
-__device__ __forceinline__ float wave_sum(float x) {
-    x += rotated16<0x128>(x); x += rotated16<0x124>(x); x += rotated16<0x122>(x); x += rotated16<0x121>(x);
-    return quad_sum(x);
-}
-
 struct ListShape { int rows, len, units, blocks; bool shared; };      // units of keys of a segment; blocks of rows
 struct PlanShare { int sums[4][4]; int list[4], at[4], ord[4], rows[4], len[4], room[4]; };      // of the waves of a workgroup; where their runs start
 
