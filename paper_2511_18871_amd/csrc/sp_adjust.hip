@@ -12,6 +12,7 @@
 // counters are filled once, and from row to row only the tokens between them are added.  Integer atomics: the order does not matter.
 #include "sp_common.hpp"
 #include "sp_launch.hpp"
+#include <algorithm>
 #include <type_traits>
 
 namespace sp {
@@ -70,27 +71,34 @@ __device__ __forceinline__ void clear_counts(const Slice& s) {
     for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) reinterpret_cast<i32x4*>(s.counts)[i] = i32x4{0, 0, 0, 0};
 }
 
-// adds `count` tokens of the prompt, or of the response; those outside the slice (or the vocabulary) are passed over
-__device__ __forceinline__ void add_prompt(const Slice& s, const int* tokens, int count) {
-    for (int i = threadIdx.x; i < count; i += AT) {
-        const unsigned k = (unsigned)tokens[i] - (unsigned)s.v0;
-        if (k < (unsigned)s.n) atomicOr(&s.counts[k >> 1], 0x8000u << (16 * (k & 1)));
+// Adds `count` tokens of the prompt, or of the response; those outside the slice (or the vocabulary) are passed over.  Four in flight per thread.
+__device__ __forceinline__ void count_one(const Slice& s, unsigned k, bool may_saturate) {
+    const int sh = 16 * (k & 1);
+    unsigned* const w = &s.counts[k >> 1];
+    if (!may_saturate) { atomicAdd(w, 1u << sh); return; }
+    unsigned have = *w;
+    while (((have >> sh) & 0x7fffu) != 0x7fffu) {
+        const unsigned seen = atomicCAS(w, have, have + (1u << sh));
+        if (seen == have) break;
+        have = seen;
     }
 }
-__device__ __forceinline__ void add_generated(const Slice& s, const int* tokens, int count, bool may_saturate) {
-    for (int i = threadIdx.x; i < count; i += AT) {
-        const unsigned k = (unsigned)tokens[i] - (unsigned)s.v0;
-        if (k >= (unsigned)s.n) continue;
-        const int sh = 16 * (k & 1);
-        unsigned* const w = &s.counts[k >> 1];
-        if (!may_saturate) { atomicAdd(w, 1u << sh); continue; }
-        unsigned have = *w;
-        while (((have >> sh) & 0x7fffu) != 0x7fffu) {
-            const unsigned seen = atomicCAS(w, have, have + (1u << sh));
-            if (seen == have) break;
-            have = seen;
-        }
+template <typename F>
+__device__ __forceinline__ void for_tokens(const Slice& s, const int* tokens, int count, F f) {
+    for (int i = threadIdx.x; i < count; i += 4 * AT) {
+        unsigned k[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = i + u * AT < count ? (unsigned)tokens[i + u * AT] - (unsigned)s.v0 : 0xffffffffu;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) if (k[u] < (unsigned)s.n) f(k[u]);
     }
+}
+__device__ __forceinline__ void add_prompt(const Slice& s, const int* tokens, int count) {
+    for_tokens(s, tokens, count, [&](unsigned k) { atomicOr(&s.counts[k >> 1], 0x8000u << (16 * (k & 1))); });
+}
+__device__ __forceinline__ void add_generated(const Slice& s, const int* tokens, int count, bool may_saturate) {
+    if (may_saturate) for_tokens(s, tokens, count, [&](unsigned k) { count_one(s, k, true); });
+    else for_tokens(s, tokens, count, [&](unsigned k) { count_one(s, k, false); });
 }
 
 // Eight elements of a row after the bias: penalties and mask, ahead of the division by the temperature; slope (SLOPE): their
@@ -197,38 +205,71 @@ struct AdjustArgs {
     int first, n_groups, vocab, slice_len;               // first: sequence of the launch's first row
 };
 
-// One workgroup per (sequence, slice).  words[g] = first sequence of the launch's group g, ahead of one word past the last.
+// One workgroup per (sequence, slice of at most ADJUST_VECS vectors to a thread), so that a slice's elements are all asked for ahead of the
+// history, whose lookups wait for each other.  words[g] = first sequence of the launch's group g, one past the last behind them, then the
+// number of the first group.
+constexpr int ADJUST_VECS = 2;
 template <typename T, bool HIST>
 __global__ __launch_bounds__(AT) void adjust_kernel(SeqArg starts, AdjustArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned lds[];
     const int seq = a.first + blockIdx.y;
     const Slice s = slice_of(blockIdx.x, a.slice_len, a.vocab, lds);
+    const int vecs = s.n / 8, loose = s.n & 7;
+    const T* const z = (const T*)a.logits + seq * a.stride + s.v0;
+    T* const out = (T*)a.out + seq * a.out_stride + s.v0;
+    const float* const bias = a.rules.bias ? a.rules.bias + s.v0 : nullptr;
+    const uint8_t* const bits = a.mask ? a.mask + seq * a.mask_stride + s.v0 / 8 : nullptr;
+    float x[ADJUST_VECS][8];
+    unsigned m[ADJUST_VECS];
+    bool there[ADJUST_VECS];
+#pragma unroll
+    for (int u = 0; u < ADJUST_VECS; ++u) {
+        const int i = threadIdx.x + u * AT;
+        there[u] = i < vecs || (i == vecs && loose);
+        if (!there[u]) continue;
+        if (i < vecs) {
+            Pack8<T> y;
+            y.template load<false>(z + 8 * i);
+            Pack8<float> b;
+            if (bias) b.template load<false>(bias + 8 * i); else b.x = (typename Pack8<float>::vec)(0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[u][e] = (float)y.x[e] + b.x[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[u][e] = e < loose ? (float)z[8 * i + e] + (bias ? bias[8 * i + e] : 0.f) : 0.f;
+        }
+        m[u] = bits ? bits[i] : 0xffu;
+    }
     if constexpr (HIST) {
         clear_counts(s);
-        __syncthreads();
+        int np = 0, nr = 0;
+        const int* prompt = nullptr;
         if (a.prompt_tokens) {
             const int* const w = words_of(starts);
             int lo = 0, hi = a.n_groups;
             while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (w[mid] <= seq) lo = mid; else hi = mid; }
             const int g = w[a.n_groups + 1] + lo;
-            const int n = max(0, (int)min((int64_t)a.prompt_lens[g], a.prompt_stride));
-            add_prompt(s, a.prompt_tokens + g * a.prompt_stride, n);
+            prompt = a.prompt_tokens + g * a.prompt_stride;
+            np = max(0, (int)min((int64_t)a.prompt_lens[g], a.prompt_stride));
         }
-        if (a.resp_tokens) {
-            const int n = max(0, (int)min((int64_t)a.resp_lens[seq], a.resp_stride));
-            add_generated(s, a.resp_tokens + seq * a.resp_stride, n, n > 0x7fff);
-        }
+        if (a.resp_tokens) nr = max(0, (int)min((int64_t)a.resp_lens[seq], a.resp_stride));
+        __syncthreads();
+        add_prompt(s, prompt, np);
+        add_generated(s, a.resp_tokens + seq * a.resp_stride, nr, nr > 0x7fff);
         __syncthreads();
     }
-    T* const out = (T*)a.out + seq * a.out_stride + s.v0;
-    for_vectors<T, HIST, false, 2>((const T*)a.logits + seq * a.stride, a.mask ? a.mask + seq * a.mask_stride : nullptr, a.rules, s,
-        [&](float (&x)[8], i32x4 c, unsigned bits, int at, int n) __attribute__((always_inline)) {
-            float none[8];
-            adjust8<false, HIST>(x, none, a.rules, c, a.mask != nullptr, bits);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= a.rules.inv_temperature;
-            store8<false>(out + at, x, n);
-        });
+    for (int u = 0; u < ADJUST_VECS; ++u) {
+        if (!there[u]) continue;
+        const int i = threadIdx.x + u * AT;
+        i32x4 c{0, 0, 0, 0};
+        if constexpr (HIST) c = reinterpret_cast<const i32x4*>(s.counts)[i];
+        float none[8];
+        adjust8<false, HIST>(x[u], none, a.rules, c, bits != nullptr, m[u]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u][e] *= a.rules.inv_temperature;
+        store8<false>(out + 8 * i, x[u], i < vecs ? 8 : loose);
+    }
 }
 
 struct LogprobArgs {
@@ -283,10 +324,13 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
                 counted = gd.tok_base + seg_start(gd, local);
                 may_saturate = seg_end - counted > 0x7fff;
                 if constexpr (HIST) {
-                    __syncthreads();
+                    __syncthreads();                     // every wave is through with the segment before
                     clear_counts(s);
                     __syncthreads();
                     add_prompt(s, a.tokens + gd.tok_base, gd.Lp);
+                    add_generated(s, a.tokens + counted, t + a.own - counted, may_saturate);
+                    counted = t + a.own;
+                    __syncthreads();
                 }
             }
         }
@@ -299,10 +343,12 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             continue;
         }
         if constexpr (HIST) {
-            __syncthreads();                             // every wave is through with the row before
-            add_generated(s, a.tokens + counted, t + a.own - counted, may_saturate);
-            counted = t + a.own;
-            __syncthreads();
+            // The tokens since the row before, by the wave that reads their counters: no wave waits for another from row to row.
+            for (; counted < t + a.own; ++counted) {
+                const unsigned k = (unsigned)a.tokens[counted] - (unsigned)s.v0;
+                if (k < (unsigned)s.n && (int)(k >> 3) % AT == (int)threadIdx.x) count_one(s, k, may_saturate);
+            }
+            __builtin_amdgcn_wave_barrier();
         }
         const T* const row = (const T*)a.logits + (int64_t)t * a.vocab;
         const uint8_t* const mask = a.mask ? a.mask + t * a.mask_stride : nullptr;
@@ -311,7 +357,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
         if constexpr (BWD) {
             T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
             const float L = a.lse[t], Lf = L == -INFINITY ? 0.f : L, gt = L == -INFINITY ? 0.f : -a.g[t] * a.rules.inv_temperature;
-            for_vectors<T, HIST, PAST, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
+            for_vectors<T, HIST, PAST, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float slope[8];
                 adjust8<true, HIST>(x, slope, a.rules, cnt, mask != nullptr, bits);
 #pragma unroll
@@ -324,7 +370,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             });
         } else {
             float m = A_LOWEST, sum = 0.f, z_label = -INFINITY;
-            for_vectors<T, HIST, false, 2>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
+            for_vectors<T, HIST, false, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float none[8];
                 adjust8<false, HIST>(x, none, a.rules, cnt, mask != nullptr, bits);
                 // against the reference from earlier elements, which serves as long as the exponentials stay in range
@@ -392,7 +438,6 @@ bool uses_history(const AdjustRules& r) { return r.repetition != 1.f || r.presen
 }  // namespace
 
 int adjust_slices(int64_t vocab) { return (int)((vocab + SLICE_MAX - 1) / SLICE_MAX); }
-static int slice_length(int64_t vocab, int slices) { return (int)(((vocab + slices - 1) / slices + 7) / 8 * 8); }
 
 size_t adjust_parts_bytes(int64_t total_tokens, int64_t vocab) {
     return (size_t)total_tokens * ((size_t)adjust_slices(vocab) * AWAVES * 8 + 4);
@@ -409,8 +454,12 @@ hipError_t launch_adjust_logits(const void* logits, int64_t stride, void* out, i
     a.resp_tokens = resp_stride > 0 ? resp_tokens : nullptr; a.resp_lens = resp_lens; a.resp_stride = resp_stride;
     a.rules = rules;
     a.vocab = (int)vocab;
-    const int slices = adjust_slices(vocab);
-    a.slice_len = slice_length(vocab, slices);
+    int n_seqs = 0;
+    for (int g = 0; g < n_groups; ++g) n_seqs += Gs ? Gs[g] : 1;
+    // Every slice reads the whole history, so slices are as long as their threads can hold, or half of that where the chip is not full.
+    a.slice_len = 8 * AT * ADJUST_VECS;
+    if ((int64_t)n_seqs * ((vocab + a.slice_len - 1) / a.slice_len) < 256) a.slice_len /= ADJUST_VECS;
+    const int64_t slices = (vocab + a.slice_len - 1) / a.slice_len;
     const bool hist = uses_history(rules) && (a.prompt_tokens || a.resp_tokens);
     const size_t lds = hist ? (size_t)a.slice_len * 2 : 0;
     // the groups of a launch are a kernel argument, and its rows a grid's second dimension: larger calls are several launches
@@ -453,9 +502,10 @@ hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labe
     a.logp = logp; a.lse = lse; a.g = g; a.dlogits = dlogits; a.parts = parts; a.tag = tag; a.rules = rules;
     a.vocab = (int)vocab;
     a.n_slices = adjust_slices(vocab);
-    a.slice_len = slice_length(vocab, a.n_slices);
+    a.slice_len = (int)std::min<int64_t>(SLICE_MAX, (vocab + 7) / 8 * 8);
     a.own = own_token; a.zero_prompt = zero_prompt;
-    const int64_t run = total_tokens * a.n_slices / 1024;
+    // Runs: a workgroup's history is read once for its rows, and 2048 workgroups fill the chip four times over.
+    const int64_t run = total_tokens * a.n_slices / 2048;
     a.run = (int)(run < 1 ? 1 : run > 16 ? 16 : run);
     while ((total_tokens + a.run - 1) / a.run > 65535) a.run *= 2;
     const bool hist = uses_history(rules);
