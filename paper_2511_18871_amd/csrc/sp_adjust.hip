@@ -102,13 +102,10 @@ __device__ __forceinline__ void add_generated(const Slice& s, const int* tokens,
 }
 
 // Eight elements of a row after the bias: penalties and mask, ahead of the division by the temperature; slope (SLOPE): their
-// derivative with respect to the raw elements, but for the temperature and the mask.  An element costs some twelve instructions if it
+// derivative with respect to the raw elements, but for the temperature and the mask, multiplied in.  An element costs some twelve instructions if it
 // is in the history of any of the wave's rows of eight, else two: few are.
 template <bool SLOPE, bool HIST>
 __device__ __forceinline__ void adjust8(float (&a)[8], float (&slope)[8], const AdjustRules& r, i32x4 counts, bool masked, unsigned bits) {
-    if constexpr (SLOPE)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) slope[e] = 1.f;
     if constexpr (HIST) {
         if (__builtin_amdgcn_ballot_w64(((counts[0] | counts[1]) | (counts[2] | counts[3])) != 0) != 0) {
 #pragma unroll
@@ -117,8 +114,8 @@ __device__ __forceinline__ void adjust8(float (&a)[8], float (&slope)[8], const 
                 if (__builtin_amdgcn_ballot_w64(c != 0) != 0) {
                     const float f = c ? (a[e] > 0.f ? r.inv_repetition : r.repetition) : 1.f;
                     const float n = (float)(c & 0x7fffu);
-                    a[e] = a[e] * f - (n * r.frequency + (n > 0.f ? r.presence : 0.f));
-                    if constexpr (SLOPE) slope[e] = f;
+                    a[e] = __builtin_fmaf(a[e], f, -__builtin_fmaf(n, r.frequency, n > 0.f ? r.presence : 0.f));
+                    if constexpr (SLOPE) slope[e] *= f;
                 }
             }
         }
@@ -359,13 +356,15 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             const float L = a.lse[t], Lf = L == -INFINITY ? 0.f : L, gt = L == -INFINITY ? 0.f : -a.g[t] * a.rules.inv_temperature;
             for_vectors<T, HIST, PAST, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float slope[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) slope[e] = gt;
                 adjust8<true, HIST>(x, slope, a.rules, cnt, mask != nullptr, bits);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    x[e] = gt * slope[e] * __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.rules.inv_temperature, -Lf) * LOG2E);
+                    x[e] = slope[e] * __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.rules.inv_temperature, -Lf) * LOG2E);
                 if (at == label_at)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) if (e == (int)(label & 7) && (bits >> e & 1)) x[e] -= gt * slope[e];
+                    for (int e = 0; e < 8; ++e) if (e == (int)(label & 7) && (bits >> e & 1)) x[e] -= slope[e];
                 store8<PAST>(out + at, x, n);
             });
         } else {
@@ -454,11 +453,11 @@ hipError_t launch_adjust_logits(const void* logits, int64_t stride, void* out, i
     a.resp_tokens = resp_stride > 0 ? resp_tokens : nullptr; a.resp_lens = resp_lens; a.resp_stride = resp_stride;
     a.rules = rules;
     a.vocab = (int)vocab;
-    int n_seqs = 0;
+    int64_t n_seqs = 0;
     for (int g = 0; g < n_groups; ++g) n_seqs += Gs ? Gs[g] : 1;
     // Every slice reads the whole history, so slices are as long as their threads can hold, or half of that where the chip is not full.
     a.slice_len = 8 * AT * ADJUST_VECS;
-    if ((int64_t)n_seqs * ((vocab + a.slice_len - 1) / a.slice_len) < 256) a.slice_len /= ADJUST_VECS;
+    if (n_seqs * ((vocab + a.slice_len - 1) / a.slice_len) < 256) a.slice_len /= ADJUST_VECS;
     const int64_t slices = (vocab + a.slice_len - 1) / a.slice_len;
     const bool hist = uses_history(rules) && (a.prompt_tokens || a.resp_tokens);
     const size_t lds = hist ? (size_t)a.slice_len * 2 : 0;
