@@ -831,15 +831,31 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(SeqArg starts, Decod
 
 // ---- the join ------------------------------------------------------------------------------------------------
 
+// over aligned groups of 16, 32 or 64 lanes
+template <int N> __device__ __forceinline__ float lanes_max(float x) {
+    if constexpr (N == 64) return wave_max(x);
+    x = fmaxf(x, rotated16<0x128>(x)); x = fmaxf(x, rotated16<0x124>(x)); x = fmaxf(x, rotated16<0x122>(x)); x = fmaxf(x, rotated16<0x121>(x));
+    if constexpr (N == 32) x = fmaxf(x, __shfl_xor(x, 16, 32));
+    return x;
+}
+template <int N> __device__ __forceinline__ float lanes_sum(float x) {
+    if constexpr (N == 64) return wave_sum(x);
+    x += rotated16<0x128>(x); x += rotated16<0x124>(x); x += rotated16<0x122>(x); x += rotated16<0x121>(x);
+    if constexpr (N == 32) x += __shfl_xor(x, 16, 32);
+    return x;
+}
+
 // One wave per sequence and q head: o = sum_c e^(m_c - M) O_c / sum_c e^(m_c - M) l_c over the chunks of the prompt and of the response.
 // Bound: the latency of three loads that wait for each other (where the sums are, the statistics, the sums); the first sums are
-// therefore asked for with the statistics.  D / 4 lanes hold a row, so that a wave has 4 x 256 / D rows in flight.
-template <typename T, int D>
+// therefore asked for with the statistics.  D / 4 lanes hold a row, so that a wave has 4 x 256 / D rows in flight.  DENSE: the lanes that
+// hold one row do all of an item, and a wave takes 256 / D of them.
+template <typename T, int D, bool DENSE>
 __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeArgs a) {
-    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, DEPTH = 4;
+    constexpr int LANES = D / 4, EACH = DENSE ? LANES : 64, AT_ONCE = EACH / LANES, DEPTH = 4;
     const int* const w = words_of(starts);
-    const int l = threadIdx.x & 63, mine = l / LANES, e0 = 4 * (l % LANES);
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int l = threadIdx.x & (EACH - 1), mine = l / LANES, e0 = 4 * (l % LANES);
+    const int64_t item = DENSE ? (int64_t)blockIdx.x * (256 / EACH) + threadIdx.x / EACH
+                               : (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (item >= (int64_t)a.n_seqs * a.Hq) return;
     unsigned in_seq;
     const int seq = (int)divmod((unsigned)item, a.q_heads, in_seq), h = (int)in_seq;
@@ -882,8 +898,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
     auto row_of = [&](int i) { return i < n_p ? base_p + (int64_t)i * stride_p : base_r + (int64_t)(i - n_p) * stride_r; };
     float M = a.m_none, L = 0.f;
     f32x4 acc = {0, 0, 0, 0};
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int count = min(64, n - i0);
+    for (int i0 = 0; i0 < n; i0 += EACH) {
+        const int count = min(EACH, n - i0);
         f32x2 st = {a.m_none, 0.f};
         f32x4 x[DEPTH];
         if (l < count) st = *reinterpret_cast<const f32x2*>(a.stats + row_of(i0 + l) * 2);
@@ -896,7 +912,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
             }
         };
         fetch(0);
-        const float mn = fmaxf(M, wave_max(st[0])), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
+        const float mn = fmaxf(M, lanes_max<EACH>(st[0])), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
         M = mn;
         L = L * alpha + wt * st[1];            // lanes hold their chunks' shares of the sums
 #pragma unroll
@@ -905,15 +921,15 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
             if (i > 0) fetch(i);
 #pragma unroll
             for (int u = 0; u < DEPTH; ++u) {
-                const float f = __shfl(wt, (i + u * AT_ONCE + mine) & 63, 64);
+                const float f = __shfl(wt, (i + u * AT_ONCE + mine) & (EACH - 1), EACH);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] += f * x[u][e];
             }
         }
     }
-    L = wave_sum(L);
+    L = lanes_sum<EACH>(L);
 #pragma unroll
-    for (int o = 32; o >= LANES; o >>= 1)
+    for (int o = EACH / 2; o >= LANES; o >>= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
     const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -1030,9 +1046,14 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
             else with_solo(std::integral_constant<int, 2>{});
         };
         if (n_groups + n_seqs > 64) with_lists(std::true_type{}); else with_lists(std::false_type{});
-        const unsigned joins = (unsigned)(((int64_t)n_seqs * Hq + 3) / 4);
-        if (cache.f32) hipLaunchKernelGGL((decode_join_kernel<float, D>), dim3(joins), dim3(256), 0, s, starts, a);
-        else hipLaunchKernelGGL((decode_join_kernel<__bf16, D>), dim3(joins), dim3(256), 0, s, starts, a);
+        auto join = [&](auto dense) {
+            const int64_t each = decltype(dense)::value ? 1024 / D : 4;
+            const unsigned joins = (unsigned)(((int64_t)n_seqs * Hq + each - 1) / each);
+            if (cache.f32) hipLaunchKernelGGL((decode_join_kernel<float, D, decltype(dense)::value>), dim3(joins), dim3(256), 0, s, starts, a);
+            else hipLaunchKernelGGL((decode_join_kernel<__bf16, D, decltype(dense)::value>), dim3(joins), dim3(256), 0, s, starts, a);
+        };
+        // more items than the chip holds waves (8192): most then have a few rows only
+        if ((int64_t)n_seqs * Hq > 8192) join(std::true_type{}); else join(std::false_type{});
     };
     if (cache.head_dim == 64) launch(std::integral_constant<int, 64>{}); else launch(std::integral_constant<int, 128>{});
     return hipGetLastError();

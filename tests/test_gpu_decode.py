@@ -127,6 +127,16 @@ def test_many_groups_take_their_table_from_memory():
     run_and_check(q, kc, vc, [1] * n, pt, prompts, rt, resp, 0.1)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_more_rows_than_the_chip_holds_waves(dtype, d):
+    """Rows with one chunk and with many side by side in a wave, rows without a key among them, an incomplete last wave."""
+    Gs = [7] * 43
+    prompts, resp = [(i * 37) % 90 for i in range(43)], [(i * 11) % 40 for i in range(301)]
+    prompts[5], prompts[6], resp[42], resp[43], resp[300] = 900, 0, 0, -1, 2100
+    q, kc, vc, pt, rt = make(dtype, d, 28, 4, 32, prompts, Gs, [max(n, 0) for n in resp])
+    run_and_check(q, kc, vc, Gs, pt, prompts, rt, resp, 0.1)
+
+
 def test_replayed_with_other_lengths_and_workspaces_shared():
     """Two captured graphs on one workspace, replayed in turn with other lengths, eager calls on it in between."""
     prompts, Gs, resp = [200, 90], [5, 3], [64] * 8
