@@ -5,6 +5,7 @@ if the library is missing, loading raises."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -590,6 +591,7 @@ def _need(name, t, dtype, shape, index):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _placed(f):
@@ -598,7 +600,7 @@ def _placed(f):
         if index < 0:
             _refuse("the tensors are not on a GPU")
         if stream is None:
-            if index == torch.cuda.current_device():
+            if index == _current_device():
                 return f(_raw_stream(index), *args)
             with torch.cuda.device(index):
                 return f(_raw_stream(index), *args)
@@ -649,13 +651,13 @@ def _ptr(t):
 
 def _token_stride(name, t, cache, heads) -> int:
     """Elements from token to token of [T, heads, d], whose heads are contiguous within a token."""
-    d = cache.head_dim
-    if t.dtype is not cache.dtype or t.get_device() != cache.index or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+    d, shape = cache.head_dim, t.shape
+    if t.dtype is not cache.dtype or t.get_device() != cache.index or shape[1:] != (heads, d):
         _refuse(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {cache.dtype} [tokens, {heads}, {d}] on {cache.device}")
     at, head, one = t.stride()
-    if t.shape[0] and (one != 1 or (heads > 1 and head != d)):
+    if shape[0] and (one != 1 or (heads > 1 and head != d)):
         _refuse(f"{name}: the heads of a token are not contiguous (strides {t.stride()})")
-    return at if t.shape[0] > 1 else heads * d
+    return at if shape[0] > 1 else heads * d
 
 
 def sp_attn_cache_append(cache: KvCache, k, v, tables, lens, rope_base: float, q=None, new_lens: Optional[Sequence[int]] = None,
@@ -695,7 +697,7 @@ def sp_attn_cache_append(cache: KvCache, k, v, tables, lens, rope_base: float, q
 @_placed
 def _append(raw, cache, q, qs, q_out, hq, k, ks, k_out, v, vs, n_seqs, new_lens, tables, lens, pos_base, lens_out, rope_base):
     if q is not None and q_out is None:
-        q_out = torch.empty((k.shape[0], hq, cache.head_dim), dtype=cache.dtype, device=cache.device)
+        q_out = torch.empty(k.shape[0], hq, cache.head_dim, dtype=cache.dtype, device=cache.device)
     if lens_out is None:
         lens_out = torch.empty_like(lens)
     if k.shape[0] == 0:                    # nothing to store; the pointers of empty tensors are null
@@ -707,6 +709,7 @@ def _append(raw, cache, q, qs, q_out, hq, k, ks, k_out, v, vs, n_seqs, new_lens,
     return q_out, lens_out
 
 
+@functools.lru_cache(maxsize=64)
 def decode_workspace_bytes(n_groups: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype_code: int) -> int:
     return load_library().sp_attn_decode_workspace_bytes(n_groups, n_seqs, n_q_heads, n_kv_heads, head_dim, dtype_code)
 
@@ -750,9 +753,9 @@ def _decode(raw, cache, q, o, lse, hq, n_groups, n_seqs, Gs, prompt, resp, softm
     if o is None:
         o = torch.empty_like(q)
     if lse is None:
-        lse = torch.empty((hq, n_seqs), dtype=torch.float32, device=cache.device)
+        lse = torch.empty(hq, n_seqs, dtype=torch.float32, device=cache.device)
     if workspace is None:
-        need = lib.sp_attn_decode_workspace_bytes(n_groups, n_seqs, hq, cache.n_kv_heads, cache.head_dim, cache.code)
+        need = decode_workspace_bytes(n_groups, n_seqs, hq, cache.n_kv_heads, cache.head_dim, cache.code)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
     pt, pw, pl = prompt
     rt, rw, rl = resp
@@ -813,7 +816,7 @@ def sp_attn_adjust_logits(logits, rules: LogitRules, Gs: Optional[Sequence[int]]
 def _adjust(raw, logits, stride, out, out_stride, rules, mask, n_groups, n_seqs, Gs, prompt, resp):
     vocab = logits.shape[1]
     if out is None:
-        out = torch.empty((n_seqs, vocab), dtype=logits.dtype, device=logits.device)
+        out = torch.empty(n_seqs, vocab, dtype=logits.dtype, device=logits.device)
     _check(load_library().sp_attn_adjust_logits(logits.data_ptr(), stride, out.data_ptr(), out_stride, vocab, rules._ref, *mask, n_groups, n_seqs,
                                                 None if Gs is None else _i32(Gs), *prompt, *resp, _dtype_code(logits), raw))
     return out
@@ -832,11 +835,16 @@ def _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, m
     return index, _mask_rows(mask, T, index)
 
 
+@functools.lru_cache(maxsize=64)
+def _adjusted_workspace_bytes(T, n_groups, n_resp, V) -> int:
+    return load_library().sp_attn_adjusted_logprob_workspace_bytes(T, n_groups, n_resp, V)
+
+
 def _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace):
     if workspace is not None:
         return workspace
     T, V = logits.shape
-    need = load_library().sp_attn_adjusted_logprob_workspace_bytes(T, len(prompt_lens), len(resp_lens_flat), V)
+    need = _adjusted_workspace_bytes(T, len(prompt_lens), len(resp_lens_flat), V)
     return torch.empty(max(256, need), dtype=torch.uint8, device=logits.device)
 
 
@@ -856,7 +864,7 @@ def sp_attn_adjusted_logprob_fwd(logits, labels, tokens, rules: LogitRules, prom
 def _adjusted_fwd(raw, logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, flags, logp, lse, workspace):
     T, V = logits.shape
     if logp is None or lse is None:
-        zeros = torch.zeros((2, T), dtype=torch.float32, device=logits.device)      # one launch for both
+        zeros = torch.zeros(2, T, dtype=torch.float32, device=logits.device)        # one launch for both
         logp, lse = zeros[0] if logp is None else logp, zeros[1] if lse is None else lse
     workspace = _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace)
     _check(load_library().sp_attn_adjusted_logprob_fwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), V,
