@@ -831,24 +831,11 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(SeqArg starts, Decod
 
 // ---- the join ------------------------------------------------------------------------------------------------
 
-// over aligned groups of 16, 32 or 64 lanes
-template <int N> __device__ __forceinline__ float lanes_max(float x) {
-    if constexpr (N == 64) return wave_max(x);
-    x = fmaxf(x, rotated16<0x128>(x)); x = fmaxf(x, rotated16<0x124>(x)); x = fmaxf(x, rotated16<0x122>(x)); x = fmaxf(x, rotated16<0x121>(x));
-    if constexpr (N == 32) x = fmaxf(x, __shfl_xor(x, 16, 32));
-    return x;
-}
-template <int N> __device__ __forceinline__ float lanes_sum(float x) {
-    if constexpr (N == 64) return wave_sum(x);
-    x += rotated16<0x128>(x); x += rotated16<0x124>(x); x += rotated16<0x122>(x); x += rotated16<0x121>(x);
-    if constexpr (N == 32) x += __shfl_xor(x, 16, 32);
-    return x;
-}
-
 // One wave per sequence and q head: o = sum_c e^(m_c - M) O_c / sum_c e^(m_c - M) l_c over the chunks of the prompt and of the response.
-// Bound: the latency of three loads that wait for each other (where the sums are, the statistics, the sums); the first sums are
-// therefore asked for with the statistics.  D / 4 lanes hold a row, so that a wave has 4 x 256 / D rows in flight.  DENSE: the lanes that
-// hold one row do all of an item, and a wave takes 256 / D of them.
+// Bound: the latency of two loads that wait for each other (where the sums are; the sums and their statistics) and of fetching code that
+// runs once.  Hence even lanes find the prompt's chunks and odd ones the response's with the same instructions, the lanes that hold a row (D / 4)
+// load its statistics too and keep a maximum of their own, and these meet at the end.  DENSE: such lanes do all of an item, and a
+// wave takes 256 / D of them.
 template <typename T, int D, bool DENSE>
 __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeArgs a) {
     constexpr int LANES = D / 4, EACH = DENSE ? LANES : 64, AT_ONCE = EACH / LANES, DEPTH = 4;
@@ -857,9 +844,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
     const int64_t item = DENSE ? (int64_t)blockIdx.x * (256 / EACH) + threadIdx.x / EACH
                                : (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (item >= (int64_t)a.n_seqs * a.Hq) return;
-    unsigned in_seq;
+    unsigned in_seq, hr;
     const int seq = (int)divmod((unsigned)item, a.q_heads, in_seq), h = (int)in_seq;
-    unsigned hr;
     const int kvh = (int)divmod((unsigned)h, a.heads_each, hr);
     int g = 0, first, members = a.members;
     if (members) {
@@ -872,66 +858,65 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
         first = w[g];
         members = w[g + 1] - first;
     }
-    const i32x4 run = a.desc[0], dp = a.desc[1 + g], dr = a.desc[1 + a.n_groups + seq];
-    // consecutive slots: those of the workers that had units of this row's segment, from the first one's on
-    auto slots = [&](const i32x4& d, int rows, int row, bool prompt, int64_t& first_row, int& stride) {
-        const bool shared = sizeof(T) == 2 && rows > SOLO_ROWS;
-        int per = SOLO_ROWS;
-        if (shared) {
-            unsigned rest;
-            const int blocks = (int)divmod((unsigned)(rows - 1), a.block_rows, rest) + 1;
-            per = 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
-        }
-        const int block = rows > per ? row / per : 0, segment = block * a.Hkv + kvh, each = shared ? run[0] : run[1];
-        const unsigned from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[3];
-        const unsigned worker0 = from / (unsigned)each, worker1 = (from + d[1] - 1) / (unsigned)each;
-        stride = shared ? a.shared_rows : prompt ? a.prompt_rows : a.resp_rows;
-        first_row = (shared ? 0 : prompt ? a.prompt_base : a.resp_base) + ((int64_t)worker0 + (int64_t)d[2] * a.Hkv + segment) * stride + row - block * per;
-        return (int)(worker1 - worker0) + 1;
-    };
-    int64_t base_p = 0, base_r = 0;
-    int stride_p = 0, stride_r = 0, n_p = 0, n = 0;
-    if (dr[3] >= 0) {
-        if (dp[1] > 0) n_p = slots(dp, members * a.rep, (seq - first) * a.rep + (int)hr, true, base_p, stride_p);
-        n = n_p + (dr[1] > 0 ? slots(dr, a.rep, (int)hr, false, base_r, stride_r) : 0);
+    // The side's chunks: consecutive slots, those of the workers that had units of this row's segment, from the first one's on.  Rows of slots
+    // are below 2^32: a workspace of so many has more than 1 TB.
+    const bool resp = l & 1;
+    const i32x4 run = a.desc[0], d = a.desc[1 + (resp ? a.n_groups + seq : g)];
+    const int rows = resp ? a.rep : members * a.rep, row = resp ? (int)hr : (seq - first) * a.rep + (int)hr;
+    const bool shared = sizeof(T) == 2 && rows > SOLO_ROWS;
+    int per = SOLO_ROWS;
+    if (sizeof(T) == 2) {
+        unsigned rest;
+        const int blocks = (int)divmod((unsigned)(rows - 1), a.block_rows, rest) + 1;
+        if (shared) per = 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
     }
-    auto row_of = [&](int i) { return i < n_p ? base_p + (int64_t)i * stride_p : base_r + (int64_t)(i - n_p) * stride_r; };
+    const int block = rows > per ? row / per : 0, segment = block * a.Hkv + kvh;
+    const unsigned each = shared ? run[0] : run[1], from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[3];
+    const unsigned worker0 = from / each, worker1 = (from + d[1] - 1) / each;
+    const unsigned stride = shared ? a.shared_rows : resp ? a.resp_rows : a.prompt_rows;
+    const unsigned at = (unsigned)(shared ? 0 : resp ? a.resp_base : a.prompt_base) + (worker0 + (unsigned)d[2] * a.Hkv + segment) * stride + row - block * per;
+    const int count = d[1] > 0 ? (int)(worker1 - worker0) + 1 : 0;
+    auto prompts = [](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x00, 0xf, 0xf, true); };     // of the even lanes
+    auto resps = [](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x55, 0xf, 0xf, true); };       // of the odd ones
+    const bool part = (int)resps(d[3]) >= 0;
+    const int n_p = part ? (int)prompts(count) : 0, n = part ? n_p + (int)resps(count) : 0;
+    const unsigned at_p = prompts(at), at_r = resps(at), stride_p = prompts(stride), stride_r = resps(stride);
     float M = a.m_none, L = 0.f;
     f32x4 acc = {0, 0, 0, 0};
-    for (int i0 = 0; i0 < n; i0 += EACH) {
-        const int count = min(EACH, n - i0);
-        f32x2 st = {a.m_none, 0.f};
+    for (int i = 0; i < n; i += DEPTH * AT_ONCE) {
+        f32x2 st[DEPTH];
         f32x4 x[DEPTH];
-        if (l < count) st = *reinterpret_cast<const f32x2*>(a.stats + row_of(i0 + l) * 2);
-        auto fetch = [&](int i) {
 #pragma unroll
-            for (int u = 0; u < DEPTH; ++u) {
-                const int k = i + u * AT_ONCE + mine;
-                x[u] = f32x4{0, 0, 0, 0};
-                if (k < count) x[u] = *reinterpret_cast<const f32x4*>(a.sums + row_of(i0 + k) * D + e0);
-            }
-        };
-        fetch(0);
-        const float mn = fmaxf(M, lanes_max<EACH>(st[0])), alpha = __builtin_amdgcn_exp2f((M - mn) * a.c), wt = __builtin_amdgcn_exp2f((st[0] - mn) * a.c);
+        for (int u = 0; u < DEPTH; ++u) {
+            const int k = min(i + u * AT_ONCE + mine, n - 1);              // behind the last: again, with no weight
+            const unsigned at_k = k < n_p ? at_p + k * stride_p : at_r + (k - n_p) * stride_r;
+            st[u] = *reinterpret_cast<const f32x2*>(a.stats + (uint64_t)at_k * 2);
+            x[u] = *reinterpret_cast<const f32x4*>(a.sums + (uint64_t)at_k * D + e0);
+        }
+        float mn = M;
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) mn = fmaxf(mn, st[u][0]);
+        const float alpha = __builtin_amdgcn_exp2f((M - mn) * a.c);
         M = mn;
-        L = L * alpha + wt * st[1];            // lanes hold their chunks' shares of the sums
+        L *= alpha;
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] *= alpha;
-        for (int i = 0; i < count; i += DEPTH * AT_ONCE) {
-            if (i > 0) fetch(i);
 #pragma unroll
-            for (int u = 0; u < DEPTH; ++u) {
-                const float f = __shfl(wt, (i + u * AT_ONCE + mine) & (EACH - 1), EACH);
+        for (int u = 0; u < DEPTH; ++u) {
+            const float wt = i + u * AT_ONCE + mine < n ? __builtin_amdgcn_exp2f((st[u][0] - mn) * a.c) : 0.f;
+            L += wt * st[u][1];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += f * x[u][e];
-            }
+            for (int e = 0; e < 4; ++e) acc[e] += wt * x[u][e];
         }
     }
-    L = lanes_sum<EACH>(L);
 #pragma unroll
-    for (int o = EACH / 2; o >= LANES; o >>= 1)
+    for (int o = EACH / 2; o >= LANES; o >>= 1) {
+        const float m2 = __shfl_xor(M, o, 64), mn = fmaxf(M, m2), wt = __builtin_amdgcn_exp2f((M - mn) * a.c), wt2 = __builtin_amdgcn_exp2f((m2 - mn) * a.c);
+        M = mn;
+        L = L * wt + __shfl_xor(L, o, 64) * wt2;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+        for (int e = 0; e < 4; ++e) acc[e] = acc[e] * wt + __shfl_xor(acc[e], o, 64) * wt2;
+    }
     const float inv = L > 0.f ? 1.f / L : 0.f;
     if (mine == 0) {
         typedef T out4 __attribute__((ext_vector_type(4)));
