@@ -14,6 +14,13 @@
 // these are, rounded, the operand of O^T += V^T P^T as they stand, if the keys of V are taken in the same order.
 //   a list of at most 32 rows   the worker is a wave: units of 32 keys through 16 KB of LDS of its own, no barriers
 //   more rows                   the worker is a workgroup: its four waves share units of 64 keys and have up to 16 NC rows each
+//
+// Measured (heads of 128, bf16, us of the kernel + of the join; bytes are those of the keys and values):
+//   32 answers of 8k to 15k tokens to 8 prompts, 32/8 heads   263 + 5     1.53 GB, 5.8 TB/s
+//   64 prompts of 64 to 192 tokens, 16 answers each, 28/4     131 + 11    0.55 GB, 4.2 TB/s; the plan of 1088 lists takes 8 of it
+//   a prompt of 16k tokens, 32 answers, 40/8                  38 + 9      90 MB; 42 MB of sums, written and read, take as long as the keys
+//   a prompt of 1k tokens, 8 answers, 28/4                    8 + 5       latency: launch, plan, pages, keys, sums one after the other
+//   one sequence of 1k tokens, 28/4                           6 + 6       the same
 #include "sp_common.hpp"
 #include "sp_launch.hpp"
 #include <algorithm>
@@ -26,7 +33,7 @@ namespace {
 
 constexpr int SOLO_ROWS = 32;              // rows of a segment that a wave takes by itself
 constexpr int MAX_NC = 3;                  // row tiles of 16 of a wave that shares its keys: 192 rows to a workgroup
-constexpr int PLAN_WGS = 512;              // workgroups that the units are dealt to: two to a CU
+constexpr int PLAN_WGS = 512;              // workgroups that the units are dealt to: two to a CU (one: 131 -> 164 us for the 64 prompts above)
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -114,7 +121,8 @@ struct Work { bool shared; int worker, list, at, ord, left, room; i32x2 list_is;
 
 // The runs of either kind, from the units and segments of all lists.  Places are dealt by cost: a segment costs, for its rows and its sums, what one and a half of its
 // units (shared) or one (solo) cost, and a shared unit what shared_cost solo ones do.  A worker that passes from one segment to another takes
-// longer; where shared segments are long against the run, each is dealt to workers of its own, in room that is a multiple of the run (`aligned`).
+// longer; where shared segments are long against the run, each is dealt to workers of its own, in room that is a multiple of the run (`aligned`: 37.8 us
+// for the prompt of 16k tokens, 41.4 without).
 struct Runs { unsigned shared_run, solo_run, used; bool aligned; };      // used: workgroups of shared segments
 template <int KIND>
 __device__ __forceinline__ void shared_runs(const DecodeArgs& a, unsigned solo, unsigned solo_segs, unsigned shared, unsigned segs, Runs& r) {
@@ -131,7 +139,7 @@ __device__ __forceinline__ void shared_runs(const DecodeArgs& a, unsigned solo, 
 
 // Every workgroup makes the whole plan.  Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time, and
 // takes a cycle a byte.
-// Up to 64 lists: a wave by itself, a list to a lane.
+// Up to 64 lists: a wave by itself, a list to a lane (one sequence of 1k tokens 5.7 us, by the workgroup 7.0; a group of 8 8.2 and 11.0).
 template <int KIND>
 __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND>& ls, int wave, int lane) {
     const DecodeArgs& a = ls.a;
@@ -292,7 +300,9 @@ struct Cursor {
     int list, seg, t, units, segs, rows, len, blocks, ord;
     __device__ __forceinline__ Cursor(const Lists<KIND>& l, Work& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
         load(w.list_is);
-        seg = (int)((float)w.at * __builtin_amdgcn_rcpf((float)w.room));        // off by one at most: there are some thousand segments
+        const float inv = __builtin_amdgcn_rcpf((float)w.room);        // a quotient, what it leaves divided again, and a step to either side
+        seg = (int)((float)w.at * inv);
+        seg += (int)((float)(w.at - seg * w.room) * inv);
         seg = __builtin_amdgcn_readfirstlane(seg);
         seg -= seg * w.room > w.at;
         seg += (unsigned)(seg + 1) * w.room <= (unsigned)w.at;
@@ -978,7 +988,8 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     a.sums = a.stats + up256((size_t)(slots.shared + slots.prompts + slots.responses) * 8) / 4;
     a.prompt_base = slots.shared;
     a.resp_base = slots.shared + slots.prompts;
-    // row tiles per wave if the rows of a shared list are dealt to as few workgroups as can hold them
+    // Row tiles per wave if the rows of a shared list are dealt to as few workgroups as can hold them, as every workgroup reads the keys.  No
+    // more than that: they are all computed (8 sequences of 7 heads to a kv head: 8.2 us with one, 10.7 with three).
     const bool prompts = prompt_width > 0;
     auto rows_of = [&](int g) { return (int64_t)a.rep * (Gs ? Gs[g] : 1); };
     a.nc = 1;
@@ -1004,7 +1015,7 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     for (int g = 0; prompts && g < n_groups; ++g) count(rows_of(g), 1, (double)prompt_width * (1 << a.log_page), a.prompt_rows);
     count(a.rep, n_seqs, (double)resp_width * (1 << a.log_page), a.resp_rows);
     const unsigned grid = (unsigned)std::min<double>(PLAN_WGS, units_shared + units_solo / 4 + 1);
-    a.shared_cost = a.nc == 1 ? 3.f : a.nc == 2 ? 4.f : 5.5f;
+    a.shared_cost = a.nc == 1 ? 3.f : a.nc == 2 ? 4.f : 5.5f;        // from their instructions; the 16k prompt takes 47 to 49 us with anything from 0.8 to 9
     a.kv_heads = make_div(a.Hkv);
     a.q_heads = make_div(Hq);
     a.heads_each = make_div(a.rep);
@@ -1026,6 +1037,7 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
                 else if (a.nc == 2) with(decode_kernel<D, 2, NS, MANY>);
                 else with(decode_kernel<D, 3, NS, MANY>);
             };
+            // one row tile per wave where 16 rows are the most (one sequence 5.7 us, with two tiles 6.5)
             if (cache.f32) with(decode_f32_kernel<D, MANY>);
             else if (std::max(a.prompt_rows, a.resp_rows) <= 16) with_solo(std::integral_constant<int, 1>{});
             else with_solo(std::integral_constant<int, 2>{});
@@ -1037,7 +1049,8 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
             if (cache.f32) hipLaunchKernelGGL((decode_join_kernel<float, D, decltype(dense)::value>), dim3(joins), dim3(256), 0, s, starts, a);
             else hipLaunchKernelGGL((decode_join_kernel<__bf16, D, decltype(dense)::value>), dim3(joins), dim3(256), 0, s, starts, a);
         };
-        // more items than the chip holds waves (8192): most then have a few rows only
+        // More items than the chip holds waves (8192): most then have a few rows only.  (28.7k items of two or three: 13 us against 19; 1280 items
+        // of 40: 12 against 9.)
         if ((int64_t)n_seqs * Hq > 8192) join(std::true_type{}); else join(std::false_type{});
     };
     if (cache.head_dim == 64) launch(std::integral_constant<int, 64>{}); else launch(std::integral_constant<int, 128>{});
