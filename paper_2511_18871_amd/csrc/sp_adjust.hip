@@ -20,6 +20,7 @@ namespace {
 
 constexpr int AT = 512;                    // threads of a workgroup
 constexpr int AWAVES = AT / 64;
+constexpr int FEW_WAVES = 2;
 constexpr int SLICE_MAX = 32768;           // ids of a slice at most: 64 KB of counters, two workgroups to a CU (half of it: forward 165 -> 180 us)
 constexpr float A_LOWEST = -3.402823466e38f;
 
@@ -67,8 +68,9 @@ __device__ __forceinline__ Slice slice_of(int index, int len, int vocab, unsigne
     return Slice{v0, min(len, vocab - v0), lds};
 }
 
+template <int THREADS>
 __device__ __forceinline__ void clear_counts(const Slice& s) {
-    for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) reinterpret_cast<i32x4*>(s.counts)[i] = i32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < (s.n + 7) / 8; i += THREADS) reinterpret_cast<i32x4*>(s.counts)[i] = i32x4{0, 0, 0, 0};
 }
 
 // Adds `count` tokens of the prompt, or of the response; those outside the slice (or the vocabulary) are passed over.  Four in flight per thread.
@@ -83,22 +85,24 @@ __device__ __forceinline__ void count_one(const Slice& s, unsigned k, bool may_s
         have = seen;
     }
 }
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ void for_tokens(const Slice& s, const int* tokens, int count, F f) {
-    for (int i = threadIdx.x; i < count; i += 4 * AT) {
+    for (int i = threadIdx.x; i < count; i += 4 * THREADS) {
         unsigned k[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) k[u] = i + u * AT < count ? (unsigned)tokens[i + u * AT] - (unsigned)s.v0 : 0xffffffffu;
+        for (int u = 0; u < 4; ++u) k[u] = i + u * THREADS < count ? (unsigned)tokens[i + u * THREADS] - (unsigned)s.v0 : 0xffffffffu;
 #pragma unroll
         for (int u = 0; u < 4; ++u) if (k[u] < (unsigned)s.n) f(k[u]);
     }
 }
+template <int THREADS>
 __device__ __forceinline__ void add_prompt(const Slice& s, const int* tokens, int count) {
-    for_tokens(s, tokens, count, [&](unsigned k) { atomicOr(&s.counts[k >> 1], 0x8000u << (16 * (k & 1))); });
+    for_tokens<THREADS>(s, tokens, count, [&](unsigned k) { atomicOr(&s.counts[k >> 1], 0x8000u << (16 * (k & 1))); });
 }
+template <int THREADS>
 __device__ __forceinline__ void add_generated(const Slice& s, const int* tokens, int count, bool may_saturate) {
-    if (may_saturate) for_tokens(s, tokens, count, [&](unsigned k) { count_one(s, k, true); });
-    else for_tokens(s, tokens, count, [&](unsigned k) { count_one(s, k, false); });
+    if (may_saturate) for_tokens<THREADS>(s, tokens, count, [&](unsigned k) { count_one(s, k, true); });
+    else for_tokens<THREADS>(s, tokens, count, [&](unsigned k) { count_one(s, k, false); });
 }
 
 // Eight elements of a row after the bias: penalties and mask, ahead of the division by the temperature; slope (SLOPE): their
@@ -131,7 +135,7 @@ __device__ __forceinline__ void adjust8(float (&a)[8], float (&slope)[8], const 
 
 // Visits the slice of one row in vectors of eight, UNROLL of them in flight per thread: f(values, counts, mask bits, index
 // of the first element within the slice, how many of them there are).  PAST: the row is read past the caches.
-template <typename T, bool HIST, bool PAST, int UNROLL, typename F>
+template <typename T, int THREADS, bool HIST, bool PAST, int UNROLL, typename F>
 __device__ __forceinline__ void for_vectors(const T* row, const uint8_t* mask, const AdjustRules& r, const Slice& s, F f) {
     const int vecs = s.n / 8;
     const T* const z = row + s.v0;
@@ -144,17 +148,17 @@ __device__ __forceinline__ void for_vectors(const T* row, const uint8_t* mask, c
         unsigned m[N];
         i32x4 c[N];
 #pragma unroll
-        for (int u = 0; u < N; ++u) x[u].template load<PAST>(z + 8 * (i + u * AT));
+        for (int u = 0; u < N; ++u) x[u].template load<PAST>(z + 8 * (i + u * THREADS));
         if (bits)
 #pragma unroll
-            for (int u = 0; u < N; ++u) m[u] = bits[i + u * AT];
+            for (int u = 0; u < N; ++u) m[u] = bits[i + u * THREADS];
         if (bias)
 #pragma unroll
-            for (int u = 0; u < N; ++u) b[u].template load<false>(bias + 8 * (i + u * AT));
+            for (int u = 0; u < N; ++u) b[u].template load<false>(bias + 8 * (i + u * THREADS));
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             c[u] = i32x4{0, 0, 0, 0};
-            if constexpr (HIST) c[u] = reinterpret_cast<const i32x4*>(s.counts)[i + u * AT];
+            if constexpr (HIST) c[u] = reinterpret_cast<const i32x4*>(s.counts)[i + u * THREADS];
         }
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -164,12 +168,12 @@ __device__ __forceinline__ void for_vectors(const T* row, const uint8_t* mask, c
             if (bias)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a[e] += b[u].x[e];
-            f(a, c[u], bits ? m[u] : 0xffu, 8 * (i + u * AT), 8);
+            f(a, c[u], bits ? m[u] : 0xffu, 8 * (i + u * THREADS), 8);
         }
     };
     int i = threadIdx.x;
-    for (; i + (UNROLL - 1) * AT < vecs; i += UNROLL * AT) several(i, std::integral_constant<int, UNROLL>{});
-    for (; i < vecs; i += AT) several(i, std::integral_constant<int, 1>{});
+    for (; i + (UNROLL - 1) * THREADS < vecs; i += UNROLL * THREADS) several(i, std::integral_constant<int, UNROLL>{});
+    for (; i < vecs; i += THREADS) several(i, std::integral_constant<int, 1>{});
     if (i == vecs && (s.n & 7)) {                       // the vocabulary's last, incomplete vector
         float a[8];
 #pragma unroll
@@ -240,7 +244,7 @@ __global__ __launch_bounds__(AT) void adjust_kernel(SeqArg starts, AdjustArgs a)
         m[u] = bits ? bits[i] : 0xffu;
     }
     if constexpr (HIST) {
-        clear_counts(s);
+        clear_counts<AT>(s);
         int np = 0, nr = 0;
         const int* prompt = nullptr;
         if (a.prompt_tokens) {
@@ -253,8 +257,8 @@ __global__ __launch_bounds__(AT) void adjust_kernel(SeqArg starts, AdjustArgs a)
         }
         if (a.resp_tokens) nr = max(0, (int)min((int64_t)a.resp_lens[seq], a.resp_stride));
         __syncthreads();
-        add_prompt(s, prompt, np);
-        add_generated(s, a.resp_tokens + seq * a.resp_stride, nr, nr > 0x7fff);
+        add_prompt<AT>(s, prompt, np);
+        add_generated<AT>(s, a.resp_tokens + seq * a.resp_stride, nr, nr > 0x7fff);
         __syncthreads();
     }
 #pragma unroll
@@ -296,15 +300,22 @@ __device__ __forceinline__ void scaled_wave(float& m, float& s, float c) {
     m = mn;
 }
 __device__ __forceinline__ float log_of(float m, float s, float inv_t) { return m * inv_t + __logf(s); }
-// no id allowed: L = -inf, and the log-probability of any label is -inf
-__device__ __forceinline__ float label_logp(float z, float L) { return L == -INFINITY ? -INFINITY : z - L; }
+// A row's results from its (m, s) and the label's z' (-inf: no id of the vocabulary).  No id allowed: L = -inf, and the log-probability of any
+// label is -inf.
+__device__ __forceinline__ void finish_row(float m, float s, float z, float inv_t, float* logp, float* lse) {
+    const float L = log_of(m, s, inv_t);
+    *lse = L;
+    *logp = L == -INFINITY ? -INFINITY : z - L;
+}
 
 // One workgroup per (slice, run of rows of the pack), its counters as the first row needs them; from row to row each wave adds to those of its
 // own vectors.  Bound, at 1470 response rows of 152k ids in bf16 with bias and mask: the forward (447 MB, 165 us, 2.7 TB/s) by vector
 // instructions, which fill 63 % of the cycles, half of them for the 2.6 ids of every 512 that the history holds; the backward (1.05 GB,
 // 219 us, 4.8 TB/s) by memory.  Four vectors of a row in flight per thread: with two 176 and 226 us.
-template <typename T, bool HIST, bool BWD, bool PAST>
-__global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, LogprobArgs a) {
+template <typename T, int WAVES, bool HIST, bool BWD, bool PAST>
+__global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg table, LogprobArgs a) {
+    constexpr int THREADS = 64 * WAVES;
+    __shared__ float row_parts[2][2 * WAVES + 1];
     extern __shared__ __attribute__((aligned(16))) unsigned lds[];
     const int* const tab = table_of(table);
     const Slice s = slice_of(blockIdx.x, a.slice_len, a.vocab, lds);
@@ -327,10 +338,10 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
                 may_saturate = seg_end - counted > 0x7fff;
                 if constexpr (HIST) {
                     __syncthreads();                     // every wave is through with the segment before
-                    clear_counts(s);
+                    clear_counts<THREADS>(s);
                     __syncthreads();
-                    add_prompt(s, a.tokens + gd.tok_base, gd.Lp);
-                    add_generated(s, a.tokens + counted, t + a.own - counted, may_saturate);
+                    add_prompt<THREADS>(s, a.tokens + gd.tok_base, gd.Lp);
+                    add_generated<THREADS>(s, a.tokens + counted, t + a.own - counted, may_saturate);
                     counted = t + a.own;
                     __syncthreads();
                 }
@@ -340,7 +351,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             if (BWD && a.zero_prompt) {
                 T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
                 const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                for (int i = threadIdx.x; i < (s.n + 7) / 8; i += AT) store8<PAST>(out + 8 * i, zero, min(8, s.n - 8 * i));
+                for (int i = threadIdx.x; i < (s.n + 7) / 8; i += THREADS) store8<PAST>(out + 8 * i, zero, min(8, s.n - 8 * i));
             }
             continue;
         }
@@ -348,7 +359,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             // The tokens since the row before, by the wave that reads their counters: no wave waits for another from row to row.
             for (; counted < t + a.own; ++counted) {
                 const unsigned k = (unsigned)a.tokens[counted] - (unsigned)s.v0;
-                if (k < (unsigned)s.n && (int)(k >> 3) % AT == (int)threadIdx.x) count_one(s, k, may_saturate);
+                if (k < (unsigned)s.n && (int)(k >> 3) % THREADS == (int)threadIdx.x) count_one(s, k, may_saturate);
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -359,7 +370,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
         if constexpr (BWD) {
             T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
             const float L = a.lse[t], Lf = L == -INFINITY ? 0.f : L, gt = L == -INFINITY ? 0.f : -a.g[t] * a.rules.inv_temperature;
-            for_vectors<T, HIST, PAST, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
+            for_vectors<T, THREADS, HIST, PAST, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float slope[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) slope[e] = gt;
@@ -374,7 +385,7 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
             });
         } else {
             float m = A_LOWEST, sum = 0.f, z_label = -INFINITY;
-            for_vectors<T, HIST, false, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
+            for_vectors<T, THREADS, HIST, false, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {
                 float none[8];
                 adjust8<false, HIST>(x, none, a.rules, cnt, mask != nullptr, bits);
                 // against the reference from earlier elements, which serves as long as the exponentials stay in range
@@ -398,10 +409,23 @@ __global__ __launch_bounds__(AT) void adjusted_logprob_kernel(TabArg table, Logp
                     for (int e = 0; e < 8; ++e) if (e == (int)(label & 7)) z_label = x[e] * a.rules.inv_temperature;
             });
             scaled_wave(m, sum, c);
-            float* const labels_z = a.parts + (int64_t)T_total * a.n_slices * AWAVES * 2;
-            if (label_at >= 0 && (int)threadIdx.x == (label_at >> 3) % AT) labels_z[t] = z_label;
+            if (a.n_slices == 1) {
+                // The workgroup has all of the row: no join.  (Two places in turn: who writes the next but one has met the reader in between.)
+                float* const mine = row_parts[t & 1];
+                if (lane == 0) { mine[2 * wave] = m; mine[2 * wave + 1] = sum; }
+                if ((int)threadIdx.x == (label_at < 0 ? 0 : (label_at >> 3) % THREADS)) mine[2 * WAVES] = z_label;
+                __syncthreads();
+                if (threadIdx.x == 0) {
+#pragma unroll
+                    for (int i = 1; i < WAVES; ++i) scaled_merge(m, sum, mine[2 * i], mine[2 * i + 1], c);
+                    finish_row(m, sum, mine[2 * WAVES], a.rules.inv_temperature, a.logp + t, a.lse + t);
+                }
+                continue;
+            }
+            float* const labels_z = a.parts + (int64_t)T_total * a.n_slices * WAVES * 2;
+            if (label_at >= 0 && (int)threadIdx.x == (label_at >> 3) % THREADS) labels_z[t] = z_label;
             if (lane == 0) {
-                float* const p = a.parts + (((int64_t)t * a.n_slices + blockIdx.x) * AWAVES + wave) * 2;
+                float* const p = a.parts + (((int64_t)t * a.n_slices + blockIdx.x) * WAVES + wave) * 2;
                 p[0] = m;
                 p[1] = sum;
             }
@@ -425,10 +449,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(TabArg table, const i
     }
     scaled_wave(m, s, c);
     if (l == 0) {
-        const float L = log_of(m, s, inv_t);
         const int y = labels[t];
-        lse[t] = L;
-        logp[t] = y >= 0 && y < vocab ? label_logp(parts[(int64_t)T_total * per_row * 2 + t], L) : -INFINITY;
+        finish_row(m, s, y >= 0 && y < vocab ? parts[(int64_t)T_total * per_row * 2 + t] : -INFINITY, inv_t, logp + t, lse + t);
     }
 }
 
@@ -508,6 +530,7 @@ hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labe
     a.n_slices = adjust_slices(vocab);
     a.slice_len = (int)std::min<int64_t>(SLICE_MAX, (vocab + 7) / 8 * 8);
     a.own = own_token; a.zero_prompt = zero_prompt;
+    const int waves = a.slice_len > 8 * 64 * FEW_WAVES * 8 ? AWAVES : FEW_WAVES;
     // Runs: a workgroup's history is read once for its rows, and 2048 workgroups fill the chip four times over (1470 rows of 152k ids: forward
     // and backward 381 us, with half as many workgroups 429, with twice as many 380).
     const int64_t run = total_tokens * a.n_slices / 2048;
@@ -523,13 +546,17 @@ hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labe
     with_kernel(f32, hist, [&](auto elem, auto with) {
         typedef decltype(elem) T;
         constexpr bool H = decltype(with)::value;
-        if (!bwd) hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, false, false>), grid, dim3(AT), lds, s, tab, a);
-        else if (past) hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, true, true>), grid, dim3(AT), lds, s, tab, a);
-        else hipLaunchKernelGGL((adjusted_logprob_kernel<T, H, true, false>), grid, dim3(AT), lds, s, tab, a);
+        auto of = [&](auto size) {
+            constexpr int W = decltype(size)::value;
+            if (!bwd) hipLaunchKernelGGL((adjusted_logprob_kernel<T, W, H, false, false>), grid, dim3(64 * W), lds, s, tab, a);
+            else if (past) hipLaunchKernelGGL((adjusted_logprob_kernel<T, W, H, true, true>), grid, dim3(64 * W), lds, s, tab, a);
+            else hipLaunchKernelGGL((adjusted_logprob_kernel<T, W, H, true, false>), grid, dim3(64 * W), lds, s, tab, a);
+        };
+        if (waves == AWAVES) of(std::integral_constant<int, AWAVES>{}); else of(std::integral_constant<int, FEW_WAVES>{});
     });
-    if (!bwd)
+    if (!bwd && a.n_slices > 1)
         hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)((total_tokens + 3) / 4)), dim3(256), 0, s, tab, labels, parts, logp, lse,
-                           a.n_slices * AWAVES, (int)vocab, rules.inv_temperature);
+                           a.n_slices * waves, (int)vocab, rules.inv_temperature);
     return hipGetLastError();
 }
 
