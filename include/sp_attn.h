@@ -256,7 +256,7 @@ sp_status sp_attn_bwd_batched_static(const void* q, const void* k, const void* v
  *          to the backward makes D use o + o_lo.  bf16 only (SP_ERR_UNSUPPORTED with SP_F32). */
 #define SP_FLAG_RESPONSE_ROWS   1u
 #define SP_FLAG_ACCUMULATE_DKDV 2u
-#define SP_FLAG_ZERO_PROMPT_ROWS 4u        /* sp_attn_logprob_bwd_ex only */
+#define SP_FLAG_ZERO_PROMPT_ROWS 4u        /* sp_attn_logprob_bwd_ex, sp_attn_adjusted_logprob_fwd / _bwd only */
 sp_status sp_attn_fwd_batched_ex(const void* q, const void* k, const void* v, void* o, float* lse,
                                  int32_t n_groups, const int32_t* prompt_lens,
                                  const int32_t* Gs, const int32_t* resp_lens_flat,
@@ -496,7 +496,8 @@ sp_status sp_attn_adjust_logits(const void* logits, int64_t logits_stride, void*
  * Forward: logp[t] = z'[t, labels[t]] - lse[t], lse[t] = ln sum_v exp(z'[t, v]); a label outside [0, vocab) or masked, and any label of a row that
  * allows nothing, gives -inf.  Backward: dlogits[t, v] = g[t] (1[v == labels[t]] - exp(z'[t, v] - lse[t])) dz'[t, v] / dz[t, v], which is
  * 0 in masked places and throughout a row that allows nothing; bias and penalties are constants.  dlogits may be logits itself.
- * flags: SP_FLAG_OWN_TOKEN (the same in both calls), backward also SP_FLAG_ZERO_PROMPT_ROWS.  Bitwise repeatable. */
+ * flags: SP_FLAG_OWN_TOKEN (the same in both calls); SP_FLAG_ZERO_PROMPT_ROWS: prompt rows of the outputs are set to 0, else they keep what they
+ * hold.  Bitwise repeatable. */
 #define SP_FLAG_OWN_TOKEN 8u               /* sp_attn_adjusted_logprob_fwd / _bwd only */
 size_t    sp_attn_adjusted_logprob_workspace_bytes(int64_t total_tokens, int32_t n_groups, int64_t total_responses, int64_t vocab);
 sp_status sp_attn_adjusted_logprob_fwd(const void* logits, const int32_t* labels, const int32_t* tokens, float* logp, float* lse,

@@ -864,8 +864,12 @@ def sp_attn_adjusted_logprob_fwd(logits, labels, tokens, rules: LogitRules, prom
 def _adjusted_fwd(raw, logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, flags, logp, lse, workspace):
     T, V = logits.shape
     if logp is None or lse is None:
-        zeros = torch.zeros(2, T, dtype=torch.float32, device=logits.device)        # one launch for both
-        logp, lse = zeros[0] if logp is None else logp, zeros[1] if lse is None else lse
+        if logp is None and lse is None:
+            flags |= SP_FLAG_ZERO_PROMPT_ROWS
+            logp, lse = (torch.empty(T, dtype=torch.float32, device=logits.device) for _ in range(2))
+        else:
+            zeros = torch.zeros(T, dtype=torch.float32, device=logits.device)
+            logp, lse = zeros if logp is None else logp, zeros if lse is None else lse
     workspace = _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace)
     _check(load_library().sp_attn_adjusted_logprob_fwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), V,
                                                        rules._ref, *mask, len(prompt_lens), _i32(prompt_lens), _i32(Gs), _i32(resp_lens_flat),

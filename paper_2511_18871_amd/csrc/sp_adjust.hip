@@ -348,6 +348,7 @@ __global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg tab
             }
         }
         if (prompt) {
+            if (!BWD && a.zero_prompt && blockIdx.x == 0 && threadIdx.x == 0) { a.logp[t] = 0.f; a.lse[t] = 0.f; }
             if (BWD && a.zero_prompt) {
                 T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
                 const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};

@@ -823,7 +823,7 @@ sp_status adjusted_logprob(bool bwd, const void* logits, const int32_t* labels, 
                            int32_t n_groups, const int32_t* prompt_lens, const int32_t* Gs, const int32_t* resp_lens_flat, sp_dtype dtype,
                            uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
     g_err[0] = 0;
-    if (flags & ~(SP_FLAG_OWN_TOKEN | (bwd ? SP_FLAG_ZERO_PROMPT_ROWS : 0u))) return fail(SP_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+    if (flags & ~(SP_FLAG_OWN_TOKEN | SP_FLAG_ZERO_PROMPT_ROWS)) return fail(SP_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
     if (!logits || !labels || !tokens || !lse || (bwd ? !g || !dlogits : !logp)) return fail(SP_ERR_INVALID_ARG, "a pointer is NULL");
     if (misaligned(logits) || misaligned(dlogits)) return fail(SP_ERR_INVALID_ARG, "tensor pointer is not 16-byte aligned");
     if (off4(labels) || off4(tokens) || off4(lse) || off4(g) || off4(logp)) return fail(SP_ERR_INVALID_ARG, "a 32-bit array is not 4-byte aligned");

@@ -175,6 +175,7 @@ def logprob_check(pl, Gs, rl, z, tokens, labels, mask, bias, g, rules, own=False
     assert torch.all(logp.cpu()[other] == 5.0) and torch.all(lse.cpu()[other] == 6.0) and torch.all(dz.cpu()[other] == 3.0)
     assert torch.all(zeroed.cpu()[other] == 0) and torch.equal(zeroed.cpu()[resp], dz.cpu()[resp])
     assert torch.equal(again[0].cpu()[resp], logp.cpu()[resp]) and torch.equal(again[1].cpu()[resp], lse.cpu()[resp])
+    assert torch.all(again[0].cpu()[other] == 0) and torch.all(again[1].cpu()[other] == 0)
     # an adjusted element is 12 units of what went into it off; an exponential of a difference adds the argument's rounding (weights that count:
     # above e^-100) and 4 units; a sum of V terms, which 512 threads share, V / 512 + 32 units; the logarithm and its sum 4 units of lse
     z_off = 12 * U24 * size
@@ -195,6 +196,22 @@ def logprob_check(pl, Gs, rl, z, tokens, labels, mask, bias, g, rules, own=False
 def test_logprob(pack, dtype, vocab):
     pl, Gs, rl, z, tokens, labels, mask, bias, g = pack_case(pack, vocab, dtype, 11)
     logprob_check(pl, Gs, rl, z, tokens, labels, mask, bias, g, RULES["all"], in_place=True)
+
+
+def test_logprob_several_rows_to_a_workgroup():
+    """More rows than the chip takes at once, of a vocabulary that one workgroup has to itself, and prompts between them."""
+    gen = torch.Generator().manual_seed(17)
+    vocab, pl, Gs, rl = 61, [700, 1, 30], [5, 4, 9], [(97 * i) % 700 + 1 for i in range(18)]
+    T = sum(pl) + sum(rl)
+    z, tokens = 3 * torch.randn(T, vocab, generator=gen), some_tokens(gen, (T,), vocab)
+    mask = random_mask(gen, T, vocab, 0.7)
+    logprob_check(pl, Gs, rl, z, tokens, some_tokens(gen, (T,), vocab), mask, torch.randn(vocab, generator=gen), torch.randn(T, generator=gen), RULES["all"])
+
+
+@pytest.mark.parametrize("dtype,vocab", [(torch.bfloat16, 8192), (torch.float32, 8193), (torch.bfloat16, 20000), (torch.float32, 32768), (torch.bfloat16, 32769)])
+def test_logprob_either_side_of_a_workgroups_sizes(dtype, vocab):
+    pl, Gs, rl, z, tokens, labels, mask, bias, g = pack_case("ragged", vocab, dtype, 12)
+    logprob_check(pl, Gs, rl, z, tokens, labels, mask, bias, g, RULES["all"])
 
 
 @pytest.mark.parametrize("rules", list(RULES))

@@ -98,7 +98,7 @@ def test_adjusted_logprob_refuses(lib):
         assert fwd(ru=rules(**kw)) == INVALID and bwd(ru=rules(**kw)) == INVALID
     for kw in (dict(z=None), dict(z=0x1004), dict(y=None), dict(y=0x1002), dict(t=None), dict(lse=None), dict(lse=0x1002), dict(V=0), dict(mask=P, ms=3), dict(flags=1), dict(flags=16)):
         assert fwd(**kw) == INVALID and bwd(**kw) == INVALID, kw
-    for kw in (dict(logp=None), dict(ng=0), dict(resp=None), dict(resp=ints(-1)), dict(flags=B.SP_FLAG_ZERO_PROMPT_ROWS)):
+    for kw in (dict(logp=None), dict(ng=0), dict(resp=None), dict(resp=ints(-1))):
         assert fwd(**kw) == INVALID, kw
     for kw in (dict(up=None), dict(dz=None), dict(dz=0x1008)):
         assert bwd(**kw) == INVALID, kw
