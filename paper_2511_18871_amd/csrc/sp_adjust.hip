@@ -309,9 +309,9 @@ __device__ __forceinline__ void finish_row(float m, float s, float z, float inv_
 }
 
 // One workgroup per (slice, run of rows of the pack), its counters as the first row needs them; from row to row each wave adds to those of its
-// own vectors.  Bound, at 1470 response rows of 152k ids in bf16 with bias and mask: the forward (447 MB, 165 us, 2.7 TB/s) by vector
-// instructions, which fill 63 % of the cycles, half of them for the 2.6 ids of every 512 that the history holds; the backward (1.05 GB,
-// 219 us, 4.8 TB/s) by memory.  Four vectors of a row in flight per thread: with two 176 and 226 us.
+// own vectors.  Bound, at 1470 response rows of 152k ids in bf16 with bias and mask: the forward (447 MB, 163 us, 2.7 TB/s) by vector
+// instructions, 118 for eight elements of a wave's rows, eight of them exponentials and a third for the 2.6 ids of every 512 that the history holds;
+// the backward (1.05 GB, 219 us, 4.8 TB/s) by memory.  Four vectors of a row in flight per thread: with two 176 and 226 us.
 template <typename T, int WAVES, bool HIST, bool BWD, bool PAST>
 __global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg table, LogprobArgs a) {
     constexpr int THREADS = 64 * WAVES;
@@ -531,6 +531,8 @@ hipError_t launch_adjusted_logprob(bool bwd, const void* logits, const int* labe
     a.n_slices = adjust_slices(vocab);
     a.slice_len = (int)std::min<int64_t>(SLICE_MAX, (vocab + 7) / 8 * 8);
     a.own = own_token; a.zero_prompt = zero_prompt;
+    // A small vocabulary leaves eight waves little to do between a row's lookups: two, as long as a thread has no more than eight vectors (1145 rows
+    // of 5003 ids in float32: forward 10.5 us, gradient 11.9; with four waves 9.8 and 14.5, with eight 14.4 and 16.5).
     const int waves = a.slice_len > 8 * 64 * FEW_WAVES * 8 ? AWAVES : FEW_WAVES;
     // Runs: a workgroup's history is read once for its rows, and 2048 workgroups fill the chip four times over (1470 rows of 152k ids: forward
     // and backward 381 us, with half as many workgroups 429, with twice as many 380).
