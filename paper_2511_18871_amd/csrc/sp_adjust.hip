@@ -309,7 +309,7 @@ __device__ __forceinline__ void finish_row(float m, float s, float z, float inv_
 }
 
 // One workgroup per (slice, run of rows of the pack), its counters as the first row needs them; from row to row each wave adds to those of its
-// own vectors.  Bound, at 1470 response rows of 152k ids in bf16 with bias and mask: the forward (447 MB, 163 us, 2.7 TB/s) by vector
+// own vectors.  Bound, at 1470 response rows of 152k ids in bf16 with bias and mask: the forward (447 MB, 163 us, 2.7 TB/s; 483 MB with mask and bias) by vector
 // instructions, 118 for eight elements of a wave's rows, eight of them exponentials and a third for the 2.6 ids of every 512 that the history holds;
 // the backward (1.05 GB, 219 us, 4.8 TB/s) by memory.  Four vectors of a row in flight per thread: with two 176 and 226 us.
 template <typename T, int WAVES, bool HIST, bool BWD, bool PAST>

@@ -18,7 +18,7 @@
 // Measured (heads of 128, bf16, us of the kernel + of the join; bytes are those of the keys and values):
 //   32 answers of 8k to 15k tokens to 8 prompts, 32/8 heads   263 + 5     1.53 GB, 5.8 TB/s
 //   64 prompts of 64 to 192 tokens, 16 answers each, 28/4     131 + 11    0.55 GB, 4.2 TB/s; the plan of 1088 lists takes 8 of it
-//   a prompt of 16k tokens, 32 answers, 40/8                  38 + 9      90 MB; 42 MB of sums, written and read, take as long as the keys
+//   a prompt of 16k tokens, 32 answers, 40/8                  38 + 9      91 MB; 36 MB of sums, written and read, take nearly as long
 //   a prompt of 1k tokens, 8 answers, 28/4                    8 + 5       latency: launch, plan, pages, keys, sums one after the other
 //   one sequence of 1k tokens, 28/4                           6 + 6       the same
 #include "sp_common.hpp"
