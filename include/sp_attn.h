@@ -447,7 +447,8 @@ sp_status sp_attn_cache_append(const sp_kv_cache* cache, const void* q, int64_t 
  *   resp_tables   [n_seqs, resp_width] (NULL if resp_width is 0), resp_lens [n_seqs]
  *   workspace     DEVICE, at least sp_attn_decode_workspace_bytes(...) bytes, which grow with n_groups and n_seqs; it carries nothing from
  *                 call to call.
- * Deterministic: no atomics are used.  Asynchronous on `stream`; errors as sp_attn_fwd. */
+ * o may be q.  SP_ERR_INVALID_ARG also where n_seqs * n_q_heads passes 2^31 - 1, or where the tables have room for more than 2e9 units of 32 keys
+ * by 32 rows.  Deterministic: no atomics are used.  Asynchronous on `stream`; errors as sp_attn_fwd. */
 size_t    sp_attn_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads,
                                          int32_t head_dim, sp_dtype dtype);
 sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float* lse, int32_t n_q_heads,

@@ -137,6 +137,35 @@ def test_more_rows_than_the_chip_holds_waves(dtype, d):
     run_and_check(q, kc, vc, Gs, pt, prompts, rt, resp, 0.1)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_more_lists_than_a_workgroup_holds(dtype):
+    Gs = [(i * 7) % 9 for i in range(1100)]
+    n = sum(Gs)
+    assert n + len(Gs) > 4096
+    prompts, resp = [(i * 5) % 40 for i in range(1100)], [(i * 13) % 19 for i in range(n)]
+    prompts[700], resp[3000] = 600, 333
+    q, kc, vc, pt, rt = make(dtype, 64, 6, 1, 16, prompts, Gs, resp)
+    run_and_check(q, kc, vc, Gs, pt, prompts, rt, resp, 0.125)
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+def test_pages_beyond_32_bits(dtype, d):
+    """Pages whose offsets pass 2^31 elements and 2^32 bytes, beside the first ones."""
+    prompts, Gs, resp = [600], [6], [40, 300, 1, 0, 77, 513]
+    q, kc, vc, pt, rt = (x.cuda() for x in make(dtype, d, 8, 2, 64, prompts, Gs, resp))
+    want = B.sp_attn_decode(B.KvCache(kc, vc), q, Gs, pt, dev32(prompts), rt, dev32(resp), 0.1)
+    n, of_page = kc.shape[0], kc[0].numel()
+    far = (2 ** 31 + 2 ** 28) // of_page
+    big = [torch.zeros(far + n, *kc.shape[1:], dtype=dtype, device="cuda") for _ in range(2)]
+    for c, b in zip((kc, vc), big):
+        b[far:] = c
+        b[:n] = c
+    assert far * of_page > 2 ** 31 and big[0].numel() * big[0].element_size() > 2 ** 32
+    for pages, resp_pages in ((pt + far, rt + far), (pt, rt + far), (pt + far, rt)):
+        got = B.sp_attn_decode(B.KvCache(*big), q, Gs, pages.to(torch.int32), dev32(prompts), resp_pages.to(torch.int32), dev32(resp), 0.1)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_replayed_with_other_lengths_and_workspaces_shared():
     """Two captured graphs on one workspace, replayed in turn with other lengths, eager calls on it in between."""
     prompts, Gs, resp = [200, 90], [5, 3], [64] * 8
@@ -178,6 +207,8 @@ def test_on_another_stream_into_given_outputs():
     assert torch.equal(guard[1:5], want[0]) and torch.equal(lse, want[1])
     assert torch.equal(free[0], want[0]) and torch.equal(free[1], want[1])
     assert torch.all(guard[0] == 3.0) and torch.all(guard[5] == 3.0)
+    B.sp_attn_decode(cache, q, Gs, pt, pl, rt, rl, 0.1, o=q)            # in place
+    assert torch.equal(q, want[0])
 
 
 def test_reserve_of_a_forward_is_given_up():

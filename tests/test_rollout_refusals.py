@@ -54,7 +54,7 @@ def test_decode_refuses(lib):
         assert decode(lib, c=cache(**kw)) == status, kw
     for kw in (dict(q=None), dict(o=None), dict(lse=None), dict(q=0x1004), dict(o=0x1008), dict(lse=0x1002), dict(hq=3), dict(hq=0), dict(ng=0), dict(n=0), dict(n=4), dict(Gs=ints(4, -1)),
                dict(Gs=None), dict(pt=None), dict(pl=None), dict(pw=0), dict(pw=-1), dict(rt=None), dict(rw=0), dict(rl=None), dict(rl=0x1001), dict(scale=0.0), dict(scale=-1.0),
-               dict(scale=float("inf")), dict(scale=float("nan"))):
+               dict(scale=float("inf")), dict(scale=float("nan")), dict(rw=2 ** 31 - 1), dict(ng=2 ** 30, n=2 ** 30, Gs=None)):
         assert decode(lib, **kw) == INVALID, kw
     for kw in (dict(ws=None), dict(ws=0x1008), dict(bytes=0), dict(bytes=B.decode_workspace_bytes(2, 3, 4, 2, 128, B.SP_BF16) - 1)):
         assert decode(lib, **kw) == WORKSPACE, kw
