@@ -420,14 +420,16 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
     }
 }
 
-// Weights of 32 keys from their scores, rounded to bf16 as the second product needs them: a rounding of 2^-8 of the weight at most, like
-// that of o itself, and of either sign.  Their sum is of the unrounded ones.
+// Weights of 32 keys from their scores, in two parts of bf16 as the second product needs them: a weight's upper 16 bits, which is not above
+// it, and what that leaves, rounded.  Both go through the matrix instructions, and 2^-15 of the weight is lost at most, so that o is off as with unrounded weights
+// (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 50 us instead of
+// 46, while calls that wait for keys cost the same).  The second part is never 0: it would turn an infinite value into NaN.
 // They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
 // range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key, or to NaN) does the wave
 // take the rows' maxima for new references, scale what it has and take the weights again.  (With the maximum of every 32 keys, 128 rows and short runs
 // rescaled nearly every time: 110 instructions a tile instead of 30.)
 template <int D, int NC>
-__device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, bf16x8 (&p)[NC]) {
+__device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, bf16x8 (&p)[NC][2]) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         float sum;
@@ -437,7 +439,9 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
             for (int e = 0; e < 8; ++e) {
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e >> 2][e & 3], c2, -mc));
                 sum += x;
-                p[c][e] = (__bf16)x;
+                const float high = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+                p[c][0][e] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(x) >> 16));
+                p[c][1][e] = (__bf16)fmaxf(x - high, 0x1p-126f);
             }
         };
         take(r.m[c] * c2);
@@ -459,7 +463,7 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
 
 // O^T += V^T P^T over 32 keys at LDS address `v`
 template <int D, int NC>
-__device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf16x8 (&p)[NC], int l) {
+__device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf16x8 (&p)[NC][2], int l) {
     const unsigned at = v + kv_off<D>(4 * (l >> 4) + ((l & 15) >> 2), (l & 3) >> 1) + ((l & 1) << 3);
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
@@ -470,7 +474,8 @@ __device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf1
         const bf16x8 a = cat4(half[0], half[1]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            r.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[c], r.o[c][dt], 0, 0, 0);
+#pragma unroll
+            for (int part = 1; part >= 0; --part) r.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[c][part], r.o[c][dt], 0, 0, 0);
         }
     }
 }
@@ -654,7 +659,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(SeqArg starts, DecodeArg
             while (same) {
                 const unsigned bits = low_bits(valid[0]) | low_bits(valid[1]) << 16;
                 f32x4 s[NS][2];
-                bf16x8 pw[NS];
+                bf16x8 pw[NS][2];
                 wait_copies<N>();
                 scores(r, kb, bits, l, s);
                 wait_lds();
@@ -717,7 +722,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(SeqArg starts, DecodeArg
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     f32x4 s[NC][2];
-                    bf16x8 pw[NC];
+                    bf16x8 pw[NC][2];
                     scores(r, kb + 2 * h * KEYS16, h ? here[1] : here[0], l, s);
                     weights(r, s, a.c, pw);
                     add_values(r, vb + 2 * h * KEYS16, pw, l);
