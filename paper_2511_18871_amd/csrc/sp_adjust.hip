@@ -326,7 +326,7 @@ __global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg tab
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const float c = a.rules.inv_temperature * LOG2E;
     if (!BWD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) a.tag[threadIdx.x] = 0u;
-    int seg_end = t0, counted = 0;
+    int seg_end = t0, counted = 0, place = 0;
     bool prompt = false, may_saturate = false;
     for (int t = t0; t < t1; ++t) {
         if (t == seg_end) {                              // another segment: its prompt, its history up to this row
@@ -414,8 +414,10 @@ __global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg tab
             });
             scaled_wave(m, sum, c);
             if (a.n_slices == 1) {
-                // The workgroup has all of the row: no join.  (Two places in turn: who writes the next but one has met the reader in between.)
-                float* const mine = row_parts[t & 1];
+                // The workgroup has all of the row: no join.  (Two places in turn, from response row to response row, whatever lies between them: who
+                // writes the next but one has met the reader at the barrier of the next.)
+                float* const mine = row_parts[place];
+                place ^= 1;
                 if (lane == 0) { mine[2 * wave] = m; mine[2 * wave + 1] = sum; }
                 if ((int)threadIdx.x == (label_at < 0 ? 0 : (label_at >> 3) % THREADS)) mine[2 * WAVES] = z_label;
                 __syncthreads();
