@@ -427,24 +427,25 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
 // They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
 // range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key, or to NaN) does the wave
 // take the rows' maxima for new references, scale what it has and take the weights again.  (With the maximum of every 32 keys, 128 rows and short runs
-// rescaled nearly every time: 110 instructions a tile instead of 30.)
+// rescaled nearly every time: 110 instructions a tile instead of 30.)  Differences are taken ahead of their scaling, so that they are exact at any
+// magnitude: of a scaled reference the rounding alone passes the exponential's range for scores above 2^30, and the chunks of a row differ in it.
 template <int D, int NC>
 __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2], float c2, bf16x8 (&p)[NC][2]) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         float sum;
-        auto take = [&](float mc) SP_INLINE {
+        auto take = [&](float m) SP_INLINE {
             sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e >> 2][e & 3], c2, -mc));
+                const float x = __builtin_amdgcn_exp2f((s[c][e >> 2][e & 3] - m) * c2);
                 sum += x;
                 const float high = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
                 p[c][0][e] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(x) >> 16));
                 p[c][1][e] = (__bf16)fmaxf(x - high, 0x1p-126f);
             }
         };
-        take(r.m[c] * c2);
+        take(r.m[c]);
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= 16384.f)) != 0, 0)) {
             float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])), fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3])));
             mx = quad_max(mx);
@@ -455,7 +456,7 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r.o[c][dt][i] *= alpha;
             r.m[c] = mn;
-            take(mn * c2);
+            take(mn);
         }
         r.l[c] += sum;
     }
