@@ -425,8 +425,9 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
 // (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 50 us instead of
 // 46, while calls that wait for keys cost the same).  The second part is never 0: it would turn an infinite value into NaN.
 // They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
-// range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key, or to NaN) does the wave
-// take the rows' maxima for new references, scale what it has and take the weights again.  (With the maximum of every 32 keys, 128 rows and short runs
+// range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key) does the wave
+// take the rows' maxima for new references, scale what it has and take the weights again.  A NaN among the scores stays in the row's sum, whichever way the
+// compiler took the comparison, and a score of +inf becomes one, as it would in a softmax of the whole row.  (With the maximum of every 32 keys, 128 rows and short runs
 // rescaled nearly every time: 110 instructions a tile instead of 30.)  Differences are taken ahead of their scaling, so that they are exact at any
 // magnitude: of a scaled reference the rounding alone passes the exponential's range for scores above 2^30, and the chunks of a row differ in it.
 template <int D, int NC>
@@ -904,7 +905,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
         f32x4 x[DEPTH];
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) {
-            const int k = min(i + u * AT_ONCE + mine, n - 1);              // behind the last: again, with no weight
+            const int k = min(i + u * AT_ONCE + mine, n - 1);              // behind the last: again, and not counted
             const unsigned at_k = k < n_p ? at_p + k * stride_p : at_r + (k - n_p) * stride_r;
             st[u] = *reinterpret_cast<const f32x2*>(a.stats + (uint64_t)at_k * 2);
             x[u] = *reinterpret_cast<const f32x4*>(a.sums + (uint64_t)at_k * D + e0);
@@ -919,7 +920,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
         for (int e = 0; e < 4; ++e) acc[e] *= alpha;
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) {
-            const float wt = i + u * AT_ONCE + mine < n ? __builtin_amdgcn_exp2f((st[u][0] - mn) * a.c) : 0.f;
+            if (i + u * AT_ONCE + mine >= n) continue;                     // (not with a weight of 0: sums may be infinite)
+            const float wt = __builtin_amdgcn_exp2f((st[u][0] - mn) * a.c);
             L += wt * st[u][1];
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += wt * x[u][e];
@@ -933,15 +935,17 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = acc[e] * wt + __shfl_xor(acc[e], o, 64) * wt2;
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    // Without a key L is 0, and a NaN among the scores is in L: by its bits, as the compiler may take a comparison for either where there is a NaN.
+    const bool none = (__float_as_uint(L) << 1) == 0;
+    const float inv = 1.f / L;
     if (mine == 0) {
         typedef T out4 __attribute__((ext_vector_type(4)));
         out4 y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (T)(L > 0.f ? acc[e] * inv : 0.f);
+        for (int e = 0; e < 4; ++e) y[e] = (T)(none ? 0.f : acc[e] * inv);
         *reinterpret_cast<out4*>((T*)a.o + item * D + e0) = y;
     }
-    if (l == 0) a.lse[(int64_t)h * a.n_seqs + seq] = L > 0.f ? M * (a.c * LN2) + __logf(L) : -INFINITY;
+    if (l == 0) a.lse[(int64_t)h * a.n_seqs + seq] = none ? -INFINITY : M * (a.c * LN2) + __logf(L);
 }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
