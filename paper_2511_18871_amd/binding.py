@@ -590,6 +590,13 @@ def _need(name, t, dtype, shape, index):
                 f"expected {dtype} {tuple(shape)} on {'the host' if index < 0 else f'cuda:{index}'}, contiguous")
 
 
+def _room(workspace, index):
+    """Refuses a workspace whose bytes a kernel would not find behind its pointer."""
+    if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
+        _refuse(f"workspace: {tuple(workspace.shape)} on {workspace.device}{'' if workspace.is_contiguous() else ', not contiguous'}; "
+                f"expected contiguous memory on {'the host' if index < 0 else f'cuda:{index}'}")
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
@@ -744,6 +751,7 @@ def sp_attn_decode(cache: KvCache, q, Gs: Optional[Sequence[int]], prompt_tables
         _need("o", o, cache.dtype, (n_seqs, hq, d), index)
     if lse is not None:
         _need("lse", lse, torch.float32, (hq, n_seqs), index)
+    _room(workspace, index)
     return _decode(index, stream, cache, q, o, lse, hq, n_groups, n_seqs, Gs, prompt, resp, softmax_scale, workspace)
 
 
@@ -760,7 +768,7 @@ def _decode(raw, cache, q, o, lse, hq, n_groups, n_seqs, Gs, prompt, resp, softm
     pt, pw, pl = prompt
     rt, rw, rl = resp
     _check(lib.sp_attn_decode(cache._ref, q.data_ptr(), o.data_ptr(), lse.data_ptr(), hq, n_groups, n_seqs, None if Gs is None else _i32(Gs),
-                              pt, pw, pl if pw else None, rt, rw, rl, softmax_scale, workspace.data_ptr(), workspace.numel(), raw))
+                              pt, pw, pl if pw else None, rt, rw, rl, softmax_scale, workspace.data_ptr(), workspace.nbytes, raw))
     return o, lse
 
 
@@ -822,8 +830,10 @@ def _adjust(raw, logits, stride, out, out_stride, rules, mask, n_groups, n_seqs,
     return out
 
 
-def _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, mask):
+def _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace):
     """What the forward and the backward check alike; returns the device's index and the mask's pointer and stride."""
+    if len(Gs) != len(prompt_lens) or sum(Gs) != len(resp_lens_flat) or min(Gs, default=0) < 0:      # the library takes no lengths of these lists
+        _refuse(f"{len(prompt_lens)} prompts, groups of {list(Gs)} responses and {len(resp_lens_flat)} lengths of responses do not fit")
     index = logits.get_device()
     T, V = logits.shape
     _need("logits", logits, logits.dtype, (T, V), index)
@@ -832,6 +842,7 @@ def _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, m
     _need("labels", labels, torch.int32, (T,), index)
     _need("tokens", tokens, torch.int32, (T,), index)
     rules._fits(V, index)
+    _room(workspace, index)
     return index, _mask_rows(mask, T, index)
 
 
@@ -853,7 +864,7 @@ def sp_attn_adjusted_logprob_fwd(logits, labels, tokens, rules: LogitRules, prom
     """Log-probability of labels[t] under the adjusted distribution at every response row t of logits [T, V]; tokens [T] are the pack's ids.
     mask [T, words] as in sp_attn_adjust_logits.  Returns (logp, lse); prompt rows keep whatever the output tensors held (zeros when
     allocated here)."""
-    index, rows = _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, mask)
+    index, rows = _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace)
     for name, t in (("logp", logp), ("lse", lse)):
         if t is not None:
             _need(name, t, torch.float32, (logits.shape[0],), index)
@@ -873,7 +884,7 @@ def _adjusted_fwd(raw, logits, labels, tokens, rules, prompt_lens, Gs, resp_lens
     workspace = _adjusted_workspace(logits, prompt_lens, resp_lens_flat, workspace)
     _check(load_library().sp_attn_adjusted_logprob_fwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), V,
                                                        rules._ref, *mask, len(prompt_lens), _i32(prompt_lens), _i32(Gs), _i32(resp_lens_flat),
-                                                       _dtype_code(logits), flags, workspace.data_ptr(), workspace.numel(), raw))
+                                                       _dtype_code(logits), flags, workspace.data_ptr(), workspace.nbytes, raw))
     return logp, lse
 
 
@@ -881,7 +892,7 @@ def sp_attn_adjusted_logprob_bwd(logits, labels, tokens, lse, g, rules: LogitRul
                                  resp_lens_flat: Sequence[int], mask=None, flags: int = 0, dlogits=None, workspace=None, stream=None):
     """Gradient with respect to the raw logits of sum_t g[t] logp[t], logp of sp_attn_adjusted_logprob_fwd.  Prompt rows of dlogits are zero
     when it is allocated here, otherwise they keep what they held (SP_FLAG_ZERO_PROMPT_ROWS: zero).  ``dlogits`` may be logits itself."""
-    index, rows = _adjusted_args(logits, labels, tokens, rules, prompt_lens, resp_lens_flat, mask)
+    index, rows = _adjusted_args(logits, labels, tokens, rules, prompt_lens, Gs, resp_lens_flat, mask, workspace)
     T, V = logits.shape
     _need("lse", lse, torch.float32, (T,), index)
     _need("g", g, torch.float32, (T,), index)
@@ -900,5 +911,5 @@ def _adjusted_bwd(raw, logits, labels, tokens, lse, g, rules, prompt_lens, Gs, r
     _check(load_library().sp_attn_adjusted_logprob_bwd(logits.data_ptr(), labels.data_ptr(), tokens.data_ptr(), lse.data_ptr(), g.data_ptr(),
                                                        dlogits.data_ptr(), logits.shape[1], rules._ref, *mask, len(prompt_lens), _i32(prompt_lens),
                                                        _i32(Gs), _i32(resp_lens_flat), _dtype_code(logits), flags, workspace.data_ptr(),
-                                                       workspace.numel(), raw))
+                                                       workspace.nbytes, raw))
     return dlogits
