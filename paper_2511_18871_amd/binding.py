@@ -619,7 +619,8 @@ def _placed(f):
 
 
 class KvCache:
-    """A paged cache: k and v [n_pages, n_kv_heads, page_size, head_dim], contiguous, bf16 or float32."""
+    """A paged cache: k and v [n_pages, n_kv_heads, page_size, head_dim], contiguous, bf16 or float32.  A call takes the memory that they have
+    then; their shape and type stay those of the construction."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         if k.dim() != 4:
@@ -631,8 +632,19 @@ class KvCache:
         self.dtype, self.device = k.dtype, k.device
         n_pages, self.n_kv_heads, page_size, self.head_dim = k.shape
         self.code = _dtype_code(k)
+        self._shape = k.shape
         self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), n_pages, page_size, self.n_kv_heads, self.head_dim, self.code)
-        self._ref = ctypes.pointer(self._struct)
+        self._pointer = ctypes.pointer(self._struct)
+
+    @property
+    def _ref(self):
+        k, v, struct = self.k, self.v, self._struct
+        at_k, at_v = k.data_ptr(), v.data_ptr()
+        if at_k != struct.k or at_v != struct.v or k.shape != self._shape or v.shape != self._shape:       # another storage
+            _need("k", k, self.dtype, self._shape, self.index)
+            _need("v", v, self.dtype, self._shape, self.index)
+            struct.k, struct.v = at_k, at_v
+        return self._pointer
 
 
 class LogitRules:
@@ -650,6 +662,7 @@ class LogitRules:
     def _fits(self, vocab, index):
         if self.bias is not None:
             _need("bias", self.bias, torch.float32, (vocab,), index)
+        self._struct.bias = _ptr(self.bias)            # where it lies now
 
 
 def _ptr(t):
