@@ -720,12 +720,13 @@ def _append(raw, cache, q, qs, q_out, hq, k, ks, k_out, v, vs, n_seqs, new_lens,
         q_out = torch.empty(k.shape[0], hq, cache.head_dim, dtype=cache.dtype, device=cache.device)
     if lens_out is None:
         lens_out = torch.empty_like(lens)
-    if k.shape[0] == 0:                    # nothing to store; the pointers of empty tensors are null
-        lens_out.copy_(lens)
+    if n_seqs == 0:
         return q_out, lens_out
-    _check(load_library().sp_attn_cache_append(cache._ref, _ptr(q), qs, _ptr(q_out), hq, k.data_ptr(), ks, _ptr(k_out), v.data_ptr(), vs, n_seqs,
-                                               None if new_lens is None else _i32(new_lens), tables.data_ptr(), tables.shape[1], lens.data_ptr(),
-                                               _ptr(pos_base), lens_out.data_ptr(), rope_base, raw))
+    at = (_ptr(q), qs, _ptr(q_out), hq, k.data_ptr(), ks, _ptr(k_out), v.data_ptr(), vs)
+    if k.shape[0] == 0:                    # the pointers of empty tensors are null, and no token is read or written
+        at = (None, 0, None, 0, cache.k.data_ptr(), ks, None, cache.v.data_ptr(), vs)
+    _check(load_library().sp_attn_cache_append(cache._ref, *at, n_seqs, None if new_lens is None else _i32(new_lens), tables.data_ptr(),
+                                               tables.shape[1], lens.data_ptr(), _ptr(pos_base), lens_out.data_ptr(), rope_base, raw))
     return q_out, lens_out
 
 
