@@ -427,8 +427,8 @@ typedef struct {
  *   new_lens      HOST array of n_seqs entries >= 0, or NULL: one token each
  *   tables        [n_seqs, table_width];  lens [n_seqs] tokens in the cache before the call
  *   pos_base      [n_seqs] or NULL (0): a response's is its prompt's length, a prompt's 0
- *   lens_out      [n_seqs] or NULL: lens + new_lens, at most table_width * page_size (tokens beyond are not stored).  Not lens
- *                 itself, which the call reads meanwhile.
+ *   lens_out      [n_seqs] or NULL: lens + new_lens, but no more than table_width * page_size (tokens beyond are not stored; a length
+ *                 that is beyond already stays).  It overlaps none of lens, pos_base and tables, which the call reads meanwhile.
  * Of a sequence with a negative length nothing is read or written (lens_out: its length).  Two tokens of one call must not
  * fall on one row of a page: such a row's contents would be either's, or parts of both.  Needs no workspace.  Asynchronous on `stream`; errors as
  * sp_attn_fwd (SP_ERR_INVALID_ARG also for rope_base <= 1 or a stride that is too small). */

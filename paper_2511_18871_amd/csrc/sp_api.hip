@@ -715,7 +715,10 @@ sp_status sp_attn_cache_append(const sp_kv_cache* cache, const void* q, int64_t 
     if (n_seqs < 1 || table_width < 1) return fail(SP_ERR_INVALID_ARG, "n_seqs=%d, table_width=%d", n_seqs, table_width);
     if (!tables || !lens) return fail(SP_ERR_INVALID_ARG, "tables / lens is NULL");
     if (off4(tables) || off4(lens) || off4(pos_base) || off4(lens_out)) return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
-    if (lens_out == lens) return fail(SP_ERR_INVALID_ARG, "lens_out must not be lens");
+    // (they are read while lens_out is written)
+    auto meets_out = [&](const int32_t* p, int64_t n) { return p && lens_out && p < lens_out + n_seqs && lens_out < p + n; };
+    if (meets_out(lens, n_seqs) || meets_out(pos_base, n_seqs) || meets_out(tables, (int64_t)n_seqs * table_width))
+        return fail(SP_ERR_INVALID_ARG, "lens_out must not overlap lens, pos_base or tables");
     if (!(rope_base > 1.0) || !std::isfinite(rope_base)) return fail(SP_ERR_INVALID_ARG, "rope_base must be finite and > 1");
     int64_t total = 0;
     for (int s = 0; new_lens && s < n_seqs; ++s) {
