@@ -403,8 +403,8 @@ sp_status sp_attn_grpo_loss(const float* logp, const float* logp_old, const floa
  * Cache: k and v [n_pages, n_kv_heads, page_size, head_dim] each.  A sequence's token j lies in page table[j / page_size], row
  * j % page_size.  Tables, lengths and position bases are DEVICE int32 arrays, read when the kernels run, so that a captured
  * graph of a step is replayed with other lengths.  They are checked there: a page index outside [0, n_pages) is never
- * followed (a token that it would receive is not stored, keys on it are not attended to), lengths are cut to what the table holds, and a
- * negative length marks a sequence that takes no part. */
+ * followed (a token that it would receive is not stored, keys on it are not attended to), lengths are cut to what the table holds (2^31 - 64
+ * tokens of it at most), and a negative length marks a sequence that takes no part. */
 typedef struct {
     void* k;                  /* DEVICE, 16-byte aligned */
     void* v;

@@ -22,7 +22,7 @@ struct AppendArgs {
     const void* q; const void* k; const void* v; void* q_out; void* k_out; void* k_cache; void* v_cache;
     int64_t q_stride, k_stride, v_stride;     // elements from token to token
     const int* tables; const int* lens; const int* pos_base; int* lens_out;
-    int64_t width, capacity;                  // pages of a sequence's table, tokens that they hold
+    int64_t width, capacity;                  // pages of a sequence's table, tokens that they hold (at most MAX_TOKENS)
     int64_t n_pages;
     int first_seq, n_seqs, one_each, Hq, Hkv, log_page;
     int64_t first_token, n_tokens;            // of the launch
@@ -147,7 +147,7 @@ hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, 
     a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_out = k_out; a.k_cache = cache.k; a.v_cache = cache.v;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
     a.tables = tables; a.lens = lens; a.pos_base = pos_base; a.lens_out = lens_out;
-    a.width = width; a.log_page = cache.log_page; a.capacity = (int64_t)width << cache.log_page; a.n_pages = cache.n_pages;
+    a.width = width; a.log_page = cache.log_page; a.capacity = std::min<int64_t>((int64_t)width << cache.log_page, MAX_TOKENS); a.n_pages = cache.n_pages;
     a.one_each = !new_lens; a.Hq = Hq; a.Hkv = cache.n_kv_heads;
     // a launch's token counts are a kernel argument: more sequences than it holds are several launches
     constexpr int MAX_SEQS = SEQ_WORDS - 1;

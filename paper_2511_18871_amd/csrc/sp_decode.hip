@@ -42,7 +42,7 @@ struct DecodeArgs {
     const char* k_cache; const char* v_cache;
     const int* prompt_tables; const int* prompt_lens; const int* resp_tables; const int* resp_lens;
     int64_t prompt_width, resp_width;
-    int prompt_cap, resp_cap;              // tokens that a table holds (at most 2^31 - 1)
+    int prompt_cap, resp_cap;              // tokens that a table holds (at most MAX_TOKENS)
     int members;                           // sequences of each group, 0: of several sizes
     int n_pages, n_groups, n_seqs, Hq, Hkv, rep, log_page;
     int nc;                                // row tiles per wave of a shared segment
@@ -1030,8 +1030,8 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
     a.q_heads = make_div(Hq);
     a.heads_each = make_div(a.rep);
     a.block_rows = make_div(64 * a.nc);
-    a.prompt_cap = (int)std::min<int64_t>((int64_t)prompt_width << a.log_page, 0x7fffffff);
-    a.resp_cap = (int)std::min<int64_t>((int64_t)resp_width << a.log_page, 0x7fffffff);
+    a.prompt_cap = (int)std::min<int64_t>((int64_t)prompt_width << a.log_page, MAX_TOKENS);
+    a.resp_cap = (int)std::min<int64_t>((int64_t)resp_width << a.log_page, MAX_TOKENS);
     a.members = Gs ? Gs[0] : 1;
     for (int g = 1; Gs && g < n_groups; ++g) if (Gs[g] != Gs[0]) a.members = 0;
     a.group_size = make_div(std::max(1, a.members));

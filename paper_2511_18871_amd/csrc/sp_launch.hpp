@@ -364,7 +364,9 @@ __device__ __forceinline__ const int* words_of(const SeqArg& t) {
     return (const int*)(const __attribute__((address_space(4))) int*)at;
 }
 
-// Paged cache of the rollout calls (sp_kv_cache, its page size as a power of two)
+// Paged cache of the rollout calls (sp_kv_cache, its page size as a power of two).  A sequence has at most MAX_TOKENS, so that the end of a unit of 64 keys
+// is an int32 as well, whatever its table holds.
+constexpr int64_t MAX_TOKENS = 0x7fffffff - 63;
 struct KvCache { void* k; void* v; int64_t n_pages; int log_page, n_kv_heads, head_dim; bool f32; };
 hipError_t launch_append(const KvCache& cache, const void* q, int64_t q_stride, void* q_out, int Hq, const void* k, int64_t k_stride,
                          void* k_out, const void* v, int64_t v_stride, int n_seqs, const int32_t* new_lens, const int* tables, int width,
