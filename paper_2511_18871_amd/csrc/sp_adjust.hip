@@ -304,14 +304,14 @@ __device__ __forceinline__ void scaled_wave(float& m, float& s, float c) {
 }
 __device__ __forceinline__ float log_of(float m, float s, float inv_t) { return m * inv_t + __logf(s); }
 // A row's results from its (m, s) and the label's z' (-inf: no id of the vocabulary).  No id allowed: L = -inf, and the log-probability of any
-// label is -inf.  Where L's own rounding is large (rows of, say, -1e9 throughout: 64 and more) z' - L may come out above 0, which it is not: cut there, by
-// bits, as the compiler may take a comparison for either where there is a NaN.
+// label is -inf.  Where L's own rounding is large (rows of, say, -1e9 throughout: 64 and more) z' - L may come out above 0, which it is not: cut there.
+// A NaN in the row is in L and stays.
 __device__ __forceinline__ void finish_row(float m, float s, float z, float inv_t, float* logp, float* lse) {
     const float L = log_of(m, s, inv_t);
     *lse = L;
     const float d = z - L;
-    const int bits = (int)__float_as_uint(d);
-    *logp = __float_as_uint(L) == 0xff800000u ? -INFINITY : bits > 0 && bits <= 0x7f800000 ? 0.f : d;
+    const int bits = (int)bits_of(d);
+    *logp = bits_of(L) == 0xff800000u ? -INFINITY : bits > 0 && bits <= 0x7f800000 ? 0.f : d;
 }
 
 // One workgroup per (slice, run of rows of the pack), its counters as the first row needs them; from row to row each wave adds to those of its
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg tab
             T* const out = (T*)a.dlogits + (int64_t)t * a.vocab + s.v0;
             // (an L that is no number, or +inf, is the slope of the whole row, so that it ends as NaN)
             const float L = a.lse[t];
-            const unsigned of_L = __float_as_uint(L);
+            const unsigned of_L = bits_of(L);
             const bool none = of_L == 0xff800000u;
             const float Lf = none ? 0.f : L, gt = none ? 0.f : (of_L & 0x7f800000u) == 0x7f800000u ? L : -a.g[t] * a.rules.inv_temperature;
             for_vectors<T, THREADS, HIST, PAST, 4>(row, mask, a.rules, s, [&](float (&x)[8], i32x4 cnt, unsigned bits, int at, int n) __attribute__((always_inline)) {

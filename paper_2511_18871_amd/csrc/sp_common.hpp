@@ -315,6 +315,13 @@ __device__ __forceinline__ float pair_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The bits of x, for tests that have to know NaN: the compiler, told that there is none, turns others back into comparisons and takes these either way.
+__device__ __forceinline__ unsigned bits_of(float x) {
+    unsigned b = __float_as_uint(x);
+    asm("" : "+v"(b));
+    return b;
+}
+
 // maximum and sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48, and over all lanes of a wave; in every lane
 template <int CTRL> __device__ __forceinline__ float rotated16(float x) {
     return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));

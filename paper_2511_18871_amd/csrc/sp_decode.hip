@@ -935,8 +935,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(SeqArg starts, DecodeA
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = acc[e] * wt + __shfl_xor(acc[e], o, 64) * wt2;
     }
-    // Without a key L is 0, and a NaN among the scores is in L: by its bits, as the compiler may take a comparison for either where there is a NaN.
-    const bool none = (__float_as_uint(L) << 1) == 0;
+    // Without a key L is 0, and a NaN among the scores is in L
+    const bool none = bits_of(L) == 0;
     const float inv = 1.f / L;
     if (mine == 0) {
         typedef T out4 __attribute__((ext_vector_type(4)));

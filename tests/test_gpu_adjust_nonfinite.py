@@ -1,0 +1,58 @@
+"""NaN and infinities in what an adjusted log-probability does depend on, and in what it does not."""
+import pytest
+import torch
+
+from paper_2511_18871_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+CASES = [pytest.mark.parametrize("rules", [(1.3, 0.4, 0.25, 0.7), (1.0, 0.0, 0.0, 1.0)]), pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32]),
+         pytest.mark.parametrize("vocab", [100, 8201, 40000])]
+
+
+def cases(f):
+    for mark in CASES:
+        f = mark(f)
+    return f
+
+
+def make(dtype, vocab, rules):
+    """A pack of 13 response rows from 3 on, of which 12 has its label masked; allowed places, and what calls forward and backward."""
+    T, gen = 16, torch.Generator().manual_seed(vocab)
+    z = (3 * torch.randn(T, vocab, generator=gen)).to(dtype)
+    tokens, labels = (torch.randint(0, vocab, (T,), generator=gen, dtype=torch.int32) for _ in range(2))
+    allowed = torch.rand(T, (vocab + 31) // 32 * 32, generator=gen) < 0.7
+    allowed[torch.arange(T), labels.long()] = True
+    allowed[7:12, vocab - 1], allowed[12, labels[12]] = True, False
+    words = (allowed.view(T, -1, 32).long() * (1 << torch.arange(32))).sum(2).to(torch.int32).cuda()
+    r, pack = B.LogitRules(*rules), ([3], [2], [8, 5])
+
+    def forward(z):
+        return B.sp_attn_adjusted_logprob_fwd(z.cuda(), labels.cuda(), tokens.cuda(), r, *pack, mask=words)
+
+    def backward(z, g):
+        lse = forward(z)[1]
+        return B.sp_attn_adjusted_logprob_bwd(z.cuda(), labels.cuda(), tokens.cuda(), lse, g.cuda(), r, *pack, mask=words).float().cpu()
+    return z, labels, allowed[:, :vocab], torch.randn(T, generator=gen), forward, backward
+
+
+def spoil(z, allowed):
+    z[3][~allowed[3]] = float("nan")                     # does not matter
+    z[4][~allowed[4]] = float("inf")
+    z[5][~allowed[5]] = torch.finfo(z.dtype).min
+    z[7, -1] = float("nan")                              # does
+    z[8, -1] = float("inf")
+
+
+@cases
+def test_forward(dtype, vocab, rules):
+    """Such a row's results are NaN, not those of a row that allows nothing; the other rows do not change."""
+    z, _, allowed, _, forward, _ = make(dtype, vocab, rules)
+    clean = [x.cpu() for x in forward(z)]
+    assert torch.isfinite(clean[0][3:12]).all() and clean[0][12] == -float("inf") and torch.isfinite(clean[1]).all()
+    spoil(z, allowed)
+    bad = torch.zeros(16, dtype=torch.bool)
+    bad[7:9] = True
+    for got, want in zip(forward(z), clean):
+        assert got[bad].isnan().all() and torch.equal(got.cpu()[~bad], want[~bad])
