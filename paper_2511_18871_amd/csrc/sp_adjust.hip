@@ -385,13 +385,18 @@ __global__ __launch_bounds__(64 * WAVES) void adjusted_logprob_kernel(TabArg tab
                 float slope[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) slope[e] = gt;
-                adjust8<true, HIST>(x, slope, a.rules, cnt, mask != nullptr, bits);
+                adjust8<true, HIST>(x, slope, a.rules, cnt, false, bits);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    x[e] = slope[e] * __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.rules.inv_temperature, -Lf) * LOG2E), 0.f, 1.f);      // (see finish_row)
+                    x[e] = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.rules.inv_temperature, -Lf) * LOG2E), 0.f, 1.f);      // (see finish_row)
                 if (at == label_at)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) if (e == (int)(label & 7) && (bits >> e & 1)) x[e] -= slope[e];
+                    for (int e = 0; e < 8; ++e) if (e == (int)(label & 7)) x[e] -= 1.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= slope[e];
+                if (mask)                                // 0 in masked places whatever the row's g and logits are
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) & (unsigned)__builtin_amdgcn_sbfe((int)bits, e, 1));
                 store8<PAST>(out + at, x, n);
             });
         } else {

@@ -56,3 +56,21 @@ def test_forward(dtype, vocab, rules):
     bad[7:9] = True
     for got, want in zip(forward(z), clean):
         assert got[bad].isnan().all() and torch.equal(got.cpu()[~bad], want[~bad])
+
+
+@cases
+def test_backward(dtype, vocab, rules):
+    """NaN in every allowed place of such rows, 0 in the masked places of all, whatever g is."""
+    z, labels, allowed, g, _, backward = make(dtype, vocab, rules)
+    clean = backward(z, g)
+    assert torch.isfinite(clean).all() and (clean[~allowed] == 0).all()
+    spoil(z, allowed)
+    g[9], g[10] = float("nan"), float("inf")             # gradients that are none
+    dz = backward(z, g)
+    assert (dz[~allowed] == 0).all()
+    for t in (7, 8, 9):
+        assert dz[t][allowed[t]].isnan().all(), t
+    # an infinite g: +inf at the label, -inf where a weight is positive, NaN where it is 0
+    assert dz[10, labels[10]] == float("inf") and not torch.isfinite(dz[10][allowed[10]]).any()
+    keep = torch.tensor([t not in (7, 8, 9, 10) for t in range(16)])
+    assert torch.equal(dz[keep], clean[keep])
