@@ -482,9 +482,10 @@ __device__ __forceinline__ void add_values(Rows<D, NC>& r, unsigned v, const bf1
     }
 }
 
-// Pages of a list's keys: a lane holds one of 64 page numbers, from page `first` on; `bad`: some of them are none of the cache's
+// Pages of a list's keys, `count` of its table: a lane holds one of 64 page numbers, from page `first` on; `bad`: some of them are none of the cache's
+// (what the table holds behind the list's last page is padding and does not matter)
 struct Pages {
-    const int* table; int width, n_pages, first, held, lane; bool bad;
+    const int* table; int count, n_pages, first, held, lane; bool bad;
     __device__ __forceinline__ int at(int page) {
         need(page);
         return __builtin_amdgcn_readlane(held, page - first);
@@ -492,10 +493,13 @@ struct Pages {
     __device__ __forceinline__ void need(int page) { if ((unsigned)(page - first) >= 64u) load(page); }
     __device__ __forceinline__ void load(int page) {
         first = page;
-        held = page + lane < width ? table[page + lane] : -1;
-        bad = __builtin_amdgcn_ballot_w64((unsigned)held >= (unsigned)n_pages) != 0;
+        const bool used = page + lane < count;
+        held = used ? table[page + lane] : -1;
+        bad = __builtin_amdgcn_ballot_w64(used && (unsigned)held >= (unsigned)n_pages) != 0;
     }
 };
+
+__device__ __forceinline__ int pages_of(int len, int log_page) { return (int)(((unsigned)len + (1u << log_page) - 1) >> log_page); }
 
 __device__ __forceinline__ uint64_t uniform64(uint64_t x) {
     return ((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)x);
@@ -591,7 +595,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(SeqArg starts, DecodeArg
     auto table_of_list = [&]() SP_INLINE {
         const bool prompt = at.list < a.n_groups;
         pages.table = prompt ? a.prompt_tables + at.list * a.prompt_width : a.resp_tables + (at.list - a.n_groups) * a.resp_width;
-        pages.width = (int)(prompt ? a.prompt_width : a.resp_width);
+        pages.count = pages_of(at.len, a.log_page);
     };
     auto next = [&]() SP_INLINE {
         const int list = at.list;
@@ -755,11 +759,12 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(SeqArg starts, Decod
     Cursor<0> at(ls, work);
     Pages pages;
     pages.lane = l;
+    pages.n_pages = a.n_pages;
     while (true) {
         SegmentRows seg(at, a, work.worker);
         const bool prompt = at.list < a.n_groups;
         pages.table = prompt ? a.prompt_tables + at.list * a.prompt_width : a.resp_tables + (at.list - a.n_groups) * a.resp_width;
-        pages.width = (int)(prompt ? a.prompt_width : a.resp_width);
+        pages.count = pages_of(at.len, a.log_page);
         const int run = min(work.left, at.units - at.t), key0 = 32 * at.t, key1 = (int)min((unsigned)at.len, 32u * (unsigned)(at.t + run));
         pages.load(key0 >> a.log_page);
         const int tiles = (seg.rows + 15) >> 4;
