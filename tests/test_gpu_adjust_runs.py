@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import rollout_oracle as ro
 from paper_2511_18871_amd import binding as B
 from tests.rollout import HALF_STEP, U24, check, numpy64
 
@@ -58,3 +59,72 @@ def test_rows_without_rules_between_short_prompts(dtype, vocab):
     rel = (tol + 12 * U24 * size + 130 * U24)[:, None]
     half = HALF_STEP[dtype] if dtype == torch.bfloat16 else U24
     check("dlogits", numpy64(dz)[rows], grad * scale, np.abs(scale) * (np.exp(want - L) * rel + np.abs(grad) * (half + 4 * U24)) + 1e-37)
+
+
+def history_and_oracle(t, z, tokens, prompts, Gs, resp, rules, bias, allowed):
+    """(z', its slope, magnitudes) of response row t."""
+    at, r = 0, 0
+    for p, members in zip(prompts, Gs):
+        start = at + p
+        for n in resp[r:r + members]:
+            if start <= t < start + n:
+                return ro.adjust_row(numpy64(z[t]), tokens[at:at + p].tolist(), tokens[start:t].tolist(), rules, bias, allowed)
+            start += n
+        at, r = start, r + members
+    raise AssertionError("not a response row")
+
+
+# one slice of eight waves; three, four and five slices; gradients above and below what is stored past the caches
+@pytest.mark.parametrize("dtype,vocab,groups", [(torch.bfloat16, 8201, 44), (torch.float32, 30000, 48), (torch.bfloat16, 70003, 15), (torch.bfloat16, 100003, 14), (torch.float32, 131072, 11)])
+def test_several_rows_of_several_slices(dtype, vocab, groups):
+    """Every row as in a call of its group alone, whose workgroups take one row each; a sample of rows against float64; the gradient in place."""
+    gen = torch.Generator().manual_seed(vocab)
+    prompts, Gs = [4 + 9 * (i % 3) for i in range(groups)], [2 + i % 3 for i in range(groups)]
+    resp = [(53 * i) % 67 for i in range(sum(Gs))]
+    T = sum(prompts) + sum(resp)
+    assert T * -(-vocab // 32768) >= 2 * 2048                       # runs of two rows or more
+    dev = torch.Generator(device="cuda").manual_seed(vocab)
+    z = (3 * torch.randn(T, vocab, generator=dev, device="cuda")).to(dtype)
+    u = torch.rand(T, generator=gen, dtype=torch.float64)
+    tokens = (vocab * u ** 4).to(torch.int32).clamp_(max=vocab - 1)
+    allowed = torch.rand(T, (vocab + 31) // 32, 32, generator=dev, device="cuda") < 0.8
+    mask = (allowed.long() * (1 << torch.arange(32, device="cuda"))).sum(2).to(torch.int32)
+    t64 = tokens.long().cuda()
+    word, bit = (t64 // 32)[:, None], (1 << (t64 % 32)).to(torch.int32)[:, None]
+    mask.scatter_(1, word, mask.gather(1, word) | bit)
+    allowed.view(T, -1).scatter_(1, t64[:, None], True)
+    bias, g = torch.randn(vocab, generator=gen), torch.randn(T, generator=gen).cuda()
+    numbers = (1.3, 0.4, 0.25, 0.7)
+    rules, tc = B.LogitRules(*numbers, bias=bias.cuda()), tokens.cuda()
+
+    def both(z, tokens, mask, g, *pack, dlogits=None):
+        logp, lse = B.sp_attn_adjusted_logprob_fwd(z, tokens, tokens, rules, *pack, mask=mask)
+        return logp, lse, B.sp_attn_adjusted_logprob_bwd(z, tokens, tokens, lse, g, rules, *pack, mask=mask, dlogits=dlogits, flags=B.SP_FLAG_ZERO_PROMPT_ROWS)
+
+    logp, lse, dz = both(z, tc, mask, g, prompts, Gs, resp)
+    at, r = 0, 0
+    for p, members in zip(prompts, Gs):
+        lens = resp[r:r + members]
+        rows = slice(at, at + p + sum(lens))
+        alone = both(z[rows].clone(), tc[rows].clone(), mask[rows].clone(), g[rows].clone(), [p], [members], lens)
+        assert torch.equal(alone[0], logp[rows]) and torch.equal(alone[1], lse[rows]) and torch.equal(alone[2], dz[rows]), at
+        at, r = rows.stop, r + members
+    response = response_rows(prompts, Gs, resp)
+    sample = response[::max(1, len(response) // 12)][:14]
+    for t in sample.tolist():
+        want, slope, size = history_and_oracle(t, z, tokens, prompts, Gs, resp, numbers, bias.double().numpy(), allowed[t].flatten()[:vocab].cpu().numpy())
+        top = want.max()
+        L = top + np.log(np.exp(want - top).sum())
+        # as above, with the rules' own operations in the 12 units; 512 threads share a slice
+        off = 12 * U24 * size[np.isfinite(want)].max()
+        tol = off + U24 * (110 + 4 + 32 + vocab / 512 + 4 * max(1.0, abs(L)))
+        y = int(tokens[t])
+        assert abs(lse[t].item() - L) <= tol and abs(logp[t].item() - (want[y] - L)) <= tol + off + U24 * abs(want[y] - L)
+        pick = np.zeros(vocab)
+        pick[y] = 1
+        p = np.exp(want - L)
+        scale = g[t].item() * slope
+        half = HALF_STEP[dtype] if dtype == torch.bfloat16 else U24
+        check(f"dlogits {t}", numpy64(dz[t]), (pick - p) * scale, np.abs(scale) * (p * (off + tol + 130 * U24) + np.abs(pick - p) * (half + 4 * U24)) + 1e-37)
+    in_place = both(z, tc, mask, g, prompts, Gs, resp, dlogits=z)[2]
+    assert in_place.data_ptr() == z.data_ptr() and torch.equal(in_place, dz)
