@@ -469,7 +469,7 @@ typedef struct {
     float repetition;         /* finite, > 0; 1: none */
     float presence;           /* finite; 0: none */
     float frequency;          /* finite; 0: none */
-    float temperature;        /* finite, > 0 */
+    float temperature;        /* finite, > 0, not so small that 1 / temperature (log-probabilities: log2(e) / temperature) passes float32 */
     const float* bias;        /* DEVICE [vocab], or NULL */
 } sp_logit_rules;
 

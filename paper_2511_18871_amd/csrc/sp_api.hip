@@ -751,6 +751,7 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
     if (n_q_heads < 1 || n_q_heads % c.n_kv_heads != 0)
         return fail(SP_ERR_INVALID_ARG, "n_q_heads=%d must be a positive multiple of n_kv_heads=%d", n_q_heads, c.n_kv_heads);
     if (!std::isfinite(softmax_scale) || softmax_scale <= 0.f) return fail(SP_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    if (!std::isfinite(softmax_scale * sp::LOG2E)) return fail(SP_ERR_INVALID_ARG, "softmax_scale times log2(e) is not finite");
     st = check_members(n_groups, n_seqs, Gs);
     if (st != SP_OK) return st;
     if (prompt_width < 0 || resp_width < 0 || (prompt_width > 0) != (prompt_tables != nullptr) || (prompt_width > 0) != (prompt_lens != nullptr) ||
@@ -834,6 +835,7 @@ sp_status adjusted_logprob(bool bwd, const void* logits, const int32_t* labels, 
     sp_status st = check_rules(rules, r);
     if (st == SP_OK) st = check_vocab(vocab, mask, mask_stride, dtype);
     if (st != SP_OK) return st;
+    if (!std::isfinite(r.inv_temperature * sp::LOG2E)) return fail(SP_ERR_INVALID_ARG, "temperature is too small: log2(e) over it is not finite");
     try {
         Layout L;
         float* scratch = nullptr;
