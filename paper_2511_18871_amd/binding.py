@@ -759,6 +759,8 @@ def sp_attn_decode(cache: KvCache, q, Gs: Optional[Sequence[int]], prompt_tables
     n_seqs, hq, d = q.shape
     _need("q", q, cache.dtype, (n_seqs, hq, cache.head_dim), index)
     n_groups = n_seqs if Gs is None else len(Gs)
+    if (prompt_tables is None) != (prompt_lens is None):
+        _refuse("prompt_tables and prompt_lens go together")
     prompt = _pages_of("prompt", prompt_tables, prompt_lens, n_groups, index)
     resp = _pages_of("resp", resp_tables, resp_lens, n_seqs, index)
     if o is not None:

@@ -36,6 +36,12 @@ def test_workspaces_whose_bytes_are_not_there(workspace):
     assert "workspace" in message(B.sp_attn_decode, B.KvCache(k, k), torch.zeros(3, 4, 64), None, None, None, i32(3, 2), i32(3), 0.1, workspace=workspace)
 
 
+def test_prompt_tables_and_lengths_go_together():
+    k, q = torch.zeros(4, 2, 16, 64), torch.zeros(3, 4, 64)
+    for tables, lens in ((i32(3, 2), None), (None, i32(3))):
+        assert "go together" in message(B.sp_attn_decode, B.KvCache(k, k), q, None, tables, lens, i32(3, 2), i32(3), 0.1)
+
+
 @pytest.mark.gpu
 def test_a_workspace_on_the_host():
     z, t, rules, ws = torch.zeros(7, 40).cuda(), i32(7).cuda(), B.LogitRules(), torch.empty(1 << 24, dtype=torch.uint8)
