@@ -442,7 +442,7 @@ sp_status sp_attn_cache_append(const sp_kv_cache* cache, const void* q, int64_t 
  * among them), which is the row that the new token would have in sp_attn_fwd on the pack.  Writes o like q and
  * lse [n_q_heads, n_seqs] float32; without a key o = 0 and lse = -inf (a negative resp_lens[s]: the prompt's are not attended to either).
  * A NaN in q or in a key that a row attends to, or a score of +inf, makes the row NaN.
- * The prompt's keys and values are read once for all rows of the group.
+ * The prompt's keys and values are read once for 192 rows of the group (sequences * n_q_heads / n_kv_heads), in float32 once for 32.
  *   Gs            HOST: sequences of each group, in order, n_seqs in all; NULL: one each (n_groups = n_seqs)
  *   prompt_tables [n_groups, prompt_width], prompt_lens [n_groups]; both NULL and prompt_width 0: no shared prompts
  *   resp_tables   [n_seqs, resp_width] (NULL if resp_width is 0), resp_lens [n_seqs]

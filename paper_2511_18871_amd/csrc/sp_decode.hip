@@ -3,7 +3,8 @@
 //   S_j = scale <q, k_j> over the keys [0, Lp) of the prompt and [0, len) of the response,
 //   o = sum_j e^(S_j - m) v_j / l, l = sum_j e^(S_j - m), lse = m + ln l; without a key o = 0 and lse = -inf.
 //
-// Bound: the keys and values, each read once.  A LIST is what is walked together: the prompt of a group, seen by its G rep rows of
+// Bound: the keys and values, each read once.  (A prompt seen by more than 192 rows in bf16, 32 in float32, is read once for each block of as many: by
+// workgroups that run side by side, so that memory is left alone, but the caches and the instructions are not.)  A LIST is what is walked together: the prompt of a group, seen by its G rep rows of
 // each kv head (rep = n_q_heads / n_kv_heads; row r is q head r % rep of the group's sequence r / rep), or the response of a
 // sequence, seen by its rep rows.  The units of keys of all lists lie one behind the other (list by list, in it block of rows by
 // block, kv head by kv head: a SEGMENT each), and every worker takes an equal run of them, across segments: no worker waits for a
@@ -18,9 +19,11 @@
 // Measured (heads of 128, bf16, us of the kernel + of the join; bytes are those of the keys and values):
 //   32 answers of 8k to 15k tokens to 8 prompts, 32/8 heads   263 + 5     1.53 GB, 5.8 TB/s
 //   64 prompts of 64 to 192 tokens, 16 answers each, 28/4     131 + 11    0.55 GB, 4.2 TB/s; the plan of 1088 lists takes 8 of it
-//   a prompt of 16k tokens, 32 answers, 40/8                  38 + 9      91 MB; 36 MB of sums, written and read, take nearly as long
+//   a prompt of 16k tokens, 32 answers, 40/8                  39 + 9      91 MB; 36 MB of sums, written and read, take nearly as long
 //   a prompt of 1k tokens, 8 answers, 28/4                    8 + 5       latency: launch, plan, pages, keys, sums one after the other
 //   one sequence of 1k tokens, 28/4                           6 + 6       the same
+// Whole calls: a prompt of 4k tokens, 32 answers, 28/4, 24 us (19 MB) and in float32, in seven blocks, 53 us (39 MB); in float32 8 sequences of 7k to 8k
+// tokens, 32/8, 115 us (497 MB, 4.3 TB/s).
 #include "sp_common.hpp"
 #include "sp_launch.hpp"
 #include <algorithm>
@@ -422,8 +425,8 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
 
 // Weights of 32 keys from their scores, in two parts of bf16 as the second product needs them: a weight's upper 16 bits, which is not above
 // it, and what that leaves, rounded.  Both go through the matrix instructions, and 2^-15 of the weight is lost at most, so that o is off as with unrounded weights
-// (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 50 us instead of
-// 46, while calls that wait for keys cost the same).  The second part is never 0: it would turn an infinite value into NaN.
+// (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 40 us instead of
+// 37, while calls that wait for keys cost the same).  The second part is never 0: it would turn an infinite value into NaN.
 // They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
 // range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key) does the wave
 // take the rows' maxima for new references, scale what it has and take the weights again.  A NaN among the scores stays in the row's sum, whichever way the
