@@ -426,7 +426,8 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
 // Weights of 32 keys from their scores, in two parts of bf16 as the second product needs them: a weight's upper 16 bits, which is not above
 // it, and what that leaves, rounded.  Both go through the matrix instructions, and 2^-15 of the weight is lost at most, so that o is off as with unrounded weights
 // (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 40 us instead of
-// 37, while calls that wait for keys cost the same).  The second part is never 0: it would turn an infinite value into NaN.
+// 37, while calls that wait for keys cost the same).  The second part has 2^-20 of the weight added, so that it is 0 only with
+// the weight: it would turn an infinite value into NaN.
 // They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
 // range: only if a lane's eight sum to more than 2^14 (or to infinity, as they do for a row that has not seen a key) does the wave
 // take the rows' maxima for new references, scale what it has and take the weights again.  A NaN among the scores stays in the row's sum, whichever way the
@@ -446,7 +447,7 @@ __device__ __forceinline__ void weights(Rows<D, NC>& r, const f32x4 (&s)[NC][2],
                 sum += x;
                 const float high = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
                 p[c][0][e] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(x) >> 16));
-                p[c][1][e] = (__bf16)fmaxf(x - high, 0x1p-126f);
+                p[c][1][e] = (__bf16)__builtin_fmaf(x, 1.f + 0x1p-20f, -high);
             }
         };
         take(r.m[c]);

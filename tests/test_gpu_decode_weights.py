@@ -33,3 +33,20 @@ def test_weights_keep_their_bits(d, hq, hkv, prompts, Gs, resp):
     tol_o, tol_lse = decode_bounds(ref, rlse, weight, reach, count, d, torch.float32)
     check("lse", lse, rlse, tol_lse)
     check("o", o, ref, tol_o + weight * 2.0 ** -15 + np.abs(ref) * 2.0 ** -8)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("members", [1, 20])                    # a list of a wave, a shared one
+def test_keys_without_weight_add_nothing(d, members):
+    """The largest values, under keys whose weights are below what float32 holds."""
+    gen = torch.Generator().manual_seed(d)
+    kc, vc = (torch.randn(3, 1, 64, d, generator=gen).bfloat16() for _ in range(2))
+    q = torch.randn(members, 2, d, generator=gen).bfloat16()
+    q[:, :, 0], kc[:, 0, :, 0] = 100.0, 1.0
+    kc[1, 0, 7, 0] = -100.0                                     # 2e4 times the scale below the others
+    vc[1, 0, 7] = 0
+    args = (q.cuda(), [members], dev32([[0, 1, 2]]), dev32([150]), None, dev32([0] * members), 0.1)
+    want = B.sp_attn_decode(B.KvCache(kc.cuda(), vc.cuda()), *args)
+    vc[1, 0, 7] = torch.finfo(torch.bfloat16).max
+    got = B.sp_attn_decode(B.KvCache(kc.cuda(), vc.cuda()), *args)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
