@@ -640,7 +640,8 @@ class KvCache:
     def _ref(self):
         k, v, struct = self.k, self.v, self._struct
         at_k, at_v = k.data_ptr(), v.data_ptr()
-        if at_k != struct.k or at_v != struct.v or k.shape != self._shape or v.shape != self._shape:       # another storage
+        if not (at_k == struct.k and at_v == struct.v and k.shape == v.shape == self._shape and k.dtype is v.dtype is self.dtype and
+                k.is_contiguous() and v.is_contiguous()):
             _need("k", k, self.dtype, self._shape, self.index)
             _need("v", v, self.dtype, self._shape, self.index)
             struct.k, struct.v = at_k, at_v

@@ -25,6 +25,15 @@ def test_a_cache_is_looked_at_again():
         cache._ref
 
 
+@pytest.mark.parametrize("view", [lambda t: t.transpose(1, 2), lambda t: t.flatten().view(torch.bfloat16)[:t.numel()].view(t.shape)])
+def test_other_views_of_the_same_memory(view):
+    cache = B.KvCache(torch.zeros(4, 16, 16, 64), torch.zeros(4, 16, 16, 64))
+    cache.v.data = view(cache.v.data)
+    assert cache.v.data_ptr() == cache._struct.v and cache.v.shape == (4, 16, 16, 64)
+    with pytest.raises(B.SpAttnError):
+        cache._ref
+
+
 def test_a_bias_is_looked_at_again():
     rules = B.LogitRules(bias=torch.zeros(40))
     rules.bias.data = torch.ones(40)
