@@ -19,7 +19,7 @@
 // Measured (heads of 128, bf16, us of the kernel + of the join; bytes are those of the keys and values):
 //   32 answers of 8k to 15k tokens to 8 prompts, 32/8 heads   263 + 5     1.53 GB, 5.8 TB/s
 //   64 prompts of 64 to 192 tokens, 16 answers each, 28/4     131 + 11    0.55 GB, 4.2 TB/s; the plan of 1088 lists takes 8 of it
-//   a prompt of 16k tokens, 32 answers, 40/8                  39 + 9      91 MB; 36 MB of sums, written and read, take nearly as long
+//   a prompt of 16k tokens, 32 answers, 40/8                  38 + 9      91 MB; 36 MB of sums, written and read, take nearly as long
 //   a prompt of 1k tokens, 8 answers, 28/4                    8 + 5       latency: launch, plan, pages, keys, sums one after the other
 //   one sequence of 1k tokens, 28/4                           6 + 6       the same
 // Whole calls: a prompt of 4k tokens, 32 answers, 28/4, 24 us (19 MB) and in float32, in seven blocks, 53 us (39 MB); in float32 8 sequences of 7k to 8k
@@ -425,7 +425,7 @@ __device__ __forceinline__ void scores(const Rows<D, NC>& r, unsigned k, unsigne
 
 // Weights of 32 keys from their scores, in two parts of bf16 as the second product needs them: a weight's upper 16 bits, which is not above
 // it, and what that leaves, rounded.  Both go through the matrix instructions, and 2^-15 of the weight is lost at most, so that o is off as with unrounded weights
-// (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 40 us instead of
+// (32 answers to a prompt of 16k tokens: o off by 1.66e-3 of its 2-norm, the rounding of o itself, where weights rounded once left 1.92e-3; for 39 us instead of
 // 37, while calls that wait for keys cost the same).  The second part has 2^-20 of the weight added, so that it is 0 only with
 // the weight: it would turn an infinite value into NaN.
 // They are taken against the reference m that the row has from earlier keys, any finite one serving as well, as long as they stay in
