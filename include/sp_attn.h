@@ -458,6 +458,73 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
                          const int32_t* resp_tables, int32_t resp_width, const int32_t* resp_lens,
                          float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Rollout that branches: several new tokens per sequence, several sequences from one ------------------------
+ * A step may bring several drafted tokens per sequence, which form a tree: each is a guess at what follows its parent.  They are appended (as
+ * one-token sequences of sp_attn_cache_append that share a table: drafted token i goes to row lens + i of the cache and stands at its depth, which is
+ * lens = lens[s] + i and pos_base = base - i + depth), attended to, and those that turn out right are kept.
+ *
+ * Attention of the drafted tokens.  Sequence s has new_lens[s] of them; its keys of them are the last new_lens[s] of its first resp_lens[s] tokens.  Row t of q
+ * [T, n_q_heads, head_dim], T = sum of new_lens, one sequence behind the other, attends to its group's prompt, to its sequence's own tokens ahead
+ * of the drafted ones, and to those drafted ones whose bit is set in row t of `ancestors`: bit m % 32 of word m / 32 is drafted token m of the same
+ * sequence, in any pattern (a token that attends to itself has its own bit set).  Writes o like q and lse [n_q_heads, T]; rows without a key, lengths, pages,
+ * NaN and infinities as in sp_attn_decode.  What a token that a row does not attend to holds does not matter to it.
+ *   new_lens      HOST array of n_seqs entries, 0 to SP_MAX_DRAFT
+ *   ancestors     DEVICE uint32 [T, mask_stride], mask_stride >= ceil(largest new_lens / 32) words; NULL (mask_stride 0): a chain, token i
+ *                 attends to drafted tokens 0 to i
+ *   workspace     DEVICE, at least sp_attn_tree_decode_workspace_bytes(...) bytes, total_new = T; it carries nothing from call to call
+ * The rest as sp_attn_decode.  o may be q.  SP_ERR_INVALID_ARG also where T * n_q_heads passes 2^31 - 1 or n_q_heads 65535.  Deterministic. */
+#define SP_MAX_DRAFT 1024
+size_t    sp_attn_tree_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int64_t total_new, int32_t n_q_heads, int32_t n_kv_heads,
+                                              int32_t head_dim, sp_dtype dtype);
+sp_status sp_attn_tree_decode(const sp_kv_cache* cache, const void* q, void* o, float* lse, int32_t n_q_heads,
+                              int32_t n_groups, int32_t n_seqs, const int32_t* Gs, const int32_t* new_lens,
+                              const uint32_t* ancestors, int64_t mask_stride,
+                              const int32_t* prompt_tables, int32_t prompt_width, const int32_t* prompt_lens,
+                              const int32_t* resp_tables, int32_t resp_width, const int32_t* resp_lens,
+                              float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The calls below change the caches of all layers at once: k and v of layer i start i * layer_stride elements behind those of `cache`, which
+ * is layer 0's (layer_stride: a multiple of 16 bytes, at least n_pages * n_kv_heads * page_size * head_dim; not looked at if n_layers is 1).  Tables are those of every layer.
+ *
+ * Keep drafted tokens: token lens[s] + kept[s][i] of sequence s becomes its token lens[s] + i, for i < n_kept[s], in every layer; the tokens behind are
+ * what they were.
+ *   kept          DEVICE int32 [n_seqs, kept_width], n_kept DEVICE int32 [n_seqs] (cut to [0, kept_width]).  A list ascends; it ends ahead of the first entry that does
+ *                 not, that is negative, or whose token the table has no room for
+ *   lens_out      DEVICE int32 [n_seqs]: lens + entries of the list; it overlaps none of the arrays that are read
+ * A sequence with a negative length takes no part (lens_out: its length).  Rows on pages outside the cache are neither read nor written.  No two
+ * tokens that the call moves or writes over may share a row.  Needs no workspace. */
+sp_status sp_attn_cache_keep(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t n_seqs,
+                             const int32_t* tables, int32_t table_width, const int32_t* lens,
+                             const int32_t* kept, int32_t kept_width, const int32_t* n_kept, int32_t* lens_out, void* stream);
+
+/* Pages are counted by the caller's array refs, DEVICE int32 [n_pages]: how many tables hold a page.  Free ones have 0; a negative count takes a page
+ * out of use.  Pages are given out in ascending order, to sequences in their order and in each to its places in theirs: results do not depend on
+ * anything else.  The arrays that a call writes overlap neither each other nor those that it reads.
+ *   workspace     DEVICE, at least sp_attn_pages_workspace_bytes(n_pages, n_seqs) bytes; it carries nothing from call to call
+ *
+ * Fit tables to lengths: behind the pages that lens[s] tokens take, places become -1 and the counts of their pages fall by one; ahead, places without a page of
+ * [0, n_pages) get free ones (also such as the same call gave back), whose counts become 1.  Where none is left they are -1.
+ *   tables        DEVICE int32 [n_seqs, table_width], changed;  lens DEVICE int32 [n_seqs], cut to what a table holds; negative: the row stays as it is
+ *   missing       DEVICE int32 [1], how many places got none, or NULL
+ * A table must not hold more than refs says: a count that falls below 0 loses its page. */
+size_t    sp_attn_pages_workspace_bytes(int64_t n_pages, int32_t n_seqs);
+sp_status sp_attn_pages_fit(int32_t* refs, int64_t n_pages, int32_t page_size, int32_t n_seqs, int32_t* tables, int32_t table_width,
+                            const int32_t* lens, int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Fork sequences: sequence s starts as a copy of sequence parents[s] of src_tables.  Its table gets the parent's whole pages, which are counted once more, a
+ * free page with the parent's tokens of the last, begun one, in every layer, and -1 behind; lens_out[s] is the parent's length (cut to what either table
+ * holds).  What the row held before is not given back (sp_attn_pages_fit with a length of 0 does).
+ *   refs          as above, n_pages of the cache
+ *   parents       DEVICE int32 [n_seqs]; outside [0, n_src): the sequence is left as it is.  Several may have the same parent
+ *   src_tables    DEVICE int32 [n_src, src_width], src_lens DEVICE int32 [n_src]; a negative length: a row of -1, lens_out that length
+ *   tables        DEVICE int32 [n_seqs, table_width], written;  lens_out DEVICE int32 [n_seqs], written
+ * Where no page is left for the last tokens the row is -1 throughout, lens_out -1, and nothing is counted.  Places outside the cache are copied as they
+ * are and not counted. */
+sp_status sp_attn_cache_fork(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t* refs, int32_t n_seqs,
+                             const int32_t* parents, int32_t n_src, const int32_t* src_tables, int32_t src_width, const int32_t* src_lens,
+                             int32_t* tables, int32_t table_width, int32_t* lens_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 /* Rules by which logits are adjusted before a token is drawn, in this order: bias, repetition, frequency and presence,
  * temperature, mask.  With h_v: id v occurs in the row's history (its prompt and its response so far), and c_v: how often it occurs
  * in the response so far (counted up to 32767),

@@ -1,5 +1,5 @@
-"""CPU fp64 oracle of the rollout step: a paged cache, the attention of one new token per sequence over it, and
-logits adjusted ahead of a draw with their log-probabilities and gradient.  Written from the formulas, token by token and
+"""CPU fp64 oracle of the rollout step: a paged cache, the attention of one new token per sequence over it or of several drafted
+ones, the pages of sequences that branch, and logits adjusted ahead of a draw with their log-probabilities and gradient.  Written from the formulas, token by token and
 row by row; imports nothing from the package."""
 import numpy as np
 
@@ -68,6 +68,120 @@ def decode(k_cache, v_cache, q, Gs, prompt_tables, prompt_lens, resp_tables, res
                     reach[h, s] = scale * (np.abs(kh) @ np.abs(qh)).max()
             s += 1
     return o, lse, weight, reach, count
+
+
+def tree_decode(k_cache, v_cache, q, Gs, new_lens, ancestors, prompt_tables, prompt_lens, resp_tables, resp_lens, scale):
+    """Attention of drafted tokens; ancestors: per row a list of the drafted tokens of its sequence that it attends to, or None (those up to
+    itself).  Returns what decode() returns, a row per token."""
+    T, hq, d = q.shape
+    hkv = k_cache.shape[1]
+    o, weight = np.zeros((T, hq, d)), np.zeros((T, hq, d))
+    lse, reach, count = np.full((hq, T), -np.inf), np.zeros((hq, T)), np.zeros(T, dtype=int)
+    s, t = 0, 0
+    n_pages, _, page, _ = k_cache.shape
+    for g, members in enumerate(Gs):
+        for _ in range(members):
+            n, length = new_lens[s], resp_lens[s]
+            table = list(resp_tables[s]) if resp_tables is not None else []
+            for i in range(n):
+                places = []
+                if length >= 0:
+                    if prompt_tables is not None:
+                        places += [(prompt_tables[g][j // page], j % page) for j in range(min(max(prompt_lens[g], 0), len(prompt_tables[g]) * page))]
+                    sees = range(i + 1) if ancestors is None else ancestors[t]
+                    own = [j for j in range(min(length, len(table) * page)) if j < length - n or j - (length - n) in sees]
+                    places += [(table[j // page], j % page) for j in own]
+                places = [(p, r) for p, r in places if 0 <= p < n_pages]
+                count[t] = len(places)
+                if places:
+                    at, row = (np.array(x) for x in zip(*places))
+                    k, v = k_cache[at, :, row].astype(np.float64), v_cache[at, :, row].astype(np.float64)
+                    for h in range(hq):
+                        kh, vh, qh = k[:, h * hkv // hq], v[:, h * hkv // hq], q[t, h].astype(np.float64)
+                        score = scale * (kh @ qh)
+                        top = score.max()
+                        p = np.exp(score - top)
+                        lse[h, t] = top + np.log(p.sum())
+                        o[t, h], weight[t, h] = (p @ vh) / p.sum(), (p @ np.abs(vh)) / p.sum()
+                        reach[h, t] = scale * (np.abs(kh) @ np.abs(qh)).max()
+                t += 1
+            s += 1
+    return o, lse, weight, reach, count
+
+
+def cache_keep(caches, tables, lens, kept, n_kept):
+    """Kept tokens moved together in caches [layers, pages, heads, page, d]; returns (caches, lens_out)."""
+    caches, lens_out = [np.array(c) for c in caches], list(lens)
+    _, n_pages, _, page, _ = caches[0].shape
+    for s, table in enumerate(tables):
+        if lens[s] < 0:
+            continue
+        before = -1
+        for i in range(min(max(n_kept[s], 0), len(kept[s]))):
+            x = kept[s][i]
+            if x <= before or lens[s] + x >= len(table) * page:
+                break
+            before = x
+            lens_out[s] += 1
+            src, dst = lens[s] + x, lens[s] + i
+            a, b = table[src // page], table[dst // page]
+            if 0 <= a < n_pages and 0 <= b < n_pages:
+                for c in caches:
+                    c[:, b, :, dst % page] = c[:, a, :, src % page]
+    return caches, lens_out
+
+
+def pages_fit(refs, page, tables, lens):
+    """Returns (refs, tables, missing)."""
+    refs, tables, missing = list(refs), [list(t) for t in tables], 0
+    n = len(refs)
+    for table, length in zip(tables, lens):
+        if length >= 0:
+            for c in range(min(-(-length // page), len(table)), len(table)):
+                if 0 <= table[c] < n:
+                    refs[table[c]] -= 1
+                table[c] = -1
+    free = [p for p in range(n) if refs[p] == 0]
+    for table, length in zip(tables, lens):
+        for c in range(min(-(-max(length, 0) // page), len(table))):
+            if not 0 <= table[c] < n:
+                table[c] = free.pop(0) if free else -1
+                if table[c] < 0:
+                    missing += 1
+                else:
+                    refs[table[c]] = 1
+    return refs, tables, missing
+
+
+def cache_fork(caches, refs, parents, src_tables, src_lens, tables, lens_out):
+    """Returns (caches, refs, tables, lens_out)."""
+    caches, refs, tables, lens_out = [np.array(c) for c in caches], list(refs), [list(t) for t in tables], list(lens_out)
+    _, n_pages, _, page, _ = caches[0].shape
+    free = [p for p in range(n_pages) if refs[p] == 0]
+    for s, parent in enumerate(parents):
+        if not 0 <= parent < len(src_tables):
+            continue
+        src, width = src_tables[parent], len(tables[s])
+        length = min(src_lens[parent], min(len(src), width) * page)
+        row = [-1] * width
+        if length >= 0:
+            whole, rest = divmod(length, page)
+            row[:whole] = src[:whole]
+            if rest:
+                row[whole] = src[whole]
+                if 0 <= src[whole] < n_pages:
+                    if not free:
+                        tables[s], lens_out[s] = [-1] * width, -1
+                        continue
+                    row[whole] = free.pop(0)
+                    refs[row[whole]] = 1
+                    for c in caches:
+                        c[:, row[whole], :, :rest] = c[:, src[whole], :, :rest]
+            for p in src[:whole]:
+                if 0 <= p < n_pages:
+                    refs[p] += 1
+        tables[s], lens_out[s] = row, length
+    return caches, refs, tables, lens_out
 
 
 def adjust_row(z, prompt, generated, rules, bias=None, allowed=None):

@@ -20,12 +20,15 @@ SP_BF16, SP_F32 = 0, 1
 SP_SCHED_SHARED, SP_SCHED_NAIVE_CAUSAL = 0, 1
 
 SP_BWD_STAGE_ROWSUM, SP_BWD_STAGE_DKDV, SP_BWD_STAGE_DQ, SP_BWD_STAGE_ALL = 1, 2, 4, 7
+SP_MAX_DRAFT = 1024
 SP_FLAG_RESPONSE_ROWS, SP_FLAG_ACCUMULATE_DKDV, SP_FLAG_ZERO_PROMPT_ROWS, SP_FLAG_OWN_TOKEN = 1, 2, 4, 8
 
 EXPORTS = ("sp_attn_workspace_bytes", "sp_attn_reserve_bytes", "sp_attn_row_parts_bytes", "sp_attn_full_workspace_bytes", "sp_attn_kept_workspace_bytes", "sp_attn_sums_bytes", "sp_attn_fwd", "sp_attn_bwd", "sp_attn_fwd_batched",
            "sp_attn_bwd_batched", "sp_attn_bwd_batched_static", "sp_attn_bwd_batched_stages", "sp_attn_fwd_multi", "sp_attn_rope", "sp_attn_rope_qk", "sp_attn_fwd_batched_ex", "sp_attn_bwd_batched_ex", "sp_attn_fwd_batched_sums", "sp_attn_bwd_batched_sums",
            "sp_attn_loss_workspace_bytes", "sp_attn_logprob_fwd", "sp_attn_logprob_bwd", "sp_attn_logprob_bwd_ex", "sp_attn_grpo_loss",
            "sp_attn_cache_append", "sp_attn_decode_workspace_bytes", "sp_attn_decode", "sp_attn_adjust_logits",
+           "sp_attn_tree_decode_workspace_bytes", "sp_attn_tree_decode", "sp_attn_cache_keep", "sp_attn_pages_workspace_bytes", "sp_attn_pages_fit",
+           "sp_attn_cache_fork",
            "sp_attn_adjusted_logprob_workspace_bytes", "sp_attn_adjusted_logprob_fwd", "sp_attn_adjusted_logprob_bwd",
            "sp_attn_segment_table", "sp_attn_row_tile", "sp_attn_dkdv_waves", "sp_attn_pieces", "sp_attn_f32_rows", "sp_attn_mfma_ceiling", "sp_attn_probe_atomic_add", "sp_attn_set_small_shape_steps", "sp_attn_last_error", "sp_attn_version")
 
@@ -124,6 +127,18 @@ def load_library() -> ctypes.CDLL:
     lib.sp_attn_decode_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int]
     lib.sp_attn_decode.restype = ctypes.c_int
     lib.sp_attn_decode.argtypes = [cache_p, vp, vp, vp, i32, i32, i32, ip, vp, i32, vp, vp, i32, vp, f32, vp, sz, vp]
+    lib.sp_attn_tree_decode_workspace_bytes.restype = sz
+    lib.sp_attn_tree_decode_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i32, ctypes.c_int]
+    lib.sp_attn_tree_decode.restype = ctypes.c_int
+    lib.sp_attn_tree_decode.argtypes = [cache_p, vp, vp, vp, i32, i32, i32, ip, ip, vp, i64, vp, i32, vp, vp, i32, vp, f32, vp, sz, vp]
+    lib.sp_attn_cache_keep.restype = ctypes.c_int
+    lib.sp_attn_cache_keep.argtypes = [cache_p, i32, i64, i32, vp, i32, vp, vp, i32, vp, vp, vp]
+    lib.sp_attn_pages_workspace_bytes.restype = sz
+    lib.sp_attn_pages_workspace_bytes.argtypes = [i64, i32]
+    lib.sp_attn_pages_fit.restype = ctypes.c_int
+    lib.sp_attn_pages_fit.argtypes = [vp, i64, i32, i32, vp, i32, vp, vp, vp, sz, vp]
+    lib.sp_attn_cache_fork.restype = ctypes.c_int
+    lib.sp_attn_cache_fork.argtypes = [cache_p, i32, i64, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]
     lib.sp_attn_adjust_logits.restype = ctypes.c_int
     lib.sp_attn_adjust_logits.argtypes = [vp, i64, vp, i64, i64, rules_p, vp, i64, i32, i32, ip, vp, i32, vp, vp, i32, vp, ctypes.c_int, vp]
     lib.sp_attn_adjusted_logprob_workspace_bytes.restype = sz
@@ -648,6 +663,47 @@ class KvCache:
         return self._pointer
 
 
+class KvLayers:
+    """The caches of all layers of a model: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim], each layer contiguous, whose sequences have the
+    same tables in every layer.  layers[i] is the KvCache of layer i.  Memory, shape and type as for KvCache."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 5 or k.shape[0] == 0:
+            _refuse(f"k: {tuple(k.shape)}, expected [n_layers, n_pages, n_kv_heads, page_size, head_dim]")
+        # (no attributes of a single layer's cache: a call for one layer refuses all of them)
+        self.index, self._dtype, self.device = k.get_device(), k.dtype, k.device
+        self._shape, self._strides = k.shape, k.stride()
+        self._check(k, v)
+        self.k, self.v = k, v
+        self.n_layers, n_pages, heads, page_size, head_dim = k.shape
+        self._stride = self._strides[0]
+        self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), n_pages, page_size, heads, head_dim, _dtype_code(k))
+        self._pointer = ctypes.pointer(self._struct)
+
+    def __len__(self) -> int:
+        return self.n_layers
+
+    def __getitem__(self, i: int) -> KvCache:
+        return KvCache(self.k[i], self.v[i])
+
+    def _check(self, k, v):
+        for name, t in (("k", k), ("v", v)):
+            if t.shape != self._shape or t.stride() != self._strides or not t[0].is_contiguous() or (t.shape[0] > 1 and t.stride(0) < t[0].numel()):
+                _refuse(f"{name}: {tuple(t.shape)} with strides {t.stride()}, expected {tuple(self._shape)} with strides {self._strides}, each layer contiguous "
+                        "and behind the last")
+            _need(name, t[0], self._dtype, self._shape[1:], self.index)
+
+    @property
+    def _ref(self):
+        k, v, struct = self.k, self.v, self._struct
+        at_k, at_v = k.data_ptr(), v.data_ptr()
+        if not (at_k == struct.k and at_v == struct.v and k.shape == v.shape == self._shape and k.dtype is v.dtype is self._dtype and
+                k.stride() == v.stride() == self._strides):
+            self._check(k, v)
+            struct.k, struct.v = at_k, at_v
+        return self._pointer
+
+
 class LogitRules:
     """How logits are adjusted ahead of a draw: bias (float32 [vocab] or None), then penalties, then the temperature."""
 
@@ -787,6 +843,165 @@ def _decode(raw, cache, q, o, lse, hq, n_groups, n_seqs, Gs, prompt, resp, softm
     _check(lib.sp_attn_decode(cache._ref, q.data_ptr(), o.data_ptr(), lse.data_ptr(), hq, n_groups, n_seqs, None if Gs is None else _i32(Gs),
                               pt, pw, pl if pw else None, rt, rw, rl, softmax_scale, workspace.data_ptr(), workspace.nbytes, raw))
     return o, lse
+
+
+@functools.lru_cache(maxsize=64)
+def tree_decode_workspace_bytes(n_groups: int, n_seqs: int, total_new: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype_code: int) -> int:
+    return load_library().sp_attn_tree_decode_workspace_bytes(n_groups, n_seqs, total_new, n_q_heads, n_kv_heads, head_dim, dtype_code)
+
+
+def sp_attn_tree_decode(cache: KvCache, q, Gs: Optional[Sequence[int]], new_lens: Sequence[int], ancestors, prompt_tables, prompt_lens, resp_tables,
+                        resp_lens, softmax_scale: float, o=None, lse=None, workspace=None, stream=None):
+    """Attention of new_lens[s] drafted tokens per sequence (host integers).  Row t of q [T, n_q_heads, d], sequence behind sequence, attends to its group's
+    prompt, to its sequence's first resp_lens[s] - new_lens[s] tokens, and to those of its drafted tokens, the last of these resp_lens[s], whose bits are set in row t of
+    ancestors [T, words] (int32 or uint32, bit m % 32 of word m / 32: drafted token m); None: to its own and those ahead of it.  The rest as
+    sp_attn_decode.  Returns (o, lse [n_q_heads, T])."""
+    index = cache.index
+    if q.dim() != 3:
+        _refuse(f"q: {tuple(q.shape)}, expected [tokens, heads, {cache.head_dim}]")
+    T, hq, d = q.shape
+    n_seqs = len(new_lens)
+    _need("q", q, cache.dtype, (T, hq, cache.head_dim), index)
+    if T != sum(new_lens):
+        _refuse(f"q has {T} tokens, new_lens add up to {sum(new_lens)}")
+    n_groups = n_seqs if Gs is None else len(Gs)
+    if (prompt_tables is None) != (prompt_lens is None):
+        _refuse("prompt_tables and prompt_lens go together")
+    rows = _mask_rows(ancestors, T, index)
+    prompt = _pages_of("prompt", prompt_tables, prompt_lens, n_groups, index)
+    resp = _pages_of("resp", resp_tables, resp_lens, n_seqs, index)
+    if o is not None:
+        _need("o", o, cache.dtype, (T, hq, d), index)
+    if lse is not None:
+        _need("lse", lse, torch.float32, (hq, T), index)
+    _room(workspace, index)
+    return _tree_decode(index, stream, cache, q, o, lse, n_groups, n_seqs, Gs, new_lens, rows, prompt, resp, softmax_scale, workspace)
+
+
+@_placed
+def _tree_decode(raw, cache, q, o, lse, n_groups, n_seqs, Gs, new_lens, mask, prompt, resp, softmax_scale, workspace):
+    T, hq, _ = q.shape
+    if o is None:
+        o = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty(hq, T, dtype=torch.float32, device=cache.device)
+    if workspace is None:
+        need = tree_decode_workspace_bytes(n_groups, n_seqs, T, hq, cache.n_kv_heads, cache.head_dim, cache.code)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
+    pt, pw, pl = prompt
+    rt, rw, rl = resp
+    at = (q.data_ptr(), o.data_ptr(), lse.data_ptr()) if T else (cache.k.data_ptr(),) * 3      # the pointers of empty tensors are null, and no row is read or written
+    ancestors, words = mask
+    _check(load_library().sp_attn_tree_decode(cache._ref, *at, hq, n_groups, n_seqs, None if Gs is None else _i32(Gs), _i32(new_lens),
+                                              ancestors, words if ancestors else 0, pt, pw, pl if pw else None, rt, rw, rl, softmax_scale,
+                                              workspace.data_ptr(), workspace.nbytes, raw))
+    return o, lse
+
+
+def _layers(cache):
+    """(number of layers, elements from one to the next) of a KvCache or of KvLayers."""
+    return (cache.n_layers, cache._stride) if isinstance(cache, KvLayers) else (1, 0)
+
+
+def _rows_of(name, t, dtype, rows, index):
+    """Width of [rows, width]."""
+    if t.dim() != 2:
+        _refuse(f"{name}: {tuple(t.shape)}, expected two dimensions")
+    _need(name, t, dtype, (rows, t.shape[1]), index)
+    return t.shape[1]
+
+
+def sp_attn_cache_keep(cache, tables, lens, kept, n_kept, lens_out=None, stream=None):
+    """Of the tokens behind the first lens[s] of sequence s, those numbered kept[s, :n_kept[s]] (ascending) become its next ones, in every layer of the cache
+    (KvCache or KvLayers).  Returns lens_out, lens + n_kept."""
+    index, int32, n_seqs = cache.index, torch.int32, lens.shape[0]
+    _need("lens", lens, int32, (n_seqs,), index)
+    _need("n_kept", n_kept, int32, (n_seqs,), index)
+    _rows_of("tables", tables, int32, n_seqs, index)
+    _rows_of("kept", kept, int32, n_seqs, index)
+    if lens_out is not None:
+        _need("lens_out", lens_out, int32, (n_seqs,), index)
+    return _keep(index, stream, cache, tables, lens, kept, n_kept, lens_out)
+
+
+@_placed
+def _keep(raw, cache, tables, lens, kept, n_kept, lens_out):
+    n_seqs = lens.shape[0]
+    if lens_out is None:
+        lens_out = torch.empty_like(lens)
+    if n_seqs:
+        _check(load_library().sp_attn_cache_keep(cache._ref, *_layers(cache), n_seqs, tables.data_ptr(), tables.shape[1], lens.data_ptr(),
+                                                 kept.data_ptr() if kept.shape[1] else None, kept.shape[1], n_kept.data_ptr(), lens_out.data_ptr(), raw))
+    return lens_out
+
+
+@functools.lru_cache(maxsize=64)
+def pages_workspace_bytes(n_pages: int, n_seqs: int) -> int:
+    return load_library().sp_attn_pages_workspace_bytes(n_pages, n_seqs)
+
+
+def _pages_workspace(n_pages, n_seqs, device, workspace):
+    return torch.empty(max(256, pages_workspace_bytes(n_pages, n_seqs)), dtype=torch.uint8, device=device) if workspace is None else workspace
+
+
+def sp_attn_pages_fit(refs, page_size: int, tables, lens, missing=None, workspace=None, stream=None):
+    """Fits tables [n_seqs, width] to sequences of lens[s] tokens: pages behind go back, missing ones ahead come from the free ones, those with refs [n_pages] of 0, lowest
+    first.  tables and refs change in place.  Returns missing [1], how many places got no page."""
+    index, int32 = refs.get_device(), torch.int32
+    if refs.dim() != 1:
+        _refuse(f"refs: {tuple(refs.shape)}, expected [n_pages]")
+    _need("refs", refs, int32, refs.shape, index)
+    n_seqs = lens.shape[0]
+    _need("lens", lens, int32, (n_seqs,), index)
+    _rows_of("tables", tables, int32, n_seqs, index)
+    if missing is not None:
+        _need("missing", missing, int32, (1,), index)
+    _room(workspace, index)
+    return _fit(index, stream, refs, page_size, tables, lens, missing, workspace)
+
+
+@_placed
+def _fit(raw, refs, page_size, tables, lens, missing, workspace):
+    n_seqs = lens.shape[0]
+    if missing is None:
+        missing = torch.empty(1, dtype=torch.int32, device=refs.device)
+    if n_seqs == 0:
+        return missing.zero_()
+    workspace = _pages_workspace(refs.shape[0], n_seqs, refs.device, workspace)
+    _check(load_library().sp_attn_pages_fit(refs.data_ptr(), refs.shape[0], page_size, n_seqs, tables.data_ptr(), tables.shape[1], lens.data_ptr(),
+                                            missing.data_ptr(), workspace.data_ptr(), workspace.nbytes, raw))
+    return missing
+
+
+def sp_attn_cache_fork(cache, refs, parents, src_tables, src_lens, tables, lens_out=None, workspace=None, stream=None):
+    """Sequence s of tables [n_seqs, width] becomes a copy of sequence parents[s] of src_tables, in every layer of the cache (KvCache or KvLayers): whole pages are shared, the
+    last tokens copied to a free page.  tables and refs [n_pages] change in place.  Returns lens_out (-1 where no page was left; rows whose parent is none keep what
+    it held, -1 when it is allocated here)."""
+    index, int32 = cache.index, torch.int32
+    _need("refs", refs, int32, (cache._shape[-4],), index)
+    n_seqs, n_src = parents.shape[0], src_lens.shape[0]
+    _need("parents", parents, int32, (n_seqs,), index)
+    _need("src_lens", src_lens, int32, (n_src,), index)
+    _rows_of("src_tables", src_tables, int32, n_src, index)
+    _rows_of("tables", tables, int32, n_seqs, index)
+    if lens_out is not None:
+        _need("lens_out", lens_out, int32, (n_seqs,), index)
+    _room(workspace, index)
+    return _fork(index, stream, cache, refs, parents, src_tables, src_lens, tables, lens_out, workspace)
+
+
+@_placed
+def _fork(raw, cache, refs, parents, src_tables, src_lens, tables, lens_out, workspace):
+    n_seqs = parents.shape[0]
+    if lens_out is None:
+        lens_out = torch.full_like(parents, -1)
+    if n_seqs == 0:
+        return lens_out
+    workspace = _pages_workspace(refs.shape[0], n_seqs, cache.device, workspace)
+    _check(load_library().sp_attn_cache_fork(cache._ref, *_layers(cache), refs.data_ptr(), n_seqs, parents.data_ptr(), src_lens.shape[0], src_tables.data_ptr(),
+                                             src_tables.shape[1], src_lens.data_ptr(), tables.data_ptr(), tables.shape[1], lens_out.data_ptr(),
+                                             workspace.data_ptr(), workspace.nbytes, raw))
+    return lens_out
 
 
 def _logit_stride(name, t, shape, dtype, index) -> int:

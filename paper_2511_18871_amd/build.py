@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsp_attn.so")
 SOURCES = ["sp_api.hip", "sp_f32.hip", "sp_fwd.hip", "sp_bwd.hip", "sp_rope.hip", "sp_loss.hip", "sp_probe.hip", "sp_edge.hip",
-           "sp_cache.hip", "sp_decode.hip", "sp_adjust.hip"]
+           "sp_cache.hip", "sp_decode.hip", "sp_adjust.hip", "sp_tree.hip", "sp_pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-fno-gpu-rdc", "-Wall", "-Wno-unused-function", "-fno-honor-nans",
          # float atomic adds as the hardware instruction (only the measurement probe uses any)

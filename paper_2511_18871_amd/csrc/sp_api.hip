@@ -791,6 +791,166 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
     return SP_OK;
 }
 
+namespace {
+// Layers of a cache that lie behind each other
+sp_status check_layers(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, sp::KvCache& c) {
+    sp_status st = check_cache(cache, c);
+    if (st != SP_OK) return st;
+    if (n_layers < 1 || (int64_t)n_layers * c.n_kv_heads > 100000) return fail(SP_ERR_INVALID_ARG, "n_layers=%d of %d heads", n_layers, c.n_kv_heads);
+    const int64_t unit = 16 / (c.f32 ? 4 : 2);
+    // (in double: the product may pass 64 bits)
+    const double layer = (double)c.n_pages * c.n_kv_heads * (1 << c.log_page) * c.head_dim;
+    if (n_layers > 1 && (layer_stride < 0 || (double)layer_stride < layer || layer_stride % unit || (double)layer_stride * n_layers > 4e18))
+        return fail(SP_ERR_INVALID_ARG, "layer_stride=%lld: a multiple of 16 bytes that holds a layer", (long long)layer_stride);
+    return SP_OK;
+}
+// whether two ranges of 32-bit words meet
+inline bool meet(const void* p, int64_t np, const void* q, int64_t nq) {
+    return p && q && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)np;
+}
+size_t tree_table_bytes(int32_t n_groups, int32_t n_seqs) { return align256(((size_t)n_groups + n_seqs + 2) * 4); }
+}  // namespace
+
+size_t sp_attn_tree_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int64_t total_new, int32_t n_q_heads, int32_t n_kv_heads,
+                                           int32_t head_dim, sp_dtype dtype) {
+    if (n_groups < 1 || n_seqs < 1 || total_new < 0 || total_new > 0x7fffffffLL || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads ||
+        (head_dim != 64 && head_dim != 128) || (dtype != SP_BF16 && dtype != SP_F32)) return 0;
+    return TAG_BYTES + tree_table_bytes(n_groups, n_seqs);
+}
+
+sp_status sp_attn_tree_decode(const sp_kv_cache* cache, const void* q, void* o, float* lse, int32_t n_q_heads, int32_t n_groups, int32_t n_seqs,
+                              const int32_t* Gs, const int32_t* new_lens, const uint32_t* ancestors, int64_t mask_stride,
+                              const int32_t* prompt_tables, int32_t prompt_width, const int32_t* prompt_lens,
+                              const int32_t* resp_tables, int32_t resp_width, const int32_t* resp_lens, float softmax_scale,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    sp::KvCache c;
+    sp_status st = check_cache(cache, c);
+    if (st != SP_OK) return st;
+    if (!q || !o || !lse) return fail(SP_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (misaligned(q) || misaligned(o)) return fail(SP_ERR_INVALID_ARG, "tensor pointer is not 16-byte aligned");
+    if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % c.n_kv_heads != 0)
+        return fail(SP_ERR_INVALID_ARG, "n_q_heads=%d must be a positive multiple of n_kv_heads=%d", n_q_heads, c.n_kv_heads);
+    if (!std::isfinite(softmax_scale) || softmax_scale <= 0.f) return fail(SP_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    if (!std::isfinite(softmax_scale * sp::LOG2E)) return fail(SP_ERR_INVALID_ARG, "softmax_scale times log2(e) is not finite");
+    st = check_members(n_groups, n_seqs, Gs);
+    if (st != SP_OK) return st;
+    if (!new_lens) return fail(SP_ERR_INVALID_ARG, "new_lens is NULL");
+    int64_t total = 0;
+    int32_t longest = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+        if (new_lens[s] < 0 || new_lens[s] > SP_MAX_DRAFT) return fail(SP_ERR_INVALID_ARG, "sequence %d: new_lens=%d (0 to %d)", s, new_lens[s], SP_MAX_DRAFT);
+        total += new_lens[s];
+        longest = std::max(longest, new_lens[s]);
+    }
+    if (ancestors ? mask_stride < (longest + 31) / 32 : mask_stride != 0)
+        return fail(SP_ERR_INVALID_ARG, "mask_stride=%lld words do not hold %d bits", (long long)mask_stride, longest);
+    if (prompt_width < 0 || resp_width < 0 || (prompt_width > 0) != (prompt_tables != nullptr) || (prompt_width > 0) != (prompt_lens != nullptr) ||
+        (resp_width > 0) != (resp_tables != nullptr) || !resp_lens)
+        return fail(SP_ERR_INVALID_ARG, "prompt_tables, prompt_lens and prompt_width, and resp_tables and resp_width, go together; resp_lens is needed");
+    if (off4(prompt_tables) || off4(prompt_lens) || off4(resp_tables) || off4(resp_lens) || off4(lse) || off4(ancestors))
+        return fail(SP_ERR_INVALID_ARG, "a 32-bit array is not 4-byte aligned");
+    if (total * n_q_heads > 0x7fffffffLL) return fail(SP_ERR_INVALID_ARG, "%lld tokens of %d heads: more than one call serves", (long long)total, n_q_heads);
+    const size_t need = sp_attn_tree_decode_workspace_bytes(n_groups, n_seqs, total, n_q_heads, c.n_kv_heads, c.head_dim, cache->dtype);
+    if (!workspace || misaligned(workspace) || workspace_bytes < need)
+        return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
+    if (total == 0) return SP_OK;
+    hipStream_t s = (hipStream_t)stream;
+    try {
+        std::vector<int32_t> words((size_t)n_groups + n_seqs + 2);
+        int32_t* const first = words.data() + n_groups + 1;
+        first[0] = 0;
+        for (int i = 0; i < n_seqs; ++i) first[i + 1] = first[i] + new_lens[i];
+        int seq = 0;
+        for (int g = 0; g < n_groups; ++g) { words[g] = first[seq]; seq += Gs ? Gs[g] : 1; }
+        words[n_groups] = (int32_t)total;
+        hipError_t e = sp::launch_prepare(words.data(), (int)words.size(), table_of(workspace), (uint32_t*)workspace, sp::ReserveTag{}, sp::TAG_CLEAR, false,
+                                          n_groups, total, 0, 0, sp::Schedule{}, sp::KEYS_AS_PACKED, s);
+        if (e == hipSuccess)
+            e = sp::launch_tree(c, q, o, lse, n_q_heads, n_groups, n_seqs, (int)total, table_of(workspace), ancestors, mask_stride, prompt_tables, prompt_width,
+                                prompt_lens, resp_tables, resp_width, resp_lens, softmax_scale, s);
+        if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+        return SP_OK;
+    } catch (const std::exception&) {
+        return fail(SP_ERR_INVALID_ARG, "no host memory for %d sequences", n_seqs);
+    }
+}
+
+sp_status sp_attn_cache_keep(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t n_seqs, const int32_t* tables,
+                             int32_t table_width, const int32_t* lens, const int32_t* kept, int32_t kept_width, const int32_t* n_kept,
+                             int32_t* lens_out, void* stream) {
+    g_err[0] = 0;
+    sp::KvCache c;
+    const sp_status st = check_layers(cache, n_layers, layer_stride, c);
+    if (st != SP_OK) return st;
+    if (n_seqs < 1 || table_width < 1 || kept_width < 0) return fail(SP_ERR_INVALID_ARG, "n_seqs=%d, table_width=%d, kept_width=%d", n_seqs, table_width, kept_width);
+    if (!tables || !lens || !n_kept || !lens_out || (kept_width > 0 && !kept)) return fail(SP_ERR_INVALID_ARG, "an array is NULL");
+    if (off4(tables) || off4(lens) || off4(kept) || off4(n_kept) || off4(lens_out)) return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
+    if (meet(lens_out, n_seqs, lens, n_seqs) || meet(lens_out, n_seqs, n_kept, n_seqs) || meet(lens_out, n_seqs, tables, (int64_t)n_seqs * table_width) ||
+        meet(lens_out, n_seqs, kept, (int64_t)n_seqs * kept_width))
+        return fail(SP_ERR_INVALID_ARG, "lens_out must not overlap lens, kept, n_kept or tables");
+    const hipError_t e = sp::launch_keep(c, n_layers, layer_stride, n_seqs, tables, table_width, lens, kept, kept_width, n_kept, lens_out, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+    return SP_OK;
+}
+
+size_t sp_attn_pages_workspace_bytes(int64_t n_pages, int32_t n_seqs) {
+    if (n_pages < 1 || n_pages > 0x7fffffffLL || n_seqs < 1) return 0;
+    return TAG_BYTES + sp::pages_room_bytes(n_pages, n_seqs);
+}
+
+sp_status sp_attn_pages_fit(int32_t* refs, int64_t n_pages, int32_t page_size, int32_t n_seqs, int32_t* tables, int32_t table_width,
+                            const int32_t* lens, int32_t* missing, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    if (n_pages < 1 || n_pages > 0x7fffffffLL) return fail(SP_ERR_INVALID_ARG, "n_pages=%lld", (long long)n_pages);
+    int log_page = 4;
+    while (log_page <= 8 && (1 << log_page) != page_size) ++log_page;
+    if (log_page > 8) return fail(SP_ERR_UNSUPPORTED, "page_size=%d (16, 32, 64, 128 or 256)", page_size);
+    if (n_seqs < 1 || table_width < 1) return fail(SP_ERR_INVALID_ARG, "n_seqs=%d, table_width=%d", n_seqs, table_width);
+    if (!refs || !tables || !lens) return fail(SP_ERR_INVALID_ARG, "an array is NULL");
+    if (off4(refs) || off4(tables) || off4(lens) || off4(missing)) return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
+    const int64_t entries = (int64_t)n_seqs * table_width;
+    if (meet(refs, n_pages, tables, entries) || meet(refs, n_pages, lens, n_seqs) || meet(tables, entries, lens, n_seqs) ||
+        meet(missing, 1, refs, n_pages) || meet(missing, 1, tables, entries) || meet(missing, 1, lens, n_seqs))
+        return fail(SP_ERR_INVALID_ARG, "refs, tables, lens and missing must not overlap");
+    const size_t need = sp_attn_pages_workspace_bytes(n_pages, n_seqs);
+    if (!workspace || misaligned(workspace) || workspace_bytes < need)
+        return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
+    const hipError_t e = sp::launch_fit(refs, n_pages, log_page, n_seqs, tables, table_width, lens, missing, (uint32_t*)workspace, (char*)workspace + TAG_BYTES,
+                                        (hipStream_t)stream);
+    if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+    return SP_OK;
+}
+
+sp_status sp_attn_cache_fork(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t* refs, int32_t n_seqs, const int32_t* parents,
+                             int32_t n_src, const int32_t* src_tables, int32_t src_width, const int32_t* src_lens, int32_t* tables,
+                             int32_t table_width, int32_t* lens_out, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    sp::KvCache c;
+    const sp_status st = check_layers(cache, n_layers, layer_stride, c);
+    if (st != SP_OK) return st;
+    if (n_layers > 32767) return fail(SP_ERR_INVALID_ARG, "n_layers=%d", n_layers);
+    if (n_seqs < 1 || n_src < 1 || src_width < 1 || table_width < 1)
+        return fail(SP_ERR_INVALID_ARG, "n_seqs=%d, n_src=%d, src_width=%d, table_width=%d", n_seqs, n_src, src_width, table_width);
+    if (!refs || !parents || !src_tables || !src_lens || !tables || !lens_out) return fail(SP_ERR_INVALID_ARG, "an array is NULL");
+    const struct { const void* p; int64_t n; bool written; } arrays[] = {
+        {refs, c.n_pages, true}, {tables, (int64_t)n_seqs * table_width, true}, {lens_out, n_seqs, true},
+        {parents, n_seqs, false}, {src_tables, (int64_t)n_src * src_width, false}, {src_lens, n_src, false}};
+    for (int i = 0; i < 6; ++i) {
+        if (off4(arrays[i].p)) return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
+        for (int j = 0; j < i; ++j)
+            if (arrays[j].written && meet(arrays[i].p, arrays[i].n, arrays[j].p, arrays[j].n))
+                return fail(SP_ERR_INVALID_ARG, "refs, tables and lens_out must not overlap each other or what the call reads");
+    }
+    const size_t need = sp_attn_pages_workspace_bytes(c.n_pages, n_seqs);
+    if (!workspace || misaligned(workspace) || workspace_bytes < need)
+        return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
+    const hipError_t e = sp::launch_fork(c, n_layers, layer_stride, refs, n_seqs, parents, n_src, src_tables, src_width, src_lens, tables, table_width, lens_out,
+                                         (uint32_t*)workspace, (char*)workspace + TAG_BYTES, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
+    return SP_OK;
+}
+
 sp_status sp_attn_adjust_logits(const void* logits, int64_t logits_stride, void* out, int64_t out_stride, int64_t vocab,
                                 const sp_logit_rules* rules, const uint32_t* mask, int64_t mask_stride, int32_t n_groups, int32_t n_seqs,
                                 const int32_t* Gs, const int32_t* prompt_tokens, int32_t prompt_stride, const int32_t* prompt_lens,

@@ -379,6 +379,20 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
                          const int* prompt_tables, int prompt_width, const int* prompt_lens, const int* resp_tables, int resp_width,
                          const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s);
 
+// starts: first token of each group, the number of tokens, first token of each sequence, the number of tokens (device memory).
+hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int* starts,
+                       const uint32_t* ancestors, int64_t mask_stride, const int* prompt_tables, int prompt_width, const int* prompt_lens,
+                       const int* resp_tables, int resp_width, const int* resp_lens, float scale, hipStream_t s);
+
+// Pages (sp_pages.hip).  layer_stride: elements from layer to layer.  room: pages_room_bytes() bytes.
+size_t pages_room_bytes(int64_t n_pages, int n_seqs);
+hipError_t launch_keep(const KvCache& cache, int n_layers, int64_t layer_stride, int n_seqs, const int* tables, int width, const int* lens,
+                       const int* kept, int kept_width, const int* n_kept, int* lens_out, hipStream_t s);
+hipError_t launch_fit(int* refs, int64_t n_pages, int log_page, int n_seqs, int* tables, int width, const int* lens, int* missing, uint32_t* tag,
+                      void* room, hipStream_t s);
+hipError_t launch_fork(const KvCache& cache, int n_layers, int64_t layer_stride, int* refs, int n_seqs, const int* parents, int n_src, const int* src_tables,
+                       int src_width, const int* src_lens, int* tables, int width, int* lens_out, uint32_t* tag, void* room, hipStream_t s);
+
 // Rules of adjusted logits (sp_logit_rules)
 struct AdjustRules { float repetition, inv_repetition, presence, frequency, inv_temperature; const float* bias; };
 hipError_t launch_adjust_logits(const void* logits, int64_t stride, void* out, int64_t out_stride, int64_t vocab, const AdjustRules& rules,

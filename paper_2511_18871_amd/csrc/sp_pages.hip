@@ -1,0 +1,357 @@
+// Pages of the paged cache when sequences branch: keeping the accepted ones of drafted tokens, forking sequences, and fitting tables of
+// pages to their sequences' lengths.  A page is free while no table holds it (its count in `refs` is 0); free pages are given out
+// in ascending order, to requests in the order of their sequences and places, so that results do not depend on how the work is dealt.
+#include "sp_common.hpp"
+#include "sp_launch.hpp"
+#include <algorithm>
+
+namespace sp {
+namespace {
+
+constexpr int CHUNK = 4096;        // pages whose free ones are counted together: 64 words of 64 bits
+typedef unsigned long long u64;
+
+// inclusive sums over the lanes of a wave
+__device__ __forceinline__ int scan_lanes(int x) {
+    const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o, 64); x += l >= o ? y : 0; }
+    return x;
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+__device__ __forceinline__ u64 ballot(bool b) { return __builtin_amdgcn_ballot_w64(b); }
+__device__ __forceinline__ int lanes_below(u64 set) { return __popcll(set & ((1ull << (threadIdx.x & 63)) - 1)); }
+
+// ---- keep ----------------------------------------------------------------------------------------------------
+
+struct KeepArgs {
+    char* k; char* v;
+    int64_t layer_bytes;                   // from layer to layer
+    const int* tables; const int* lens; const int* kept; const int* n_kept; int* lens_out;
+    int64_t width, capacity, n_pages, kept_width;
+    int n_seqs, items, Hkv, log_page;      // items: layers * 2 * Hkv of a sequence
+    Div heads;
+};
+
+// Token lens + kept[i] of a sequence becomes its token lens + i.  A wave takes a (layer, K or V, head) of a sequence and moves its rows in
+// order, 64 lanes of 16 bytes at a time.  kept ascends, so kept[j] >= j > i for j > i: a row is read before or in the step in which it is
+// written over, and no row that a later step reads has been written.
+template <int ROW>        // bytes of a row
+__global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
+    constexpr int LANES = ROW / 16, ROWS = 64 / LANES;
+    const int l = threadIdx.x & 63, seq = blockIdx.x;
+    const int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (item >= a.items) return;
+    const int64_t have = a.lens[seq];
+    const int* const kept = a.kept + seq * a.kept_width;
+    const int most = have < 0 ? 0 : (int)min((int64_t)max(a.n_kept[seq], 0), a.kept_width);
+    int n = 0;                             // of the list up to its first entry that does not ascend or that the table has no room for
+    while (n < most) {
+        const int i = n + l;
+        bool good = false;
+        if (i < most) {
+            const int x = kept[i], before = i > 0 ? kept[i - 1] : -1;
+            good = x > before && have + x < a.capacity;
+        }
+        const u64 bad = ~ballot(good);
+        const int run = bad ? __ffsll(bad) - 1 : 64;
+        n += run;
+        if (run < 64) break;
+    }
+    if (item == 0 && l == 0) a.lens_out[seq] = (int)(have + n);
+    unsigned head;
+    const int lk = (int)divmod((unsigned)item, a.heads, head);
+    char* const base = (lk & 1 ? a.v : a.k) + (lk >> 1) * a.layer_bytes;
+    const int* const table = a.tables + seq * a.width;
+    auto row_of = [&](int64_t j) -> char* {
+        const int64_t page = table[j >> a.log_page];
+        if (page < 0 || page >= a.n_pages) return nullptr;
+        return base + (((page * a.Hkv + head) << a.log_page) + (j & ((1 << a.log_page) - 1))) * ROW + (l % LANES) * 16;
+    };
+    for (int i0 = 0; i0 < n; i0 += ROWS) {
+        const int i = i0 + l / LANES;
+        if (i >= n) continue;
+        const int from = kept[i];
+        if (from == i) continue;
+        const char* const src = row_of(have + from);
+        char* const dst = row_of(have + i);
+        if (src && dst) *reinterpret_cast<i32x4*>(dst) = *reinterpret_cast<const i32x4*>(src);
+    }
+}
+
+// ---- free pages ------------------------------------------------------------------------------------------------
+
+struct Pool { int* refs; u64* free; int* counts; int64_t n_pages; int n_chunks; };      // free: a bit per page; counts: of each chunk
+
+// which pages of chunk `c` are free, and how many (256 threads)
+__device__ __forceinline__ void count_chunk(const Pool& p, int64_t c, int* sh) {
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+    int sum = 0;
+#pragma unroll 4
+    for (int i = 0; i < CHUNK / 256; ++i) {
+        const int64_t page = c * CHUNK + i * 256 + threadIdx.x;
+        const u64 set = ballot(page < p.n_pages && p.refs[page] == 0);
+        sum += __popcll(set);
+        if (l == 0) p.free[c * 64 + i * 4 + w] = set;
+    }
+    if (l == 0) sh[w] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) p.counts[c] = sh[0] + sh[1] + sh[2] + sh[3];
+}
+
+// The free pages that requests first .. first + n - 1 get, n <= 64, in the wave's slots (-1: none is left).  A lane holds one of a chunk's 64
+// words and deals out its bits.
+__device__ __forceinline__ void take_pages(const Pool& p, int64_t first, int n, int* slots) {
+    const int l = threadIdx.x & 63;
+    slots[l] = -1;
+    int64_t before = 0;                    // free pages ahead of the chunk
+    int given = 0;
+    for (int64_t c0 = 0; c0 < p.n_chunks && given < n; c0 += 64) {
+        const int mine = c0 + l < p.n_chunks ? p.counts[c0 + l] : 0, to = scan_lanes(mine);
+        if (before + last_lane(to) > first + given) {
+            u64 here = ballot(mine > 0 && before + to > first + given && before + to - mine < first + n);
+            while (here) {
+                const int k = __ffsll(here) - 1;
+                here &= here - 1;
+                const int64_t ahead = before + __builtin_amdgcn_readlane(to - mine, k);
+                u64 bits = p.free[(c0 + k) * 64 + l];
+                const int mask = __popcll(bits);
+                int64_t nth = ahead + scan_lanes(mask) - mask - first;
+                for (; bits; bits &= bits - 1, ++nth)
+                    if (nth >= 0 && nth < n) slots[nth] = (int)((c0 + k) * CHUNK + l * 64 + __ffsll(bits) - 1);
+                given = (int)min((int64_t)n, ahead + __builtin_amdgcn_readlane(mine, k) - first);
+            }
+        }
+        before += last_lane(to);
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// ---- fit -------------------------------------------------------------------------------------------------------
+
+struct FitArgs {
+    Pool pool;
+    int* tables; const int* lens; int* missing; int* wants; uint32_t* tag;
+    int64_t width; int n_seqs, log_page;
+    Div unused;
+};
+__device__ __forceinline__ int64_t pages_needed(const FitArgs& a, int seq) {
+    const int64_t n = a.lens[seq];
+    return n < 0 ? -1 : min((n + (1 << a.log_page) - 1) >> a.log_page, a.width);
+}
+
+// One wave per sequence: what lies behind its last page goes back, and its empty places ahead are counted.
+__global__ __launch_bounds__(256) void release_kernel(FitArgs a) {
+    const int l = threadIdx.x & 63, seq = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
+    if (seq >= a.n_seqs) return;
+    const int64_t need = pages_needed(a, seq);
+    int wants = 0;
+    for (int64_t c0 = 0; need >= 0 && c0 < a.width; c0 += 64) {
+        const int64_t c = c0 + l;
+        const int page = c < a.width ? a.tables[seq * a.width + c] : -1;
+        const bool held = page >= 0 && page < a.pool.n_pages;
+        wants += __popcll(ballot(c < need && !held));
+        if (c < a.width && c >= need && page != -1) {
+            if (held) atomicSub(&a.pool.refs[page], 1);
+            a.tables[seq * a.width + c] = -1;
+        }
+    }
+    if (l == 0) a.wants[seq] = wants;
+}
+
+__global__ __launch_bounds__(256) void count_free_kernel(Pool p) {
+    __shared__ int sh[4];
+    count_chunk(p, blockIdx.x, sh);
+}
+
+// One wave per sequence: its empty places get pages.  The first workgroup says how many places of all got none.
+__global__ __launch_bounds__(256) void assign_kernel(FitArgs a) {
+    __shared__ int slots[4][64];
+    __shared__ int sh[4];
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), seq0 = (int)blockIdx.x * 4, seq = seq0 + w;
+    auto over_workgroup = [&](int x) {
+        x = last_lane(scan_lanes(x));
+        __syncthreads();
+        if (l == 0) sh[w] = x;
+        __syncthreads();
+        return sh[0] + sh[1] + sh[2] + sh[3];
+    };
+    if (blockIdx.x == 0 && a.missing) {
+        int all = 0, free = 0;
+        for (int s = threadIdx.x; s < a.n_seqs; s += 256) all += a.wants[s];
+        for (int c = threadIdx.x; c < a.pool.n_chunks; c += 256) free += a.pool.counts[c];
+        all = over_workgroup(all);
+        free = over_workgroup(free);
+        if (threadIdx.x == 0) a.missing[0] = max(0, all - free);
+    }
+    int ahead = 0;
+    for (int s = threadIdx.x; s < seq0; s += 256) ahead += a.wants[s];
+    ahead = over_workgroup(ahead);
+    if (seq >= a.n_seqs) return;
+    for (int s = seq0; s < seq; ++s) ahead += a.wants[s];
+    int left = a.wants[seq];
+    const int64_t need = pages_needed(a, seq);
+    for (int64_t c0 = 0; left > 0 && c0 < need; c0 += 64) {
+        const int64_t c = c0 + l;
+        int* const at = a.tables + seq * a.width + c;
+        const int page = c < need ? *at : 0;
+        const bool empty = c < need && (page < 0 || page >= a.pool.n_pages);
+        const u64 set = ballot(empty);
+        const int n = __popcll(set);
+        if (n == 0) continue;
+        take_pages(a.pool, ahead, n, slots[w]);
+        if (empty) {
+            const int got = slots[w][lanes_below(set)];
+            *at = got;
+            if (got >= 0) a.pool.refs[got] = 1;
+        }
+        ahead += n;
+        left -= n;
+    }
+}
+
+// ---- fork ------------------------------------------------------------------------------------------------------
+
+struct ForkArgs {
+    Pool pool;
+    char* k; char* v;
+    int64_t layer_bytes, row_bytes;
+    const int* parents; const int* src_tables; const int* src_lens;
+    int* tables; int* lens_out; int* order; uint32_t* tag;
+    int64_t src_width, width, capacity;    // capacity: tokens that both tables hold
+    int n_seqs, n_src, Hkv, log_page;
+};
+struct Child { int parent; int64_t len, whole; int rest; bool takes; int last; };      // takes: a page for the `rest` tokens of page `last`
+__device__ __forceinline__ Child child_of(const ForkArgs& a, int seq) {
+    Child c{-1, 0, 0, 0, false, -1};
+    const int parent = a.parents[seq];
+    if (parent < 0 || parent >= a.n_src) return c;
+    c.parent = parent;
+    c.len = min((int64_t)a.src_lens[parent], a.capacity);
+    if (c.len < 0) return c;
+    c.whole = c.len >> a.log_page;
+    c.rest = (int)(c.len & ((1 << a.log_page) - 1));
+    if (c.rest) c.last = a.src_tables[parent * a.src_width + c.whole];
+    c.takes = c.rest && c.last >= 0 && c.last < a.pool.n_pages;
+    return c;
+}
+
+// Counts free pages; one workgroup more numbers the children that need one.
+__global__ __launch_bounds__(256) void fork_count_kernel(ForkArgs a) {
+    __shared__ int sh[4];
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if ((int)blockIdx.x < a.pool.n_chunks) { count_chunk(a.pool, blockIdx.x, sh); return; }
+    if (threadIdx.x < 64) a.tag[l] = 0u;
+    int before = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 256) {
+        const int s = s0 + threadIdx.x;
+        const bool takes = s < a.n_seqs && child_of(a, s).takes;
+        const u64 set = ballot(takes);
+        __syncthreads();
+        if (l == 0) sh[w] = __popcll(set);
+        __syncthreads();
+        int at = before + lanes_below(set);
+        for (int i = 0; i < 4; ++i) { at += i < w ? sh[i] : 0; before += sh[i]; }
+        if (s < a.n_seqs) a.order[s] = at;
+    }
+}
+
+// A workgroup takes K or V of a layer of a child, and copies the tokens of its last page; the first of a child writes its table.
+__global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
+    __shared__ int slots[64];
+    const int seq = blockIdx.x, layer = blockIdx.y >> 1;
+    const Child c = child_of(a, seq);
+    if (c.parent < 0) return;
+    const bool tells = blockIdx.y == 0;
+    if (!tells && !c.takes) return;
+    int to = -1;
+    if (c.takes) {
+        if (threadIdx.x < 64) take_pages(a.pool, a.order[seq], 1, slots);
+        __syncthreads();
+        to = __builtin_amdgcn_readfirstlane(slots[0]);
+    }
+    const bool none = c.takes && to < 0;
+    if (tells) {
+        if (threadIdx.x == 0) a.lens_out[seq] = none ? -1 : (int)c.len;
+        for (int64_t i = threadIdx.x; i < a.width; i += 256) {
+            int page = -1;
+            if (!none && c.len >= 0 && i < c.whole) {
+                page = a.src_tables[c.parent * a.src_width + i];
+                if (page >= 0 && page < a.pool.n_pages) atomicAdd(&a.pool.refs[page], 1);
+            } else if (!none && c.rest && i == c.whole) {
+                page = c.takes ? to : c.last;
+                if (c.takes) a.pool.refs[to] = 1;
+            }
+            a.tables[seq * a.width + i] = page;
+        }
+    }
+    if (to < 0) return;
+    char* const base = (blockIdx.y & 1 ? a.v : a.k) + layer * a.layer_bytes;
+    const int64_t page_bytes = a.row_bytes << a.log_page, granules = c.rest * a.row_bytes / 16;
+    for (int h = 0; h < a.Hkv; ++h) {
+        const i32x4* const src = reinterpret_cast<const i32x4*>(base + ((int64_t)c.last * a.Hkv + h) * page_bytes);
+        i32x4* const dst = reinterpret_cast<i32x4*>(base + ((int64_t)to * a.Hkv + h) * page_bytes);
+        for (int64_t i = threadIdx.x; i < granules; i += 256) dst[i] = src[i];
+    }
+}
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+int64_t chunks_of(int64_t n_pages) { return (n_pages + CHUNK - 1) / CHUNK; }
+
+// behind the tag: a word per sequence, bits of the free pages, counts
+Pool make_pool(int* refs, int64_t n_pages, int n_seqs, void* room) {
+    char* const at = (char*)room + up256((size_t)n_seqs * 4);
+    const int64_t chunks = chunks_of(n_pages);
+    return Pool{refs, (u64*)at, (int*)(at + (size_t)chunks * 512), n_pages, (int)chunks};
+}
+
+}  // namespace
+
+size_t pages_room_bytes(int64_t n_pages, int n_seqs) { return up256((size_t)n_seqs * 4) + (size_t)chunks_of(n_pages) * 516; }
+
+hipError_t launch_keep(const KvCache& cache, int n_layers, int64_t layer_stride, int n_seqs, const int* tables, int width, const int* lens,
+                       const int* kept, int kept_width, const int* n_kept, int* lens_out, hipStream_t s) {
+    const int elem = cache.f32 ? 4 : 2, row = cache.head_dim * elem;
+    KeepArgs a{};
+    a.k = (char*)cache.k; a.v = (char*)cache.v; a.layer_bytes = layer_stride * elem;
+    a.tables = tables; a.lens = lens; a.kept = kept; a.n_kept = n_kept; a.lens_out = lens_out;
+    a.width = width; a.capacity = std::min<int64_t>((int64_t)width << cache.log_page, MAX_TOKENS); a.n_pages = cache.n_pages; a.kept_width = kept_width;
+    a.n_seqs = n_seqs; a.items = n_layers * 2 * cache.n_kv_heads; a.Hkv = cache.n_kv_heads; a.log_page = cache.log_page;
+    a.heads = make_div(cache.n_kv_heads);
+    const dim3 grid((unsigned)n_seqs, (unsigned)((a.items + 3) / 4));
+    if (row == 128) hipLaunchKernelGGL(keep_kernel<128>, grid, dim3(256), 0, s, a);
+    else if (row == 256) hipLaunchKernelGGL(keep_kernel<256>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(keep_kernel<512>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_fit(int* refs, int64_t n_pages, int log_page, int n_seqs, int* tables, int width, const int* lens, int* missing, uint32_t* tag,
+                      void* room, hipStream_t s) {
+    FitArgs a{};
+    a.pool = make_pool(refs, n_pages, n_seqs, room);
+    a.tables = tables; a.lens = lens; a.missing = missing; a.wants = (int*)room; a.tag = tag;
+    a.width = width; a.n_seqs = n_seqs; a.log_page = log_page;
+    const dim3 waves((unsigned)((n_seqs + 3) / 4));
+    hipLaunchKernelGGL(release_kernel, waves, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(count_free_kernel, dim3((unsigned)a.pool.n_chunks), dim3(256), 0, s, a.pool);
+    hipLaunchKernelGGL(assign_kernel, waves, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_fork(const KvCache& cache, int n_layers, int64_t layer_stride, int* refs, int n_seqs, const int* parents, int n_src, const int* src_tables,
+                       int src_width, const int* src_lens, int* tables, int width, int* lens_out, uint32_t* tag, void* room, hipStream_t s) {
+    const int elem = cache.f32 ? 4 : 2;
+    ForkArgs a{};
+    a.pool = make_pool(refs, cache.n_pages, n_seqs, room);
+    a.k = (char*)cache.k; a.v = (char*)cache.v; a.layer_bytes = layer_stride * elem; a.row_bytes = (int64_t)cache.head_dim * elem;
+    a.parents = parents; a.src_tables = src_tables; a.src_lens = src_lens; a.tables = tables; a.lens_out = lens_out; a.order = (int*)room; a.tag = tag;
+    a.src_width = src_width; a.width = width; a.capacity = std::min<int64_t>((int64_t)std::min(src_width, width) << cache.log_page, MAX_TOKENS);
+    a.n_seqs = n_seqs; a.n_src = n_src; a.Hkv = cache.n_kv_heads; a.log_page = cache.log_page;
+    hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)a.pool.n_chunks + 1), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n_seqs, (unsigned)(2 * n_layers)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace sp

@@ -1,0 +1,202 @@
+"""Pages of sequences that branch, on the GPU, against the oracle: whole numbers and copied rows are equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rollout_oracle as ro
+from paper_2511_18871_amd import binding as B
+from tests.branching import dev32
+from tests.rollout import make_tables, numpy64
+
+pytestmark = pytest.mark.gpu
+TYPES = [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 128), (torch.float32, 64)]
+
+
+def layers(gen, n, pages, hkv, page, d, dtype):
+    return [torch.randn(n, pages, hkv, page, d, generator=gen).to(dtype) for _ in range(2)]
+
+
+def check_keep(k, v, tables, lens, kept, n_kept, single=False):
+    kd, vd = k.cuda(), v.cuda()
+    cache = B.KvCache(kd[0], vd[0]) if single else B.KvLayers(kd, vd)
+    out = B.sp_attn_cache_keep(cache, tables.cuda(), dev32(lens), dev32(kept).view(len(lens), -1), dev32(n_kept))
+    torch.cuda.synchronize()
+    want, now = ro.cache_keep([numpy64(k), numpy64(v)], tables.tolist(), lens, kept, n_kept)
+    assert out.tolist() == now
+    assert np.array_equal(numpy64(kd), want[0]) and np.array_equal(numpy64(vd), want[1])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_keep(dtype, d, page):
+    gen = torch.Generator().manual_seed(page)
+    lens, nodes = [0, 1, 15, 16, 40, 250, -1, 33, 7], 40
+    tables, pages = make_tables(gen, [n + nodes if n >= 0 else 0 for n in lens], page)
+    k, v = layers(gen, 3, pages, 3, page, d, dtype)
+    kept, n_kept = [], [0, 1, 40, 7, 13, 21, 5, 39, 2]
+    for n in n_kept:
+        path = sorted(torch.randperm(nodes, generator=gen)[:n].tolist())
+        kept.append(path + [-9] * (nodes - n))
+    check_keep(k, v, tables, lens, kept, n_kept)
+    check_keep(k[:1], v[:1], tables, lens, kept, n_kept, single=True)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES[:3])
+def test_keep_long_lists_that_end_early(dtype, d):
+    """More entries than lanes; lists that do not ascend, are negative, or leave the table; counts beyond the list; pages that the cache does not have."""
+    gen = torch.Generator().manual_seed(2)
+    lens, nodes, page = [3, 30, 0, 100, 2 ** 31 - 1, 60, 5], 300, 32
+    tables, pages = make_tables(gen, [340] * 7, page)
+    k, v = layers(gen, 2, pages, 2, page, d, dtype)
+    kept = [sorted(torch.randperm(nodes, generator=gen)[:200].tolist()) for _ in lens]
+    kept[1][70] = kept[1][69]
+    kept[2][130] = -1
+    kept[3][150:] = range(400, 450)
+    kept[5][64] = 5
+    tables[6, 2] = pages
+    tables[6, 4] = -1
+    n_kept = [200, 200, 200, 200, 10, 2 ** 31 - 1, 199]
+    check_keep(k, v, tables, lens, kept, n_kept)
+    check_keep(k, v, tables, lens, [x[:0] for x in kept], n_kept)
+
+
+def test_keep_layers_with_room_between_them():
+    gen = torch.Generator().manual_seed(4)
+    tables, pages = make_tables(gen, [50, 60], 16)
+    k, v = layers(gen, 4, pages, 2, 16, 64, torch.bfloat16)
+    kd, vd = k.cuda(), v.cuda()
+    every_other = B.KvLayers(kd[::2], vd[::2])
+    assert len(every_other) == 2 and torch.equal(every_other[1].k, kd[2])
+    args = ([10, 20], [[1, 5, 30], [0, 2, 4]], [3, 2])
+    out = B.sp_attn_cache_keep(every_other, tables.cuda(), dev32(args[0]), dev32(args[1]), dev32(args[2]))
+    want, now = ro.cache_keep([numpy64(k[::2]), numpy64(v[::2])], tables.tolist(), *args)
+    assert out.tolist() == now and torch.equal(kd[1::2].cpu(), k[1::2])
+    assert np.array_equal(numpy64(kd[::2]), want[0]) and np.array_equal(numpy64(vd[::2]), want[1])
+
+
+def check_fit(refs, page, tables, lens):
+    r, t = dev32(refs), dev32(tables)
+    missing = B.sp_attn_pages_fit(r, page, t, dev32(lens))
+    torch.cuda.synchronize()
+    want_r, want_t, want_m = ro.pages_fit(refs, page, tables, lens)
+    assert missing.item() == want_m and t.tolist() == want_t and r.tolist() == want_r
+    return want_r, want_t
+
+
+@pytest.mark.parametrize("n_seqs,width,pages", [(1, 1, 1), (3, 5, 7), (5, 70, 400), (33, 40, 1000), (300, 9, 4096), (64, 200, 9000), (1100, 20, 20000)])
+def test_fit_step_by_step(n_seqs, width, pages):
+    """Tables that grow, shrink, end and begin, with too few pages at times."""
+    rng = np.random.default_rng(n_seqs)
+    for page in (16, 128):
+        refs, tables = [0] * pages, [[-1] * width for _ in range(n_seqs)]
+        refs[pages // 2] = -1                                           # out of use
+        for step in range(6):
+            lens = [int(x) for x in rng.integers(0, width * page + 40, n_seqs)]
+            for s in range(n_seqs):
+                if rng.random() < 0.2:
+                    lens[s] = (0, -1, -2 ** 31, 2 ** 31 - 1)[rng.integers(0, 4)]
+            refs, tables = check_fit(refs, page, tables, lens)
+
+
+def test_fit_shared_pages_holes_and_foreign_places():
+    refs = [2, 1, 0, 3, 1, 0, 0, 1]
+    tables = [[0, 3, 7, -1, 900], [0, 3, -1, 4, 8], [3, -5, 1, -1, -1]]
+    check_fit(refs, 16, tables, [80, 80, 80])
+    check_fit(refs, 16, tables, [0, 0, 0])
+    check_fit(refs, 16, tables, [17, -1, 33])
+    check_fit([1] * 8, 16, tables, [80, 16, 48])
+
+
+@pytest.mark.parametrize("pages", [4095, 4096, 4097, 300000])
+def test_fit_takes_pages_across_chunks(pages):
+    """Free pages that lie apart, in more than 64 chunks too."""
+    rng = np.random.default_rng(pages)
+    refs = (rng.random(pages) < 0.999).astype(int).tolist()
+    refs[0] = refs[pages - 1] = 0
+    check_fit(refs, 32, [[-1] * 100 for _ in range(7)], [int(x) for x in rng.integers(0, 3300, 7)])
+    check_fit([1] * pages, 32, [[-1] * 3], [70])
+    check_fit([1] * (pages - 1) + [0], 32, [[-1] * 3], [70])
+
+
+def check_fork(k, v, refs, parents, src_tables, src_lens, tables, lens_out, single=False):
+    kd, vd, r, t, lo = k.cuda(), v.cuda(), dev32(refs), dev32(tables), dev32(lens_out)
+    cache = B.KvCache(kd[0], vd[0]) if single else B.KvLayers(kd, vd)
+    assert B.sp_attn_cache_fork(cache, r, dev32(parents), dev32(src_tables), dev32(src_lens), t, lens_out=lo) is lo
+    torch.cuda.synchronize()
+    want, want_r, want_t, want_l = ro.cache_fork([numpy64(k), numpy64(v)], refs, parents, src_tables, src_lens, tables, lens_out)
+    assert lo.tolist() == want_l and t.tolist() == want_t and r.tolist() == want_r
+    assert np.array_equal(numpy64(kd), want[0]) and np.array_equal(numpy64(vd), want[1])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_fork(dtype, d, page):
+    gen = torch.Generator().manual_seed(page)
+    src_lens = [0, 1, page, 3 * page - 1, 2 * page + 5, -4, 700]
+    src, pages = make_tables(gen, src_lens, page, spare=12)
+    k, v = layers(gen, 2, pages, 3, page, d, dtype)
+    refs = [sum(p == x for t in src.tolist() for x in t) for p in range(pages)]
+    parents = [3, 3, 6, 0, -1, 4, 1, 2, 5, 7, 6, 6]
+    for width in (src.shape[1], src.shape[1] + 3, 2):
+        check_fork(k, v, refs, parents, src.tolist(), src_lens, [[7] * width for _ in parents], [-8] * 12)
+    check_fork(k[:1], v[:1], refs, parents[:3], src.tolist(), src_lens, [[-1] * 4 for _ in range(3)], [0] * 3, single=True)
+
+
+def test_fork_many_and_out_of_pages():
+    """More children than threads, some of which get no page; parents' places that the cache does not have."""
+    gen = torch.Generator().manual_seed(8)
+    src_lens = [33, 48, 5, 70, 64, 20]
+    src, pages = make_tables(gen, src_lens, 16, spare=200)
+    k, v = layers(gen, 1, pages, 1, 16, 64, torch.bfloat16)
+    refs = [sum(p == x for t in src.tolist() for x in t) for p in range(pages)]
+    src[5, 0], src[5, 1] = pages + 3, -1
+    parents = torch.randint(-1, 6, (700,), generator=gen).tolist()
+    check_fork(k, v, refs, parents, src.tolist(), src_lens, [[-1] * 5 for _ in parents], [-1] * 700)
+
+
+def test_calls_in_a_graph():
+    """Fit, fork and keep captured together, replayed with other lengths and parents, against the same calls made at once."""
+    gen = torch.Generator().manual_seed(5)
+    page, n, pages = 16, 6, 300
+    state = [x.cuda() for x in layers(gen, 2, pages, 2, page, 64, torch.bfloat16)]
+    def fresh():
+        return [x.clone() for x in state] + [dev32([0] * pages), dev32([[-1] * 20] * n), dev32([[-1] * 20] * 8)]
+    def step(s, lens, parents, kept, n_kept, out):
+        k, v, refs, tables, children = s
+        cache = B.KvLayers(k, v)
+        B.sp_attn_pages_fit(refs, page, children, out["none"], missing=out["m0"], workspace=out["ws"])
+        B.sp_attn_pages_fit(refs, page, tables, lens, missing=out["m1"], workspace=out["ws"])
+        B.sp_attn_cache_fork(cache, refs, parents, tables, lens, children, lens_out=out["forked"], workspace=out["ws"])
+        B.sp_attn_cache_keep(cache, tables, lens, kept, n_kept, lens_out=out["kept"])
+    def outputs():
+        return dict(none=dev32([0] * 8), m0=dev32([0]), m1=dev32([0]), forked=dev32([0] * 8), kept=dev32([0] * n),
+                    ws=torch.empty(B.pages_workspace_bytes(pages, 8), dtype=torch.uint8, device="cuda"))
+    eager, graphed, out_e, out_g = fresh(), fresh(), outputs(), outputs()
+    args = [dev32([10, 40, 0, 300, 17, 100]), dev32([0, 1, 3, 3, -1, 5, 4, 1]), dev32([[1, 3, 9]] * n), dev32([3, 2, 1, 0, 3, 3])]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(graphed, *args, out_g)
+    for i in range(5):
+        args[0].copy_(dev32([(37 * i + 61 * s) % 310 for s in range(n)]))
+        args[1].copy_(dev32([(i + s) % 7 - 1 for s in range(8)]))
+        args[3].copy_(dev32([(i + s) % 4 for s in range(n)]))
+        step(eager, *args, out_e)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, graphed))
+        assert all(torch.equal(out_e[x], out_g[x]) for x in ("m0", "m1", "forked", "kept"))
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Keep and fork in the last pages of layers of 2.6 GB each."""
+    d, hkv, page, n_pages = 128, 8, 256, 5000
+    k, v = (torch.empty(2, n_pages, hkv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rows = torch.randn(2, hkv, page, d, device="cuda").bfloat16()
+    k[:, 4998], v[:, 4998] = rows, -rows
+    tables, refs = dev32([[4998]]), dev32([1] * 4999 + [0])
+    out = B.sp_attn_cache_keep(B.KvLayers(k, v), tables, dev32([100]), dev32([[3, 50]]), dev32([2]))
+    rows[:, :, 100], rows[:, :, 101] = rows[:, :, 103].clone(), rows[:, :, 150].clone()
+    assert out.tolist() == [102] and torch.equal(k[:, 4998], rows) and torch.equal(v[:, 4998], -rows)
+    child = dev32([[-1]])
+    assert B.sp_attn_cache_fork(B.KvLayers(k, v), refs, dev32([0]), tables, out, child).tolist() == [102] and child.tolist() == [[4999]]
+    assert torch.equal(k[:, 4999, :, :102], rows[:, :, :102]) and torch.equal(v[:, 4999, :, :102], -rows[:, :, :102])
