@@ -472,7 +472,7 @@ sp_status sp_attn_decode(const sp_kv_cache* cache, const void* q, void* o, float
  *   ancestors     DEVICE uint32 [T, mask_stride], mask_stride >= ceil(largest new_lens / 32) words; NULL (mask_stride 0): a chain, token i
  *                 attends to drafted tokens 0 to i
  *   workspace     DEVICE, at least sp_attn_tree_decode_workspace_bytes(...) bytes, total_new = T; it carries nothing from call to call
- * The rest as sp_attn_decode.  o may be q.  SP_ERR_INVALID_ARG also where T * n_q_heads passes 2^31 - 1 or n_q_heads 65535.  Deterministic. */
+ * The rest as sp_attn_decode.  o may be q.  SP_ERR_INVALID_ARG also where T * n_q_heads passes 2^31 - 1.  Deterministic. */
 #define SP_MAX_DRAFT 1024
 size_t    sp_attn_tree_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int64_t total_new, int32_t n_q_heads, int32_t n_kv_heads,
                                               int32_t head_dim, sp_dtype dtype);

@@ -808,14 +808,13 @@ sp_status check_layers(const sp_kv_cache* cache, int32_t n_layers, int64_t layer
 inline bool meet(const void* p, int64_t np, const void* q, int64_t nq) {
     return p && q && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)np;
 }
-size_t tree_table_bytes(int32_t n_groups, int32_t n_seqs) { return align256(((size_t)n_groups + n_seqs + 2) * 4); }
 }  // namespace
 
 size_t sp_attn_tree_decode_workspace_bytes(int32_t n_groups, int32_t n_seqs, int64_t total_new, int32_t n_q_heads, int32_t n_kv_heads,
                                            int32_t head_dim, sp_dtype dtype) {
-    if (n_groups < 1 || n_seqs < 1 || total_new < 0 || total_new > 0x7fffffffLL || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads ||
+    if (n_groups < 1 || n_seqs < 1 || total_new < 0 || n_q_heads < 1 || total_new > 0x7fffffffLL / n_q_heads || n_kv_heads < 1 || n_q_heads % n_kv_heads ||
         (head_dim != 64 && head_dim != 128) || (dtype != SP_BF16 && dtype != SP_F32)) return 0;
-    return TAG_BYTES + tree_table_bytes(n_groups, n_seqs);
+    return TAG_BYTES + sp::tree_table_bytes(n_groups, n_seqs) + sp::tree_partial_bytes(n_groups, n_seqs, total_new, n_q_heads, n_kv_heads, head_dim, dtype == SP_F32);
 }
 
 sp_status sp_attn_tree_decode(const sp_kv_cache* cache, const void* q, void* o, float* lse, int32_t n_q_heads, int32_t n_groups, int32_t n_seqs,
@@ -829,7 +828,7 @@ sp_status sp_attn_tree_decode(const sp_kv_cache* cache, const void* q, void* o, 
     if (st != SP_OK) return st;
     if (!q || !o || !lse) return fail(SP_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (misaligned(q) || misaligned(o)) return fail(SP_ERR_INVALID_ARG, "tensor pointer is not 16-byte aligned");
-    if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % c.n_kv_heads != 0)
+    if (n_q_heads < 1 || n_q_heads % c.n_kv_heads != 0)
         return fail(SP_ERR_INVALID_ARG, "n_q_heads=%d must be a positive multiple of n_kv_heads=%d", n_q_heads, c.n_kv_heads);
     if (!std::isfinite(softmax_scale) || softmax_scale <= 0.f) return fail(SP_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
     if (!std::isfinite(softmax_scale * sp::LOG2E)) return fail(SP_ERR_INVALID_ARG, "softmax_scale times log2(e) is not finite");
@@ -864,11 +863,11 @@ sp_status sp_attn_tree_decode(const sp_kv_cache* cache, const void* q, void* o, 
         int seq = 0;
         for (int g = 0; g < n_groups; ++g) { words[g] = first[seq]; seq += Gs ? Gs[g] : 1; }
         words[n_groups] = (int32_t)total;
-        hipError_t e = sp::launch_prepare(words.data(), (int)words.size(), table_of(workspace), (uint32_t*)workspace, sp::ReserveTag{}, sp::TAG_CLEAR, false,
-                                          n_groups, total, 0, 0, sp::Schedule{}, sp::KEYS_AS_PACKED, s);
-        if (e == hipSuccess)
-            e = sp::launch_tree(c, q, o, lse, n_q_heads, n_groups, n_seqs, (int)total, table_of(workspace), ancestors, mask_stride, prompt_tables, prompt_width,
-                                prompt_lens, resp_tables, resp_width, resp_lens, softmax_scale, s);
+        if (sp::tree_units(n_groups, n_seqs, n_q_heads, c.n_kv_heads, (int64_t)prompt_width << c.log_page, (int64_t)resp_width << c.log_page, words.data()) > 2e9)
+            return fail(SP_ERR_INVALID_ARG, "%d sequences with tables of %d and %d pages: more than one call serves", n_seqs, prompt_width, resp_width);
+        const hipError_t e = sp::launch_tree(c, q, o, lse, n_q_heads, n_groups, n_seqs, (int)total, words.data(), table_of(workspace), ancestors, mask_stride, prompt_tables,
+                                             prompt_width, prompt_lens, resp_tables, resp_width, resp_lens, softmax_scale, (uint32_t*)workspace,
+                                             (char*)workspace + TAG_BYTES + sp::tree_table_bytes(n_groups, n_seqs), s);
         if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
         return SP_OK;
     } catch (const std::exception&) {

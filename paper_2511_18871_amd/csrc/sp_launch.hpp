@@ -379,10 +379,14 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
                          const int* prompt_tables, int prompt_width, const int* prompt_lens, const int* resp_tables, int resp_width,
                          const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s);
 
-// starts: first token of each group, the number of tokens, first token of each sequence, the number of tokens (device memory).
-hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int* starts,
+// starts: first token of each group, the number of tokens, first token of each sequence, the number of tokens (host); dev_starts: room for as
+// much, tree_table_bytes().  partials: tree_partial_bytes() bytes.
+size_t tree_table_bytes(int n_groups, int n_seqs);
+size_t tree_partial_bytes(int n_groups, int n_seqs, int64_t total, int Hq, int Hkv, int d, bool f32);
+double tree_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_tokens, int64_t resp_tokens, const int32_t* starts);
+hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int32_t* starts, int* dev_starts,
                        const uint32_t* ancestors, int64_t mask_stride, const int* prompt_tables, int prompt_width, const int* prompt_lens,
-                       const int* resp_tables, int resp_width, const int* resp_lens, float scale, hipStream_t s);
+                       const int* resp_tables, int resp_width, const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s);
 
 // Pages (sp_pages.hip).  layer_stride: elements from layer to layer.  room: pages_room_bytes() bytes.
 size_t pages_room_bytes(int64_t n_pages, int n_seqs);

@@ -1,98 +1,149 @@
 // Attention of drafted tokens that form trees, over the paged cache: several rows per sequence, each with the drafted tokens that it sees.
 //   S_j = scale <q, k_j> over the prompt's keys, the sequence's own ahead of its drafted ones, and those drafted ones whose bit is set,
 //   o = sum_j e^(S_j - m) v_j / l, l = sum_j e^(S_j - m), lse = m + ln l; without a key o = 0 and lse = -inf.
-#include "sp_common.hpp"
-#include "sp_launch.hpp"
+//
+// The kernels are those of one new token per sequence (sp_decode.hpp) with more rows to a list: a prompt is seen by the drafted tokens of all its
+// sequences, a response by those of its own.  Only units of keys that hold drafted tokens look at the mask.
+#include "sp_decode.hpp"
 #include <algorithm>
+#include <type_traits>
 
 namespace sp {
 namespace {
 
-struct TreeArgs {
-    const void* q; void* o; float* lse; const void* k_cache; const void* v_cache;
-    const uint32_t* ancestors; int64_t mask_stride;
-    const int* starts;                     // first token of each group, of each sequence; the number of tokens behind either
-    const int* prompt_tables; const int* prompt_lens; const int* resp_tables; const int* resp_lens;
-    int64_t prompt_width, resp_width, prompt_cap, resp_cap, n_pages;
-    int n_groups, n_seqs, T, Hq, Hkv, rep, log_page;
-    float c;
-};
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t desc_bytes(int64_t lists) { return up256(((size_t)lists + 1) * sizeof(i32x4)); }
 
-// One wave per token and q head: a lane scores one of 64 keys, then holds D / 64 elements of the output.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void tree_kernel(TreeArgs a) {
-    constexpr int E = D / 64;
-    __shared__ float q[D], p[64];
-    __shared__ int64_t at[64];
-    const int l = threadIdx.x, tok = blockIdx.x, h = blockIdx.y, kvh = h / a.rep;
-    auto find = [&](const int* w, int n) {
-        int b = 0, e = n;
-        while (e - b > 1) { const int mid = (b + e) >> 1; if (w[mid] <= tok) b = mid; else e = mid; }
-        return b;
-    };
-    const int g = find(a.starts, a.n_groups);
-    const int* const first = a.starts + a.n_groups + 1;
-    const int s = find(first, a.n_seqs), node = tok - first[s], n = first[s + 1] - first[s];
-    for (int e = l; e < D; e += 64) q[e] = (float)((const T*)a.q)[((int64_t)tok * a.Hq + h) * D + e];
-    __syncthreads();
-    float m = -3.4e38f / fmaxf(1.f, a.c), sum = 0.f, o[E];
-    for (int i = 0; i < E; ++i) o[i] = 0.f;
-    const int64_t own = a.resp_lens[s], base = own - n;
-    const uint32_t* const row = a.ancestors ? a.ancestors + (int64_t)tok * a.mask_stride : nullptr;
-    auto list = [&](const int* table, int64_t len, bool prompt) {
-        for (int64_t j0 = 0; j0 < len; j0 += 64) {
-            const int64_t j = j0 + l;
-            int64_t k = -1;
-            if (j < len) {
-                const int64_t page = table[j >> a.log_page], i = j - base;
-                const bool seen = prompt || i < 0 || (row ? row[i >> 5] >> (i & 31) & 1 : i <= node);
-                if (seen && page >= 0 && page < a.n_pages) k = (((page * a.Hkv + kvh) << a.log_page) + (j & ((1 << a.log_page) - 1))) * D;
-            }
-            float x = -INFINITY;
-            if (k >= 0) {
-                x = 0.f;
-                for (int e = 0; e < D; ++e) x += q[e] * (float)((const T*)a.k_cache)[k + e];
-            }
-            const float mn = fmaxf(m, wave_max(x)), alpha = __builtin_amdgcn_exp2f((m - mn) * a.c);
-            const float w = k >= 0 ? __builtin_amdgcn_exp2f((x - mn) * a.c) : 0.f;
-            m = mn;
-            sum = sum * alpha + wave_sum(w);
-            p[l] = w;
-            at[l] = k;
-            __syncthreads();
-            for (int i = 0; i < E; ++i) o[i] *= alpha;
-            for (int u = 0; u < 64; ++u)
-                if (at[u] >= 0 && bits_of(p[u]) != 0)
-                    for (int i = 0; i < E; ++i) o[i] += p[u] * (float)((const T*)a.v_cache)[at[u] + 64 * i + l];
-            __syncthreads();
-        }
-    };
-    if (own >= 0) {
-        if (a.prompt_width) list(a.prompt_tables + g * a.prompt_width, min((int64_t)a.prompt_lens[g], a.prompt_cap), true);
-        list(a.resp_tables + s * a.resp_width, min(own, a.resp_cap), false);
-    }
-    const bool none = bits_of(sum) == 0;
-    for (int i = 0; i < E; ++i) ((T*)a.o)[((int64_t)tok * a.Hq + h) * D + 64 * i + l] = (T)(none ? 0.f : o[i] / sum);
-    if (l == 0) a.lse[(int64_t)h * a.T + tok] = none ? -INFINITY : m * (a.c * LN2) + __logf(sum);
+// Rows of slots at most, whatever the sequences' counts.  A worker leaves a slot per segment and one more for each worker that shares it.  Shared: a list
+// of r rows in b blocks takes at most r + 16 b rows for its segments of a kv head, and has at most r / 64 + 1 blocks; there are at most 2 all / 33 such lists.
+struct SlotRows { int64_t shared, prompts, responses; };
+SlotRows slot_rows(int64_t n_groups, int64_t n_seqs, int64_t total, int64_t Hq, int64_t Hkv, bool f32) {
+    const int64_t all = total * (Hq / Hkv), widest = std::min<int64_t>(64 * MAX_NC, (all + 63) / 64 * 64), solo = std::min<int64_t>(SOLO_ROWS, all);
+    const int64_t more = f32 ? all / SOLO_ROWS : 0;      // blocks of solo lists beyond the first
+    SlotRows s;
+    s.shared = !f32 && all > SOLO_ROWS ? PLAN_WGS * widest + Hkv * (2 * all + 16 * (std::min(n_groups + n_seqs, 2 * all / (SOLO_ROWS + 1) + 1) + 2 * all / 64)) : 0;
+    s.prompts = (4 * PLAN_WGS + Hkv * (n_groups + more)) * solo;
+    s.responses = (4 * PLAN_WGS + Hkv * (n_groups + n_seqs + 2 * more)) * solo;
+    return s;
 }
 
 }  // namespace
 
-hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int* starts,
+size_t tree_partial_bytes(int n_groups, int n_seqs, int64_t total, int Hq, int Hkv, int d, bool f32) {
+    const SlotRows s = slot_rows(n_groups, n_seqs, total, Hq, Hkv, f32);
+    const size_t rows = (size_t)(s.shared + s.prompts + s.responses);
+    return desc_bytes((int64_t)n_groups + n_seqs) + up256(rows * 8) + up256(rows * d * 4);
+}
+
+size_t tree_table_bytes(int n_groups, int n_seqs) { return up256(((size_t)n_groups + n_seqs + 2) * 4); }
+
+// units of 32 keys by 32 rows that the tables have room for
+double tree_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_tokens, int64_t resp_tokens, const int32_t* starts) {
+    const double rep = Hq / Hkv;
+    double units = 0;
+    for (int g = 0; g < n_groups; ++g) units += ((double)prompt_tokens / 32 + 1) * ((starts[g + 1] - starts[g]) * rep / SOLO_ROWS + 1);
+    const int32_t* const first = starts + n_groups + 1;
+    for (int s = 0; s < n_seqs; ++s) units += ((double)resp_tokens / 32 + 1) * ((first[s + 1] - first[s]) * rep / SOLO_ROWS + 1);
+    return units * Hkv;
+}
+
+hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int32_t* starts, int* dev_starts,
                        const uint32_t* ancestors, int64_t mask_stride, const int* prompt_tables, int prompt_width, const int* prompt_lens,
-                       const int* resp_tables, int resp_width, const int* resp_lens, float scale, hipStream_t s) {
-    TreeArgs a{};
-    a.q = q; a.o = o; a.lse = lse; a.k_cache = cache.k; a.v_cache = cache.v; a.ancestors = ancestors; a.mask_stride = mask_stride; a.starts = starts;
+                       const int* resp_tables, int resp_width, const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s) {
+    DecodeArgs a{};
+    a.q = q; a.o = o; a.lse = lse; a.k_cache = (const char*)cache.k; a.v_cache = (const char*)cache.v;
     a.prompt_tables = prompt_tables; a.prompt_lens = prompt_lens; a.resp_tables = resp_tables; a.resp_lens = resp_lens;
-    a.prompt_width = prompt_width; a.resp_width = resp_width; a.n_pages = cache.n_pages;
-    a.prompt_cap = std::min<int64_t>((int64_t)prompt_width << cache.log_page, MAX_TOKENS);
-    a.resp_cap = std::min<int64_t>((int64_t)resp_width << cache.log_page, MAX_TOKENS);
-    a.n_groups = n_groups; a.n_seqs = n_seqs; a.T = total; a.Hq = Hq; a.Hkv = cache.n_kv_heads; a.rep = Hq / cache.n_kv_heads; a.log_page = cache.log_page;
+    a.prompt_width = prompt_width; a.resp_width = resp_width; a.n_pages = (int)cache.n_pages;
+    a.n_groups = n_groups; a.n_seqs = n_seqs; a.n_tok = total; a.Hq = Hq; a.Hkv = cache.n_kv_heads; a.rep = Hq / cache.n_kv_heads; a.log_page = cache.log_page;
+    a.ancestors = ancestors; a.mask_stride = mask_stride;
     a.c = scale * LOG2E;
-    const dim3 grid((unsigned)total, (unsigned)Hq);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, a); };
-    if (cache.f32) { if (cache.head_dim == 64) launch(tree_kernel<float, 64>); else launch(tree_kernel<float, 128>); }
-    else { if (cache.head_dim == 64) launch(tree_kernel<__bf16, 64>); else launch(tree_kernel<__bf16, 128>); }
+    a.m_none = -3.4e38f / fmaxf(1.f, a.c);
+    a.tag = tag;
+    const SlotRows slots = slot_rows(n_groups, n_seqs, total, Hq, a.Hkv, cache.f32);
+    a.desc = (i32x4*)partials;
+    a.stats = (float*)((char*)partials + desc_bytes((int64_t)n_groups + n_seqs));
+    a.sums = a.stats + up256((size_t)(slots.shared + slots.prompts + slots.responses) * 8) / 4;
+    a.prompt_base = slots.shared;
+    a.resp_base = slots.shared + slots.prompts;
+    // Groups and sequences of one count need no table of where they start
+    const int32_t* const first = starts + n_groups + 1;
+    a.members = starts[1] - starts[0];
+    a.each = first[1] - first[0];
+    for (int g = 1; g < n_groups; ++g) if (starts[g + 1] - starts[g] != a.members) a.members = 0;
+    for (int i = 1; i < n_seqs; ++i) if (first[i + 1] - first[i] != a.each) a.each = 0;
+    if (a.each == 0) a.members = 0;
+    a.group_size = make_div(std::max(1, a.members));
+    a.seq_size = make_div(std::max(1, a.each));
+    TreeArg table;
+    table.dev = nullptr;
+    const int n_words = n_groups + n_seqs + 2;
+    if (!a.members && n_words <= TREE_WORDS && total <= 0xffff) {
+        for (int i = 0; i < n_words; ++i) table.words[i] = (uint16_t)starts[i];
+    } else if (!a.members) {
+        table.dev = dev_starts;
+        const hipError_t e = launch_prepare(starts, n_words, dev_starts, tag, ReserveTag{}, TAG_CLEAR, false, n_groups, total, 0, 0, Schedule{}, KEYS_AS_PACKED, s);
+        if (e != hipSuccess) return e;
+    }
+    const bool prompts = prompt_width > 0;
+    const int n_lists = n_groups + n_seqs;
+    // (prompts, then responses)
+    auto rows_of = [&](int i) { const int k = i < n_groups ? i : i + 1; return (int64_t)a.rep * (starts[k + 1] - starts[k]); };
+    // Row tiles per wave and workgroups: as in launch_decode()
+    a.nc = 1;
+    for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) {
+        const int64_t rows = rows_of(i);
+        if (rows <= SOLO_ROWS || cache.f32) continue;
+        const int64_t tiles = (rows + 15) / 16, blocks = (tiles + 4 * MAX_NC - 1) / (4 * MAX_NC), per = (tiles + blocks - 1) / blocks;
+        a.nc = std::max(a.nc, (int)((per + 3) / 4));
+    }
+    double units_shared = 0, units_solo = 0;
+    for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) {
+        const int64_t rows = rows_of(i);
+        const double tokens = (double)(i < n_groups ? prompt_width : resp_width) * (1 << a.log_page);
+        if (rows > SOLO_ROWS && !cache.f32) {
+            const int64_t tiles = (rows + 15) / 16, blocks = (rows + 64 * a.nc - 1) / (64 * a.nc);
+            a.shared_rows = std::max(a.shared_rows, (int)(16 * ((tiles + blocks - 1) / blocks)));
+            units_shared += (double)blocks * (tokens / 64 + 1) * a.Hkv;
+        } else {
+            int& solo = i < n_groups ? a.prompt_rows : a.resp_rows;
+            solo = std::max(solo, (int)std::min<int64_t>(rows, SOLO_ROWS));
+            units_solo += (double)((rows + SOLO_ROWS - 1) / SOLO_ROWS) * (tokens / 32 + 1) * a.Hkv;
+        }
+    }
+    const unsigned grid = (unsigned)std::min<double>(PLAN_WGS, units_shared + units_solo / 4 + 1);
+    a.shared_cost = a.nc == 1 ? 3.f : a.nc == 2 ? 4.f : 5.5f;
+    a.kv_heads = make_div(a.Hkv);
+    a.q_heads = make_div(Hq);
+    a.heads_each = make_div(a.rep);
+    a.block_rows = make_div(64 * a.nc);
+    a.prompt_cap = (int)std::min<int64_t>((int64_t)prompt_width << a.log_page, MAX_TOKENS);
+    a.resp_cap = (int)std::min<int64_t>((int64_t)resp_width << a.log_page, MAX_TOKENS);
+    auto launch = [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        auto with_lists = [&](auto many) {
+            constexpr bool MANY = decltype(many)::value;
+            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, table, a); };
+            auto with_solo = [&](auto ns) {
+                constexpr int NS = decltype(ns)::value;
+                if (units_shared == 0) with(decode_kernel<D, 0, NS, MANY, true>);
+                else if (a.nc == 1) with(decode_kernel<D, 1, NS, MANY, true>);
+                else if (a.nc == 2) with(decode_kernel<D, 2, NS, MANY, true>);
+                else with(decode_kernel<D, 3, NS, MANY, true>);
+            };
+            if (cache.f32) with(decode_f32_kernel<D, MANY, true>);
+            else if (std::max(a.prompt_rows, a.resp_rows) <= 16) with_solo(std::integral_constant<int, 1>{});
+            else with_solo(std::integral_constant<int, 2>{});
+        };
+        if (n_lists > 64) with_lists(std::true_type{}); else with_lists(std::false_type{});
+        auto join = [&](auto dense) {
+            const int64_t each = decltype(dense)::value ? 1024 / D : 4;
+            const unsigned joins = (unsigned)(((int64_t)total * Hq + each - 1) / each);
+            if (cache.f32) hipLaunchKernelGGL((decode_join_kernel<float, D, decltype(dense)::value, true>), dim3(joins), dim3(256), 0, s, table, a);
+            else hipLaunchKernelGGL((decode_join_kernel<__bf16, D, decltype(dense)::value, true>), dim3(joins), dim3(256), 0, s, table, a);
+        };
+        if ((int64_t)total * Hq > 8192) join(std::true_type{}); else join(std::false_type{});
+    };
+    if (cache.head_dim == 64) launch(std::integral_constant<int, 64>{}); else launch(std::integral_constant<int, 128>{});
     return hipGetLastError();
 }
 

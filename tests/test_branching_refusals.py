@@ -15,20 +15,20 @@ def lib():
     return B.load_library()
 
 
-def tree(lib, c=None, q=P, o=P, lse=P, hq=4, ng=2, n=3, Gs=ints(1, 2), new=ints(3, 0, 40), anc=P, ms=2, pt=P, pw=2, pl=P, rt=P, rw=2, rl=P, scale=0.1, ws=P, bytes=1 << 26):
+def tree(lib, c=None, q=P, o=P, lse=P, hq=4, ng=2, n=3, Gs=ints(1, 2), new=ints(3, 0, 40), anc=P, ms=2, pt=P, pw=2, pl=P, rt=P, rw=2, rl=P, scale=0.1, ws=P, bytes=1 << 28):
     return lib.sp_attn_tree_decode(cache() if c is None else c, q, o, lse, hq, ng, n, Gs, new, anc, ms, pt, pw, pl, rt, rw, rl, scale, ws, bytes, None)
 
 
 def test_tree_refuses(lib):
     for kw, status in BAD_CACHES[1:]:
         assert tree(lib, c=cache(**kw)) == status, kw
-    for kw in (dict(q=None), dict(o=None), dict(lse=None), dict(q=0x1004), dict(o=0x1008), dict(lse=0x1002), dict(hq=3), dict(hq=0), dict(hq=65538), dict(ng=0), dict(n=0), dict(n=4),
+    for kw in (dict(q=None), dict(o=None), dict(lse=None), dict(q=0x1004), dict(o=0x1008), dict(lse=0x1002), dict(hq=3), dict(hq=0), dict(ng=0), dict(n=0), dict(n=4),
                dict(Gs=ints(4, -1)), dict(Gs=None), dict(new=None), dict(new=ints(1, -1, 1)), dict(new=ints(1, 1025, 1)), dict(ms=1), dict(ms=-1), dict(anc=None), dict(anc=0x1002), dict(pt=None),
                dict(pl=None), dict(pw=0), dict(pw=-1), dict(rt=None), dict(rw=0), dict(rl=None), dict(rl=0x1001), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")),
-               dict(scale=float("nan")), dict(scale=3e38)):
+               dict(scale=float("nan")), dict(scale=3e38), dict(rw=2 ** 31 - 1)):
         assert tree(lib, **kw) == INVALID, kw
     need = lib.sp_attn_tree_decode_workspace_bytes(2, 3, 43, 4, 2, 128, B.SP_BF16)
-    assert 256 < need < 1 << 26
+    assert 256 < need < 1 << 28
     for kw in (dict(ws=None), dict(ws=0x1008), dict(bytes=0), dict(bytes=need - 1)):
         assert tree(lib, **kw) == WORKSPACE, kw
     assert tree(lib, new=ints(0, 0, 0), anc=None, ms=0) == B.SP_OK       # no row, no launch
