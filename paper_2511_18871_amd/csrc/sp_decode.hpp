@@ -36,6 +36,7 @@ namespace {
 #define SP_INLINE __attribute__((always_inline))      // lambdas: what they refer to has to stay in registers
 
 constexpr int SOLO_ROWS = 32;              // rows of a segment that a wave takes by itself
+constexpr int WIDE_ROWS = 128;             // rows of drafted tokens that a workgroup takes: 32 to a wave
 constexpr int MAX_NC = 3;                  // row tiles of 16 of a wave that shares its keys: 192 rows to a workgroup
 constexpr int PLAN_WGS = 512;              // workgroups that the units are dealt to: two to a CU (one: 131 -> 164 us for the 64 prompts above)
 
@@ -83,9 +84,9 @@ __device__ __forceinline__ int scan64(int x) {
 }
 struct ListShape {                        // units of keys of a segment; blocks of rows
     int rows, len, units, blocks; bool shared;
-    // what a list adds to `ord`: its blocks, of a shared list of drafted tokens the row tiles of its blocks
+    // what a list adds to `ord`: its blocks, a shared list of drafted tokens its row tiles of 16
     template <bool TREE> __device__ __forceinline__ int places() const {
-        if constexpr (TREE) { if (shared) return blocks == 1 ? (rows + 15) >> 4 : (((rows + 15) >> 4) + blocks - 1) / blocks * blocks; }
+        if constexpr (TREE) { if (shared) return (rows + 15) >> 4; }
         return blocks;
     }
 };
@@ -386,14 +387,14 @@ struct SegmentRows {
         unsigned k;
         block = c.blocks > 1 ? (int)divmod((unsigned)c.seg, a.kv_heads, k) : 0;
         kvh = c.blocks > 1 ? (int)k : c.seg;
-        const int per = c.shared ? 16 * (((((c.rows + 15) >> 4)) + c.blocks - 1) / c.blocks) : SOLO_ROWS;
+        const int per = !c.shared ? SOLO_ROWS : TREE ? WIDE_ROWS : 16 * (((((c.rows + 15) >> 4)) + c.blocks - 1) / c.blocks);
         row0 = block * per;
         rows = min(per, c.rows - row0);
         seq0 = c.ls.first_seq(c.list);
         rep = a.rep; Hq = a.Hq; heads_each = a.heads_each;
         if constexpr (TREE && KIND) {
             if (c.shared) {      // (the segment's own rows lie behind those of the segments ahead of it, not each in room for the largest)
-                base = (int64_t)worker * a.shared_rows + ((int64_t)c.ord * a.Hkv + c.seg * (per >> 4)) * 16;
+                base = (int64_t)worker * a.shared_rows + ((int64_t)(c.ord + block * (WIDE_ROWS / 16)) * a.Hkv + kvh * ((rows + 15) >> 4)) * 16;
                 return;
             }
         }
@@ -559,68 +560,28 @@ __device__ __forceinline__ void hide(const DecodeArgs& a, const SegmentRows& seg
     }
 }
 
-// (which the compiler, told that there is no NaN, would fold into a sum's result)
-__device__ __forceinline__ float unknown_infinity() {
-    float x = INFINITY;
-    asm("" : "+v"(x));
-    return x;
-}
-
-// Infinite and NaN elements of four dwords of bf16 values: taken out of x; 1 in `up` where x was +inf or NaN, in `down` where -inf or NaN
-__device__ __forceinline__ bool split_nonfinite(bf16x8& x, bf16x8& up, bf16x8& down) {
-    i32x4 w = __builtin_bit_cast(i32x4, x), u = {0, 0, 0, 0}, d = u;
-    int any = 0;
+// A weight of 0 does not leave out an infinite or NaN value in a product.  Where rows see some of the keys only, such elements are therefore taken out
+// of the values, and the row's statistics say so: the join then adds them to the rows that see their keys.
+__device__ __forceinline__ i32x4 only_finite(i32x4 w, bool& found) {      // bf16
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const unsigned e = (unsigned)w[i] >> (16 * half) & 0xffffu;
-            const bool bad = (e & 0x7f80u) == 0x7f80u, nan = bad && (e & 0x7fu), neg = e & 0x8000u;
-            any |= bad;
-            if (bad && (nan || !neg)) u[i] |= 0x3f80 << (16 * half);
-            if (bad && (nan || neg)) d[i] |= 0x3f80 << (16 * half);
-            if (bad) w[i] &= (int)~(0xffffu << (16 * half));
-        }
-    x = __builtin_bit_cast(bf16x8, w);
-    up = __builtin_bit_cast(bf16x8, u);
-    down = __builtin_bit_cast(bf16x8, d);
-    return any;
-}
-
-// add_values() where rows may see some of the keys only: a weight of 0 leaves out what its key's value holds.  Infinite and NaN values do not go through the
-// products (0 times them is NaN); products of ones count how many of them meet a weight, and these make an element infinite or NaN.
-template <int D, int NC>
-__device__ __forceinline__ void add_seen_values(Rows<D, NC>& r, unsigned v, const bf16x8 (&p)[NC][2], int l) {
-    const unsigned at = v + kv_off<D>(4 * (l >> 4) + ((l & 15) >> 2), (l & 3) >> 1) + ((l & 1) << 3);
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) {
-        s16x4 half[2];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-            half[kt] = lds_at_tr4((at ^ (dt << 5)) + kt * (32 * D));
-        bf16x8 a = cat4(half[0], half[1]), up, down;
-        const bool bad = split_nonfinite(a, up, down);
-        const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-#pragma unroll
-            for (int part = 1; part >= 0; --part) r.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[c][part], r.o[c][dt], 0, 0, 0);
-            if (any) {
-                // (as words: the bits of an element of a vector, cast one by one, were those of its first)
-                i32x4 w = __builtin_bit_cast(i32x4, p[c][0]) | __builtin_bit_cast(i32x4, p[c][1]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = (w[i] & 0x7fff ? 0x3f80 : 0) | (w[i] & 0x7fff0000 ? 0x3f800000 : 0);
-                const bf16x8 met = __builtin_bit_cast(bf16x8, w);
-                const f32x4 zero = {0, 0, 0, 0};
-                const f32x4 ups = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, met, zero, 0, 0, 0), downs = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, met, zero, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    r.o[c][dt][i] += ups[i] > 0.f ? unknown_infinity() : 0.f;
-                    r.o[c][dt][i] -= downs[i] > 0.f ? unknown_infinity() : 0.f;
-                }
-            }
-        }
+    for (int i = 0; i < 4; ++i) {
+        const bool low = (w[i] & 0x7f80) == 0x7f80, high = (w[i] & 0x7f800000) == 0x7f800000;
+        found |= low || high;
+        w[i] &= (low ? (int)0xffff0000 : -1) & (high ? 0xffff : -1);
     }
+    return w;
+}
+// of `granules` of 16 bytes at LDS address `at`, 64 lanes (or more: `step`) in turn; true if any was found (by this lane)
+__device__ __forceinline__ bool clean(unsigned at, int first, int granules, int step) {
+    bool any = false;
+    for (int g = first; g < granules; g += step) {
+        auto* const p = (__attribute__((address_space(3))) i32x4*)(uintptr_t)(at + 16u * g);
+        bool found = false;
+        const i32x4 w = only_finite(*p, found);
+        if (found) *p = w;
+        any |= found;
+    }
+    return any;
 }
 
 // O^T += V^T P^T over 32 keys at LDS address `v`
@@ -711,8 +672,14 @@ __device__ __forceinline__ void load_rows(Rows<D, NC>& r, const __bf16* q, const
     }
 }
 
-template <int D, int NC>
-__device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArgs& a, const SegmentRows& pr, int row0, int tiles, int l) {
+// Statistics of a row of a slot: m and l; TREE: also l of the weights as the second product took them, and whether values were left out of it
+template <bool TREE> __device__ __forceinline__ void put_stats(const DecodeArgs& a, int64_t row, float m, float l, float l_product, bool left_out) {
+    if constexpr (TREE) *reinterpret_cast<f32x4*>(a.stats + row * 4) = f32x4{m, l, l_product, left_out ? 1.f : 0.f};
+    else *reinterpret_cast<f32x2*>(a.stats + row * 2) = f32x2{m, l};
+}
+
+template <bool TREE, int D, int NC>
+__device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArgs& a, const SegmentRows& pr, int row0, int tiles, int l, bool left_out = false) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int row = row0 + 16 * c + (l & 15);
@@ -721,7 +688,7 @@ __device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArg
         float* const out = a.sums + (pr.base + row) * D + 4 * (l >> 4);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(out + 16 * dt) = r.o[c][dt];
-        if (l < 16) *reinterpret_cast<f32x2*>(a.stats + (pr.base + row) * 2) = f32x2{r.m[c], lt};
+        if (l < 16) put_stats<TREE>(a, pr.base + row, r.m[c], lt, lt, left_out);
     }
 }
 
@@ -731,6 +698,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
     constexpr int KEYS16 = 32 * D, KIND = NC > 0;       // bytes of 16 keys
     __shared__ __attribute__((aligned(1024))) char lds[16 * KEYS16];
     __shared__ PlanShare share;
+    __shared__ int left_out;                         // TREE: values were left out of the segment's products
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<KIND, TREE> ls{words_of(starts), a};
@@ -823,7 +791,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
             const int tiles = (seg.rows + 15) >> 4;
             load_rows(r, q, seg, 0, tiles, l);
             r.clear(a.m_none);
-            bool more = true, same = true;
+            bool more = true, same = true, left_out = false;
             while (same) {
                 const unsigned bits = low_bits(valid[0]) | low_bits(valid[1]) << 16;
                 f32x4 s[NS][2];
@@ -841,12 +809,238 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
                 if (more) { next(); fetch(); issue(kc, kb); }
                 weights(r, s, a.c, pw);
                 if (more) wait_copies<N>(); else wait_copies<0>();
-                if (TREE && some) add_seen_values(r, vb, pw, l); else add_values(r, vb, pw, l);
+                if (TREE && some) {
+                    left_out |= __builtin_amdgcn_ballot_w64(clean(vb, l, 2 * KEYS16 / 16, 64)) != 0;
+                    wait_lds();
+                }
+                add_values(r, vb, pw, l);
                 wait_lds();
                 if (more) issue(vc, vb);
             }
-            store_rows(r, a, seg, 0, tiles, l);
+            store_rows<TREE>(r, a, seg, 0, tiles, l, left_out);
             if (!more) return;
+        }
+    } else if constexpr (TREE) {
+        // Many drafted tokens: four waves of 32 rows, products on matrix instructions of 32 x 32, software-pipelined as in the forward over a pack: while
+        // step j's matrix instructions form O^T += V(j-1)^T P(j-1)^T and S(j+1) = K(j+1) Q^T, its vector ones turn S(j) into P(j), a score to a
+        // matrix instruction (two, heads of 64).  Two buffers of 64 keys each of K and of V, a barrier per step: V(j) and K(j+2) are copied under step j.
+        constexpr int TILE = 4 * KEYS16, KS = D / 16, MF = 2 * KS, DB = D / 32, PER = 32 / (2 * MF), RD = 3;
+        const int c32 = l & 31, hh = l >> 5, j16 = l & 15;
+        unsigned row_at[KS], tr_at[DB][2];         // operands within the first buffers
+#pragma unroll
+        for (int i = 0; i < KS; ++i) { row_at[i] = buf + kv_off<D>(c32, 2 * i + hh); asm volatile("" : "+v"(row_at[i])); }
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int col4 = 32 * db + 16 * ((l >> 4) & 1) + 4 * (j16 & 3);
+                tr_at[db][half] = buf + 2 * TILE + kv_off<D>(4 * hh + (j16 >> 2) + 8 * half, col4 >> 3) + ((col4 & 4) << 1);
+                asm volatile("" : "+v"(tr_at[db][half]));
+            }
+        auto ldK = [&](int b, int i) SP_INLINE { return lds_at_row8(row_at[i >> 1] + TILE * b + 2 * KEYS16 * (i & 1)); };
+        auto ldV = [&](int b, int i) SP_INLINE {
+            const int off = TILE * b + KEYS16 * (i / DB);
+            return cat4(lds_at_tr4(tr_at[i % DB][0] + off), lds_at_tr4(tr_at[i % DB][1] + off));
+        };
+        auto operand = [&](const unsigned (&p)[16], int i) SP_INLINE {      // of product i of O^T: keys 16 (i / DB) ...
+            typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+            const int k = 4 * (i / DB);
+            return __builtin_bit_cast(bf16x8, u32x4{p[k], p[k + 1], p[k + 2], p[k + 3]});
+        };
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        auto pack2 = [&](float x, float y) SP_INLINE { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y}); };
+        auto sum2 = [&](unsigned p, float acc) SP_INLINE {
+            return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p), bf16x2{(__bf16)1.f, (__bf16)1.f}, acc, false);
+        };
+        const float cs = a.c;
+        const f32x16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        while (true) {
+            const SegmentRows seg(at, a, work.worker);
+            const int total = min(work.left, at.units - at.t), key0 = 64 * at.t;
+            const bool active = 32 * w < seg.rows;
+            // A tile of keys: this wave's 16 of them (place, how many there are), and which of all 64 there are
+            struct Tile { uint64_t off; int valid; unsigned lo, hi; };
+            auto fetch = [&](int j) SP_INLINE {
+                Tile t{0, 16, 0xffffffffu, 0xffffffffu};
+                const int key = key0 + 64 * j;
+                if (whole(key, 64)) {
+                    t.off = offset(key + 16 * w, __builtin_amdgcn_readfirstlane(pages.at((key + 16 * w) >> a.log_page)));
+                    return t;
+                }
+                t.lo = t.hi = 0;
+#pragma unroll 1
+                for (int h = 0; h < 4; ++h) {
+                    uint64_t off;
+                    int v;
+                    locate(key + 16 * h, off, v);
+                    if (h == w) { t.off = off; t.valid = v; }
+                    (h < 2 ? t.lo : t.hi) |= low_bits(v) << (16 * (h & 1));
+                }
+                return t;
+            };
+            auto issue = [&](uint64_t cache, const Tile& t, int b) SP_INLINE { copy.rows16(cache + t.off, t.valid, buf + (unsigned)b * TILE + w * KEYS16); };
+            auto tail = [&](int j) SP_INLINE { return key0 + 64 * (int64_t)j + 64 > drafted.base; };      // holds drafted tokens
+            auto mask = [&](const Tile& t, int j, f32x16 (&S)[2]) SP_INLINE {
+                const bool some = tail(j);
+                if (!some && (t.lo & t.hi) == 0xffffffffu) return;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    unsigned bits = kb ? t.hi : t.lo;
+                    if (some) bits &= drafted.bits(a, seg, 32 * w + c32, key0 + 64 * j + 32 * kb);
+                    mask16(S[kb], bits >> (4 * hh));
+                }
+            };
+            auto clean_tile = [&](int j, int b) SP_INLINE {      // of V(j), if it holds drafted tokens; every wave its share
+                if (j < 0 || !tail(j)) return;
+                if (clean(buf + (2 + b) * TILE, threadIdx.x, TILE / 16, 256)) left_out = 1;
+                wait_lds();
+                __syncthreads();
+            };
+            __syncthreads();                           // the last segment's reads from LDS are done
+            pages.load(key0 >> a.log_page);
+            Tile t0 = fetch(0), t1 = t0, t2 = t0;
+            issue(kc, t0, 0);
+            if (total > 1) { t1 = fetch(1); issue(kc, t1, 1); }
+            bf16x8 qreg[KS];
+            {
+                const __bf16* const p = q + seg.q_row(min(32 * w + c32, seg.rows - 1)) * D + 8 * hh;
+#pragma unroll
+                for (int i = 0; i < KS; ++i) qreg[i] = *reinterpret_cast<const bf16x8*>(p + 16 * i);
+            }
+            // V(-1), which P = 0 is multiplied with: LDS may hold what reads as NaN
+            for (int i = threadIdx.x; i < TILE / 16; i += 256) *(__attribute__((address_space(3))) i32x4*)(uintptr_t)(buf + 3 * TILE + 16 * i) = i32x4{0, 0, 0, 0};
+            if (threadIdx.x == 0) left_out = 0;
+            f32x16 o[DB], sA[2], sB[2];
+            unsigned pA[16], pB[16];
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db] = zero16;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { pA[i] = 0u; pB[i] = 0u; }
+            float m = a.m_none, lsum = 0.f, lprod = 0.f;
+            wait_copies<0>();
+            wait_lds();
+            __syncthreads();
+            if (active) {
+#pragma unroll
+                for (int i = 0; i < MF; ++i) sA[i & 1] = mfma32(ldK(0, i), qreg[i >> 1], i < 2 ? zero16 : sA[i & 1]);
+                mask(t0, 0, sA);
+                float mx = sA[0][0];
+#pragma unroll
+                for (int e = 1; e < 32; ++e) mx = fmaxf(mx, sA[e >> 4][e & 15]);
+                m = fmaxf(m, pair_max(mx));
+            }
+            // A row's weights are 2^(S c - R).  R is m c as rounded, where that is small, so that one operation makes the exponent; else m c itself, and
+            // differences are taken ahead of their scaling, in the branch below, which then every step takes.  d = R - m c.
+            constexpr float LARGE = 4194304.f;
+            auto beyond = [&](float x) SP_INLINE { return !(fabsf(x * cs) <= LARGE); };
+            auto offset_of = [&](float x) SP_INLINE { return beyond(x) ? 0.f : __builtin_fmaf(-x, cs, x * cs); };
+            auto step = [&](int j, const Tile& t, auto par, f32x16 (&S)[2], f32x16 (&Snext)[2], const unsigned (&p)[16], unsigned (&pnew)[16]) SP_INLINE {
+                constexpr int R = decltype(par)::value;
+                mask(t, j, S);
+                __builtin_amdgcn_sched_barrier(0);
+                const float mc = m * cs;
+                float tsum = 0.f, tprod = 0.f, pe[32];
+                auto valu = [&](int e) SP_INLINE {
+                    pe[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[e >> 4][e & 15], cs, -mc));
+                    asm volatile("" : "+v"(pe[e]));
+                    if (e >= 1) { tsum += pe[e - 1]; asm volatile("" : "+v"(tsum)); }
+                    if (e >= 2 && (e & 1) == 0) { pnew[(e - 2) >> 1] = pack2(pe[e - 2], pe[e - 1]); asm volatile("" : "+v"(pnew[(e - 2) >> 1])); }
+                    if (e >= 3 && (e & 1) == 1) { tprod = sum2(pnew[(e - 3) >> 1], tprod); asm volatile("" : "+v"(tprod)); }
+                };
+                auto operand_at = [&](int i) SP_INLINE { return i < MF ? ldV(1 - R, i) : ldK(1 - R, i - MF); };
+                bf16x8 ring[RD];
+#pragma unroll
+                for (int i = 0; i < RD - 1; ++i) ring[i] = operand_at(i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 2 * MF; ++i) {
+                    if (i + RD - 1 < 2 * MF) ring[(i + RD - 1) % RD] = operand_at(i + RD - 1);
+                    if (i < MF) o[i % DB] = mfma32(ring[i % RD], operand(p, i), o[i % DB]);
+                    else Snext[i & 1] = mfma32(ring[i % RD], qreg[(i - MF) >> 1], i < MF + 2 ? zero16 : Snext[i & 1]);
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) valu(PER * i + e);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                tsum += pe[31];
+                pnew[15] = pack2(pe[30], pe[31]);
+                tprod = sum2(pnew[15], tprod);
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(tsum <= 16384.f) || beyond(m)) != 0, 0)) {
+                    float mx = S[0][0];
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) mx = fmaxf(mx, S[e >> 4][e & 15]);
+                    const float mn = fmaxf(m, pair_max(mx)), d = offset_of(mn);
+                    const float alpha = __builtin_amdgcn_exp2f(__builtin_fmaf(m - mn, cs, offset_of(m) - d));
+                    lsum *= alpha;
+                    lprod *= alpha;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+                    m = mn;
+                    tsum = tprod = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k >> 3][(2 * k) & 15] - mn, cs, -d));
+                        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k >> 3][((2 * k) & 15) + 1] - mn, cs, -d));
+                        tsum += p0 + p1;
+                        pnew[k] = pack2(p0, p1);
+                        tprod = sum2(pnew[k], tprod);
+                    }
+                }
+                lsum += tsum;
+                lprod += tprod;
+            };
+            int vlast = 1;
+            for (int j = 0; j < total; j += 2) {
+                wait_copies<0>();
+                __syncthreads();
+                clean_tile(j - 1, 1);
+                issue(vc, t0, 2);
+                if (j + 2 < total) { t2 = fetch(j + 2); issue(kc, t2, 0); }
+                if (active) step(j, t0, std::integral_constant<int, 0>{}, sA, sB, pA, pB);
+                if (j + 1 >= total) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) pA[i] = pB[i];
+                    vlast = 0;
+                    break;
+                }
+                wait_copies<0>();
+                __syncthreads();
+                clean_tile(j, 0);
+                issue(vc, t1, 3);
+                t0 = t2;
+                if (j + 3 < total) { t2 = fetch(j + 3); issue(kc, t2, 1); }
+                if (active) step(j + 1, t1, std::integral_constant<int, 1>{}, sB, sA, pB, pA);
+                t1 = t2;
+            }
+            wait_copies<0>();
+            __syncthreads();
+            clean_tile(total - 1, vlast);
+            if (active) {
+#pragma unroll
+                for (int i = 0; i < MF; ++i) {
+                    const unsigned off = TILE * vlast + KEYS16 * (i / DB);
+                    const bf16x8 x = cat4(lds_at_tr4(tr_at[i % DB][0] + off), lds_at_tr4(tr_at[i % DB][1] + off));
+                    o[i % DB] = mfma32(x, operand(pA, i), o[i % DB]);
+                }
+                // from R to m c
+                const float f = __builtin_amdgcn_exp2f(offset_of(m)), lt = pair_sum(lsum) * f, lp = pair_sum(lprod) * f;
+                const int row = 32 * w + c32;
+                if (row < seg.rows) {
+                    float* const out = a.sums + (seg.base + row) * D + 4 * hh;
+#pragma unroll
+                    for (int n = 0; n < 4 * DB; ++n) {
+                        const f32x16& x = o[n >> 2];
+                        const int r = 4 * (n & 3);
+                        *reinterpret_cast<f32x4*>(out + 32 * (n >> 2) + 8 * (n & 3)) = f32x4{x[r] * f, x[r + 1] * f, x[r + 2] * f, x[r + 3] * f};
+                    }
+                    if (hh == 0) put_stats<true>(a, seg.base + row, m, lt, lp, left_out);
+                }
+            }
+            work.left -= total;
+            if (work.left == 0) return;
+            at.t += total - 1;
+            next();
         }
     } else if constexpr (KIND) {
         // Four waves: a unit of K and V in one half of LDS while the next is copied into the other, a wave copying 16 keys of each,
@@ -891,27 +1085,17 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
                 half ^= 1;
                 more = --work.left > 0;
                 same = more && at.t + 1 < at.units;
-                const Drafted tail = drafted;
-                const int key0 = 64 * at.t;
                 if (more) { next(); issue(buf + half * 8 * KEYS16); }
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     f32x4 s[NC][2];
                     bf16x8 pw[NC][2];
                     scores(r, kb + 2 * h * KEYS16, h ? here[1] : here[0], l, s);
-                    if constexpr (TREE) {
-                        if (key0 + 32 * (int64_t)h + 32 > tail.base) {
-                            hide<D>(a, seg, tail, 16 * t0, key0 + 32 * h, l, s);
-                            weights(r, s, a.c, pw);
-                            add_seen_values(r, vb + 2 * h * KEYS16, pw, l);
-                            continue;
-                        }
-                    }
                     weights(r, s, a.c, pw);
                     add_values(r, vb + 2 * h * KEYS16, pw, l);
                 }
             }
-            store_rows(r, a, seg, 16 * t0, tiles, l);
+            store_rows<TREE>(r, a, seg, 16 * t0, tiles, l);
             if (!more) return;
         }
     }
@@ -950,6 +1134,7 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(StartsArg<TREE> star
         float q[NC][D / 4];
         f32x4 o[NC][HALVES][4];
         float m[NC], sum[NC];
+        bool left_out = false;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int row = 16 * c + m16;
@@ -984,19 +1169,23 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(StartsArg<TREE> star
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h) v[i][h] = f32x4{0, 0, 0, 0};
             }
-            // Where rows see some of the keys only, infinite and NaN values are kept from the products, as in add_seen_values()
-            bool some = false, any = false;
+            bool some = false;
             if constexpr (TREE) {
                 some = key + (int64_t)16 > drafted.base;
                 if (some) {
-                    bool bad = false;
+                    bool found = false;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) bad |= (bits_of(v[i][h][e]) & 0x7f800000u) == 0x7f800000u;
-                    any = __builtin_amdgcn_ballot_w64(bad) != 0;
+                            for (int e = 0; e < 4; ++e) {
+                                const unsigned x = bits_of(v[i][h][e]);
+                                const bool bad = (x & 0x7f800000u) == 0x7f800000u;
+                                v[i][h][e] = __uint_as_float(bad ? 0u : x);
+                                found |= bad;
+                            }
+                    left_out |= __builtin_amdgcn_ballot_w64(found) != 0;
                 }
             }
 #pragma unroll
@@ -1025,24 +1214,6 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(StartsArg<TREE> star
                     for (int e = 0; e < 4; ++e) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[c][h][e][i] *= alpha;
-                        if (TREE && any) {
-                            f32x4 ups = {0, 0, 0, 0}, downs = ups;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const unsigned x = bits_of(v[i][h][e]);
-                                const bool bad = (x & 0x7f800000u) == 0x7f800000u, nan = bad && (x & 0x7fffffu), neg = x >> 31;
-                                const float met = bits_of(s[i]) ? 1.f : 0.f;
-                                ups = __builtin_amdgcn_mfma_f32_16x16x4f32(bad && (nan || !neg) ? 1.f : 0.f, met, ups, 0, 0, 0);
-                                downs = __builtin_amdgcn_mfma_f32_16x16x4f32(bad && (nan || neg) ? 1.f : 0.f, met, downs, 0, 0, 0);
-                                o[c][h][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(bad ? 0.f : __uint_as_float(x), s[i], o[c][h][e], 0, 0, 0);
-                            }
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                o[c][h][e][i] += ups[i] > 0.f ? unknown_infinity() : 0.f;
-                                o[c][h][e][i] -= downs[i] > 0.f ? unknown_infinity() : 0.f;
-                            }
-                            continue;
-                        }
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[c][h][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][h][e], s[i], o[c][h][e], 0, 0, 0);
                     }
@@ -1059,7 +1230,7 @@ __global__ __launch_bounds__(256, 2) void decode_f32_kernel(StartsArg<TREE> star
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     *reinterpret_cast<f32x4*>(out + 64 * h + 4 * i) = f32x4{o[c][h][0][i], o[c][h][1][i], o[c][h][2][i], o[c][h][3][i]};
-            if (j == 0) *reinterpret_cast<f32x2*>(a.stats + (seg.base + row) * 2) = f32x2{m[c], lt};
+            if (j == 0) put_stats<TREE>(a, seg.base + row, m[c], lt, lt, left_out);
         }
         work.left -= run;
         if (work.left == 0) return;
@@ -1118,30 +1289,33 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
     if (sizeof(T) == 2) {
         unsigned rest;
         const int blocks = (int)divmod((unsigned)(rows - 1), a.block_rows, rest) + 1;
-        if (shared) per = 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
+        if (shared) per = TREE ? WIDE_ROWS : 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
     }
     const int block = rows > per ? row / per : 0, segment = block * a.Hkv + kvh;
     const unsigned each = shared ? run[0] : run[1], from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[3];
     const unsigned worker0 = from / each, worker1 = (from + d[1] - 1) / each;
     const unsigned stride = shared ? a.shared_rows : resp ? a.resp_rows : a.prompt_rows;
     unsigned at = (unsigned)(shared ? 0 : resp ? a.resp_base : a.prompt_base) + (worker0 + (unsigned)d[2] * a.Hkv + segment) * stride + row - block * per;
-    if (TREE && shared) at = worker0 * stride + ((unsigned)d[2] * a.Hkv + segment * (per >> 4)) * 16 + row - block * per;
+    if (TREE && shared)
+        at = worker0 * stride + ((unsigned)(d[2] + block * (per >> 4)) * a.Hkv + kvh * ((min(per, rows - block * per) + 15) >> 4)) * 16 + row - block * per;
     const int count = d[1] > 0 ? (int)(worker1 - worker0) + 1 : 0;
     auto prompts = [](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x00, 0xf, 0xf, true); };     // of the even lanes
     auto resps = [](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x55, 0xf, 0xf, true); };       // of the odd ones
     const bool part = (int)resps(d[3]) >= 0;
     const int n_p = part ? (int)prompts(count) : 0, n = part ? n_p + (int)resps(count) : 0;
     const unsigned at_p = prompts(at), at_r = resps(at), stride_p = prompts(stride), stride_r = resps(stride);
-    float M = a.m_none, L = 0.f;
+    typedef std::conditional_t<TREE, f32x4, f32x2> Stats;
+    float M = a.m_none, L = 0.f, LP = 0.f;             // LP: of the weights that the products took (TREE)
+    bool left_out = false;
     f32x4 acc = {0, 0, 0, 0};
     for (int i = 0; i < n; i += DEPTH * AT_ONCE) {
-        f32x2 st[DEPTH];
+        Stats st[DEPTH];
         f32x4 x[DEPTH];
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) {
             const int k = min(i + u * AT_ONCE + mine, n - 1);              // behind the last: again, and not counted
             const unsigned at_k = k < n_p ? at_p + k * stride_p : at_r + (k - n_p) * stride_r;
-            st[u] = *reinterpret_cast<const f32x2*>(a.stats + (uint64_t)at_k * 2);
+            st[u] = *reinterpret_cast<const Stats*>(a.stats + (uint64_t)at_k * (sizeof(Stats) / 4));
             x[u] = *reinterpret_cast<const f32x4*>(a.sums + (uint64_t)at_k * D + e0);
         }
         float mn = M;
@@ -1150,6 +1324,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
         const float alpha = __builtin_amdgcn_exp2f((M - mn) * a.c);
         M = mn;
         L *= alpha;
+        if constexpr (TREE) LP *= alpha;
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] *= alpha;
 #pragma unroll
@@ -1157,6 +1332,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
             if (i + u * AT_ONCE + mine >= n) continue;                     // (not with a weight of 0: sums may be infinite)
             const float wt = __builtin_amdgcn_exp2f((st[u][0] - mn) * a.c);
             L += wt * st[u][1];
+            if constexpr (TREE) { LP += wt * st[u][2]; left_out |= bits_of(st[u][3]) != 0; }
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += wt * x[u][e];
         }
@@ -1166,12 +1342,30 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
         const float m2 = __shfl_xor(M, o, 64), mn = fmaxf(M, m2), wt = __builtin_amdgcn_exp2f((M - mn) * a.c), wt2 = __builtin_amdgcn_exp2f((m2 - mn) * a.c);
         M = mn;
         L = L * wt + __shfl_xor(L, o, 64) * wt2;
+        if constexpr (TREE) { LP = LP * wt + __shfl_xor(LP, o, 64) * wt2; left_out |= (bool)__shfl_xor((int)left_out, o, 64); }
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = acc[e] * wt + __shfl_xor(acc[e], o, 64) * wt2;
     }
     // Without a key L is 0, and a NaN among the scores is in L
     const bool none = bits_of(L) == 0;
-    const float inv = 1.f / L;
+    const float inv = 1.f / (TREE ? LP : L);
+    if constexpr (TREE) {
+        // Infinite and NaN values that the products left out: those of the keys that the row sees, from the first unit with drafted ones on
+        if (left_out) {
+            const int len = min(a.resp_lens[seq], a.resp_cap), base = a.resp_lens[seq] - own, words = (own + 31) >> 5;
+            const uint32_t* const mask = a.ancestors ? a.ancestors + (int64_t)tok * a.mask_stride : nullptr;
+            for (int key = max(base & ~63, 0); key < len; ++key) {
+                const int page = a.resp_tables[seq * a.resp_width + (key >> a.log_page)];
+                if ((unsigned)page >= (unsigned)a.n_pages || !(drafted_bits(mask, words, node, key - base) & 1)) continue;
+                const T* const v = (const T*)a.v_cache + (((((int64_t)page * a.Hkv + kvh) << a.log_page) + (key & ((1 << a.log_page) - 1))) * D + e0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = (float)v[e];
+                    if ((bits_of(x) & 0x7f800000u) == 0x7f800000u) acc[e] += x;
+                }
+            }
+        }
+    }
     if (mine == 0) {
         typedef T out4 __attribute__((ext_vector_type(4)));
         out4 y;

@@ -14,14 +14,14 @@ namespace {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t desc_bytes(int64_t lists) { return up256(((size_t)lists + 1) * sizeof(i32x4)); }
 
-// Rows of slots at most, whatever the sequences' counts.  A worker leaves a slot per segment and one more for each worker that shares it.  Shared: a list
-// of r rows in b blocks takes at most r + 16 b rows for its segments of a kv head, and has at most r / 64 + 1 blocks; there are at most 2 all / 33 such lists.
+// Rows of slots at most, whatever the sequences' counts.  A worker leaves a slot per segment and one more for each worker that shares it.  A shared
+// list of r rows takes at most r + 15 for its segments of a kv head.
 struct SlotRows { int64_t shared, prompts, responses; };
 SlotRows slot_rows(int64_t n_groups, int64_t n_seqs, int64_t total, int64_t Hq, int64_t Hkv, bool f32) {
-    const int64_t all = total * (Hq / Hkv), widest = std::min<int64_t>(64 * MAX_NC, (all + 63) / 64 * 64), solo = std::min<int64_t>(SOLO_ROWS, all);
+    const int64_t all = total * (Hq / Hkv), widest = std::min<int64_t>(WIDE_ROWS, (all + 15) / 16 * 16), solo = std::min<int64_t>(SOLO_ROWS, all);
     const int64_t more = f32 ? all / SOLO_ROWS : 0;      // blocks of solo lists beyond the first
     SlotRows s;
-    s.shared = !f32 && all > SOLO_ROWS ? PLAN_WGS * widest + Hkv * (2 * all + 16 * (std::min(n_groups + n_seqs, 2 * all / (SOLO_ROWS + 1) + 1) + 2 * all / 64)) : 0;
+    s.shared = !f32 && all > SOLO_ROWS ? PLAN_WGS * widest + Hkv * (2 * all + 16 * std::min(n_groups + n_seqs, 2 * all / (SOLO_ROWS + 1) + 1)) : 0;
     s.prompts = (4 * PLAN_WGS + Hkv * (n_groups + more)) * solo;
     s.responses = (4 * PLAN_WGS + Hkv * (n_groups + n_seqs + 2 * more)) * solo;
     return s;
@@ -32,7 +32,7 @@ SlotRows slot_rows(int64_t n_groups, int64_t n_seqs, int64_t total, int64_t Hq, 
 size_t tree_partial_bytes(int n_groups, int n_seqs, int64_t total, int Hq, int Hkv, int d, bool f32) {
     const SlotRows s = slot_rows(n_groups, n_seqs, total, Hq, Hkv, f32);
     const size_t rows = (size_t)(s.shared + s.prompts + s.responses);
-    return desc_bytes((int64_t)n_groups + n_seqs) + up256(rows * 8) + up256(rows * d * 4);
+    return desc_bytes((int64_t)n_groups + n_seqs) + up256(rows * 16) + up256(rows * d * 4);
 }
 
 size_t tree_table_bytes(int n_groups, int n_seqs) { return up256(((size_t)n_groups + n_seqs + 2) * 4); }
@@ -62,7 +62,7 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
     const SlotRows slots = slot_rows(n_groups, n_seqs, total, Hq, a.Hkv, cache.f32);
     a.desc = (i32x4*)partials;
     a.stats = (float*)((char*)partials + desc_bytes((int64_t)n_groups + n_seqs));
-    a.sums = a.stats + up256((size_t)(slots.shared + slots.prompts + slots.responses) * 8) / 4;
+    a.sums = a.stats + up256((size_t)(slots.shared + slots.prompts + slots.responses) * 16) / 4;
     a.prompt_base = slots.shared;
     a.resp_base = slots.shared + slots.prompts;
     // Groups and sequences of one count need no table of where they start
@@ -88,22 +88,13 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
     const int n_lists = n_groups + n_seqs;
     // (prompts, then responses)
     auto rows_of = [&](int i) { const int k = i < n_groups ? i : i + 1; return (int64_t)a.rep * (starts[k + 1] - starts[k]); };
-    // Row tiles per wave and workgroups: as in launch_decode()
-    a.nc = 1;
-    for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) {
-        const int64_t rows = rows_of(i);
-        if (rows <= SOLO_ROWS || cache.f32) continue;
-        const int64_t tiles = (rows + 15) / 16, blocks = (tiles + 4 * MAX_NC - 1) / (4 * MAX_NC), per = (tiles + blocks - 1) / blocks;
-        a.nc = std::max(a.nc, (int)((per + 3) / 4));
-    }
     double units_shared = 0, units_solo = 0;
     for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) {
         const int64_t rows = rows_of(i);
         const double tokens = (double)(i < n_groups ? prompt_width : resp_width) * (1 << a.log_page);
         if (rows > SOLO_ROWS && !cache.f32) {
-            const int64_t tiles = (rows + 15) / 16, blocks = (rows + 64 * a.nc - 1) / (64 * a.nc);
-            a.shared_rows = std::max(a.shared_rows, (int)(16 * ((tiles + blocks - 1) / blocks)));
-            units_shared += (double)blocks * (tokens / 64 + 1) * a.Hkv;
+            a.shared_rows = std::max(a.shared_rows, (int)std::min<int64_t>(WIDE_ROWS, (rows + 15) / 16 * 16));
+            units_shared += (double)((rows + WIDE_ROWS - 1) / WIDE_ROWS) * (tokens / 64 + 1) * a.Hkv;
         } else {
             int& solo = i < n_groups ? a.prompt_rows : a.resp_rows;
             solo = std::max(solo, (int)std::min<int64_t>(rows, SOLO_ROWS));
@@ -111,11 +102,11 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
         }
     }
     const unsigned grid = (unsigned)std::min<double>(PLAN_WGS, units_shared + units_solo / 4 + 1);
-    a.shared_cost = a.nc == 1 ? 3.f : a.nc == 2 ? 4.f : 5.5f;
+    a.shared_cost = 4.f;
     a.kv_heads = make_div(a.Hkv);
     a.q_heads = make_div(Hq);
     a.heads_each = make_div(a.rep);
-    a.block_rows = make_div(64 * a.nc);
+    a.block_rows = make_div(WIDE_ROWS);
     a.prompt_cap = (int)std::min<int64_t>((int64_t)prompt_width << a.log_page, MAX_TOKENS);
     a.resp_cap = (int)std::min<int64_t>((int64_t)resp_width << a.log_page, MAX_TOKENS);
     auto launch = [&](auto dim) {
@@ -126,9 +117,7 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
             auto with_solo = [&](auto ns) {
                 constexpr int NS = decltype(ns)::value;
                 if (units_shared == 0) with(decode_kernel<D, 0, NS, MANY, true>);
-                else if (a.nc == 1) with(decode_kernel<D, 1, NS, MANY, true>);
-                else if (a.nc == 2) with(decode_kernel<D, 2, NS, MANY, true>);
-                else with(decode_kernel<D, 3, NS, MANY, true>);
+                else with(decode_kernel<D, 1, NS, MANY, true>);
             };
             if (cache.f32) with(decode_f32_kernel<D, MANY, true>);
             else if (std::max(a.prompt_rows, a.resp_rows) <= 16) with_solo(std::integral_constant<int, 1>{});
