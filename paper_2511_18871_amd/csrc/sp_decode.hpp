@@ -182,6 +182,14 @@ __device__ __forceinline__ void shared_runs(const DecodeArgs& a, unsigned solo, 
     }
 }
 
+// Which run of the shared units a workgroup takes.  Drafted tokens: consecutive runs go to one XCD (workgroups are dealt round-robin over the 8), and
+// the segments of a kv head lie one behind the other, so that the workgroups that read a head's keys for different rows find them in one L2.
+template <bool TREE> __device__ __forceinline__ unsigned shared_worker(unsigned used) {
+    if constexpr (!TREE) return blockIdx.x;
+    const unsigned x = blockIdx.x & 7, each = used >> 3, more = used & 7;
+    return x * each + min(x, more) + (blockIdx.x >> 3);
+}
+
 // Every workgroup makes the whole plan.  Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time, and
 // takes a cycle a byte.
 // Up to 64 lists: a wave by itself, a list to a lane (one sequence of 1k tokens 5.7 us, by the workgroup 7.0; a group of 8 8.2 and 11.0).
@@ -217,7 +225,7 @@ __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, 
     }
     Work work;
     work.shared = blockIdx.x < runs.used;
-    work.worker = work.shared ? (int)blockIdx.x : (int)(blockIdx.x - runs.used) * 4 + wave;
+    work.worker = work.shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * 4 + wave;
     const unsigned run = work.shared ? runs.shared_run : runs.solo_run, all = work.shared ? shared_room : solo, pos = (unsigned)work.worker * run;
     // (through a lane read: without it the compiler left the comparison out and took the difference, wrapped, as it was)
     work.left = pos < all ? __builtin_amdgcn_readfirstlane((int)min(run, all - pos)) : 0;
@@ -297,7 +305,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     // this workgroup's runs start at `first` and multiples of the run behind it
     Work work;
     const bool shared = work.shared = blockIdx.x < runs.used;
-    const unsigned run = shared ? runs.shared_run : runs.solo_run, many = shared ? 1 : 4, first = (shared ? blockIdx.x : 4 * (blockIdx.x - runs.used)) * run;
+    const unsigned run = shared ? runs.shared_run : runs.solo_run, many = shared ? 1 : 4, first = (shared ? shared_worker<TREE>(runs.used) : 4 * (blockIdx.x - runs.used)) * run;
     const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know
     const int mine = KIND && shared ? SHARED : 0;
     const unsigned through = (unsigned)(mine ? to[SHARED] : to[0]) * a.Hkv, ahead = through - (unsigned)(mine ? own[SHARED] : own[0]) * a.Hkv;
@@ -330,7 +338,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     const int slot = shared ? 0 : wave;
     const unsigned pos = first + slot * run, end = mine ? all[SHARED] : all[0];
     work.left = pos < end ? scalar((int)min(run, end - pos)) : 0;
-    work.worker = scalar(shared ? (int)blockIdx.x : (int)(blockIdx.x - runs.used) * 4 + wave);
+    work.worker = scalar(shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * 4 + wave);
     work.list = scalar(share.list[slot]);
     work.at = scalar(share.at[slot]);
     work.ord = scalar(share.ord[slot]);
@@ -339,7 +347,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     return work;
 }
 
-// A place among the units: of list `list` segment `seg` (block * n_kv_heads + kv head), unit `t`
+// A place among the units: of list `list` segment `seg` (block * n_kv_heads + kv head; drafted tokens: kv head * blocks + block), unit `t`
 template <int KIND, bool TREE = false>
 struct Cursor {
     const Lists<KIND, TREE>& ls;
@@ -364,6 +372,9 @@ struct Cursor {
         segs = blocks * ls.a.Hkv;
         return s.shared == shared;
     }
+    __device__ __forceinline__ int kv_head() const {      // TREE
+        return blocks > 1 ? __builtin_amdgcn_readfirstlane((int)((unsigned)seg / (unsigned)blocks)) : seg;
+    }
     // the next unit; there is one
     __device__ __forceinline__ void next() {
         if (++t < units) return;
@@ -384,9 +395,14 @@ struct SegmentRows {
     int64_t base;                                // of row0 among the rows of sums
     Div heads_each;
     template <int KIND, bool TREE> __device__ __forceinline__ SegmentRows(const Cursor<KIND, TREE>& c, const DecodeArgs& a, int worker) {
-        unsigned k;
-        block = c.blocks > 1 ? (int)divmod((unsigned)c.seg, a.kv_heads, k) : 0;
-        kvh = c.blocks > 1 ? (int)k : c.seg;
+        if constexpr (TREE) {
+            kvh = c.kv_head();
+            block = c.seg - kvh * c.blocks;
+        } else {
+            unsigned k;
+            block = c.blocks > 1 ? (int)divmod((unsigned)c.seg, a.kv_heads, k) : 0;
+            kvh = c.blocks > 1 ? (int)k : c.seg;
+        }
         const int per = !c.shared ? SOLO_ROWS : TREE ? WIDE_ROWS : 16 * (((((c.rows + 15) >> 4)) + c.blocks - 1) / c.blocks);
         row0 = block * per;
         rows = min(per, c.rows - row0);
@@ -394,7 +410,7 @@ struct SegmentRows {
         rep = a.rep; Hq = a.Hq; heads_each = a.heads_each;
         if constexpr (TREE && KIND) {
             if (c.shared) {      // (the segment's own rows lie behind those of the segments ahead of it, not each in room for the largest)
-                base = (int64_t)worker * a.shared_rows + ((int64_t)(c.ord + block * (WIDE_ROWS / 16)) * a.Hkv + kvh * ((rows + 15) >> 4)) * 16;
+                base = (int64_t)worker * a.shared_rows + ((int64_t)c.ord * a.Hkv + kvh * c.places + block * (WIDE_ROWS / 16)) * 16;
                 return;
             }
         }
@@ -712,6 +728,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
     if (work.left == 0) return;
     Cursor<KIND, TREE> at(ls, work);
     auto kv_head = [&]() SP_INLINE {
+        if constexpr (TREE) return at.kv_head();
         unsigned k = (unsigned)at.seg;
         if (KIND && at.blocks > 1) divmod((unsigned)at.seg, a.kv_heads, k);
         return (int)k;
@@ -1265,19 +1282,26 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
         first = tok - (int)rest;
         if constexpr (TREE) { seq = (int)divmod((unsigned)tok, a.seq_size, rest); node = (int)rest; own = a.each; }
     } else {
-        auto last_from = [&](int b, int e) {      // the last of words b .. e - 1 that is not above the token
-            while (e - b > 1) { const int mid = (b + e) >> 1; if (w[mid] <= tok) b = mid; else e = mid; }
-            return b;
-        };
-        g = last_from(0, a.n_groups);
+        if constexpr (TREE) {
+            // the last of the groups, and of the sequences, that starts at the token or ahead of it: as many candidates at a time as the row has lanes
+            auto narrow = [&](int& b, int& e) {
+                const int step = (e - b + EACH - 1) / EACH, i = b + l * step;
+                const uint64_t all = __builtin_amdgcn_ballot_w64(i < e && w[i] <= tok);
+                const uint64_t mine = EACH == 64 ? all : all >> (threadIdx.x & 63 & ~(EACH - 1)) & ((1ull << (EACH & 63)) - 1);
+                b += (__popcll(mine) - 1) * step;
+                e = min(e, b + step);
+            };
+            int ge = a.n_groups, sb = a.n_groups + 1, se = sb + a.n_seqs;
+            while (__builtin_amdgcn_ballot_w64(ge - g > 1 || se - sb > 1)) { narrow(g, ge); narrow(sb, se); }
+            seq = sb - a.n_groups - 1;
+            node = tok - w[sb];
+            own = w[sb + 1] - w[sb];
+        } else {
+            int hi = a.n_groups;
+            while (hi - g > 1) { const int mid = (g + hi) >> 1; if (w[mid] <= tok) g = mid; else hi = mid; }
+        }
         first = w[g];
         members = w[g + 1] - first;
-        if constexpr (TREE) {
-            const int at = last_from(a.n_groups + 1, a.n_groups + 1 + a.n_seqs);
-            seq = at - a.n_groups - 1;
-            node = tok - w[at];
-            own = w[at + 1] - w[at];
-        }
     }
     // The side's chunks: consecutive slots, those of the workers that had units of this row's segment, from the first one's on.  Rows of slots
     // are below 2^32: a workspace of so many has more than 1 TB.
@@ -1291,13 +1315,13 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
         const int blocks = (int)divmod((unsigned)(rows - 1), a.block_rows, rest) + 1;
         if (shared) per = TREE ? WIDE_ROWS : 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
     }
-    const int block = rows > per ? row / per : 0, segment = block * a.Hkv + kvh;
+    const int block = rows > per ? row / per : 0, segment = TREE ? kvh * ((rows + per - 1) / per) + block : block * a.Hkv + kvh;
     const unsigned each = shared ? run[0] : run[1], from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[3];
     const unsigned worker0 = from / each, worker1 = (from + d[1] - 1) / each;
     const unsigned stride = shared ? a.shared_rows : resp ? a.resp_rows : a.prompt_rows;
     unsigned at = (unsigned)(shared ? 0 : resp ? a.resp_base : a.prompt_base) + (worker0 + (unsigned)d[2] * a.Hkv + segment) * stride + row - block * per;
     if (TREE && shared)
-        at = worker0 * stride + ((unsigned)(d[2] + block * (per >> 4)) * a.Hkv + kvh * ((min(per, rows - block * per) + 15) >> 4)) * 16 + row - block * per;
+        at = worker0 * stride + ((unsigned)d[2] * a.Hkv + kvh * ((rows + 15) >> 4) + block * (per >> 4)) * 16 + row - block * per;
     const int count = d[1] > 0 ? (int)(worker1 - worker0) + 1 : 0;
     auto prompts = [](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x00, 0xf, 0xf, true); };     // of the even lanes
     auto resps = [](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x55, 0xf, 0xf, true); };       // of the odd ones
