@@ -36,7 +36,10 @@ namespace {
 #define SP_INLINE __attribute__((always_inline))      // lambdas: what they refer to has to stay in registers
 
 constexpr int SOLO_ROWS = 32;              // rows of a segment that a wave takes by itself
-constexpr int WIDE_ROWS = 128;             // rows of drafted tokens that a workgroup takes: 32 to a wave
+// Drafted tokens
+constexpr int WIDE_ROWS = 256;             // rows that a workgroup takes at most: 32 to a wave
+constexpr int TREE_SOLO_ROWS = 48;         // rows of a list that a wave takes by itself where other lists are shared (bf16)
+constexpr int WIDE_PAD = 3;                // units that a segment of many rows costs beside its own: first loads, last product, sums
 constexpr int MAX_NC = 3;                  // row tiles of 16 of a wave that shares its keys: 192 rows to a workgroup
 constexpr int PLAN_WGS = 512;              // workgroups that the units are dealt to: two to a CU (one: 131 -> 164 us for the 64 prompts above)
 
@@ -55,6 +58,8 @@ struct DecodeArgs {
     Div seq_size;                          // of `each`
     const uint32_t* ancestors;             // a row per token, NULL: a chain
     int64_t mask_stride;
+    Div solo_rows;                         // rows of a block of a solo list
+    int wide_prompts, wide_resps;          // prompts, responses with more rows than this are shared
     int nc;                                // row tiles per wave of a shared segment
     float shared_cost;                     // of a shared unit, against a solo one
     Div group_size, block_rows;            // of `members`, of the rows of a shared segment (64 nc)
@@ -90,7 +95,7 @@ struct ListShape {                        // units of keys of a segment; blocks 
         return blocks;
     }
 };
-struct PlanShare { int sums[4][5]; int list[4], at[4], ord[4], rows[4], len[4], room[4]; };      // of the waves of a workgroup; where their runs start
+template <int NW> struct PlanShare { int sums[NW][5]; int list[NW], at[NW], ord[NW], rows[NW], len[NW], room[NW]; };      // of the waves of a workgroup; where their runs start
 
 // First tokens of the groups, the number of tokens, first tokens of the sequences, and that number again: in 16 bits among the kernel's arguments, or in
 // the workspace.  (A table that is stored by a launch of its own costs 5 us for each 896 words.)
@@ -132,14 +137,15 @@ struct Lists {
         else if (prompt) members = a.members ? a.members : starts[i + 1] - starts[i];
         return i32x2{a.rep * members, min(max(n, -1), prompt ? prompt_cap : resp_cap)};
     }
-    __device__ __forceinline__ ListShape shape(i32x2 x) const {
+    __device__ __forceinline__ ListShape shape(i32x2 x, int i) const {
         ListShape s;
         s.rows = x[0];
         s.len = x[1];
-        s.shared = KIND && s.rows > SOLO_ROWS;
+        s.shared = KIND && s.rows > (!TREE ? SOLO_ROWS : i < a.n_groups ? a.wide_prompts : a.wide_resps);
         s.units = s.rows > 0 && s.len > 0 ? (int)(((unsigned)s.len + (s.shared ? 63u : 31u)) >> (s.shared ? 6 : 5)) : 0;
         unsigned rest;
-        s.blocks = s.shared ? (int)divmod((unsigned)(s.rows - 1), a.block_rows, rest) + 1 : (s.rows + SOLO_ROWS - 1) / SOLO_ROWS;
+        if constexpr (TREE) s.blocks = s.rows <= 0 ? 0 : (int)divmod((unsigned)(s.rows - 1), s.shared ? a.block_rows : a.solo_rows, rest) + 1;
+        else s.blocks = s.shared ? (int)divmod((unsigned)(s.rows - 1), a.block_rows, rest) + 1 : (s.rows + SOLO_ROWS - 1) / SOLO_ROWS;
         return s;
     }
     __device__ __forceinline__ int first_seq(int i) const {      // TREE: its first token
@@ -159,26 +165,28 @@ __device__ __forceinline__ unsigned per_place(unsigned total, unsigned places) {
     return max(c, 1u);
 }
 // units of room that a segment has among those of its kind
-__device__ __forceinline__ int room_of(int units, unsigned run, bool aligned) { return aligned && units > 0 ? (int)(per_place(units, run) * run) : units; }
+template <bool TREE> __device__ __forceinline__ int room_of(int units, unsigned run, bool aligned) {
+    return units <= 0 ? units : aligned ? (int)(per_place(units, run) * run) : TREE ? units + WIDE_PAD : units;
+}
 
 // What a worker does: `left` units from unit `at` of a list on (counted over the list's segments).
-struct Work { bool shared; int worker, list, at, ord, left, room; i32x2 list_is; };
+struct Work { bool shared; int worker, list, at, ord, left, room, pad; i32x2 list_is; };      // pad: units of a segment's room that are none
 
 // The runs of either kind, from the units and segments of all lists.  Places are dealt by cost: a segment costs, for its rows and its sums, what one and a half of its
 // units (shared) or one (solo) cost, and a shared unit what shared_cost solo ones do.  A worker that passes from one segment to another takes
 // longer; where shared segments are long against the run, each is dealt to workers of its own, in room that is a multiple of the run (`aligned`: 37.8 us
 // for the prompt of 16k tokens, 41.4 without).
 struct Runs { unsigned shared_run, solo_run, used; bool aligned; };      // used: workgroups of shared segments
-template <int KIND>
+template <int KIND, bool TREE, int WGS>
 __device__ __forceinline__ void shared_runs(const DecodeArgs& a, unsigned solo, unsigned solo_segs, unsigned shared, unsigned segs, Runs& r) {
     r = Runs{1, 1, 0, false};
     if constexpr (KIND) {
         if (shared == 0) return;
-        const float cost = a.shared_cost * ((float)shared + 1.5f * (float)segs);
-        int wgs = (int)(PLAN_WGS * (cost * __builtin_amdgcn_rcpf(cost + (float)solo + (float)solo_segs)));
-        wgs = max(1, min(wgs, solo ? PLAN_WGS - 1 : PLAN_WGS));
+        const float cost = a.shared_cost * ((float)shared + (TREE ? (float)WIDE_PAD : 1.5f) * (float)segs);
+        int wgs = (int)(WGS * (cost * __builtin_amdgcn_rcpf(cost + (float)solo + (float)solo_segs)));
+        wgs = max(1, min(wgs, solo ? WGS - 1 : WGS));
         r.aligned = 4 * segs <= (unsigned)wgs;
-        r.shared_run = per_place(shared, r.aligned ? wgs - segs : wgs);
+        r.shared_run = r.aligned ? per_place(shared, wgs - segs) : per_place(shared + (TREE ? WIDE_PAD * segs : 0), wgs);
     }
 }
 
@@ -193,14 +201,15 @@ template <bool TREE> __device__ __forceinline__ unsigned shared_worker(unsigned 
 // Every workgroup makes the whole plan.  Written for few instructions: what a workgroup runs once comes from memory, 64 bytes at a time, and
 // takes a cycle a byte.
 // Up to 64 lists: a wave by itself, a list to a lane (one sequence of 1k tokens 5.7 us, by the workgroup 7.0; a group of 8 8.2 and 11.0).
-template <int KIND, bool TREE>
+template <int NW, int KIND, bool TREE>
 __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, int wave, int lane) {
+    constexpr int WGS = 4 * PLAN_WGS / NW;
     const DecodeArgs& a = ls.a;
     const int n = a.n_groups + a.n_seqs;
     const bool there = lane < n;
     i32x2 mine{0, 0};
     if (there) mine = ls.read(lane);
-    const ListShape s = ls.shape(mine);
+    const ListShape s = ls.shape(mine, lane);
     auto last = [](int x) SP_INLINE { return (unsigned)__builtin_amdgcn_readlane(x, 63); };
     const int solo_units = s.shared ? 0 : s.units * s.blocks, solo_blocks = s.shared ? 0 : s.blocks;
     const int to_solo = scan64(solo_units), ord_solo = scan64(solo_blocks);
@@ -211,21 +220,21 @@ __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, 
     if constexpr (KIND) {
         const int shared_units = s.shared ? s.units * s.blocks : 0, shared_blocks = s.shared ? s.template places<TREE>() : 0;
         const int ord_shared = scan64(shared_blocks), segments = TREE ? scan64(s.shared ? s.blocks : 0) : ord_shared;
-        shared_runs<KIND>(a, solo, last(ord_solo) * a.Hkv, last(scan64(shared_units)) * a.Hkv, last(segments) * a.Hkv, runs);
-        if (s.shared) { room = room_of(s.units, runs.shared_run, runs.aligned); units = room * s.blocks; ord = ord_shared - shared_blocks; }
+        shared_runs<KIND, TREE, WGS>(a, solo, last(ord_solo) * a.Hkv, last(scan64(shared_units)) * a.Hkv, last(segments) * a.Hkv, runs);
+        if (s.shared) { room = room_of<TREE>(s.units, runs.shared_run, runs.aligned); units = room * s.blocks; ord = ord_shared - shared_blocks; }
         const int to_shared = scan64(s.shared ? units : 0);
         if (s.shared) to = to_shared;
         shared_room = last(to_shared) * a.Hkv;
         if (shared_room) runs.used = per_place(shared_room, runs.shared_run);
     }
-    if (solo) runs.solo_run = per_place(solo, 4 * (PLAN_WGS - runs.used));
+    if (solo) runs.solo_run = per_place(solo, NW * (WGS - runs.used));
     if (blockIdx.x == 0 && wave == 0) {          // what the join needs to know
         if (there) a.desc[1 + lane] = i32x4{to - units, s.units, ord, s.len < 0 ? -1 : room};
         if (lane == 0) a.desc[0] = i32x4{(int)runs.shared_run, (int)runs.solo_run, 0, 0};
     }
     Work work;
     work.shared = blockIdx.x < runs.used;
-    work.worker = work.shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * 4 + wave;
+    work.worker = work.shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * NW + wave;
     const unsigned run = work.shared ? runs.shared_run : runs.solo_run, all = work.shared ? shared_room : solo, pos = (unsigned)work.worker * run;
     // (through a lane read: without it the compiler left the comparison out and took the difference, wrapped, as it was)
     work.left = pos < all ? __builtin_amdgcn_readfirstlane((int)min(run, all - pos)) : 0;
@@ -236,24 +245,26 @@ __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, 
     work.at = (int)(pos - (unsigned)of((int)from));
     work.ord = of(ord);
     work.room = of(room);
+    work.pad = TREE && work.shared && !runs.aligned ? WIDE_PAD : 0;
     work.list_is = i32x2{of(mine[0]), of(mine[1])};
     return work;
 }
 
 // More lists: a thread adds up the units of its share of them (they lie in LDS meanwhile, if there are no more than n_held), the workgroup their sums.
-template <int KIND, bool TREE>
-__device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* held, int n_held, PlanShare& share, int wave, int lane) {
+template <int NW, int KIND, bool TREE>
+__device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* held, int n_held, PlanShare<NW>& share, int wave, int lane) {
     constexpr int SUMS = KIND ? TREE ? 5 : 4 : 2;       // solo units and blocks, shared units and blocks (TREE: and places)
+    constexpr int WGS = 4 * PLAN_WGS / NW, ALL = 64 * NW;
     const DecodeArgs& a = ls.a;
-    const int n = a.n_groups + a.n_seqs, per = (n + 255) >> 8, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
+    const int n = a.n_groups + a.n_seqs, per = (n + 64 * NW - 1) / (64 * NW), i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
     const bool in_lds = n <= n_held;
     if (in_lds) {
-        for (int i = threadIdx.x; i < n; i += 256 * 4) {      // four reads in flight
+        for (int i = threadIdx.x; i < n; i += ALL * 4) {      // four reads in flight
             i32x2 x[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) if (i + 256 * u < n) x[u] = ls.read(i + 256 * u);
+            for (int u = 0; u < 4; ++u) if (i + ALL * u < n) x[u] = ls.read(i + ALL * u);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) if (i + 256 * u < n) held[i + 256 * u] = x[u];
+            for (int u = 0; u < 4; ++u) if (i + ALL * u < n) held[i + ALL * u] = x[u];
         }
         __syncthreads();
     }
@@ -277,35 +288,35 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
         __syncthreads();
         unsigned sum = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) { const int x = share.sums[w][k]; to[k] += w < wave ? x : 0; sum += x; }
+        for (int w = 0; w < NW; ++w) { const int x = share.sums[w][k]; to[k] += w < wave ? x : 0; sum += x; }
         all[k] = sum * a.Hkv;
     };
 #pragma unroll 1
     for (int i = i0; i < i1; ++i) {
-        const ListShape s = ls.shape(list_of(i));
+        const ListShape s = ls.shape(list_of(i), i);
         add(own, s, s.units);
     }
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) over_waves(k);
     Runs runs{1, 1, 0, false};
     if constexpr (KIND) {
-        shared_runs<KIND>(a, all[0], all[1], all[SHARED], all[SEGS], runs);
-        if (runs.aligned) {
+        shared_runs<KIND, TREE, WGS>(a, all[0], all[1], all[SHARED], all[SEGS], runs);
+        if (runs.aligned || TREE) {
             own[SHARED] = 0;
 #pragma unroll 1
             for (int i = i0; i < i1; ++i) {
-                const ListShape s = ls.shape(list_of(i));
-                own[SHARED] += s.shared ? room_of(s.units, runs.shared_run, true) * s.blocks : 0;
+                const ListShape s = ls.shape(list_of(i), i);
+                own[SHARED] += s.shared ? room_of<TREE>(s.units, runs.shared_run, runs.aligned) * s.blocks : 0;
             }
             over_waves(SHARED);
         }
         if (all[SHARED]) runs.used = per_place(all[SHARED], runs.shared_run);
     }
-    if (all[0]) runs.solo_run = per_place(all[0], 4 * (PLAN_WGS - runs.used));
+    if (all[0]) runs.solo_run = per_place(all[0], NW * (WGS - runs.used));
     // this workgroup's runs start at `first` and multiples of the run behind it
     Work work;
     const bool shared = work.shared = blockIdx.x < runs.used;
-    const unsigned run = shared ? runs.shared_run : runs.solo_run, many = shared ? 1 : 4, first = (shared ? shared_worker<TREE>(runs.used) : 4 * (blockIdx.x - runs.used)) * run;
+    const unsigned run = shared ? runs.shared_run : runs.solo_run, many = shared ? 1 : NW, first = (shared ? shared_worker<TREE>(runs.used) : NW * (blockIdx.x - runs.used)) * run;
     const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know
     const int mine = KIND && shared ? SHARED : 0;
     const unsigned through = (unsigned)(mine ? to[SHARED] : to[0]) * a.Hkv, ahead = through - (unsigned)(mine ? own[SHARED] : own[0]) * a.Hkv;
@@ -316,8 +327,8 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
 #pragma unroll 1
         for (int i = i0; i < i1; ++i) {
             const i32x2 x = list_of(i);
-            const ListShape s = ls.shape(x);
-            const int units = s.shared ? at[SHARED] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1], room = room_of(s.units, runs.shared_run, s.shared && runs.aligned);
+            const ListShape s = ls.shape(x, i);
+            const int units = s.shared ? at[SHARED] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1], room = s.shared ? room_of<TREE>(s.units, runs.shared_run, runs.aligned) : s.units;
             const unsigned from = (unsigned)units * a.Hkv, end = from + (unsigned)(room * s.blocks) * a.Hkv;
             if (s.shared == shared)
 #pragma unroll 1
@@ -338,11 +349,12 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     const int slot = shared ? 0 : wave;
     const unsigned pos = first + slot * run, end = mine ? all[SHARED] : all[0];
     work.left = pos < end ? scalar((int)min(run, end - pos)) : 0;
-    work.worker = scalar(shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * 4 + wave);
+    work.worker = scalar(shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * NW + wave);
     work.list = scalar(share.list[slot]);
     work.at = scalar(share.at[slot]);
     work.ord = scalar(share.ord[slot]);
     work.room = scalar(share.room[slot]);
+    work.pad = TREE && shared && !runs.aligned ? WIDE_PAD : 0;
     work.list_is = i32x2{share.rows[slot], share.len[slot]};
     return work;
 }
@@ -362,10 +374,16 @@ struct Cursor {
         seg -= seg * w.room > w.at;
         seg += (unsigned)(seg + 1) * w.room <= (unsigned)w.at;
         t = w.at - seg * w.room;
-        if (w.room > units) w.left = min(w.left, units - t);        // a run of the segment's own, the last one shorter
+        if (TREE && w.pad) {
+            if (t >= units) {                                      // behind the segment's last unit
+                w.left -= w.room - t;
+                t = units - 1;
+                if (w.left > 0) next();
+            }
+        } else if (w.room > units) w.left = min(w.left, units - t);        // a run of the segment's own, the last one shorter
     }
     __device__ __forceinline__ bool load(i32x2 x) {
-        const ListShape s = ls.shape(x);
+        const ListShape s = ls.shape(x, list);
         auto scalar = [](int x) SP_INLINE { return __builtin_amdgcn_readfirstlane(x); };
         rows = scalar(s.rows); len = scalar(s.len); units = scalar(s.units); blocks = scalar(s.blocks);
         places = TREE ? scalar(s.template places<TREE>()) : blocks;
@@ -403,14 +421,14 @@ struct SegmentRows {
             block = c.blocks > 1 ? (int)divmod((unsigned)c.seg, a.kv_heads, k) : 0;
             kvh = c.blocks > 1 ? (int)k : c.seg;
         }
-        const int per = !c.shared ? SOLO_ROWS : TREE ? WIDE_ROWS : 16 * (((((c.rows + 15) >> 4)) + c.blocks - 1) / c.blocks);
+        const int per = !c.shared ? (TREE ? (int)a.solo_rows.d : SOLO_ROWS) : TREE ? (int)a.block_rows.d : 16 * (((((c.rows + 15) >> 4)) + c.blocks - 1) / c.blocks);
         row0 = block * per;
         rows = min(per, c.rows - row0);
         seq0 = c.ls.first_seq(c.list);
         rep = a.rep; Hq = a.Hq; heads_each = a.heads_each;
         if constexpr (TREE && KIND) {
             if (c.shared) {      // (the segment's own rows lie behind those of the segments ahead of it, not each in room for the largest)
-                base = (int64_t)worker * a.shared_rows + ((int64_t)c.ord * a.Hkv + kvh * c.places + block * (WIDE_ROWS / 16)) * 16;
+                base = (int64_t)worker * a.shared_rows + ((int64_t)c.ord * a.Hkv + kvh * c.places + block * (per >> 4)) * 16;
                 return;
             }
         }
@@ -709,24 +727,27 @@ __device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArg
 }
 
 // NC: row tiles of a wave in a shared segment, 0: no list is shared.  NS: in a solo one.
-template <int D, int NC, int NS, bool MANY, bool TREE = false>
-__global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, DecodeArgs a) {
+// NW: waves of a workgroup; eight (TREE) for lists of many rows.
+template <int D, int NC, int NS, bool MANY, bool TREE = false, int NW = 4>
+__global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> starts, DecodeArgs a) {
     constexpr int KEYS16 = 32 * D, KIND = NC > 0;       // bytes of 16 keys
-    __shared__ __attribute__((aligned(1024))) char lds[16 * KEYS16];
-    __shared__ PlanShare share;
-    __shared__ int left_out;                         // TREE: values were left out of the segment's products
+    __shared__ __attribute__((aligned(1024))) char lds[4 * NW * KEYS16];
+    __shared__ PlanShare<NW> share;
+    // Wide segments of drafted tokens: values were left out of the products; some pages are none of the cache's; pages of 16 keys each
+    __shared__ int left_out, bad_pages, place[TREE && KIND ? 256 : 1];
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<KIND, TREE> ls{words_of(starts), a};
     Work work;
     if constexpr (MANY) {
-        work = find_work(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
+        work = find_work<NW>(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
         __syncthreads();                             // the lists' place is free
     } else {
-        work = find_work_in_lanes(ls, w, l);
+        work = find_work_in_lanes<NW>(ls, w, l);
     }
     if (work.left == 0) return;
     Cursor<KIND, TREE> at(ls, work);
+    if (TREE && work.left <= 0) return;
     auto kv_head = [&]() SP_INLINE {
         if constexpr (TREE) return at.kv_head();
         unsigned k = (unsigned)at.seg;
@@ -747,7 +768,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
     auto next = [&]() SP_INLINE {
         const int list = at.list;
         at.next();
-        if (at.list != list) { table_of_list(); pages.load(0); }
+        if (at.list != list) { table_of_list(); if (!TREE || !work.shared) pages.load(0); }
         if (at.t == 0) kvh = kv_head();
     };
     table_of_list();
@@ -838,10 +859,11 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
             if (!more) return;
         }
     } else if constexpr (TREE) {
-        // Many drafted tokens: four waves of 32 rows, products on matrix instructions of 32 x 32, software-pipelined as in the forward over a pack: while
+        // Many drafted tokens: four or eight waves of 32 rows, products on matrix instructions of 32 x 32, software-pipelined as in the forward over a pack: while
         // step j's matrix instructions form O^T += V(j-1)^T P(j-1)^T and S(j+1) = K(j+1) Q^T, its vector ones turn S(j) into P(j), a score to a
-        // matrix instruction (two, heads of 64).  Two buffers of 64 keys each of K and of V, a barrier per step: V(j) and K(j+2) are copied under step j.
-        constexpr int TILE = 4 * KEYS16, KS = D / 16, MF = 2 * KS, DB = D / 32, PER = 32 / (2 * MF), RD = 3;
+        // matrix instruction (two, heads of 64).  Four waves: two buffers of 64 keys each of K and of V, a barrier per step; V(j) and K(j+2) are copied under step
+        // j, and two workgroups share a CU.  Eight waves: four buffers each, two steps to a barrier; a copy serves twice the rows and has twice the time.
+        constexpr int TILE = 4 * KEYS16, KS = D / 16, MF = 2 * KS, DB = D / 32, PER = 32 / (2 * MF), RD = 3, NB = NW == 8 ? 4 : 2;
         const int c32 = l & 31, hh = l >> 5, j16 = l & 15;
         unsigned row_at[KS], tr_at[DB][2];         // operands within the first buffers
 #pragma unroll
@@ -851,7 +873,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int col4 = 32 * db + 16 * ((l >> 4) & 1) + 4 * (j16 & 3);
-                tr_at[db][half] = buf + 2 * TILE + kv_off<D>(4 * hh + (j16 >> 2) + 8 * half, col4 >> 3) + ((col4 & 4) << 1);
+                tr_at[db][half] = buf + NB * TILE + kv_off<D>(4 * hh + (j16 >> 2) + 8 * half, col4 >> 3) + ((col4 & 4) << 1);
                 asm volatile("" : "+v"(tr_at[db][half]));
             }
         auto ldK = [&](int b, int i) SP_INLINE { return lds_at_row8(row_at[i >> 1] + TILE * b + 2 * KEYS16 * (i & 1)); };
@@ -875,49 +897,57 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
             const SegmentRows seg(at, a, work.worker);
             const int total = min(work.left, at.units - at.t), key0 = 64 * at.t;
             const bool active = 32 * w < seg.rows;
-            // A tile of keys: this wave's 16 of them (place, how many there are), and which of all 64 there are
-            struct Tile { uint64_t off; int valid; unsigned lo, hi; };
-            auto fetch = [&](int j) SP_INLINE {
-                Tile t{0, 16, 0xffffffffu, 0xffffffffu};
-                const int key = key0 + 64 * j;
-                if (whole(key, 64)) {
-                    t.off = offset(key + 16 * w, __builtin_amdgcn_readfirstlane(pages.at((key + 16 * w) >> a.log_page)));
-                    return t;
+            // Pages of every 16 keys of up to 64 tiles, -1: none, filled in by all threads ahead of their use
+            auto fill = [&](int j, int tiles) SP_INLINE {
+                if ((int)threadIdx.x >= 4 * tiles) return;
+                const unsigned key = (unsigned)key0 + 64u * j + 16u * threadIdx.x;
+                int page = -1;
+                if (key < (unsigned)at.len) {
+                    page = pages.table[key >> a.log_page];
+                    if ((unsigned)page >= (unsigned)a.n_pages) { page = -1; bad_pages = 1; }
                 }
-                t.lo = t.hi = 0;
-#pragma unroll 1
-                for (int h = 0; h < 4; ++h) {
-                    uint64_t off;
-                    int v;
-                    locate(key + 16 * h, off, v);
-                    if (h == w) { t.off = off; t.valid = v; }
-                    (h < 2 ? t.lo : t.hi) |= low_bits(v) << (16 * (h & 1));
-                }
-                return t;
+                place[(4 * j + threadIdx.x) & 255] = page;
             };
-            auto issue = [&](uint64_t cache, const Tile& t, int b) SP_INLINE { copy.rows16(cache + t.off, t.valid, buf + (unsigned)b * TILE + w * KEYS16); };
+            struct Tile { uint64_t off; int valid; };      // this wave's 16 keys of a tile
+            auto fetch = [&](int j) SP_INLINE {
+                const int page = __builtin_amdgcn_readfirstlane(place[(4 * j + (w & 3)) & 255]), key = key0 + 64 * j + 16 * (w & 3);
+                return Tile{offset(key, max(page, 0)), page < 0 ? 0 : min(16, at.len - key)};
+            };
+            auto copy_k = [&](int j, int b) SP_INLINE {         // K(j) into buffer b; of eight waves, the first four
+                if (j >= total || (NW == 8 && w >= 4)) return;
+                const Tile t = fetch(j);
+                copy.rows16(kc + t.off, t.valid, buf + (unsigned)b * TILE + (w & 3) * KEYS16);
+            };
+            auto copy_v = [&](int j, int b) SP_INLINE {
+                if (j >= total || (NW == 8 && w < 4)) return;
+                const Tile t = fetch(j);
+                copy.rows16(vc + t.off, t.valid, buf + (unsigned)(NB + b) * TILE + (w & 3) * KEYS16);
+            };
             auto tail = [&](int j) SP_INLINE { return key0 + 64 * (int64_t)j + 64 > drafted.base; };      // holds drafted tokens
-            auto mask = [&](const Tile& t, int j, f32x16 (&S)[2]) SP_INLINE {
+            bool bad = false;
+            auto mask = [&](int j, f32x16 (&S)[2]) SP_INLINE {
                 const bool some = tail(j);
-                if (!some && (t.lo & t.hi) == 0xffffffffu) return;
+                const int n = at.len - key0 - 64 * j;
+                if (!some && !bad && n >= 64) return;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
-                    unsigned bits = kb ? t.hi : t.lo;
+                    unsigned bits = low_bits(n - 32 * kb);
+                    if (bad) bits &= (place[(4 * j + 2 * kb) & 255] < 0 ? 0xffff0000u : ~0u) & (place[(4 * j + 2 * kb + 1) & 255] < 0 ? 0xffffu : ~0u);
                     if (some) bits &= drafted.bits(a, seg, 32 * w + c32, key0 + 64 * j + 32 * kb);
                     mask16(S[kb], bits >> (4 * hh));
                 }
             };
-            auto clean_tile = [&](int j, int b) SP_INLINE {      // of V(j), if it holds drafted tokens; every wave its share
-                if (j < 0 || !tail(j)) return;
-                if (clean(buf + (2 + b) * TILE, threadIdx.x, TILE / 16, 256)) left_out = 1;
+            // takes infinite and NaN values out of V(j) ... V(j + n - 1), in buffers from b on, where these hold drafted tokens; every wave its share
+            auto clean_tiles = [&](int j, int n, int b) SP_INLINE {
+                if (j + n <= 0 || !tail(j + n - 1)) return;
+#pragma unroll
+                for (int i = 0; i < n; ++i)
+                    if (clean(buf + (unsigned)(NB + ((b + i) & (NB - 1))) * TILE, threadIdx.x, TILE / 16, 64 * NW)) left_out = 1;
                 wait_lds();
                 __syncthreads();
             };
             __syncthreads();                           // the last segment's reads from LDS are done
-            pages.load(key0 >> a.log_page);
-            Tile t0 = fetch(0), t1 = t0, t2 = t0;
-            issue(kc, t0, 0);
-            if (total > 1) { t1 = fetch(1); issue(kc, t1, 1); }
+            if (threadIdx.x == 0) left_out = bad_pages = 0;
             bf16x8 qreg[KS];
             {
                 const __bf16* const p = q + seg.q_row(min(32 * w + c32, seg.rows - 1)) * D + 8 * hh;
@@ -925,8 +955,16 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
                 for (int i = 0; i < KS; ++i) qreg[i] = *reinterpret_cast<const bf16x8*>(p + 16 * i);
             }
             // V(-1), which P = 0 is multiplied with: LDS may hold what reads as NaN
-            for (int i = threadIdx.x; i < TILE / 16; i += 256) *(__attribute__((address_space(3))) i32x4*)(uintptr_t)(buf + 3 * TILE + 16 * i) = i32x4{0, 0, 0, 0};
-            if (threadIdx.x == 0) left_out = 0;
+            for (int i = threadIdx.x; i < TILE / 16; i += 64 * NW) *(__attribute__((address_space(3))) i32x4*)(uintptr_t)(buf + (2 * NB - 1) * TILE + 16 * i) = i32x4{0, 0, 0, 0};
+            wait_lds();
+            __syncthreads();
+            fill(0, 64);
+            wait_lds();
+            __syncthreads();
+            bad = bad_pages;
+            copy_k(0, 0);
+            copy_k(1, 1);
+            if constexpr (NB == 4) { copy_k(2, 2); copy_v(0, 0); }
             f32x16 o[DB], sA[2], sB[2];
             unsigned pA[16], pB[16];
 #pragma unroll
@@ -940,7 +978,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
             if (active) {
 #pragma unroll
                 for (int i = 0; i < MF; ++i) sA[i & 1] = mfma32(ldK(0, i), qreg[i >> 1], i < 2 ? zero16 : sA[i & 1]);
-                mask(t0, 0, sA);
+                mask(0, sA);
                 float mx = sA[0][0];
 #pragma unroll
                 for (int e = 1; e < 32; ++e) mx = fmaxf(mx, sA[e >> 4][e & 15]);
@@ -951,9 +989,9 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
             constexpr float LARGE = 4194304.f;
             auto beyond = [&](float x) SP_INLINE { return !(fabsf(x * cs) <= LARGE); };
             auto offset_of = [&](float x) SP_INLINE { return beyond(x) ? 0.f : __builtin_fmaf(-x, cs, x * cs); };
-            auto step = [&](int j, const Tile& t, auto par, f32x16 (&S)[2], f32x16 (&Snext)[2], const unsigned (&p)[16], unsigned (&pnew)[16]) SP_INLINE {
+            auto step = [&](int j, auto par, f32x16 (&S)[2], f32x16 (&Snext)[2], const unsigned (&p)[16], unsigned (&pnew)[16]) SP_INLINE {
                 constexpr int R = decltype(par)::value;
-                mask(t, j, S);
+                mask(j, S);
                 __builtin_amdgcn_sched_barrier(0);
                 const float mc = m * cs;
                 float tsum = 0.f, tprod = 0.f, pe[32];
@@ -964,7 +1002,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
                     if (e >= 2 && (e & 1) == 0) { pnew[(e - 2) >> 1] = pack2(pe[e - 2], pe[e - 1]); asm volatile("" : "+v"(pnew[(e - 2) >> 1])); }
                     if (e >= 3 && (e & 1) == 1) { tprod = sum2(pnew[(e - 3) >> 1], tprod); asm volatile("" : "+v"(tprod)); }
                 };
-                auto operand_at = [&](int i) SP_INLINE { return i < MF ? ldV(1 - R, i) : ldK(1 - R, i - MF); };
+                auto operand_at = [&](int i) SP_INLINE { return i < MF ? ldV((R + NB - 1) % NB, i) : ldK((R + 1) % NB, i - MF); };
                 bf16x8 ring[RD];
 #pragma unroll
                 for (int i = 0; i < RD - 1; ++i) ring[i] = operand_at(i);
@@ -1007,32 +1045,57 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
                 lsum += tsum;
                 lprod += tprod;
             };
-            int vlast = 1;
-            for (int j = 0; j < total; j += 2) {
-                wait_copies<0>();
-                __syncthreads();
-                clean_tile(j - 1, 1);
-                issue(vc, t0, 2);
-                if (j + 2 < total) { t2 = fetch(j + 2); issue(kc, t2, 0); }
-                if (active) step(j, t0, std::integral_constant<int, 0>{}, sA, sB, pA, pB);
-                if (j + 1 >= total) {
+            int vlast = NB - 1;        // buffer of the last V
+            // step j, and whether it was the last one; P of an odd count of steps is in the other registers
+            auto even = [&](int j, auto r) SP_INLINE {
+                if (active) step(j, r, sA, sB, pA, pB);
+                if (j + 1 < total) return false;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) pA[i] = pB[i];
-                    vlast = 0;
-                    break;
-                }
+                for (int i = 0; i < 16; ++i) pA[i] = pB[i];
+                vlast = decltype(r)::value;
+                return true;
+            };
+            auto odd = [&](int j, auto r) SP_INLINE {
+                if (active) step(j, r, sB, sA, pB, pA);
+                vlast = decltype(r)::value;
+                return j + 1 >= total;
+            };
+            auto arrived = [&](int j) SP_INLINE {        // what was copied under the last steps; then the next pages, far ahead of their use
                 wait_copies<0>();
                 __syncthreads();
-                clean_tile(j, 0);
-                issue(vc, t1, 3);
-                t0 = t2;
-                if (j + 3 < total) { t2 = fetch(j + 3); issue(kc, t2, 1); }
-                if (active) step(j + 1, t1, std::integral_constant<int, 1>{}, sB, sA, pB, pA);
-                t1 = t2;
+                if ((j & 31) == 0 && j > 0 && j + 32 < total) fill(j + 32, 32);
+                if ((j & 31) == 4) bad = bad_pages;
+            };
+            constexpr std::integral_constant<int, 0> b0{};
+            constexpr std::integral_constant<int, 1> b1{};
+            if constexpr (NB == 4) {
+                constexpr std::integral_constant<int, 2> b2{};
+                constexpr std::integral_constant<int, 3> b3{};
+                for (int j = 0;; j += 4) {
+                    arrived(j);
+                    clean_tiles(j - 1, 2, 3);
+                    copy_v(j + 1, 1); copy_v(j + 2, 2); copy_k(j + 3, 3); copy_k(j + 4, 0);
+                    if (even(j, b0) || odd(j + 1, b1)) break;
+                    arrived(j + 2);
+                    clean_tiles(j + 1, 2, 1);
+                    copy_v(j + 3, 3); copy_v(j + 4, 0); copy_k(j + 5, 1); copy_k(j + 6, 2);
+                    if (even(j + 2, b2) || odd(j + 3, b3)) break;
+                }
+            } else {
+                for (int j = 0;; j += 2) {
+                    arrived(j);
+                    clean_tiles(j - 1, 1, 1);
+                    copy_v(j, 0); copy_k(j + 2, 0);
+                    if (even(j, b0)) break;
+                    arrived(j + 1);
+                    clean_tiles(j, 1, 0);
+                    copy_v(j + 1, 1); copy_k(j + 3, 1);
+                    if (odd(j + 1, b1)) break;
+                }
             }
             wait_copies<0>();
             __syncthreads();
-            clean_tile(total - 1, vlast);
+            clean_tiles(total - 1, 1, vlast);
             if (active) {
 #pragma unroll
                 for (int i = 0; i < MF; ++i) {
@@ -1055,7 +1118,8 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
                 }
             }
             work.left -= total;
-            if (work.left == 0) return;
+            if (at.t + total >= at.units) work.left -= work.pad;
+            if (work.left <= 0) return;
             at.t += total - 1;
             next();
         }
@@ -1126,13 +1190,13 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(StartsArg<TREE> starts, 
 template <int D, bool MANY, bool TREE = false>
 __global__ __launch_bounds__(256, 2) void decode_f32_kernel(StartsArg<TREE> starts, DecodeArgs a) {
     __shared__ i32x2 lists[4096];
-    __shared__ PlanShare share;
+    __shared__ PlanShare<4> share;
     constexpr int NC = SOLO_ROWS / 16, HALVES = D / 64;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, m16 = l & 15, j = l >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<0, TREE> ls{words_of(starts), a};
     Work work;
-    if constexpr (MANY) work = find_work(ls, lists, 4096, share, w, l); else work = find_work_in_lanes(ls, w, l);
+    if constexpr (MANY) work = find_work<4>(ls, lists, 4096, share, w, l); else work = find_work_in_lanes<4>(ls, w, l);
     if (work.left == 0) return;
     Cursor<0, TREE> at(ls, work);
     Pages pages;
@@ -1308,12 +1372,12 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
     const bool resp = l & 1;
     const i32x4 run = a.desc[0], d = a.desc[1 + (resp ? a.n_groups + seq : g)];
     const int rows = resp ? own * a.rep : members * a.rep, row = resp ? node * a.rep + (int)hr : (tok - first) * a.rep + (int)hr;
-    const bool shared = sizeof(T) == 2 && rows > SOLO_ROWS;
-    int per = SOLO_ROWS;
+    const bool shared = sizeof(T) == 2 && rows > (!TREE ? SOLO_ROWS : resp ? a.wide_resps : a.wide_prompts);
+    int per = TREE ? (int)a.solo_rows.d : SOLO_ROWS;
     if (sizeof(T) == 2) {
         unsigned rest;
         const int blocks = (int)divmod((unsigned)(rows - 1), a.block_rows, rest) + 1;
-        if (shared) per = TREE ? WIDE_ROWS : 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
+        if (shared) per = TREE ? (int)a.block_rows.d : 16 * ((((rows + 15) >> 4) + blocks - 1) / blocks);
     }
     const int block = rows > per ? row / per : 0, segment = TREE ? kvh * ((rows + per - 1) / per) + block : block * a.Hkv + kvh;
     const unsigned each = shared ? run[0] : run[1], from = (unsigned)d[0] * a.Hkv + (unsigned)segment * d[3];

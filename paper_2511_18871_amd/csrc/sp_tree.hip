@@ -11,17 +11,19 @@
 namespace sp {
 namespace {
 
+constexpr int FEW_UNITS = 8192, SHORT_LIST = 512;      // below: which lists waves take by themselves
+
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t desc_bytes(int64_t lists) { return up256(((size_t)lists + 1) * sizeof(i32x4)); }
 
 // Rows of slots at most, whatever the sequences' counts.  A worker leaves a slot per segment and one more for each worker that shares it.  A shared
-// list of r rows takes at most r + 15 for its segments of a kv head.
+// list of r rows takes at most r + 15 for its segments of a kv head; a solo one has blocks of 16 rows or more.
 struct SlotRows { int64_t shared, prompts, responses; };
 SlotRows slot_rows(int64_t n_groups, int64_t n_seqs, int64_t total, int64_t Hq, int64_t Hkv, bool f32) {
-    const int64_t all = total * (Hq / Hkv), widest = std::min<int64_t>(WIDE_ROWS, (all + 15) / 16 * 16), solo = std::min<int64_t>(SOLO_ROWS, all);
-    const int64_t more = f32 ? all / SOLO_ROWS : 0;      // blocks of solo lists beyond the first
+    const int64_t all = total * (Hq / Hkv), widest = std::min<int64_t>(WIDE_ROWS, (all + 15) / 16 * 16), solo = std::min<int64_t>(f32 ? SOLO_ROWS : TREE_SOLO_ROWS, all);
+    const int64_t more = all / SOLO_ROWS;      // blocks of solo lists beyond the first
     SlotRows s;
-    s.shared = !f32 && all > SOLO_ROWS ? PLAN_WGS * widest + Hkv * (2 * all + 16 * std::min(n_groups + n_seqs, 2 * all / (SOLO_ROWS + 1) + 1)) : 0;
+    s.shared = !f32 && all > TREE_SOLO_ROWS ? PLAN_WGS * widest + Hkv * (2 * all + 16 * std::min(n_groups + n_seqs, 2 * all / (TREE_SOLO_ROWS + 1) + 1)) : 0;
     s.prompts = (4 * PLAN_WGS + Hkv * (n_groups + more)) * solo;
     s.responses = (4 * PLAN_WGS + Hkv * (n_groups + n_seqs + 2 * more)) * solo;
     return s;
@@ -88,40 +90,69 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
     const int n_lists = n_groups + n_seqs;
     // (prompts, then responses)
     auto rows_of = [&](int i) { const int k = i < n_groups ? i : i + 1; return (int64_t)a.rep * (starts[k + 1] - starts[k]); };
-    double units_shared = 0, units_solo = 0;
+    // Which lists are shared.  A segment of many rows costs a workgroup three units beside its own, and code that comes from memory once: not where all lists are
+    // few units of 32 keys by 32 rows (one sequence of 1k tokens with 8 drafted ones, 28/4 heads: 17.2 -> 15.8 us), nor those whose tables hold few keys (64 prompts
+    // of 64 to 192 tokens with 16 answers each: 245 -> 241 us; chunks of 150 tokens behind 700: 223 us without, 195 with, hence no more than that).
+    constexpr int NEVER = 0x7fffffff;
+    double units = 0;                      // of 32 keys by 32 rows that the tables have room for
+    auto tokens_of = [&](int i) { return (double)(i < n_groups ? prompt_width : resp_width) * (1 << a.log_page); };
+    for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) units += (tokens_of(i) / 32 + 1) * ((double)rows_of(i) / SOLO_ROWS + 1) * a.Hkv;
+    const bool few = units <= FEW_UNITS;
+    a.wide_prompts = cache.f32 || few || tokens_of(0) < SHORT_LIST ? NEVER : TREE_SOLO_ROWS;
+    a.wide_resps = cache.f32 || few || tokens_of(n_groups) < SHORT_LIST ? NEVER : TREE_SOLO_ROWS;
+    double units_shared = 0, units_solo = 0, units_256 = 0, weighted = 0;
+    int solo_most = 0;                     // rows of the largest solo list
     for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) {
         const int64_t rows = rows_of(i);
-        const double tokens = (double)(i < n_groups ? prompt_width : resp_width) * (1 << a.log_page);
-        if (rows > SOLO_ROWS && !cache.f32) {
+        if (rows > (i < n_groups ? a.wide_prompts : a.wide_resps)) {
+            const double keys = tokens_of(i) / 64 + 1, more = (double)((rows + 127) / 128) * keys * a.Hkv;
             a.shared_rows = std::max(a.shared_rows, (int)std::min<int64_t>(WIDE_ROWS, (rows + 15) / 16 * 16));
-            units_shared += (double)((rows + WIDE_ROWS - 1) / WIDE_ROWS) * (tokens / 64 + 1) * a.Hkv;
+            units_shared += more;
+            units_256 += (double)((rows + 255) / 256) * keys * a.Hkv;
+            weighted += more * keys;
         } else {
-            int& solo = i < n_groups ? a.prompt_rows : a.resp_rows;
-            solo = std::max(solo, (int)std::min<int64_t>(rows, SOLO_ROWS));
-            units_solo += (double)((rows + SOLO_ROWS - 1) / SOLO_ROWS) * (tokens / 32 + 1) * a.Hkv;
+            solo_most = std::max(solo_most, (int)std::min<int64_t>(rows, TREE_SOLO_ROWS + 1));
+            units_solo += (double)((rows + SOLO_ROWS - 1) / SOLO_ROWS) * (tokens_of(i) / 32 + 1) * a.Hkv;
         }
     }
-    const unsigned grid = (unsigned)std::min<double>(PLAN_WGS, units_shared + units_solo / 4 + 1);
-    a.shared_cost = 4.f;
+    // tiles of 16 rows of a solo wave: as many as the largest such list has; of lists in several blocks three (241 us for those prompts, with two 262), or
+    // two where units are few
+    const int ns = cache.f32 ? 2 : solo_most > TREE_SOLO_ROWS ? (few ? 2 : 3) : std::max(1, (solo_most + 15) / 16);
+    a.solo_rows = make_div(16 * ns);
+    for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) {
+        if (rows_of(i) > (i < n_groups ? a.wide_prompts : a.wide_resps)) continue;
+        int& solo = i < n_groups ? a.prompt_rows : a.resp_rows;
+        solo = std::max(solo, (int)std::min<int64_t>(rows_of(i), 16 * ns));
+    }
+    // Workgroups of eight waves, where that leaves few of 256 rows empty and segments are long: they read keys and values half as often, but there is one to
+    // a CU.  (4 chunks of 192 to 256 tokens behind 4k to 8k, 32/8 heads: 160 -> 150 us; a prompt of 1k tokens with 8 trees of 16: 27.5 us either way; 22
+    // groups of short prompts 130 -> 177.)
+    const bool eight = a.shared_rows && 2 * units_256 <= 1.2 * units_shared && weighted >= 32 * units_shared;
+    const int nw = eight ? 8 : 4;
+    a.shared_rows = std::min(a.shared_rows, 32 * nw);
+    const unsigned grid = (unsigned)std::min<double>(4 * PLAN_WGS / nw, units_shared + units_solo / nw + 1);
+    a.shared_cost = 2.f;                   // (64 short prompts with 16 answers each, all prompts shared: 1: 303 us, 2 and 4: 245; long answers beside a long prompt 104, 98, 108)
     a.kv_heads = make_div(a.Hkv);
     a.q_heads = make_div(Hq);
     a.heads_each = make_div(a.rep);
-    a.block_rows = make_div(WIDE_ROWS);
+    a.block_rows = make_div(32 * nw);
     a.prompt_cap = (int)std::min<int64_t>((int64_t)prompt_width << a.log_page, MAX_TOKENS);
     a.resp_cap = (int)std::min<int64_t>((int64_t)resp_width << a.log_page, MAX_TOKENS);
     auto launch = [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         auto with_lists = [&](auto many) {
             constexpr bool MANY = decltype(many)::value;
-            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, table, a); };
+            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * (eight ? 8 : 4)), 0, s, table, a); };
             auto with_solo = [&](auto ns) {
                 constexpr int NS = decltype(ns)::value;
                 if (units_shared == 0) with(decode_kernel<D, 0, NS, MANY, true>);
+                else if (eight) with(decode_kernel<D, 1, NS, MANY, true, 8>);
                 else with(decode_kernel<D, 1, NS, MANY, true>);
             };
             if (cache.f32) with(decode_f32_kernel<D, MANY, true>);
-            else if (std::max(a.prompt_rows, a.resp_rows) <= 16) with_solo(std::integral_constant<int, 1>{});
-            else with_solo(std::integral_constant<int, 2>{});
+            else if (ns == 1) with_solo(std::integral_constant<int, 1>{});
+            else if (ns == 2) with_solo(std::integral_constant<int, 2>{});
+            else with_solo(std::integral_constant<int, 3>{});
         };
         if (n_lists > 64) with_lists(std::true_type{}); else with_lists(std::false_type{});
         auto join = [&](auto dense) {
