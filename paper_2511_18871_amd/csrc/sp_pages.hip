@@ -100,14 +100,19 @@ __device__ __forceinline__ void count_chunk(const Pool& p, int64_t c, int* sh) {
 }
 
 // The free pages that requests first .. first + n - 1 get, n <= 64, in the wave's slots (-1: none is left).  A lane holds one of a chunk's 64
-// words and deals out its bits.
-__device__ __forceinline__ void take_pages(const Pool& p, int64_t first, int n, int* slots) {
+// words and deals out its bits; `mine` is its chunk's count among the first 64 chunks.
+__device__ __forceinline__ int first_counts(const Pool& p) {
+    const int l = threadIdx.x & 63;
+    return l < p.n_chunks ? p.counts[l] : 0;
+}
+__device__ __forceinline__ void take_pages(const Pool& p, int mine, int64_t first, int n, int* slots) {
     const int l = threadIdx.x & 63;
     slots[l] = -1;
     int64_t before = 0;                    // free pages ahead of the chunk
     int given = 0;
     for (int64_t c0 = 0; c0 < p.n_chunks && given < n; c0 += 64) {
-        const int mine = c0 + l < p.n_chunks ? p.counts[c0 + l] : 0, to = scan_lanes(mine);
+        if (c0) mine = c0 + l < p.n_chunks ? p.counts[c0 + l] : 0;
+        const int to = scan_lanes(mine);
         if (before + last_lane(to) > first + given) {
             u64 here = ballot(mine > 0 && before + to > first + given && before + to - mine < first + n);
             while (here) {
@@ -134,7 +139,6 @@ struct FitArgs {
     Pool pool;
     int* tables; const int* lens; int* missing; int* wants; uint32_t* tag;
     int64_t width; int n_seqs, log_page;
-    Div unused;
 };
 __device__ __forceinline__ int64_t pages_needed(const FitArgs& a, int seq) {
     const int64_t n = a.lens[seq];
@@ -192,6 +196,7 @@ __global__ __launch_bounds__(256) void assign_kernel(FitArgs a) {
     if (seq >= a.n_seqs) return;
     for (int s = seq0; s < seq; ++s) ahead += a.wants[s];
     int left = a.wants[seq];
+    const int counts = first_counts(a.pool);
     const int64_t need = pages_needed(a, seq);
     for (int64_t c0 = 0; left > 0 && c0 < need; c0 += 64) {
         const int64_t c = c0 + l;
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(256) void assign_kernel(FitArgs a) {
         const u64 set = ballot(empty);
         const int n = __popcll(set);
         if (n == 0) continue;
-        take_pages(a.pool, ahead, n, slots[w]);
+        take_pages(a.pool, counts, ahead, n, slots[w]);
         if (empty) {
             const int got = slots[w][lanes_below(set)];
             *at = got;
@@ -210,6 +215,105 @@ __global__ __launch_bounds__(256) void assign_kernel(FitArgs a) {
         ahead += n;
         left -= n;
     }
+}
+
+// The same in one launch, for what one workgroup sees at a time: FIT_PLACES places of all tables in FIT_ITEMS pieces of 64, and 64 pages to a thread.  The places that
+// want a page are listed in LDS, in order; a lane keeps a bit per page of its own, and a wave deals out the free ones among 64 at a time.
+// Bound: the launch, three loads that wait for each other, and code that runs once.
+constexpr int FIT_PLACES = 16384, FIT_ITEMS = 2048, FIT_PAGES = 65536, FIT_AHEAD = 4;
+__global__ __launch_bounds__(1024) void fit_small_kernel(FitArgs a, Div pieces) {      // pieces: of 64 places of a table
+    __shared__ int places[FIT_PLACES];
+    __shared__ u64 sets[FIT_ITEMS];        // of a piece's places, those that want a page
+    __shared__ int first[FIT_ITEMS], sums[16];
+    const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (tid < 64) a.tag[l] = 0u;
+    const int items = a.n_seqs * (int)pieces.d, width = (int)a.width;
+    auto place_of = [&](int item, int& seq) {
+        unsigned piece;
+        seq = (int)divmod((unsigned)item, pieces, piece);
+        return (int)piece * 64 + l;
+    };
+    // what lies behind a sequence's last page goes back
+    for (int i0 = w; i0 < items; i0 += 16 * FIT_AHEAD) {
+        int page[FIT_AHEAD], seq[FIT_AHEAD], c[FIT_AHEAD], len[FIT_AHEAD];
+#pragma unroll
+        for (int u = 0; u < FIT_AHEAD; ++u) {
+            c[u] = place_of(min(i0 + 16 * u, items - 1), seq[u]);
+            page[u] = c[u] < width ? a.tables[seq[u] * width + c[u]] : -1;
+            len[u] = a.lens[seq[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < FIT_AHEAD; ++u) {
+            if (i0 + 16 * u >= items) break;
+            const int need = len[u] < 0 ? 0 : (int)min(((int64_t)len[u] + (1 << a.log_page) - 1) >> a.log_page, (int64_t)width);
+            const bool held = page[u] >= 0 && page[u] < a.pool.n_pages;
+            const u64 set = ballot(c[u] < need && !held);
+            if (l == 0) sets[i0 + 16 * u] = set;
+            if (len[u] >= 0 && c[u] >= need && page[u] != -1) {
+                if (held) atomicSub(&a.pool.refs[page[u]], 1);
+                a.tables[seq[u] * width + c[u]] = -1;
+            }
+        }
+    }
+    __threadfence();                       // the counts that fell are read below
+    __syncthreads();
+    auto over_waves = [&](int x, int& all) {       // the sum over earlier threads and over all
+        const int to = scan_lanes(x);
+        __syncthreads();
+        if (l == 63) sums[w] = to;
+        __syncthreads();
+        int ahead = to - x;
+        all = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { ahead += i < w ? sums[i] : 0; all += sums[i]; }
+        return ahead;
+    };
+    int total;
+    {
+        const int n0 = 2 * tid < items ? __popcll(sets[2 * tid]) : 0, n1 = 2 * tid + 1 < items ? __popcll(sets[2 * tid + 1]) : 0;
+        const int at = over_waves(n0 + n1, total);
+        first[2 * tid] = at;
+        first[2 * tid + 1] = at + n0;
+    }
+    if (total == 0) {
+        if (tid == 0 && a.missing) a.missing[0] = 0;
+        return;
+    }
+    // free pages: lane l of a wave looks at pages page0 + 64 j
+    const int n_pages = (int)a.pool.n_pages, turns = (n_pages + 1023) >> 10, page0 = w * 64 * turns + l;
+    u64 mask = 0;
+    int found = 0;                         // of the wave
+    for (int j0 = 0; j0 < turns; j0 += 8) {
+        int refs[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) refs[j] = j0 + j < turns && page0 + 64 * (j0 + j) < n_pages ? a.pool.refs[page0 + 64 * (j0 + j)] : 1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            mask |= (u64)(refs[j] == 0) << ((j0 + j) & 63);
+            found += __popcll(ballot(refs[j] == 0));
+        }
+    }
+    __syncthreads();
+    for (int item = w; item < items; item += 16) {
+        const u64 set = sets[item];
+        int seq;
+        const int c = place_of(item, seq);
+        if (set >> l & 1) places[first[item] + lanes_below(set)] = seq * width + c;
+    }
+    int all, nth = over_waves(l == 0 ? found : 0, all);       // (its barriers stand behind the list as well)
+    nth = __builtin_amdgcn_readfirstlane(nth);
+    if (tid == 0 && a.missing) a.missing[0] = max(0, total - all);
+    for (int j = 0; j < turns && nth < total; ++j) {
+        const u64 set = ballot(mask >> j & 1);
+        const int k = nth + lanes_below(set);
+        if ((set >> l & 1) && k < total) {
+            a.tables[places[k]] = page0 + 64 * j;
+            a.pool.refs[page0 + 64 * j] = 1;
+        }
+        nth += __popcll(set);
+    }
+    // places that no page was left for
+    for (int i = all + tid; i < total; i += 1024) a.tables[places[i]] = -1;
 }
 
 // ---- fork ------------------------------------------------------------------------------------------------------
@@ -268,7 +372,7 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
     if (!tells && !c.takes) return;
     int to = -1;
     if (c.takes) {
-        if (threadIdx.x < 64) take_pages(a.pool, a.order[seq], 1, slots);
+        if (threadIdx.x < 64) take_pages(a.pool, first_counts(a.pool), a.order[seq], 1, slots);
         __syncthreads();
         to = __builtin_amdgcn_readfirstlane(slots[0]);
     }
@@ -333,6 +437,11 @@ hipError_t launch_fit(int* refs, int64_t n_pages, int log_page, int n_seqs, int*
     a.pool = make_pool(refs, n_pages, n_seqs, room);
     a.tables = tables; a.lens = lens; a.missing = missing; a.wants = (int*)room; a.tag = tag;
     a.width = width; a.n_seqs = n_seqs; a.log_page = log_page;
+    const int64_t pieces = ((int64_t)width + 63) / 64;
+    if (n_seqs * pieces <= FIT_ITEMS && (int64_t)n_seqs * width <= FIT_PLACES && n_pages <= FIT_PAGES) {
+        hipLaunchKernelGGL(fit_small_kernel, dim3(1), dim3(1024), 0, s, a, make_div((int)pieces));
+        return hipGetLastError();
+    }
     const dim3 waves((unsigned)((n_seqs + 3) / 4));
     hipLaunchKernelGGL(release_kernel, waves, dim3(256), 0, s, a);
     hipLaunchKernelGGL(count_free_kernel, dim3((unsigned)a.pool.n_chunks), dim3(256), 0, s, a.pool);
