@@ -29,54 +29,60 @@ struct KeepArgs {
     int64_t layer_bytes;                   // from layer to layer
     const int* tables; const int* lens; const int* kept; const int* n_kept; int* lens_out;
     int64_t width, capacity, n_pages, kept_width;
-    int n_seqs, items, Hkv, log_page;      // items: layers * 2 * Hkv of a sequence
+    int items, per_wave, Hkv, log_page;    // items: layers * 2 * Hkv of a sequence
     Div heads;
 };
 
-// Token lens + kept[i] of a sequence becomes its token lens + i.  A wave takes a (layer, K or V, head) of a sequence and moves its rows in
-// order, 64 lanes of 16 bytes at a time.  kept ascends, so kept[j] >= j > i for j > i: a row is read before or in the step in which it is
-// written over, and no row that a later step reads has been written.
+// Token lens + kept[i] of a sequence becomes its token lens + i.  A wave looks 64 entries of the list up at a time, a lane each, and moves their rows of `per_wave`
+// (layer, K or V, head) in turn, 64 AHEAD lanes of 16 bytes on their way.  It reads a batch of rows ahead of writing any, and kept ascends, so that
+// kept[j] >= j > i for j > i: no row that is still to be read is written over.
+// Bound: bytes, and for small calls four loads that wait for each other.
+constexpr int KEEP_AHEAD = 4;
 template <int ROW>        // bytes of a row
 __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
     constexpr int LANES = ROW / 16, ROWS = 64 / LANES;
-    const int l = threadIdx.x & 63, seq = blockIdx.x;
-    const int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    if (item >= a.items) return;
+    __shared__ int64_t moves[4][64][2];    // bytes from the head's place in page 0: from, to
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), seq = blockIdx.x;
+    const int item0 = ((int)blockIdx.y * 4 + w) * a.per_wave;
+    if (item0 >= a.items) return;
     const int64_t have = a.lens[seq];
     const int* const kept = a.kept + seq * a.kept_width;
+    const int* const table = a.tables + seq * a.width;
     const int most = have < 0 ? 0 : (int)min((int64_t)max(a.n_kept[seq], 0), a.kept_width);
+    auto row_of = [&](int64_t j) -> int64_t {
+        const int64_t page = table[j >> a.log_page];
+        return page < 0 || page >= a.n_pages ? -1 : (((page * a.Hkv) << a.log_page) + (j & ((1 << a.log_page) - 1))) * ROW;
+    };
     int n = 0;                             // of the list up to its first entry that does not ascend or that the table has no room for
-    while (n < most) {
-        const int i = n + l;
-        bool good = false;
-        if (i < most) {
-            const int x = kept[i], before = i > 0 ? kept[i - 1] : -1;
-            good = x > before && have + x < a.capacity;
-        }
-        const u64 bad = ~ballot(good);
+    for (bool more = true; more && n < most;) {
+        const int i = n + l, x = i < most ? kept[i] : -1, before = i > 0 && i < most ? kept[i - 1] : -1;
+        const u64 bad = ~ballot(x > before && have + x < a.capacity);
         const int run = bad ? __ffsll(bad) - 1 : 64;
         n += run;
-        if (run < 64) break;
+        more = run == 64;
+        const bool moves_row = l < run && x != i;
+        const int64_t from = moves_row ? row_of(have + x) : -1, to = moves_row ? row_of(have + i) : -1;
+        const u64 set = ballot(from >= 0 && to >= 0);
+        if (set >> l & 1) { moves[w][lanes_below(set)][0] = from; moves[w][lanes_below(set)][1] = to; }
+        const int count = __popcll(set);
+        __builtin_amdgcn_wave_barrier();
+        for (int item = item0; item < min(item0 + a.per_wave, a.items); ++item) {
+            unsigned head;
+            const int lk = (int)divmod((unsigned)item, a.heads, head);
+            char* const base = (lk & 1 ? a.v : a.k) + (lk >> 1) * a.layer_bytes + (((int64_t)head * ROW) << a.log_page) + (l % LANES) * 16;
+            for (int r0 = l / LANES; r0 < count; r0 += ROWS * KEEP_AHEAD) {
+                i32x4 x[KEEP_AHEAD];
+#pragma unroll
+                for (int u = 0; u < KEEP_AHEAD; ++u)
+                    if (r0 + ROWS * u < count) x[u] = *reinterpret_cast<const i32x4*>(base + moves[w][r0 + ROWS * u][0]);
+#pragma unroll
+                for (int u = 0; u < KEEP_AHEAD; ++u)
+                    if (r0 + ROWS * u < count) *reinterpret_cast<i32x4*>(base + moves[w][r0 + ROWS * u][1]) = x[u];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
-    if (item == 0 && l == 0) a.lens_out[seq] = (int)(have + n);
-    unsigned head;
-    const int lk = (int)divmod((unsigned)item, a.heads, head);
-    char* const base = (lk & 1 ? a.v : a.k) + (lk >> 1) * a.layer_bytes;
-    const int* const table = a.tables + seq * a.width;
-    auto row_of = [&](int64_t j) -> char* {
-        const int64_t page = table[j >> a.log_page];
-        if (page < 0 || page >= a.n_pages) return nullptr;
-        return base + (((page * a.Hkv + head) << a.log_page) + (j & ((1 << a.log_page) - 1))) * ROW + (l % LANES) * 16;
-    };
-    for (int i0 = 0; i0 < n; i0 += ROWS) {
-        const int i = i0 + l / LANES;
-        if (i >= n) continue;
-        const int from = kept[i];
-        if (from == i) continue;
-        const char* const src = row_of(have + from);
-        char* const dst = row_of(have + i);
-        if (src && dst) *reinterpret_cast<i32x4*>(dst) = *reinterpret_cast<const i32x4*>(src);
-    }
+    if (item0 == 0 && l == 0) a.lens_out[seq] = (int)(have + n);
 }
 
 // ---- free pages ------------------------------------------------------------------------------------------------
@@ -422,9 +428,11 @@ hipError_t launch_keep(const KvCache& cache, int n_layers, int64_t layer_stride,
     a.k = (char*)cache.k; a.v = (char*)cache.v; a.layer_bytes = layer_stride * elem;
     a.tables = tables; a.lens = lens; a.kept = kept; a.n_kept = n_kept; a.lens_out = lens_out;
     a.width = width; a.capacity = std::min<int64_t>((int64_t)width << cache.log_page, MAX_TOKENS); a.n_pages = cache.n_pages; a.kept_width = kept_width;
-    a.n_seqs = n_seqs; a.items = n_layers * 2 * cache.n_kv_heads; a.Hkv = cache.n_kv_heads; a.log_page = cache.log_page;
+    a.items = n_layers * 2 * cache.n_kv_heads; a.Hkv = cache.n_kv_heads; a.log_page = cache.log_page;
     a.heads = make_div(cache.n_kv_heads);
-    const dim3 grid((unsigned)n_seqs, (unsigned)((a.items + 3) / 4));
+    // as many items to a wave as leave the chip twice its waves (16384)
+    a.per_wave = (int)std::max<int64_t>(1, std::min<int64_t>(8, (int64_t)n_seqs * a.items / 16384));
+    const dim3 grid((unsigned)n_seqs, (unsigned)((a.items + 4 * a.per_wave - 1) / (4 * a.per_wave)));
     if (row == 128) hipLaunchKernelGGL(keep_kernel<128>, grid, dim3(256), 0, s, a);
     else if (row == 256) hipLaunchKernelGGL(keep_kernel<256>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(keep_kernel<512>, grid, dim3(256), 0, s, a);
