@@ -865,7 +865,7 @@ sp_status sp_attn_tree_decode(const sp_kv_cache* cache, const void* q, void* o, 
         words[n_groups] = (int32_t)total;
         if (sp::tree_units(n_groups, n_seqs, n_q_heads, c.n_kv_heads, (int64_t)prompt_width << c.log_page, (int64_t)resp_width << c.log_page, words.data()) > 2e9)
             return fail(SP_ERR_INVALID_ARG, "%d sequences with tables of %d and %d pages: more than one call serves", n_seqs, prompt_width, resp_width);
-        const hipError_t e = sp::launch_tree(c, q, o, lse, n_q_heads, n_groups, n_seqs, (int)total, words.data(), table_of(workspace), ancestors, mask_stride, prompt_tables,
+        const hipError_t e = sp::launch_tree(c, q, o, lse, n_q_heads, n_groups, n_seqs, Gs, (int)total, words.data(), table_of(workspace), ancestors, mask_stride, prompt_tables,
                                              prompt_width, prompt_lens, resp_tables, resp_width, resp_lens, softmax_scale, (uint32_t*)workspace,
                                              (char*)workspace + TAG_BYTES + sp::tree_table_bytes(n_groups, n_seqs), s);
         if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));

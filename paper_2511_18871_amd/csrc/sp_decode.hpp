@@ -60,6 +60,10 @@ struct DecodeArgs {
     int64_t mask_stride;
     Div solo_rows;                         // rows of a block of a solo list
     int wide_prompts, wide_resps;          // prompts, responses with more rows than this are shared
+    // joined: a sequence's list is its prompt and behind it its own keys, and prompts are no lists; groups are of `group_seqs` sequences.  direct: a row
+    // whose keys one worker has seen goes to o and lse at once
+    bool joined, direct;
+    Div group_seqs;
     int nc;                                // row tiles per wave of a shared segment
     float shared_cost;                     // of a shared unit, against a solo one
     Div group_size, block_rows;            // of `members`, of the rows of a shared segment (64 nc)
@@ -87,15 +91,15 @@ __device__ __forceinline__ int scan64(int x) {
     x = dpp_add<0x111, 0xf>(x); x = dpp_add<0x112, 0xf>(x); x = dpp_add<0x114, 0xf>(x); x = dpp_add<0x118, 0xf>(x);      // within 16 lanes
     x = dpp_add<0x142, 0xa>(x); return dpp_add<0x143, 0xc>(x);                                                      // across them
 }
-struct ListShape {                        // units of keys of a segment; blocks of rows
-    int rows, len, units, blocks; bool shared;
+struct ListShape {                        // units of keys of a segment, `ahead` of them of the prompt (TREE); blocks of rows
+    int rows, len, units, blocks, ahead; bool shared;
     // what a list adds to `ord`: its blocks, a shared list of drafted tokens its row tiles of 16
     template <bool TREE> __device__ __forceinline__ int places() const {
         if constexpr (TREE) { if (shared) return (rows + 15) >> 4; }
         return blocks;
     }
 };
-template <int NW> struct PlanShare { int sums[NW][5]; int list[NW], at[NW], ord[NW], rows[NW], len[NW], room[NW]; };      // of the waves of a workgroup; where their runs start
+template <int NW> struct PlanShare { int sums[NW][5]; int list[NW], at[NW], ord[NW], rows[NW], len[NW], room[NW], ahead[NW]; };      // of the waves of a workgroup; where their runs start
 
 // First tokens of the groups, the number of tokens, first tokens of the sequences, and that number again: in 16 bits among the kernel's arguments, or in
 // the workspace.  (A table that is stored by a launch of its own costs 5 us for each 896 words.)
@@ -115,6 +119,7 @@ template <bool TREE> using Starts = std::conditional_t<TREE, TreeStarts, const i
 
 // KIND 0: all lists are solo, 1: shared ones too.  TREE: a sequence has several rows per q head, one for each of its drafted tokens; `members` are
 // the tokens of a group.
+template <bool TREE> using ListIs = std::conditional_t<TREE, i32x4, i32x2>;      // rows, length; TREE: tokens of the prompt ahead of it
 template <int KIND, bool TREE = false>
 struct Lists {
     Starts<TREE> starts;                     // first sequence (token) of each group, where groups are of several sizes
@@ -126,23 +131,35 @@ struct Lists {
         const int k = prompt ? i : i + 1;
         return starts[k + 1] - starts[k];
     }
-    __device__ __forceinline__ i32x2 read(int i) const {      // rows and length, -1: takes no part
+    __device__ __forceinline__ ListIs<TREE> read(int i) const {      // length -1: takes no part
         const bool prompt = i < a.n_groups;
         const int prompt_cap = a.prompt_cap, resp_cap = a.resp_cap;
         const int* const prompt_lens = a.prompt_lens;
         const int* const resp_lens = a.resp_lens - a.n_groups;
         const int n = prompt && !prompt_cap ? 0 : (prompt ? prompt_lens : resp_lens)[i];
         int members = 1;
-        if constexpr (TREE) members = tokens(i);
-        else if (prompt) members = a.members ? a.members : starts[i + 1] - starts[i];
-        return i32x2{a.rep * members, min(max(n, -1), prompt ? prompt_cap : resp_cap)};
+        if constexpr (TREE) {
+            if (a.joined && prompt) return i32x4{0, 0, 0, 0};
+            members = tokens(i);
+            const int len = min(max(n, -1), prompt ? prompt_cap : resp_cap);
+            int ahead = 0;
+            if (a.joined && len >= 0) {
+                unsigned rest;
+                ahead = min(max(prompt_lens[divmod((unsigned)(i - a.n_groups), a.group_seqs, rest)], 0), prompt_cap);
+            }
+            return i32x4{a.rep * members, len, ahead, 0};
+        } else if (prompt) members = a.members ? a.members : starts[i + 1] - starts[i];
+        if constexpr (!TREE) return i32x2{a.rep * members, min(max(n, -1), prompt ? prompt_cap : resp_cap)};
     }
-    __device__ __forceinline__ ListShape shape(i32x2 x, int i) const {
+    __device__ __forceinline__ ListShape shape(ListIs<TREE> x, int i) const {
         ListShape s;
         s.rows = x[0];
         s.len = x[1];
         s.shared = KIND && s.rows > (!TREE ? SOLO_ROWS : i < a.n_groups ? a.wide_prompts : a.wide_resps);
-        s.units = s.rows > 0 && s.len > 0 ? (int)(((unsigned)s.len + (s.shared ? 63u : 31u)) >> (s.shared ? 6 : 5)) : 0;
+auto units = [&](int n) { return n > 0 ? (int)(((unsigned)n + (s.shared ? 63u : 31u)) >> (s.shared ? 6 : 5)) : 0; };
+        s.units = s.rows > 0 ? units(s.len) : 0;
+        s.ahead = 0;
+        if constexpr (TREE) { if (s.rows > 0) s.ahead = units(x[2]); s.units += s.ahead; }
         unsigned rest;
         if constexpr (TREE) s.blocks = s.rows <= 0 ? 0 : (int)divmod((unsigned)(s.rows - 1), s.shared ? a.block_rows : a.solo_rows, rest) + 1;
         else s.blocks = s.shared ? (int)divmod((unsigned)(s.rows - 1), a.block_rows, rest) + 1 : (s.rows + SOLO_ROWS - 1) / SOLO_ROWS;
@@ -170,7 +187,7 @@ template <bool TREE> __device__ __forceinline__ int room_of(int units, unsigned 
 }
 
 // What a worker does: `left` units from unit `at` of a list on (counted over the list's segments).
-struct Work { bool shared; int worker, list, at, ord, left, room, pad; i32x2 list_is; };      // pad: units of a segment's room that are none
+template <bool TREE> struct Work { bool shared; int worker, list, at, ord, left, room, pad; ListIs<TREE> list_is; };      // pad: units of a segment's room that are none
 
 // The runs of either kind, from the units and segments of all lists.  Places are dealt by cost: a segment costs, for its rows and its sums, what one and a half of its
 // units (shared) or one (solo) cost, and a shared unit what shared_cost solo ones do.  A worker that passes from one segment to another takes
@@ -202,12 +219,12 @@ template <bool TREE> __device__ __forceinline__ unsigned shared_worker(unsigned 
 // takes a cycle a byte.
 // Up to 64 lists: a wave by itself, a list to a lane (one sequence of 1k tokens 5.7 us, by the workgroup 7.0; a group of 8 8.2 and 11.0).
 template <int NW, int KIND, bool TREE>
-__device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, int wave, int lane) {
+__device__ __forceinline__ Work<TREE> find_work_in_lanes(const Lists<KIND, TREE>& ls, int wave, int lane) {
     constexpr int WGS = 4 * PLAN_WGS / NW;
     const DecodeArgs& a = ls.a;
     const int n = a.n_groups + a.n_seqs;
     const bool there = lane < n;
-    i32x2 mine{0, 0};
+    ListIs<TREE> mine{};
     if (there) mine = ls.read(lane);
     const ListShape s = ls.shape(mine, lane);
     auto last = [](int x) SP_INLINE { return (unsigned)__builtin_amdgcn_readlane(x, 63); };
@@ -232,7 +249,7 @@ __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, 
         if (there) a.desc[1 + lane] = i32x4{to - units, s.units, ord, s.len < 0 ? -1 : room};
         if (lane == 0) a.desc[0] = i32x4{(int)runs.shared_run, (int)runs.solo_run, 0, 0};
     }
-    Work work;
+    Work<TREE> work;
     work.shared = blockIdx.x < runs.used;
     work.worker = work.shared ? (int)shared_worker<TREE>(runs.used) : (int)(blockIdx.x - runs.used) * NW + wave;
     const unsigned run = work.shared ? runs.shared_run : runs.solo_run, all = work.shared ? shared_room : solo, pos = (unsigned)work.worker * run;
@@ -246,13 +263,14 @@ __device__ __forceinline__ Work find_work_in_lanes(const Lists<KIND, TREE>& ls, 
     work.ord = of(ord);
     work.room = of(room);
     work.pad = TREE && work.shared && !runs.aligned ? WIDE_PAD : 0;
-    work.list_is = i32x2{of(mine[0]), of(mine[1])};
+    if constexpr (TREE) work.list_is = i32x4{of(mine[0]), of(mine[1]), of(mine[2]), 0};
+    else work.list_is = i32x2{of(mine[0]), of(mine[1])};
     return work;
 }
 
 // More lists: a thread adds up the units of its share of them (they lie in LDS meanwhile, if there are no more than n_held), the workgroup their sums.
 template <int NW, int KIND, bool TREE>
-__device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* held, int n_held, PlanShare<NW>& share, int wave, int lane) {
+__device__ __forceinline__ Work<TREE> find_work(const Lists<KIND, TREE>& ls, ListIs<TREE>* held, int n_held, PlanShare<NW>& share, int wave, int lane) {
     constexpr int SUMS = KIND ? TREE ? 5 : 4 : 2;       // solo units and blocks, shared units and blocks (TREE: and places)
     constexpr int WGS = 4 * PLAN_WGS / NW, ALL = 64 * NW;
     const DecodeArgs& a = ls.a;
@@ -260,7 +278,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     const bool in_lds = n <= n_held;
     if (in_lds) {
         for (int i = threadIdx.x; i < n; i += ALL * 4) {      // four reads in flight
-            i32x2 x[4];
+            ListIs<TREE> x[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) if (i + ALL * u < n) x[u] = ls.read(i + ALL * u);
 #pragma unroll
@@ -314,7 +332,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     }
     if (all[0]) runs.solo_run = per_place(all[0], NW * (WGS - runs.used));
     // this workgroup's runs start at `first` and multiples of the run behind it
-    Work work;
+    Work<TREE> work;
     const bool shared = work.shared = blockIdx.x < runs.used;
     const unsigned run = shared ? runs.shared_run : runs.solo_run, many = shared ? 1 : NW, first = (shared ? shared_worker<TREE>(runs.used) : NW * (blockIdx.x - runs.used)) * run;
     const bool tells = blockIdx.x == 0;          // the first workgroup writes down what the join needs to know
@@ -326,7 +344,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
         for (int k = 0; k < SUMS; ++k) at[k] = to[k] - own[k];
 #pragma unroll 1
         for (int i = i0; i < i1; ++i) {
-            const i32x2 x = list_of(i);
+            const ListIs<TREE> x = list_of(i);
             const ListShape s = ls.shape(x, i);
             const int units = s.shared ? at[SHARED] : at[0], blocks = s.shared ? at[SUMS - 1] : at[1], room = s.shared ? room_of<TREE>(s.units, runs.shared_run, runs.aligned) : s.units;
             const unsigned from = (unsigned)units * a.Hkv, end = from + (unsigned)(room * s.blocks) * a.Hkv;
@@ -337,6 +355,7 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
                     if (pos >= from && pos < end) {
                         share.list[k] = i; share.at[k] = (int)(pos - from); share.ord[k] = blocks;
                         share.rows[k] = x[0]; share.len[k] = x[1]; share.room[k] = room;
+                        if constexpr (TREE) share.ahead[k] = x[2];
                     }
                 }
             if (tells) a.desc[1 + i] = i32x4{units, s.units, blocks, s.len < 0 ? -1 : room};
@@ -355,7 +374,8 @@ __device__ __forceinline__ Work find_work(const Lists<KIND, TREE>& ls, i32x2* he
     work.ord = scalar(share.ord[slot]);
     work.room = scalar(share.room[slot]);
     work.pad = TREE && shared && !runs.aligned ? WIDE_PAD : 0;
-    work.list_is = i32x2{share.rows[slot], share.len[slot]};
+    if constexpr (TREE) work.list_is = i32x4{share.rows[slot], share.len[slot], share.ahead[slot], 0};
+    else work.list_is = i32x2{share.rows[slot], share.len[slot]};
     return work;
 }
 
@@ -365,7 +385,8 @@ struct Cursor {
     const Lists<KIND, TREE>& ls;
     const bool shared;
     int list, seg, t, units, segs, rows, len, blocks, ord, places;
-    __device__ __forceinline__ Cursor(const Lists<KIND, TREE>& l, Work& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
+    int ahead, ahead_len;                  // units and tokens of the prompt that are the first of the list (TREE)
+    __device__ __forceinline__ Cursor(const Lists<KIND, TREE>& l, Work<TREE>& w) : ls(l), shared(w.shared), list(w.list), ord(w.ord) {
         load(w.list_is);
         const float inv = __builtin_amdgcn_rcpf((float)w.room);        // a quotient, what it leaves divided again, and a step to either side
         seg = (int)((float)w.at * inv);
@@ -382,10 +403,11 @@ struct Cursor {
             }
         } else if (w.room > units) w.left = min(w.left, units - t);        // a run of the segment's own, the last one shorter
     }
-    __device__ __forceinline__ bool load(i32x2 x) {
+    __device__ __forceinline__ bool load(ListIs<TREE> x) {
         const ListShape s = ls.shape(x, list);
         auto scalar = [](int x) SP_INLINE { return __builtin_amdgcn_readfirstlane(x); };
         rows = scalar(s.rows); len = scalar(s.len); units = scalar(s.units); blocks = scalar(s.blocks);
+        if constexpr (TREE) { ahead = scalar(s.ahead); ahead_len = scalar(x[2]); }
         places = TREE ? scalar(s.template places<TREE>()) : blocks;
         segs = blocks * ls.a.Hkv;
         return s.shared == shared;
@@ -727,6 +749,34 @@ __device__ __forceinline__ void store_rows(const Rows<D, NC>& r, const DecodeArg
 }
 
 // NC: row tiles of a wave in a shared segment, 0: no list is shared.  NS: in a solo one.
+// Rows whose keys this worker has all seen (TREE): o and lse, and a mark for the join
+constexpr float DONE = 2.f;
+template <int D, int NC>
+__device__ __forceinline__ void finish_rows(const Rows<D, NC>& r, const DecodeArgs& a, const SegmentRows& pr, int tiles, int l) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int row = 16 * c + (l & 15);
+        const float lt = quad_sum(r.l[c]);
+        if (c >= tiles || row >= pr.rows) continue;
+        const bool none = bits_of(lt) == 0;
+        const float inv = 1.f / lt;
+        unsigned hr;
+        const int tok = pr.seq0 + (int)divmod((unsigned)(pr.row0 + row), pr.heads_each, hr), h = pr.kvh * pr.rep + (int)hr;
+        __bf16* const out = (__bf16*)a.o + ((int64_t)tok * pr.Hq + h) * D + 4 * (l >> 4);
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            bf16x4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = (__bf16)(none ? 0.f : r.o[c][dt][i] * inv);
+            *reinterpret_cast<bf16x4*>(out + 16 * dt) = y;
+        }
+        if (l < 16) {
+            a.lse[(int64_t)h * a.n_tok + tok] = none ? -INFINITY : r.m[c] * (a.c * LN2) + __logf(lt);
+            *reinterpret_cast<f32x4*>(a.stats + (pr.base + row) * 4) = f32x4{0.f, 0.f, 0.f, DONE};
+        }
+    }
+}
+
 // NW: waves of a workgroup; eight (TREE) for lists of many rows.
 template <int D, int NC, int NS, bool MANY, bool TREE = false, int NW = 4>
 __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> starts, DecodeArgs a) {
@@ -738,9 +788,9 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<KIND, TREE> ls{words_of(starts), a};
-    Work work;
+    Work<TREE> work;
     if constexpr (MANY) {
-        work = find_work<NW>(ls, reinterpret_cast<i32x2*>(lds), (int)sizeof(lds) / 8, share, w, l);
+        work = find_work<NW>(ls, reinterpret_cast<ListIs<TREE>*>(lds), (int)(sizeof(lds) / sizeof(ListIs<TREE>)), share, w, l);
         __syncthreads();                             // the lists' place is free
     } else {
         work = find_work_in_lanes<NW>(ls, w, l);
@@ -759,16 +809,32 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
     pages.lane = l;
     pages.n_pages = a.n_pages;
     Drafted drafted;
+    // The part of the list that the unit lies in: its length and first unit (TREE: the prompt's or the sequence's own)
+    int part_len = 0, part_unit = 0;
+    auto prompt_of = [&]() SP_INLINE {             // table of the prompt ahead of the list's keys
+        unsigned rest;
+        return a.prompt_tables + (int64_t)divmod((unsigned)(at.list - a.n_groups), a.group_seqs, rest) * a.prompt_width;
+    };
     auto table_of_list = [&]() SP_INLINE {
         const bool prompt = at.list < a.n_groups;
         pages.table = prompt ? a.prompt_tables + at.list * a.prompt_width : a.resp_tables + (at.list - a.n_groups) * a.resp_width;
-        pages.count = pages_of(at.len, a.log_page);
-        if constexpr (TREE) drafted.of(ls, at.list);
+        if constexpr (TREE) {
+            drafted.of(ls, at.list);
+            const bool ahead = at.t < at.ahead;
+            if (ahead) pages.table = prompt_of();
+            part_len = ahead ? at.ahead_len : at.len;
+            part_unit = ahead ? 0 : at.ahead;
+            pages.count = pages_of(part_len, a.log_page);
+        } else {
+            pages.count = pages_of(at.len, a.log_page);
+        }
     };
+    auto length = [&]() SP_INLINE { return TREE ? part_len : at.len; };
+    auto unit = [&]() SP_INLINE { return TREE ? at.t - part_unit : at.t; };
     auto next = [&]() SP_INLINE {
         const int list = at.list;
         at.next();
-        if (at.list != list) { table_of_list(); if (!TREE || !work.shared) pages.load(0); }
+        if (at.list != list || (TREE && at.ahead > 0 && (at.t == 0 || at.t == at.ahead))) { table_of_list(); if (!TREE || !work.shared) pages.load(0); }
         if (at.t == 0) kvh = kv_head();
     };
     table_of_list();
@@ -780,7 +846,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
     };
     // the same of 16 keys, and how many of them there are
     auto locate = [&](int key, uint64_t& off, int& valid) SP_INLINE {
-        valid = min(16, at.len - key);
+        valid = min(16, length() - key);
         off = 0;
         if (valid <= 0) return;
         const int page = __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page));
@@ -789,7 +855,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
     };
     // whether all of `count` keys are there (the pages held include the last one's; if any of those held is none, it is looked at in turn)
     auto whole = [&](int key, int count) SP_INLINE {
-        if (key + count > at.len) return false;
+        if (key + count > length()) return false;
         pages.need(key >> a.log_page);
         pages.need((key + count - 1) >> a.log_page);
         return !pages.bad && (unsigned)((key >> a.log_page) - pages.first) < 64u;
@@ -805,7 +871,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
         uint64_t off[2];
         int valid[2];
         auto fetch = [&]() SP_INLINE {
-            const int key = 32 * at.t;
+            const int key = 32 * unit();
             if (whole(key, 32)) {
                 valid[0] = valid[1] = 16;
                 off[0] = offset(key, __builtin_amdgcn_readfirstlane(pages.at(key >> a.log_page)));
@@ -820,7 +886,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
             copy.rows16(cache + off[1], valid[1], dst + KEYS16);
         };
         constexpr int N = 2 * Copier<D>::COPIES;
-        pages.load(32 * at.t >> a.log_page);
+        pages.load(32 * unit() >> a.log_page);
         fetch();
         issue(kc, kb);
         issue(vc, vb);
@@ -830,6 +896,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
             load_rows(r, q, seg, 0, tiles, l);
             r.clear(a.m_none);
             bool more = true, same = true, left_out = false;
+            const bool from_first = at.t == 0;
+            bool to_last = false;
             while (same) {
                 const unsigned bits = low_bits(valid[0]) | low_bits(valid[1]) << 16;
                 f32x4 s[NS][2];
@@ -838,12 +906,13 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
                 scores(r, kb, bits, l, s);
                 bool some = false;             // whether rows see some of the unit's keys only
                 if constexpr (TREE) {
-                    some = 32 * (int64_t)at.t + 32 > drafted.base;
-                    if (some) hide<D>(a, seg, drafted, 0, 32 * at.t, l, s);
+                    some = at.t >= at.ahead && 32 * (int64_t)unit() + 32 > drafted.base;
+                    if (some) hide<D>(a, seg, drafted, 0, 32 * unit(), l, s);
                 }
                 wait_lds();
                 more = --work.left > 0;
                 same = more && at.t + 1 < at.units;
+                if constexpr (TREE) to_last = at.t + 1 == at.units;
                 if (more) { next(); fetch(); issue(kc, kb); }
                 weights(r, s, a.c, pw);
                 if (more) wait_copies<N>(); else wait_copies<0>();
@@ -855,7 +924,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
                 wait_lds();
                 if (more) issue(vc, vb);
             }
-            store_rows<TREE>(r, a, seg, 0, tiles, l, left_out);
+            if (TREE && a.direct && from_first && to_last && !left_out) finish_rows(r, a, seg, tiles, l);
+            else store_rows<TREE>(r, a, seg, 0, tiles, l, left_out);
             if (!more) return;
         }
     } else if constexpr (TREE) {
@@ -895,23 +965,30 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
         const f32x16 zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         while (true) {
             const SegmentRows seg(at, a, work.worker);
-            const int total = min(work.left, at.units - at.t), key0 = 64 * at.t;
+            const int total = min(work.left, at.units - at.t), tile0 = at.t;
+            const int* const own_table = a.resp_tables + (at.list - a.n_groups) * a.resp_width;
+            const int* const table = at.list < a.n_groups ? a.prompt_tables + at.list * a.prompt_width : own_table;
+            const int* const table_ahead = at.ahead ? prompt_of() : nullptr;
+            // tile j is of the prompt ahead or not; its first key there, and the keys from it on
+            auto is_ahead = [&](int j) SP_INLINE { return tile0 + j < at.ahead; };
+            auto key_of = [&](int j) SP_INLINE { return 64 * (tile0 + j - (is_ahead(j) ? 0 : at.ahead)); };
+            auto keys_from = [&](int j) SP_INLINE { return (is_ahead(j) ? at.ahead_len : at.len) - key_of(j); };
             const bool active = 32 * w < seg.rows;
             // Pages of every 16 keys of up to 64 tiles, -1: none, filled in by all threads ahead of their use
             auto fill = [&](int j, int tiles) SP_INLINE {
                 if ((int)threadIdx.x >= 4 * tiles) return;
-                const unsigned key = (unsigned)key0 + 64u * j + 16u * threadIdx.x;
+                const int jt = j + ((int)threadIdx.x >> 2), in_tile = 16 * ((int)threadIdx.x & 3);
                 int page = -1;
-                if (key < (unsigned)at.len) {
-                    page = pages.table[key >> a.log_page];
+                if (tile0 + jt < at.units && in_tile < keys_from(jt)) {
+                    page = (is_ahead(jt) ? table_ahead : table)[(unsigned)(key_of(jt) + in_tile) >> a.log_page];
                     if ((unsigned)page >= (unsigned)a.n_pages) { page = -1; bad_pages = 1; }
                 }
                 place[(4 * j + threadIdx.x) & 255] = page;
             };
             struct Tile { uint64_t off; int valid; };      // this wave's 16 keys of a tile
             auto fetch = [&](int j) SP_INLINE {
-                const int page = __builtin_amdgcn_readfirstlane(place[(4 * j + (w & 3)) & 255]), key = key0 + 64 * j + 16 * (w & 3);
-                return Tile{offset(key, max(page, 0)), page < 0 ? 0 : min(16, at.len - key)};
+                const int page = __builtin_amdgcn_readfirstlane(place[(4 * j + (w & 3)) & 255]), in_tile = 16 * (w & 3);
+                return Tile{offset(key_of(j) + in_tile, max(page, 0)), page < 0 ? 0 : min(16, keys_from(j) - in_tile)};
             };
             auto copy_k = [&](int j, int b) SP_INLINE {         // K(j) into buffer b; of eight waves, the first four
                 if (j >= total || (NW == 8 && w >= 4)) return;
@@ -923,17 +1000,17 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
                 const Tile t = fetch(j);
                 copy.rows16(vc + t.off, t.valid, buf + (unsigned)(NB + b) * TILE + (w & 3) * KEYS16);
             };
-            auto tail = [&](int j) SP_INLINE { return key0 + 64 * (int64_t)j + 64 > drafted.base; };      // holds drafted tokens
+            auto tail = [&](int j) SP_INLINE { return !is_ahead(j) && key_of(j) + (int64_t)64 > drafted.base; };      // holds drafted tokens
             bool bad = false;
             auto mask = [&](int j, f32x16 (&S)[2]) SP_INLINE {
                 const bool some = tail(j);
-                const int n = at.len - key0 - 64 * j;
+                const int n = keys_from(j);
                 if (!some && !bad && n >= 64) return;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     unsigned bits = low_bits(n - 32 * kb);
                     if (bad) bits &= (place[(4 * j + 2 * kb) & 255] < 0 ? 0xffff0000u : ~0u) & (place[(4 * j + 2 * kb + 1) & 255] < 0 ? 0xffffu : ~0u);
-                    if (some) bits &= drafted.bits(a, seg, 32 * w + c32, key0 + 64 * j + 32 * kb);
+                    if (some) bits &= drafted.bits(a, seg, 32 * w + c32, key_of(j) + 32 * kb);
                     mask16(S[kb], bits >> (4 * hh));
                 }
             };
@@ -1106,7 +1183,24 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
                 // from R to m c
                 const float f = __builtin_amdgcn_exp2f(offset_of(m)), lt = pair_sum(lsum) * f, lp = pair_sum(lprod) * f;
                 const int row = 32 * w + c32;
-                if (row < seg.rows) {
+                if (row < seg.rows && a.direct && tile0 == 0 && total == at.units && !left_out) {
+                    const bool none = bits_of(lt) == 0;
+                    const float inv = f / lp;
+                    unsigned hr;
+                    const int tok = seg.seq0 + (int)divmod((unsigned)(seg.row0 + row), seg.heads_each, hr), h = seg.kvh * seg.rep + (int)hr;
+                    __bf16* const out = (__bf16*)a.o + ((int64_t)tok * seg.Hq + h) * D + 4 * hh;
+#pragma unroll
+                    for (int n = 0; n < 4 * DB; ++n) {
+                        bf16x4 y;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = (__bf16)(none ? 0.f : o[n >> 2][4 * (n & 3) + i] * inv);
+                        *reinterpret_cast<bf16x4*>(out + 32 * (n >> 2) + 8 * (n & 3)) = y;
+                    }
+                    if (hh == 0) {
+                        a.lse[(int64_t)h * a.n_tok + tok] = none ? -INFINITY : m * (a.c * LN2) + __logf(lt);
+                        *reinterpret_cast<f32x4*>(a.stats + (seg.base + row) * 4) = f32x4{0.f, 0.f, 0.f, DONE};
+                    }
+                } else if (row < seg.rows) {
                     float* const out = a.sums + (seg.base + row) * D + 4 * hh;
 #pragma unroll
                     for (int n = 0; n < 4 * DB; ++n) {
@@ -1189,13 +1283,13 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
 // tile (h, e) is element 64 h + 4 m + e, so that V is read in pieces of 16 bytes as well.
 template <int D, bool MANY, bool TREE = false>
 __global__ __launch_bounds__(256, 2) void decode_f32_kernel(StartsArg<TREE> starts, DecodeArgs a) {
-    __shared__ i32x2 lists[4096];
+    __shared__ ListIs<TREE> lists[4096];
     __shared__ PlanShare<4> share;
     constexpr int NC = SOLO_ROWS / 16, HALVES = D / 64;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, m16 = l & 15, j = l >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 64) a.tag[l] = 0u;
     const Lists<0, TREE> ls{words_of(starts), a};
-    Work work;
+    Work<TREE> work;
     if constexpr (MANY) work = find_work<4>(ls, lists, 4096, share, w, l); else work = find_work_in_lanes<4>(ls, w, l);
     if (work.left == 0) return;
     Cursor<0, TREE> at(ls, work);
@@ -1393,6 +1487,9 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
     const int n_p = part ? (int)prompts(count) : 0, n = part ? n_p + (int)resps(count) : 0;
     const unsigned at_p = prompts(at), at_r = resps(at), stride_p = prompts(stride), stride_r = resps(stride);
     typedef std::conditional_t<TREE, f32x4, f32x2> Stats;
+    if constexpr (TREE) {
+        if (a.direct && n == 1 && a.stats[(uint64_t)(n_p ? at_p : at_r) * 4 + 3] == DONE) return;
+    }
     float M = a.m_none, L = 0.f, LP = 0.f;             // LP: of the weights that the products took (TREE)
     bool left_out = false;
     f32x4 acc = {0, 0, 0, 0};

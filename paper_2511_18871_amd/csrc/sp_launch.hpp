@@ -384,7 +384,7 @@ hipError_t launch_decode(const KvCache& cache, const void* q, void* o, float* ls
 size_t tree_table_bytes(int n_groups, int n_seqs);
 size_t tree_partial_bytes(int n_groups, int n_seqs, int64_t total, int Hq, int Hkv, int d, bool f32);
 double tree_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_tokens, int64_t resp_tokens, const int32_t* starts);
-hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int32_t* starts, int* dev_starts,
+hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, int total, const int32_t* starts, int* dev_starts,
                        const uint32_t* ancestors, int64_t mask_stride, const int* prompt_tables, int prompt_width, const int* prompt_lens,
                        const int* resp_tables, int resp_width, const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s);
 

@@ -49,7 +49,7 @@ double tree_units(int n_groups, int n_seqs, int Hq, int Hkv, int64_t prompt_toke
     return units * Hkv;
 }
 
-hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, int total, const int32_t* starts, int* dev_starts,
+hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse, int Hq, int n_groups, int n_seqs, const int32_t* Gs, int total, const int32_t* starts, int* dev_starts,
                        const uint32_t* ancestors, int64_t mask_stride, const int* prompt_tables, int prompt_width, const int* prompt_lens,
                        const int* resp_tables, int resp_width, const int* resp_lens, float scale, uint32_t* tag, void* partials, hipStream_t s) {
     DecodeArgs a{};
@@ -86,7 +86,16 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
         const hipError_t e = launch_prepare(starts, n_words, dev_starts, tag, ReserveTag{}, TAG_CLEAR, false, n_groups, total, 0, 0, Schedule{}, KEYS_AS_PACKED, s);
         if (e != hipSuccess) return e;
     }
-    const bool prompts = prompt_width > 0;
+    bool groups_alike = true;              // of as many sequences
+    for (int g = 1; Gs && g < n_groups; ++g) groups_alike = groups_alike && Gs[g] == Gs[0];
+    a.group_seqs = make_div(std::max(1, Gs ? Gs[0] : 1));
+    // Prompts ahead of their sequences' own keys, in one list: a row then leaves one set of sums, or none, in place of two, and a prompt is read for each of its
+    // sequences, from the caches.  Where that is little, or up to eight times what the sums are (64 prompts of 64 to 192 tokens with 16 answers each, 28/4 heads: 242 ->
+    // 216 us; 32 chains of 150 tokens behind prompts of 700, 32/8: 199 -> 146; 22 prompts of 400 with 18 answers, heads of 64, at the limit: 138 -> 141; a prompt of 16k
+    // tokens with 32 answers 118 -> 254, hence not there).
+    const double again = (double)(n_seqs - n_groups) * ((double)prompt_width * (1 << a.log_page)) * a.Hkv * 2 * cache.head_dim * 2;
+    const double sums = (double)total * Hq * (4 * cache.head_dim + 16) * 2;
+    a.joined = prompt_width > 0 && !cache.f32 && groups_alike && (again <= 32e6 || again <= 8 * sums);
     const int n_lists = n_groups + n_seqs;
     // (prompts, then responses)
     auto rows_of = [&](int i) { const int k = i < n_groups ? i : i + 1; return (int64_t)a.rep * (starts[k + 1] - starts[k]); };
@@ -94,9 +103,16 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
     // few units of 32 keys by 32 rows (one sequence of 1k tokens with 8 drafted ones, 28/4 heads: 17.2 -> 15.8 us), nor those whose tables hold few keys (64 prompts
     // of 64 to 192 tokens with 16 answers each: 245 -> 241 us; chunks of 150 tokens behind 700: 223 us without, 195 with, hence no more than that).
     constexpr int NEVER = 0x7fffffff;
-    double units = 0;                      // of 32 keys by 32 rows that the tables have room for
-    auto tokens_of = [&](int i) { return (double)(i < n_groups ? prompt_width : resp_width) * (1 << a.log_page); };
-    for (int i = prompts ? 0 : n_groups; i < n_lists; ++i) units += (tokens_of(i) / 32 + 1) * ((double)rows_of(i) / SOLO_ROWS + 1) * a.Hkv;
+    auto tokens_of = [&](int i) { return ((double)(i < n_groups ? prompt_width : resp_width) + (a.joined ? prompt_width : 0)) * (1 << a.log_page); };
+    auto units_of = [&](int from) {        // of 32 keys by 32 rows that the tables of lists `from` ... have room for
+        double units = 0;
+        for (int i = from; i < n_lists; ++i) units += (tokens_of(i) / 32 + 1) * ((double)rows_of(i) / SOLO_ROWS + 1) * a.Hkv;
+        return units;
+    };
+    a.joined = a.joined && units_of(n_groups) <= 2e9;
+    const bool prompts = prompt_width > 0 && !a.joined;      // as lists of their own
+    a.direct = !prompts && !cache.f32;
+    const double units = units_of(prompts ? 0 : n_groups);
     const bool few = units <= FEW_UNITS;
     a.wide_prompts = cache.f32 || few || tokens_of(0) < SHORT_LIST ? NEVER : TREE_SOLO_ROWS;
     a.wide_resps = cache.f32 || few || tokens_of(n_groups) < SHORT_LIST ? NEVER : TREE_SOLO_ROWS;
