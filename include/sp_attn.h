@@ -516,13 +516,15 @@ sp_status sp_attn_pages_fit(int32_t* refs, int64_t n_pages, int32_t page_size, i
  * holds).  What the row held before is not given back (sp_attn_pages_fit with a length of 0 does).
  *   refs          as above, n_pages of the cache
  *   parents       DEVICE int32 [n_seqs]; outside [0, n_src): the sequence is left as it is.  Several may have the same parent
+ *   flags         SP_FLAG_MARK_ORPHANS: lens_out of sequences without a parent becomes -1
  *   src_tables    DEVICE int32 [n_src, src_width], src_lens DEVICE int32 [n_src]; a negative length: a row of -1, lens_out that length
  *   tables        DEVICE int32 [n_seqs, table_width], written;  lens_out DEVICE int32 [n_seqs], written
  * Where no page is left for the last tokens the row is -1 throughout, lens_out -1, and nothing is counted.  Places outside the cache are copied as they
  * are and not counted. */
+#define SP_FLAG_MARK_ORPHANS 16u           /* sp_attn_cache_fork only */
 sp_status sp_attn_cache_fork(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t* refs, int32_t n_seqs,
                              const int32_t* parents, int32_t n_src, const int32_t* src_tables, int32_t src_width, const int32_t* src_lens,
-                             int32_t* tables, int32_t table_width, int32_t* lens_out,
+                             int32_t* tables, int32_t table_width, int32_t* lens_out, uint32_t flags,
                              void* workspace, size_t workspace_bytes, void* stream);
 
 /* Rules by which logits are adjusted before a token is drawn, in this order: bias, repetition, frequency and presence,

@@ -21,7 +21,7 @@ SP_SCHED_SHARED, SP_SCHED_NAIVE_CAUSAL = 0, 1
 
 SP_BWD_STAGE_ROWSUM, SP_BWD_STAGE_DKDV, SP_BWD_STAGE_DQ, SP_BWD_STAGE_ALL = 1, 2, 4, 7
 SP_MAX_DRAFT = 1024
-SP_FLAG_RESPONSE_ROWS, SP_FLAG_ACCUMULATE_DKDV, SP_FLAG_ZERO_PROMPT_ROWS, SP_FLAG_OWN_TOKEN = 1, 2, 4, 8
+SP_FLAG_RESPONSE_ROWS, SP_FLAG_ACCUMULATE_DKDV, SP_FLAG_ZERO_PROMPT_ROWS, SP_FLAG_OWN_TOKEN, SP_FLAG_MARK_ORPHANS = 1, 2, 4, 8, 16
 
 EXPORTS = ("sp_attn_workspace_bytes", "sp_attn_reserve_bytes", "sp_attn_row_parts_bytes", "sp_attn_full_workspace_bytes", "sp_attn_kept_workspace_bytes", "sp_attn_sums_bytes", "sp_attn_fwd", "sp_attn_bwd", "sp_attn_fwd_batched",
            "sp_attn_bwd_batched", "sp_attn_bwd_batched_static", "sp_attn_bwd_batched_stages", "sp_attn_fwd_multi", "sp_attn_rope", "sp_attn_rope_qk", "sp_attn_fwd_batched_ex", "sp_attn_bwd_batched_ex", "sp_attn_fwd_batched_sums", "sp_attn_bwd_batched_sums",
@@ -138,7 +138,7 @@ def load_library() -> ctypes.CDLL:
     lib.sp_attn_pages_fit.restype = ctypes.c_int
     lib.sp_attn_pages_fit.argtypes = [vp, i64, i32, i32, vp, i32, vp, vp, vp, sz, vp]
     lib.sp_attn_cache_fork.restype = ctypes.c_int
-    lib.sp_attn_cache_fork.argtypes = [cache_p, i32, i64, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]
+    lib.sp_attn_cache_fork.argtypes = [cache_p, i32, i64, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, ctypes.c_uint32, vp, sz, vp]
     lib.sp_attn_adjust_logits.restype = ctypes.c_int
     lib.sp_attn_adjust_logits.argtypes = [vp, i64, vp, i64, i64, rules_p, vp, i64, i32, i32, ip, vp, i32, vp, vp, i32, vp, ctypes.c_int, vp]
     lib.sp_attn_adjusted_logprob_workspace_bytes.restype = sz
@@ -992,14 +992,14 @@ def sp_attn_cache_fork(cache, refs, parents, src_tables, src_lens, tables, lens_
 
 @_placed
 def _fork(raw, cache, refs, parents, src_tables, src_lens, tables, lens_out, workspace):
-    n_seqs = parents.shape[0]
+    n_seqs, flags = parents.shape[0], 0
     if lens_out is None:
-        lens_out = torch.full_like(parents, -1)
+        lens_out, flags = torch.empty_like(parents), SP_FLAG_MARK_ORPHANS
     if n_seqs == 0:
         return lens_out
     workspace = _pages_workspace(refs.shape[0], n_seqs, cache.device, workspace)
     _check(load_library().sp_attn_cache_fork(cache._ref, *_layers(cache), refs.data_ptr(), n_seqs, parents.data_ptr(), src_lens.shape[0], src_tables.data_ptr(),
-                                             src_tables.shape[1], src_lens.data_ptr(), tables.data_ptr(), tables.shape[1], lens_out.data_ptr(),
+                                             src_tables.shape[1], src_lens.data_ptr(), tables.data_ptr(), tables.shape[1], lens_out.data_ptr(), flags,
                                              workspace.data_ptr(), workspace.nbytes, raw))
     return lens_out
 

@@ -923,8 +923,9 @@ sp_status sp_attn_pages_fit(int32_t* refs, int64_t n_pages, int32_t page_size, i
 
 sp_status sp_attn_cache_fork(const sp_kv_cache* cache, int32_t n_layers, int64_t layer_stride, int32_t* refs, int32_t n_seqs, const int32_t* parents,
                              int32_t n_src, const int32_t* src_tables, int32_t src_width, const int32_t* src_lens, int32_t* tables,
-                             int32_t table_width, int32_t* lens_out, void* workspace, size_t workspace_bytes, void* stream) {
+                             int32_t table_width, int32_t* lens_out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
     g_err[0] = 0;
+    if (flags & ~SP_FLAG_MARK_ORPHANS) return fail(SP_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
     sp::KvCache c;
     const sp_status st = check_layers(cache, n_layers, layer_stride, c);
     if (st != SP_OK) return st;
@@ -945,7 +946,7 @@ sp_status sp_attn_cache_fork(const sp_kv_cache* cache, int32_t n_layers, int64_t
     if (!workspace || misaligned(workspace) || workspace_bytes < need)
         return fail(SP_ERR_WORKSPACE, "workspace %p of %zu bytes; need %zu bytes, 16-byte aligned", workspace, workspace_bytes, need);
     const hipError_t e = sp::launch_fork(c, n_layers, layer_stride, refs, n_seqs, parents, n_src, src_tables, src_width, src_lens, tables, table_width, lens_out,
-                                         (uint32_t*)workspace, (char*)workspace + TAG_BYTES, (hipStream_t)stream);
+                                         (flags & SP_FLAG_MARK_ORPHANS) != 0, (uint32_t*)workspace, (char*)workspace + TAG_BYTES, (hipStream_t)stream);
     if (e != hipSuccess) return fail(SP_ERR_DEVICE, "HIP launch failed: %s", hipGetErrorString(e));
     return SP_OK;
 }

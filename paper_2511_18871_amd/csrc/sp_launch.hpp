@@ -395,7 +395,7 @@ hipError_t launch_keep(const KvCache& cache, int n_layers, int64_t layer_stride,
 hipError_t launch_fit(int* refs, int64_t n_pages, int log_page, int n_seqs, int* tables, int width, const int* lens, int* missing, uint32_t* tag,
                       void* room, hipStream_t s);
 hipError_t launch_fork(const KvCache& cache, int n_layers, int64_t layer_stride, int* refs, int n_seqs, const int* parents, int n_src, const int* src_tables,
-                       int src_width, const int* src_lens, int* tables, int width, int* lens_out, uint32_t* tag, void* room, hipStream_t s);
+                       int src_width, const int* src_lens, int* tables, int width, int* lens_out, bool mark_orphans, uint32_t* tag, void* room, hipStream_t s);
 
 // Rules of adjusted logits (sp_logit_rules)
 struct AdjustRules { float repetition, inv_repetition, presence, frequency, inv_temperature; const float* bias; };

@@ -332,6 +332,7 @@ struct ForkArgs {
     int* tables; int* lens_out; int* order; uint32_t* tag;
     int64_t src_width, width, capacity;    // capacity: tokens that both tables hold
     int n_seqs, n_src, Hkv, log_page;
+    bool mark_orphans;                     // lens_out of sequences without a parent becomes -1
 };
 struct Child { int parent; int64_t len, whole; int rest; bool takes; int last; };      // takes: a page for the `rest` tokens of page `last`
 __device__ __forceinline__ Child child_of(const ForkArgs& a, int seq) {
@@ -373,8 +374,11 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
     __shared__ int slots[64];
     const int seq = blockIdx.x, layer = blockIdx.y >> 1;
     const Child c = child_of(a, seq);
-    if (c.parent < 0) return;
     const bool tells = blockIdx.y == 0;
+    if (c.parent < 0) {
+        if (a.mark_orphans && tells && threadIdx.x == 0) a.lens_out[seq] = -1;
+        return;
+    }
     if (!tells && !c.takes) return;
     int to = -1;
     if (c.takes) {
@@ -458,7 +462,7 @@ hipError_t launch_fit(int* refs, int64_t n_pages, int log_page, int n_seqs, int*
 }
 
 hipError_t launch_fork(const KvCache& cache, int n_layers, int64_t layer_stride, int* refs, int n_seqs, const int* parents, int n_src, const int* src_tables,
-                       int src_width, const int* src_lens, int* tables, int width, int* lens_out, uint32_t* tag, void* room, hipStream_t s) {
+                       int src_width, const int* src_lens, int* tables, int width, int* lens_out, bool mark_orphans, uint32_t* tag, void* room, hipStream_t s) {
     const int elem = cache.f32 ? 4 : 2;
     ForkArgs a{};
     a.pool = make_pool(refs, cache.n_pages, n_seqs, room);
@@ -466,6 +470,7 @@ hipError_t launch_fork(const KvCache& cache, int n_layers, int64_t layer_stride,
     a.parents = parents; a.src_tables = src_tables; a.src_lens = src_lens; a.tables = tables; a.lens_out = lens_out; a.order = (int*)room; a.tag = tag;
     a.src_width = src_width; a.width = width; a.capacity = std::min<int64_t>((int64_t)std::min(src_width, width) << cache.log_page, MAX_TOKENS);
     a.n_seqs = n_seqs; a.n_src = n_src; a.Hkv = cache.n_kv_heads; a.log_page = cache.log_page;
+    a.mark_orphans = mark_orphans;
     hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)a.pool.n_chunks + 1), dim3(256), 0, s, a);
     hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n_seqs, (unsigned)(2 * n_layers)), dim3(256), 0, s, a);
     return hipGetLastError();

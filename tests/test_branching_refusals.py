@@ -65,8 +65,8 @@ def test_fit_refuses(lib):
     assert [lib.sp_attn_pages_workspace_bytes(*x) for x in ((0, 1), (1, 0), (1 << 31, 1), (-1, 1))] == [0] * 4
 
 
-def fork(lib, c=None, layers=1, stride=0, refs=FAR[0], n=2, parents=FAR[1], ns=3, st=FAR[2], sw=4, sl=FAR[3], t=FAR[4], w=5, out=FAR[5], ws=FAR[6], bytes=1 << 20):
-    return lib.sp_attn_cache_fork(cache() if c is None else c, layers, stride, refs, n, parents, ns, st, sw, sl, t, w, out, ws, bytes, None)
+def fork(lib, c=None, layers=1, stride=0, refs=FAR[0], n=2, parents=FAR[1], ns=3, st=FAR[2], sw=4, sl=FAR[3], t=FAR[4], w=5, out=FAR[5], flags=0, ws=FAR[6], bytes=1 << 20):
+    return lib.sp_attn_cache_fork(cache() if c is None else c, layers, stride, refs, n, parents, ns, st, sw, sl, t, w, out, flags, ws, bytes, None)
 
 
 def test_fork_refuses(lib):
@@ -74,7 +74,7 @@ def test_fork_refuses(lib):
         assert fork(lib, c=cache(**kw)) == status, kw
     for kw in (dict(layers=0), dict(layers=2), dict(layers=40000, stride=1 << 20), dict(refs=None), dict(parents=None), dict(st=None), dict(sl=None), dict(t=None), dict(out=None), dict(n=0), dict(ns=0),
                dict(sw=0), dict(w=0), dict(refs=FAR[0] + 1), dict(out=FAR[5] + 2), dict(t=FAR[2] + 44), dict(out=FAR[3] + 8), dict(out=FAR[1]), dict(t=FAR[0] - 36), dict(out=FAR[4] + 36),
-               dict(t=FAR[1]), dict(sl=FAR[0] + 12)):
+               dict(t=FAR[1]), dict(sl=FAR[0] + 12), dict(flags=8), dict(flags=32)):
         assert fork(lib, **kw) == INVALID, kw
     need = lib.sp_attn_pages_workspace_bytes(4, 2)
     for kw in (dict(ws=None), dict(ws=FAR[6] + 8), dict(bytes=need - 1)):

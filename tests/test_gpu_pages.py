@@ -154,6 +154,16 @@ def test_fork_many_and_out_of_pages():
     check_fork(k, v, refs, parents, src.tolist(), src_lens, [[-1] * 5 for _ in parents], [-1] * 700)
 
 
+def test_fork_without_a_parent():
+    """The length of such a sequence is -1 in an array that the call makes, and untouched in a given one."""
+    gen = torch.Generator().manual_seed(6)
+    k, v = (x.cuda() for x in layers(gen, 1, 8, 1, 16, 64, torch.bfloat16))
+    tables = dev32([[5, 5]] * 3)
+    out = B.sp_attn_cache_fork(B.KvLayers(k, v), dev32([1, 0, 0, 0, 0, 0, 0, 0]), dev32([-1, 0, 1]), dev32([[0, -1]]), dev32([7]), tables)
+    assert out.tolist() == [-1, 7, -1] and tables.tolist() == [[5, 5], [1, -1], [5, 5]]
+    assert torch.equal(k[:, 1, :, :7], k[:, 0, :, :7])
+
+
 def test_calls_in_a_graph():
     """Fit, fork and keep captured together, replayed with other lengths and parents, against the same calls made at once."""
     gen = torch.Generator().manual_seed(5)
