@@ -1445,8 +1445,9 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
             auto narrow = [&](int& b, int& e) {
                 const int step = (e - b + EACH - 1) / EACH, i = b + l * step;
                 const uint64_t all = __builtin_amdgcn_ballot_w64(i < e && w[i] <= tok);
-                const uint64_t mine = EACH == 64 ? all : all >> (threadIdx.x & 63 & ~(EACH - 1)) & ((1ull << (EACH & 63)) - 1);
-                b += (__popcll(mine) - 1) * step;
+                const unsigned half = threadIdx.x & 32 ? (unsigned)(all >> 32) : (unsigned)all;
+                const int ahead = EACH == 64 ? __popcll(all) : __popc(EACH == 32 ? half : half >> (threadIdx.x & 31 & ~(EACH - 1)) & ((1u << (EACH & 31)) - 1));
+                b += (ahead - 1) * step;
                 e = min(e, b + step);
             };
             int ge = a.n_groups, sb = a.n_groups + 1, se = sb + a.n_seqs;

@@ -20,7 +20,10 @@ __device__ __forceinline__ int scan_lanes(int x) {
 }
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 __device__ __forceinline__ u64 ballot(bool b) { return __builtin_amdgcn_ballot_w64(b); }
-__device__ __forceinline__ int lanes_below(u64 set) { return __popcll(set & ((1ull << (threadIdx.x & 63)) - 1)); }
+// Shifts by an amount of the lane's own are of 32 bits here: those of 64 gave wrong results, a wave now and then, where the compiler had put the amount into the
+// last register of the wave's allocation (v39 of 40).
+__device__ __forceinline__ int lanes_below(u64 set) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0u)); }
+__device__ __forceinline__ bool has_lane(u64 set) { return ((threadIdx.x & 32 ? (unsigned)(set >> 32) : (unsigned)set) >> (threadIdx.x & 31)) & 1; }
 
 // ---- keep ----------------------------------------------------------------------------------------------------
 
@@ -62,8 +65,9 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
         more = run == 64;
         const bool moves_row = l < run && x != i;
         const int64_t from = moves_row ? row_of(have + x) : -1, to = moves_row ? row_of(have + i) : -1;
-        const u64 set = ballot(from >= 0 && to >= 0);
-        if (set >> l & 1) { moves[w][lanes_below(set)][0] = from; moves[w][lanes_below(set)][1] = to; }
+        const bool both = from >= 0 && to >= 0;
+        const u64 set = ballot(both);
+        if (both) { moves[w][lanes_below(set)][0] = from; moves[w][lanes_below(set)][1] = to; }
         const int count = __popcll(set);
         __builtin_amdgcn_wave_barrier();
         for (int item = item0; item < min(item0 + a.per_wave, a.items); ++item) {
@@ -92,11 +96,15 @@ struct Pool { int* refs; u64* free; int* counts; int64_t n_pages; int n_chunks; 
 // which pages of chunk `c` are free, and how many (256 threads)
 __device__ __forceinline__ void count_chunk(const Pool& p, int64_t c, int* sh) {
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
-    int sum = 0;
-#pragma unroll 4
+    int sum = 0, refs[CHUNK / 256];
+#pragma unroll
     for (int i = 0; i < CHUNK / 256; ++i) {
         const int64_t page = c * CHUNK + i * 256 + threadIdx.x;
-        const u64 set = ballot(page < p.n_pages && p.refs[page] == 0);
+        refs[i] = page < p.n_pages ? p.refs[page] : 1;
+    }
+#pragma unroll
+    for (int i = 0; i < CHUNK / 256; ++i) {
+        const u64 set = ballot(refs[i] == 0);
         sum += __popcll(set);
         if (l == 0) p.free[c * 64 + i * 4 + w] = set;
     }
@@ -105,17 +113,18 @@ __device__ __forceinline__ void count_chunk(const Pool& p, int64_t c, int* sh) {
     if (threadIdx.x == 0) p.counts[c] = sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-// The free pages that requests first .. first + n - 1 get, n <= 64, in the wave's slots (-1: none is left).  A lane holds one of a chunk's 64
-// words and deals out its bits; `mine` is its chunk's count among the first 64 chunks.
+// The free page that request first + l gets in lane l < n (-1: none is left).  Each lane holds one of a chunk's 64 words; a request finds its word among them by their ranks,
+// then its bit by halves: 36 -> 30 us for the two calls of a step of 1024 sequences, against words that deal out their bits one by one.
+// `mine`: the chunk's count, a lane each, among the first 64 chunks.
 __device__ __forceinline__ int first_counts(const Pool& p) {
     const int l = threadIdx.x & 63;
     return l < p.n_chunks ? p.counts[l] : 0;
 }
-__device__ __forceinline__ void take_pages(const Pool& p, int mine, int64_t first, int n, int* slots) {
+__device__ __forceinline__ int take_pages(const Pool& p, int mine, int64_t first, int n) {
     const int l = threadIdx.x & 63;
-    slots[l] = -1;
+    const int64_t nth = first + l;
+    int got = -1, given = 0;
     int64_t before = 0;                    // free pages ahead of the chunk
-    int given = 0;
     for (int64_t c0 = 0; c0 < p.n_chunks && given < n; c0 += 64) {
         if (c0) mine = c0 + l < p.n_chunks ? p.counts[c0 + l] : 0;
         const int to = scan_lanes(mine);
@@ -125,22 +134,36 @@ __device__ __forceinline__ void take_pages(const Pool& p, int mine, int64_t firs
                 const int k = __ffsll(here) - 1;
                 here &= here - 1;
                 const int64_t ahead = before + __builtin_amdgcn_readlane(to - mine, k);
-                u64 bits = p.free[(c0 + k) * 64 + l];
-                const int mask = __popcll(bits);
-                int64_t nth = ahead + scan_lanes(mask) - mask - first;
-                for (; bits; bits &= bits - 1, ++nth)
-                    if (nth >= 0 && nth < n) slots[nth] = (int)((c0 + k) * CHUNK + l * 64 + __ffsll(bits) - 1);
-                given = (int)min((int64_t)n, ahead + __builtin_amdgcn_readlane(mine, k) - first);
+                const int count = __builtin_amdgcn_readlane(mine, k);
+                const u64 word = p.free[(c0 + k) * 64 + l];
+                const int mask = __popcll(word), rank = scan_lanes(mask) - mask;
+                const bool asks = l < n && nth >= ahead && nth < ahead + count;
+                int r = asks ? (int)(nth - ahead) : 0, at = 0;
+#pragma unroll
+                for (int o = 32; o; o >>= 1) at += __shfl(rank, at + o, 64) <= r ? o : 0;      // the last word that starts at r or ahead of it
+                r -= __shfl(rank, at, 64);
+                const unsigned low_half = (unsigned)__shfl((int)word, at, 64), high_half = (unsigned)__shfl((int)(word >> 32), at, 64);
+                const bool high = r >= __popc(low_half);
+                r -= high ? __popc(low_half) : 0;
+                unsigned bits = high ? high_half : low_half;
+                int bit = high ? 32 : 0;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) {
+                    const int low = __popc(bits & ((1u << o) - 1));
+                    if (r >= low) { r -= low; bits >>= o; bit += o; }
+                }
+                if (asks) got = (int)((c0 + k) * CHUNK + at * 64 + bit);
+                given = (int)min((int64_t)n, ahead + count - first);
             }
         }
         before += last_lane(to);
     }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    return got;
 }
 
 // ---- fit -------------------------------------------------------------------------------------------------------
 
+constexpr int FIT_AHEAD = 4;           // pieces of 64 places that a wave looks at together
 struct FitArgs {
     Pool pool;
     int* tables; const int* lens; int* missing; int* wants; uint32_t* tag;
@@ -178,7 +201,6 @@ __global__ __launch_bounds__(256) void count_free_kernel(Pool p) {
 
 // One wave per sequence: its empty places get pages.  The first workgroup says how many places of all got none.
 __global__ __launch_bounds__(256) void assign_kernel(FitArgs a) {
-    __shared__ int slots[4][64];
     __shared__ int sh[4];
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), seq0 = (int)blockIdx.x * 4, seq = seq0 + w;
     auto over_workgroup = [&](int x) {
@@ -196,37 +218,44 @@ __global__ __launch_bounds__(256) void assign_kernel(FitArgs a) {
         free = over_workgroup(free);
         if (threadIdx.x == 0) a.missing[0] = max(0, all - free);
     }
+    // places are looked at FIT_AHEAD * 64 at a time, the first of them while the sums are on their way
+    int left = seq < a.n_seqs ? a.wants[seq] : 0;
+    const int counts = first_counts(a.pool);
+    const int64_t need = left > 0 ? pages_needed(a, seq) : 0;
+    int* const table = a.tables + seq * a.width;
+    int page[FIT_AHEAD];
+    auto look_up = [&](int64_t c0) {
+#pragma unroll
+        for (int u = 0; u < FIT_AHEAD; ++u) page[u] = c0 + 64 * u + l < need ? table[c0 + 64 * u + l] : 0;
+    };
+    look_up(0);
     int ahead = 0;
     for (int s = threadIdx.x; s < seq0; s += 256) ahead += a.wants[s];
     ahead = over_workgroup(ahead);
-    if (seq >= a.n_seqs) return;
-    for (int s = seq0; s < seq; ++s) ahead += a.wants[s];
-    int left = a.wants[seq];
-    const int counts = first_counts(a.pool);
-    const int64_t need = pages_needed(a, seq);
-    for (int64_t c0 = 0; left > 0 && c0 < need; c0 += 64) {
-        const int64_t c = c0 + l;
-        int* const at = a.tables + seq * a.width + c;
-        const int page = c < need ? *at : 0;
-        const bool empty = c < need && (page < 0 || page >= a.pool.n_pages);
-        const u64 set = ballot(empty);
-        const int n = __popcll(set);
-        if (n == 0) continue;
-        take_pages(a.pool, counts, ahead, n, slots[w]);
-        if (empty) {
-            const int got = slots[w][lanes_below(set)];
-            *at = got;
-            if (got >= 0) a.pool.refs[got] = 1;
+    for (int s = seq0; s < min(seq, a.n_seqs); ++s) ahead += a.wants[s];
+    for (int64_t c0 = 0; left > 0 && c0 < need; c0 += 64 * FIT_AHEAD) {
+        if (c0) look_up(c0);
+#pragma unroll
+        for (int u = 0; u < FIT_AHEAD; ++u) {
+            const bool empty = c0 + 64 * u + l < need && (page[u] < 0 || page[u] >= a.pool.n_pages);
+            const u64 set = ballot(empty);
+            const int n = __popcll(set);
+            if (n == 0) continue;
+            const int got = __shfl(take_pages(a.pool, counts, ahead, n), lanes_below(set) & 63, 64);
+            if (empty) {
+                table[c0 + 64 * u + l] = got;
+                if (got >= 0) a.pool.refs[got] = 1;
+            }
+            ahead += n;
+            left -= n;
         }
-        ahead += n;
-        left -= n;
     }
 }
 
 // The same in one launch, for what one workgroup sees at a time: FIT_PLACES places of all tables in FIT_ITEMS pieces of 64, and 64 pages to a thread.  The places that
 // want a page are listed in LDS, in order; a lane keeps a bit per page of its own, and a wave deals out the free ones among 64 at a time.
 // Bound: the launch, three loads that wait for each other, and code that runs once.
-constexpr int FIT_PLACES = 16384, FIT_ITEMS = 2048, FIT_PAGES = 65536, FIT_AHEAD = 4;
+constexpr int FIT_PLACES = 16384, FIT_ITEMS = 2048, FIT_PAGES = 65536;
 __global__ __launch_bounds__(1024) void fit_small_kernel(FitArgs a, Div pieces) {      // pieces: of 64 places of a table
     __shared__ int places[FIT_PLACES];
     __shared__ u64 sets[FIT_ITEMS];        // of a piece's places, those that want a page
@@ -304,15 +333,16 @@ __global__ __launch_bounds__(1024) void fit_small_kernel(FitArgs a, Div pieces) 
         const u64 set = sets[item];
         int seq;
         const int c = place_of(item, seq);
-        if (set >> l & 1) places[first[item] + lanes_below(set)] = seq * width + c;
+        if (has_lane(set)) places[first[item] + lanes_below(set)] = seq * width + c;
     }
     int all, nth = over_waves(l == 0 ? found : 0, all);       // (its barriers stand behind the list as well)
     nth = __builtin_amdgcn_readfirstlane(nth);
     if (tid == 0 && a.missing) a.missing[0] = max(0, total - all);
     for (int j = 0; j < turns && nth < total; ++j) {
-        const u64 set = ballot(mask >> j & 1);
+        const bool free = mask >> j & 1;
+        const u64 set = ballot(free);
         const int k = nth + lanes_below(set);
-        if ((set >> l & 1) && k < total) {
+        if (free && k < total) {
             a.tables[places[k]] = page0 + 64 * j;
             a.pool.refs[page0 + 64 * j] = 1;
         }
@@ -371,7 +401,7 @@ __global__ __launch_bounds__(256) void fork_count_kernel(ForkArgs a) {
 
 // A workgroup takes K or V of a layer of a child, and copies the tokens of its last page; the first of a child writes its table.
 __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
-    __shared__ int slots[64];
+    __shared__ int page_of_child;
     const int seq = blockIdx.x, layer = blockIdx.y >> 1;
     const Child c = child_of(a, seq);
     const bool tells = blockIdx.y == 0;
@@ -382,9 +412,12 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
     if (!tells && !c.takes) return;
     int to = -1;
     if (c.takes) {
-        if (threadIdx.x < 64) take_pages(a.pool, first_counts(a.pool), a.order[seq], 1, slots);
+        if (threadIdx.x < 64) {
+            const int got = take_pages(a.pool, first_counts(a.pool), a.order[seq], 1);
+            if (threadIdx.x == 0) page_of_child = got;
+        }
         __syncthreads();
-        to = __builtin_amdgcn_readfirstlane(slots[0]);
+        to = __builtin_amdgcn_readfirstlane(page_of_child);
     }
     const bool none = c.takes && to < 0;
     if (tells) {
