@@ -224,3 +224,74 @@ def test_two_calls_at_once():
     for x, (wo, wl) in list(zip(inputs, want)) * 3:
         o, lse = B.sp_attn_tree_decode(cache, x, *args, workspace=rooms[0])
         assert torch.equal(o, wo) and torch.equal(lse, wl)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_rows_without_a_key_in_long_lists(d):
+    """Many rows to a workgroup, some of which see nothing, one key, or the last one only."""
+    new, resp = [1024, 40], [1024, 70]
+    q, kc, vc, _, rt, _, _ = make(torch.bfloat16, d, 8, 1, 32, [0], new, resp, words=32)
+    rows = [[] if i % 5 == 0 else [1023] if i % 5 == 1 else [i] if i % 5 == 2 else list(range(i % 7, 1024, 61)) for i in range(1024)] + [[] for _ in range(40)]
+    o, lse = run_and_check(q, kc, vc, None, rt, rows, mask_words(rows, 32), None, new, None, resp, d ** -0.5)
+    assert torch.all(o[:1024:5] == 0) and torch.all(torch.isneginf(lse[:, :1024:5])) and torch.isfinite(lse[:, 1024:]).all()
+
+
+def test_long_tables_of_short_sequences():
+    """The work is split by what tables hold; here lengths are far below that, or negative, or beyond."""
+    Gs, prompts, new = [4, 4], [1500, 1500], [40] * 8
+    q, kc, vc, pt, rt, rows, mask = make(torch.bfloat16, 128, 32, 8, 16, prompts, new, [900] * 8)
+    for prompt_lens, resp in (([3, 0], [40, 41, 39, -1, 77, 0, 900, 1000]), ([-5, 1500], [-1] * 8), ([1500, 17], [1, 2, 900, 40, -7, 64, 65, 300])):
+        run_and_check(q, kc, vc, pt, rt, rows, mask, Gs, new, prompt_lens, resp, 0.1)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_long_lists_do_not_see_what_is_masked(bad):
+    """Neither key nor value of a drafted token matters to the rows that do not see it, in workgroups of four waves and of eight."""
+    for n, ahead in ((200, 1500), (300, 3900)):
+        new, resp = [n, n], [ahead + n, ahead]
+        q, kc, vc, _, rt, _, _ = make(torch.bfloat16, 128, 16, 4, 16, [0], new, resp)
+        rows = [sorted({0, i, i // 2} - {2, n - 1}) for i in range(n)] * 2
+        args = (q.cuda(), None, new, mask_words(rows, -(-n // 32)).cuda(), None, None, rt.cuda(), dev32(resp), 0.1)
+        clean, clean_lse = B.sp_attn_tree_decode(B.KvCache(kc.cuda(), vc.cuda()), *args)
+        for s in range(2):
+            for j in (resp[s] - n + 2, resp[s] - 1):
+                kc[rt[s, j // 16], :, j % 16] = bad
+                vc[rt[s, j // 16], :, j % 16] = bad
+        o, lse = B.sp_attn_tree_decode(B.KvCache(kc.cuda(), vc.cuda()), *args)
+        assert torch.equal(o, clean) and torch.equal(lse, clean_lse) and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("n,ahead,prompt", [(200, 2900, 100), (300, 3900, 0)])
+def test_large_scores_in_long_lists(n, ahead, prompt):
+    """Scores far apart and far from 0, which rise along the list: rows take new references again and again."""
+    prompts, new, resp = [prompt], [n], [ahead + n]
+    q, kc, vc, pt, rt, rows, mask = make(torch.bfloat16, 128, 8, 2, 16, prompts, new, resp)
+    q, kc = q.abs(), kc * 8
+    for j in range(0, ahead, 50):
+        kc[rt[0, j // 16], :, j % 16] = kc[rt[0, j // 16], :, j % 16].abs() * (j / ahead)
+    run_and_check(q, kc, vc, pt, rt, rows, mask, [1], new, prompts, resp, 1.0)
+
+
+@pytest.mark.parametrize("where", ["prompt", "ahead"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_keys_and_values_that_all_rows_of_long_lists_see(where, bad):
+    """A value's element reaches its heads' rows in its place, a NaN key makes their rows NaN."""
+    n, ahead, prompt = 200, 2900, 100
+    q, kc, vc, pt, rt, _, _ = make(torch.bfloat16, 128, 16, 4, 16, [prompt], [n], [ahead + n])
+    page, at = (pt[0, 2], 7) if where == "prompt" else (rt[0, 100], 3)
+    def call(k, v):
+        return B.sp_attn_tree_decode(B.KvCache(k.cuda(), v.cuda()), q.cuda(), [1], [n], None, pt.cuda(), dev32([prompt]), rt.cuda(), dev32([ahead + n]), 0.1)
+    clean, clean_lse = call(kc, vc)
+    v2 = vc.clone()
+    v2[page, 1, at, 9] = bad
+    o, lse = call(kc, v2)
+    hit = o[:, 4:8, 9]
+    assert torch.equal(lse, clean_lse) and (torch.all(hit.isnan()) if bad != bad else torch.all(hit == bad))
+    o[:, 4:8, 9] = clean[:, 4:8, 9]
+    assert torch.equal(o, clean)
+    if bad != bad:
+        k2 = kc.clone()
+        k2[page, 1, at, 9] = bad
+        o, lse = call(k2, vc)
+        assert torch.all(o[:, 4:8].isnan()) and torch.all(lse[4:8].isnan())
+        assert torch.equal(o[:, :4], clean[:, :4]) and torch.equal(o[:, 8:], clean[:, 8:]) and torch.equal(lse[:4], clean_lse[:4])
