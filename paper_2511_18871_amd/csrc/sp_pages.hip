@@ -39,7 +39,7 @@ struct KeepArgs {
 // Token lens + kept[i] of a sequence becomes its token lens + i.  A wave looks 64 entries of the list up at a time, a lane each, and moves their rows of `per_wave`
 // (layer, K or V, head) in turn, 64 AHEAD lanes of 16 bytes on their way.  It reads a batch of rows ahead of writing any, and kept ascends, so that
 // kept[j] >= j > i for j > i: no row that is still to be read is written over.
-// Bound: bytes, and for small calls four loads that wait for each other.
+// Bound: bytes, and for small calls four loads that wait for each other: 3.5 us for 8 paths in 2 layers; 128 paths in 16 layers 45 us for 193 MB, 4.3 TB/s.
 constexpr int KEEP_AHEAD = 4;
 template <int ROW>        // bytes of a row
 __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
