@@ -39,6 +39,9 @@ constexpr int SOLO_ROWS = 32;              // rows of a segment that a wave take
 // Drafted tokens
 constexpr int WIDE_ROWS = 256;             // rows that a workgroup takes at most: 32 to a wave
 constexpr int TREE_SOLO_ROWS = 48;         // rows of a list that a wave takes by itself where other lists are shared (bf16)
+// Units that a worker takes at least, where few segments are dealt to many: it leaves 64 KB of sums or more, and pays its plan and first loads, whatever the run (a prompt
+// of 1k tokens with 8 trees of 16: 28.0 us at 2, 24.9 at 3, 25.4 at 4, 26.7 at 6)
+constexpr unsigned LEAST_RUN = 3;
 constexpr int WIDE_PAD = 3;                // units that a segment of many rows costs beside its own: first loads, last product, sums
 constexpr int MAX_NC = 3;                  // row tiles of 16 of a wave that shares its keys: 192 rows to a workgroup
 constexpr int PLAN_WGS = 512;              // workgroups that the units are dealt to: two to a CU (one: 131 -> 164 us for the 64 prompts above)
@@ -204,6 +207,7 @@ __device__ __forceinline__ void shared_runs(const DecodeArgs& a, unsigned solo, 
         wgs = max(1, min(wgs, solo ? WGS - 1 : WGS));
         r.aligned = 4 * segs <= (unsigned)wgs;
         r.shared_run = r.aligned ? per_place(shared, wgs - segs) : per_place(shared + (TREE ? WIDE_PAD * segs : 0), wgs);
+        if (TREE && r.aligned) r.shared_run = max(r.shared_run, LEAST_RUN);
     }
 }
 

@@ -10,7 +10,7 @@
 //   chunks of 192 to 256 tokens behind 4k to 8k, 32/8 heads     155 + 14   101 GFLOP, 650 TFLOP/s; matrix units are busy for 28 % of its cycles at 2.4 GHz, in the 16k prompt for 29
 //   a prompt of 16k tokens, 32 answers, trees of 8, 40/8        108 to 121 + 9   87 GFLOP, 720 to 800 TFLOP/s
 //   64 prompts of 64 to 192 tokens, 16 answers each, 3 to 5 drafted tokens, 28/4   178 + 45   0.84 GB read, 4.7 TB/s; half the rows are finished by one worker
-//   a prompt of 1k tokens, 8 answers, trees of 16, 28/4         22 + 7     latency: plan, pages, first keys, code that comes from memory once
+//   a prompt of 1k tokens, 8 answers, trees of 16, 28/4         20 + 5     latency: plan, pages, first keys, code that comes from memory once
 //   one sequence of 1k tokens, a tree of 8, 28/4                10 + 6     the same
 #include "sp_decode.hpp"
 #include <algorithm>
@@ -149,7 +149,7 @@ hipError_t launch_tree(const KvCache& cache, const void* q, void* o, float* lse,
         solo = std::max(solo, (int)std::min<int64_t>(rows_of(i), 16 * ns));
     }
     // Workgroups of eight waves, where that leaves few of 256 rows empty and segments are long: they read keys and values half as often, but there is one to
-    // a CU.  (4 chunks of 192 to 256 tokens behind 4k to 8k, 32/8 heads: 160 -> 150 us; a prompt of 1k tokens with 8 trees of 16: 27.5 us either way; 22
+    // a CU.  (4 chunks of 192 to 256 tokens behind 4k to 8k, 32/8 heads: 160 -> 150 us; a prompt of 1k tokens with 8 trees of 16, runs of two units: 27.5 us either way; 22
     // groups of short prompts 130 -> 177.)
     const bool eight = a.shared_rows && 2 * units_256 <= 1.2 * units_shared && weighted >= 32 * units_shared;
     const int nw = eight ? 8 : 4;
