@@ -295,3 +295,19 @@ def test_keys_and_values_that_all_rows_of_long_lists_see(where, bad):
         o, lse = call(k2, vc)
         assert torch.all(o[:, 4:8].isnan()) and torch.all(lse[4:8].isnan())
         assert torch.equal(o[:, :4], clean[:, :4]) and torch.equal(o[:, 8:], clean[:, 8:]) and torch.equal(lse[:4], clean_lse[:4])
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("case", SPLITS, ids=lambda c: c[0].replace(" ", "_"))
+def test_in_place_at_every_split(d, case):
+    """o may be q: rows that one worker finishes by itself among them."""
+    _, Gs, prompts, ahead, new, hq, hkv = case
+    resp = [a + n for a, n in zip(ahead, new)]
+    q, kc, vc, pt, rt, _, mask = make(torch.bfloat16, d, hq, hkv, 16, prompts, new, resp, seed=d)
+    cache, q = B.KvCache(kc.cuda(), vc.cuda()), q.cuda()
+    args = (Gs, new, mask.cuda(), pt.cuda(), dev32(prompts), rt.cuda(), dev32(resp), d ** -0.5)
+    want, want_lse = B.sp_attn_tree_decode(cache, q, *args)
+    for _ in range(3):
+        mine = q.clone()
+        o, lse = B.sp_attn_tree_decode(cache, mine, *args, o=mine)
+        assert torch.equal(o, want) and torch.equal(lse, want_lse)
