@@ -311,3 +311,36 @@ def test_in_place_at_every_split(d, case):
         mine = q.clone()
         o, lse = B.sp_attn_tree_decode(cache, mine, *args, o=mine)
         assert torch.equal(o, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("Gs,n,table", [([1] * 70, 32, 640), ([2, 1] * 25, 32, 700), ([33, 33], 64, 2304), ([1] * 66, 64, 2304), ([3] * 30, 40, 1100)])
+@pytest.mark.parametrize("d", [128, 64])
+def test_many_lists_of_many_rows(Gs, n, table, d):
+    """More lists than lanes, each of many rows, in workgroups of four waves and of eight; most of the sequences are far shorter than their tables."""
+    gen = torch.Generator().manual_seed(table + d)
+    S, G = sum(Gs), len(Gs)
+    new = [n] * S if Gs[0] != 2 else [n - s % 3 for s in range(S)]
+    held = [n + (table - n if s % 12 == 5 else int(torch.randint(0, 90, (1,), generator=gen))) for s in range(S)]
+    prompts = [table if g % 20 == 3 else int(torch.randint(0, 70, (1,), generator=gen)) for g in range(G)]
+    q, kc, vc, pt, rt, rows, mask = make(torch.bfloat16, d, 8, 2, 64, prompts, new, held)
+    resp = [-1 if s % 17 == 9 else x for s, x in enumerate(held)]
+    run_and_check(q, kc, vc, pt, rt, rows, mask, Gs, new, prompts, resp, d ** -0.5)
+
+
+@pytest.mark.parametrize("new", [300, 120])
+def test_long_lists_beyond_32_bit_offsets(new):
+    """Pages far behind the first 4 GB of a cache, in lists of many rows."""
+    d, hkv, page, n_pages = 128, 8, 256, 10000
+    kc, vc = (torch.empty(n_pages, hkv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    gen = torch.Generator().manual_seed(3)
+    used = [9999, 3, 8700, 9000, 9998, 5001, 8193, 7777, 9001, 42]
+    small_k, small_v = (torch.randn(10, hkv, page, d, generator=gen).bfloat16().cuda() for _ in range(2))
+    kc[used], vc[used] = small_k, small_v
+    q = torch.randn(new, 16, d, generator=gen).bfloat16().cuda()
+    near = B.KvCache(small_k, small_v)
+    for prompt, resp in ((used[:2], used[2:]), (used[:1], used[1:])):
+        at = [used.index(p) for p in resp]
+        lens = dev32([256 * len(prompt) - 3]), dev32([256 * len(resp) - 9])
+        far = B.sp_attn_tree_decode(B.KvCache(kc, vc), q, [1], [new], None, dev32([prompt]), lens[0], dev32([resp]), lens[1], 0.1)
+        want = B.sp_attn_tree_decode(near, q, [1], [new], None, dev32([list(range(len(prompt)))]), lens[0], dev32([at]), lens[1], 0.1)
+        assert torch.equal(far[0], want[0]) and torch.equal(far[1], want[1]) and torch.isfinite(far[1]).all()
