@@ -1026,12 +1026,13 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
                     mask16(S[kb], bits >> (4 * hh));
                 }
             };
-            // takes infinite and NaN values out of V(j) ... V(j + n - 1), in buffers from b on, where these hold drafted tokens; every wave its share
+            // takes infinite and NaN values out of those of V(j) ... V(j + n - 1), in buffers from b on, that hold drafted tokens; every wave its share.  (Not out of the
+            // others, whose keys all rows see: the join would not add them.)
             auto clean_tiles = [&](int j, int n, int b) SP_INLINE {
-                if (j + n <= 0 || !tail(j + n - 1)) return;
+                if (j + n <= 0 || !tail(j + n - 1)) return;        // tiles behind the first one with drafted tokens hold some as well
 #pragma unroll
                 for (int i = 0; i < n; ++i)
-                    if (clean(buf + (unsigned)(NB + ((b + i) & (NB - 1))) * TILE, threadIdx.x, TILE / 16, 64 * NW)) left_out = 1;
+                    if (tail(j + i) && clean(buf + (unsigned)(NB + ((b + i) & (NB - 1))) * TILE, threadIdx.x, TILE / 16, 64 * NW)) left_out = 1;
                 wait_lds();
                 __syncthreads();
             };
