@@ -263,6 +263,14 @@ __device__ __forceinline__ s16x4 lds_at_tr4(unsigned addr) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)addr);
 }
 
+// The half of a wave's set of lanes that the lane itself is in.  A 64-bit shift by a lane's own amount gave wrong results, in one wave of some ten thousand, where the
+// compiler had put the amount into the last register of the wave's allocation (v39 of 40), and right ones in 32 bits.  Why is not known; such shifts are
+// not written where it was seen, and the empty statement keeps the compiler from making one of this choice.
+__device__ __forceinline__ unsigned half_of_lane(unsigned long long set) {
+    unsigned high = (unsigned)(set >> 32);
+    asm("" : "+v"(high));
+    return threadIdx.x & 32 ? high : (unsigned)set;
+}
 // the n lowest bits set (none for n <= 0, all from 32 on)
 __device__ __forceinline__ unsigned low_bits(int n) { return n <= 0 ? 0u : 0xffffffffu >> (32 - min(n, 32)); }
 // Masks a 32 x 32 score block: S[r], of row (or key) 8 (r / 4) + 4 (lane / 32) + r % 4 of the block, becomes -inf unless

@@ -1459,7 +1459,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(StartsArg<TREE> starts
             // the last of the groups, and of the sequences, that starts at the token or ahead of it: as many candidates at a time as the row has lanes
             auto of_row = [](bool b) {
                 const uint64_t all = __builtin_amdgcn_ballot_w64(b);
-                const unsigned half = threadIdx.x & 32 ? (unsigned)(all >> 32) : (unsigned)all;
+                const unsigned half = half_of_lane(all);
                 return EACH == 64 ? __popcll(all) : __popc(EACH == 32 ? half : half >> (threadIdx.x & 31 & ~(EACH - 1)) & ((1u << (EACH & 31)) - 1));
             };
             int ge = a.n_groups, sb = a.n_groups + 1, se = sb + a.n_seqs;

@@ -20,10 +20,9 @@ __device__ __forceinline__ int scan_lanes(int x) {
 }
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 __device__ __forceinline__ u64 ballot(bool b) { return __builtin_amdgcn_ballot_w64(b); }
-// Shifts by an amount of the lane's own are of 32 bits here: those of 64 gave wrong results, a wave now and then, where the compiler had put the amount into the
-// last register of the wave's allocation (v39 of 40).
+// (no shifts of 64 bits by a lane's own amount: half_of_lane())
 __device__ __forceinline__ int lanes_below(u64 set) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0u)); }
-__device__ __forceinline__ bool has_lane(u64 set) { return ((threadIdx.x & 32 ? (unsigned)(set >> 32) : (unsigned)set) >> (threadIdx.x & 31)) & 1; }
+__device__ __forceinline__ bool has_lane(u64 set) { return half_of_lane(set) >> (threadIdx.x & 31) & 1; }
 
 // ---- keep ----------------------------------------------------------------------------------------------------
 
