@@ -1019,6 +1019,8 @@ def _mask_rows(mask, rows, index):
     if mask.dtype not in (torch.int32, torch.uint32) or mask.dim() != 2:
         _refuse(f"mask: {mask.dtype} {tuple(mask.shape)}, expected rows of int32 or uint32 words")
     _need("mask", mask, mask.dtype, (rows, mask.shape[1]), index)
+    if rows and not mask.shape[1]:                                       # (its null address would read as no mask)
+        _refuse(f"mask: {tuple(mask.shape)}, rows of no words")
     return mask.data_ptr(), mask.shape[1]
 
 
