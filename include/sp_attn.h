@@ -506,7 +506,7 @@ sp_status sp_attn_cache_keep(const sp_kv_cache* cache, int32_t n_layers, int64_t
  * [0, n_pages) get free ones (also such as the same call gave back), whose counts become 1.  Where none is left they are -1.
  *   tables        DEVICE int32 [n_seqs, table_width], changed;  lens DEVICE int32 [n_seqs], cut to what a table holds; negative: the row stays as it is
  *   missing       DEVICE int32 [1], how many places got none, or NULL
- * A table must not hold more than refs says: a count that falls below 0 loses its page. */
+ * A table must not hold more than refs says: a count that falls below 0 loses its page.  SP_ERR_INVALID_ARG also where n_seqs * table_width passes 2^31 - 1. */
 size_t    sp_attn_pages_workspace_bytes(int64_t n_pages, int32_t n_seqs);
 sp_status sp_attn_pages_fit(int32_t* refs, int64_t n_pages, int32_t page_size, int32_t n_seqs, int32_t* tables, int32_t table_width,
                             const int32_t* lens, int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);

@@ -909,6 +909,7 @@ sp_status sp_attn_pages_fit(int32_t* refs, int64_t n_pages, int32_t page_size, i
     if (!refs || !tables || !lens) return fail(SP_ERR_INVALID_ARG, "an array is NULL");
     if (off4(refs) || off4(tables) || off4(lens) || off4(missing)) return fail(SP_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
     const int64_t entries = (int64_t)n_seqs * table_width;
+    if (entries > 0x7fffffffLL) return fail(SP_ERR_INVALID_ARG, "%d tables of %d places: more than one call counts", n_seqs, table_width);
     if (meet(refs, n_pages, tables, entries) || meet(refs, n_pages, lens, n_seqs) || meet(tables, entries, lens, n_seqs) ||
         meet(missing, 1, refs, n_pages) || meet(missing, 1, tables, entries) || meet(missing, 1, lens, n_seqs))
         return fail(SP_ERR_INVALID_ARG, "refs, tables, lens and missing must not overlap");
