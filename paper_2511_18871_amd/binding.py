@@ -663,6 +663,10 @@ class KvCache:
         return self._pointer
 
 
+class _AllLayersError(SpAttnError, AttributeError):
+    """A call for one layer was given the caches of all of them."""
+
+
 class KvLayers:
     """The caches of all layers of a model: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim], each layer contiguous, whose sequences have the
     same tables in every layer.  layers[i] is the KvCache of layer i.  Memory, shape and type as for KvCache."""
@@ -679,6 +683,11 @@ class KvLayers:
         self._stride = self._strides[0]
         self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), n_pages, page_size, heads, head_dim, _dtype_code(k))
         self._pointer = ctypes.pointer(self._struct)
+
+    def __getattr__(self, name):
+        if name in ("dtype", "code", "n_kv_heads", "head_dim"):
+            raise _AllLayersError(SP_ERR_INVALID_ARG, "the call takes the cache of one layer: layers[i] of KvLayers")
+        raise AttributeError(f"KvLayers has no attribute {name!r}")
 
     def __len__(self) -> int:
         return self.n_layers
