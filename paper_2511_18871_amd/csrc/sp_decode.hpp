@@ -159,7 +159,7 @@ struct Lists {
         s.rows = x[0];
         s.len = x[1];
         s.shared = KIND && s.rows > (!TREE ? SOLO_ROWS : i < a.n_groups ? a.wide_prompts : a.wide_resps);
-auto units = [&](int n) { return n > 0 ? (int)(((unsigned)n + (s.shared ? 63u : 31u)) >> (s.shared ? 6 : 5)) : 0; };
+        auto units = [&](int n) { return n > 0 ? (int)(((unsigned)n + (s.shared ? 63u : 31u)) >> (s.shared ? 6 : 5)) : 0; };
         s.units = s.rows > 0 ? units(s.len) : 0;
         s.ahead = 0;
         if constexpr (TREE) { if (s.rows > 0) s.ahead = units(x[2]); s.units += s.ahead; }
@@ -944,7 +944,10 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(StartsArg<TREE> star
         // matrix instruction (two, heads of 64).  Four waves: two buffers of 64 keys each of K and of V, a barrier per step; V(j) and K(j+2) are copied under step
         // j, and two workgroups share a CU.  A weight is rounded once, to bf16, and o divided by the sum of the rounded ones, which takes what their errors have in
         // common out of it (o off by 1.76e-3 of its 2-norm against 1.66e-3 with weights in two parts, whose second product would be of twice the instructions); lse
-        // has the sum of the others.  Eight waves: four buffers each, two steps to a barrier; a copy serves twice the rows and has twice the time.
+        // has the sum of the others.  An element is off by 2^-8 of sum p |v| and of |o| for the weights, at most, and by 2^-8 of |o| for its own rounding.
+        // Heads of 128: 256 registers to a wave, and 88 to 104 bytes of scratch, written where a segment starts and read there, where pages are looked
+        // up, values cleaned or drafted tokens masked, and behind the last step; steps without drafted tokens do not touch it.
+        // Eight waves: four buffers each, two steps to a barrier; a copy serves twice the rows and has twice the time.
         constexpr int TILE = 4 * KEYS16, KS = D / 16, MF = 2 * KS, DB = D / 32, PER = 32 / (2 * MF), RD = 3, NB = NW == 8 ? 4 : 2;
         const int c32 = l & 31, hh = l >> 5, j16 = l & 15;
         unsigned row_at[KS], tr_at[DB][2];         // operands within the first buffers

@@ -6,12 +6,12 @@
 // sequences, a response by those of its own.  Only units of keys that hold drafted tokens look at the mask.
 //
 // Bound: the keys and values, read once for a list's rows as long as these are few; the matrix instructions from some hundred rows on; for a few
-// sequences latency.  Measured (heads of 128, bf16, us of the kernel + of the join):
-//   chunks of 192 to 256 tokens behind 4k to 8k, 32/8 heads     154 + 13   101 GFLOP, 650 TFLOP/s; matrix units are busy for 28 % of its cycles at 2.4 GHz, in the 16k prompt for 29
-//   a prompt of 16k tokens, 32 answers, trees of 8, 40/8        108 to 121 + 9   87 GFLOP, 720 to 800 TFLOP/s
-//   64 prompts of 64 to 192 tokens, 16 answers each, 3 to 5 drafted tokens, 28/4   176 + 39   0.84 GB read, 4.8 TB/s; half the rows are finished by one worker
+// sequences latency.  Measured (heads of 128, bf16, us of the kernel + of the join, medians of traced launches):
+//   chunks of 192 to 256 tokens behind 4k to 8k, 32/8 heads     156 + 14   101 GFLOP, 650 TFLOP/s; matrix units are busy for 28 % of its cycles at 2.4 GHz, in the 16k prompt for 29
+//   a prompt of 16k tokens, 32 answers, trees of 8, 40/8        124 + 10   87 GFLOP, 700 TFLOP/s
+//   64 prompts of 64 to 192 tokens, 16 answers each, 3 to 5 drafted tokens, 28/4   177 + 39   0.84 GB read, 4.8 TB/s; half the rows are finished by one worker
 //   a prompt of 1k tokens, 8 answers, trees of 16, 28/4         20 + 5     latency: plan, pages, first keys, code that comes from memory once
-//   one sequence of 1k tokens, a tree of 8, 28/4                10 + 6     the same
+//   one sequence of 1k tokens, a tree of 8, 28/4                11 + 6     the same
 #include "sp_decode.hpp"
 #include <algorithm>
 #include <type_traits>
